@@ -48,7 +48,9 @@ extern "C" {
                                kf_stage_prefill_noalloc; kf_ring_generate's hidden_out_dev (kafila_ring.h);
                                the kf_shard_* loader (kafila_shard.h);
                             5: a head stage's decode may keep its output rows (hidden_out_dev NULL)
-                               for kf_head_logits / kf_head_argmax with hidden_dev NULL */
+                               for kf_head_logits / kf_head_argmax with hidden_dev NULL.
+                            Calls added since leave the others as they are: kf_kv_create_typed,
+                            kf_kv_format, kf_kv_copy, kf_kv_fork */
 #define KF_KV_PAGE 64     /* positions per KV cache page */
 #define KF_MAX_BATCH 4
 
@@ -216,6 +218,26 @@ kf_status kf_kv_create(kf_stage* stage, int32_t max_users, int32_t max_ctx, kf_k
  * table [max_users][P] maps each user's page index to a pool page.
  */
 kf_status kf_kv_create_paged(kf_stage* stage, int32_t max_users, int32_t max_ctx, int32_t n_pages, kf_kv** out);
+
+/*
+ * A cache of a given type: KF_KV_F16 as kf_kv_create (n_pages 0) and kf_kv_create_paged
+ * (n_pages >= 1) make it, or KF_KV_MXFP4, reserved or paged alike, which takes 17/64 of the bytes.
+ * An MXFP4 cache holds each head vector of a key or value in blocks of 32 consecutive
+ * values: E2M1 elements (0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign), rounded to
+ * nearest even, times one power of two 2^e.  A value x is rounded to fp16 first; e is
+ * the exponent of the block's largest |x|, rounded to one mantissa bit, less 2, in
+ * [-23, 13], so that the largest rounds to 4 or 6 times 2^e; magnitudes past 6 2^13 = 49152
+ * become that.  Every stored value is an fp16 number.  Infinities and what fp16 rounds
+ * to one are stored as 49152, a NaN as 0, and all three raise the stage's range
+ * error (KF_ERANGE from kf_stage_sync).
+ * kf_stage_decode and kf_stage_prefill take KF_KV_F16 caches only (else KF_EUNSUPPORTED).  KF_EINVAL for a negative n_pages or an unknown type.
+ */
+typedef enum { KF_KV_F16 = 0, KF_KV_MXFP4 = 1 } kf_kv_type;
+kf_status kf_kv_create_typed(kf_stage* stage, int32_t max_users, int32_t max_ctx, int32_t n_pages, kf_kv_type type,
+                             kf_kv** out);
+
+/* A cache's type and the device bytes it holds (pages, tables and workspaces).  Any output pointer may be NULL.  Host-only. */
+kf_status kf_kv_format(const kf_kv* kv, kf_kv_type* type, int64_t* bytes);
 kf_status kf_kv_destroy(kf_kv* kv);
 
 /* Pages of the cache and, for a paged cache, how many are free (-1 for a reserved cache, whose users
@@ -248,6 +270,30 @@ kf_status kf_kv_write(kf_kv* kv, int32_t layer, int32_t user, int32_t pos0, int3
  * KF_ERANGE for positions on pages the user does not hold (paged caches). */
 kf_status kf_kv_read(const kf_kv* kv, int32_t layer, int32_t user, int32_t pos0, int32_t n, float* k_dev,
                      float* v_dev);
+
+/*
+ * Copy positions [pos0, pos0 + n) of src_user, in every layer the stage holds, to the
+ * same positions of dst_user in the same cache or another one of the stage (a user
+ * handed from one cache to another, e.g. an idle one from fp16 into 4 bits).  Between
+ * types the values are converted: to MXFP4 as kf_kv_write stores them, to fp16 exactly.
+ * Does not change lengths (a paged destination lends the pages up to pos0 + n;
+ * KF_ENOMEM if it cannot).  KF_ERANGE past either cache's max_ctx or for positions on
+ * pages that src_user does not hold; KF_EINVAL for caches of different stages and for a
+ * user copied onto itself.  Enqueued on the stage's stream.
+ */
+kf_status kf_kv_copy(kf_kv* dst, int32_t dst_user, const kf_kv* src, int32_t src_user, int32_t pos0, int32_t n);
+
+/*
+ * Give dst_user the first n positions of src_user (n at most its length) in place of
+ * whatever it held, and the length n: several continuations of one prompt.  A reserved
+ * cache copies the positions.  In a paged cache the two users share the pages, at no
+ * cost in pages; a user that writes to a page others hold too (decode, prefill,
+ * kf_kv_write, kf_kv_copy) first gets a copy of its own from the pool (KF_ENOMEM
+ * if it has none), so that no user sees another's writes.  A shared page returns to the pool when
+ * its last user gives it back.  KF_EINVAL for src_user == dst_user, KF_ERANGE for n
+ * above src_user's length.
+ */
+kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n);
 
 /*
  * Forward one token for each of `batch` (1..KF_MAX_BATCH) users (decode): the

@@ -1,0 +1,406 @@
+// Kernels that move KV cache contents: MXFP4 encoding and decoding, copies
+// between users and caches, copies of shared pages.
+//
+// All of them are bound by the bytes they move; what they compute per value is a
+// few instructions.  MXFP4: a block is 32 consecutive values x of a head, rounded
+// to fp16.  With a = max |x|, e = (exponent of a rounded to one mantissa bit,
+// nearest even) - 2, clamped: a / 2^e then rounds to at most 6, the largest
+// E2M1 number, wherever the clamp does not bind.  Each x / 2^e is rounded to
+// E2M1, nearest even, and saturates at 6.
+#include <algorithm>
+
+#include "kernels.h"
+
+namespace kf {
+
+namespace {
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+
+enum : int { kRowsF32 = 0, kRowsBF16 = 1, kRowsF16 = 2, kPagesF16 = 3 };  // the first three are kf_dtype values
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_f(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
+}
+
+// 8 consecutive values of a row as fp32; `wide`: at is 16-byte aligned.
+__device__ __forceinline__ void load8(const void* base, int type, int64_t at, bool wide, float (&f)[8]) {
+  if (type == kRowsF32) {
+    const float* p = reinterpret_cast<const float*>(base) + at;
+    if (wide) {
+      const v4f a = __builtin_nontemporal_load(reinterpret_cast<const v4f*>(p));
+      const v4f b = __builtin_nontemporal_load(reinterpret_cast<const v4f*>(p) + 1);
+      f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+      f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = p[i];
+    }
+    return;
+  }
+  const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + at;
+  uint16_t h[8];
+  if (wide) {
+    const v4u w = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = p[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    f[i] = type == kRowsBF16 ? __uint_as_float((uint32_t)h[i] << 16) : (float)__builtin_bit_cast(_Float16, h[i]);
+}
+}  // namespace
+
+struct MxEncodeParams {
+  uint8_t* dst;  // MXFP4 records
+  KvPages dp;
+  int dst_user;
+  int64_t dst_layer;  // bytes per layer
+  const void *sk, *sv;
+  int src_type;
+  int wide;  // rows: sk and sv are 16-byte aligned
+  KvPages sp;  // kPagesF16
+  int src_user;
+  int64_t src_layer;  // bytes per layer
+  int pos0, n, nkv;
+  int* err_flag;
+};
+
+// Workgroup (page, K or V of one KV head, layer): encodes the page's positions that
+// lie in [pos0, pos0 + n) and leaves the others as they are.  Four lanes hold a
+// block, 8 values each.  K codes go out as they are made (8 codes are 4 bytes of a
+// row); V codes, whose bytes hold neighbouring positions, meet in LDS first.  One
+// workgroup owns all of a head's page, so no byte has two writers.
+template <int HD>
+__global__ __launch_bounds__(256) void mx_encode_kernel(const MxEncodeParams p) {
+  constexpr int UPR = HD / 8;  // 8-value units per position
+  constexpr int REC = mx_record(HD), CODES = mx_codes(HD), EXPS = mx_exps(HD);
+  __shared__ uint32_t codes[kKvPage * UPR];
+  const int page = p.pos0 / kKvPage + blockIdx.x, g = blockIdx.y >> 1, is_v = blockIdx.y & 1, tid = threadIdx.x;
+  const int a = max(p.pos0 - page * kKvPage, 0), b = min(p.pos0 + p.n - page * kKvPage, kKvPage);
+  uint8_t* rec = p.dst + blockIdx.z * p.dst_layer + (int64_t)kv_page(p.dp, p.dst_user, page) * p.dp.page_stride +
+                 (int64_t)g * REC + (is_v ? CODES + EXPS : 0);
+  const void* src = is_v ? p.sv : p.sk;
+  bool bad = false;
+  // Every load goes out before the first is used.
+  constexpr int NU = kKvPage * UPR / 256;
+  float f[NU][8];
+#pragma unroll
+  for (int k = 0; k < NU; ++k) {
+    const int u = tid + 256 * k, t = u / UPR, d0 = (u % UPR) * 8;
+    if (t < a || t >= b) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[k][i] = 0.f;
+    } else if (p.src_type == kPagesF16) {
+      const char* base = reinterpret_cast<const char*>(src) + blockIdx.z * p.src_layer;
+      load8(base, kRowsF16, kv_offset(p.sp, p.src_user, g, page * kKvPage + t, HD) + d0, true, f[k]);
+    } else {
+      load8(src, p.src_type, ((int64_t)(page * kKvPage + t - p.pos0) * p.nkv + g) * HD + d0, p.wide, f[k]);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < NU; ++k) {
+    const int u = tid + 256 * k, t = u / UPR, d0 = (u % UPR) * 8;
+    int e;
+    const uint32_t w = mx_encode8(f[k], e, bad);
+    const bool live = t >= a && t < b;
+    if (!is_v) {
+      if (live) *reinterpret_cast<uint32_t*>(rec + mx_k_byte<HD>(t, d0)) = w;
+    } else {
+      codes[u] = w;
+    }
+    if (live && u % 4 == 0) rec[CODES + (is_v ? mx_v_exp<HD>(t, d0 / kMxBlock) : mx_k_exp(t, d0 / kMxBlock))] = (uint8_t)(e + 127);
+  }
+  raise_err(p.err_flag, bad, kErrF16Range);
+  if (!is_v) return;
+  __syncthreads();
+  const uint8_t* lds = reinterpret_cast<const uint8_t*>(codes);
+#pragma unroll
+  for (int k = 0; k < CODES / 4 / 256; ++k) {
+    const int w = tid + 256 * k;  // dword of the V codes: 8 positions of one d
+    const int s = w & 1, d = (2 * (w >> 8) + ((w >> 1) & 1)) * 16 + ((w >> 2) & 15), grp = (w >> 6) & 3;
+    uint32_t v = 0, mask = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int t = 16 * (2 * s + j / 4) + 4 * grp + j % 4;
+      v |= (uint32_t)((lds[t * (HD / 2) + d / 2] >> (4 * (d & 1))) & 15) << (4 * j);
+      if (t >= a && t < b) mask |= 15u << (4 * j);
+    }
+    uint32_t* out = reinterpret_cast<uint32_t*>(rec) + w;
+    if (mask == ~0u) *out = v;
+    else if (mask) *out = (*out & ~mask) | (v & mask);
+  }
+}
+
+struct MxDecodeParams {
+  const uint8_t* src;
+  KvPages sp;
+  int src_user;
+  int64_t src_layer;
+  uint8_t *dk, *dv;  // fp32 rows [n][nkv][hd], or (to_pages) fp16 pages
+  int to_pages;
+  int wide;  // rows: dk and dv are 16-byte aligned
+  KvPages dp;
+  int dst_user;
+  int64_t dst_layer;
+  int pos0, n, nkv;
+};
+
+// The way back, exactly: workgroups as above.  V codes pass through LDS, where each
+// thread collects the nibbles of its 8 values.
+template <int HD>
+__global__ __launch_bounds__(256) void mx_decode_kernel(const MxDecodeParams p) {
+  constexpr int UPR = HD / 8;
+  constexpr int REC = mx_record(HD), CODES = mx_codes(HD), EXPS = mx_exps(HD);
+  __shared__ v4u codes[CODES / 16];
+  const int page = p.pos0 / kKvPage + blockIdx.x, g = blockIdx.y >> 1, is_v = blockIdx.y & 1, tid = threadIdx.x;
+  const int a = max(p.pos0 - page * kKvPage, 0), b = min(p.pos0 + p.n - page * kKvPage, kKvPage);
+  const uint8_t* rec = p.src + blockIdx.z * p.src_layer + (int64_t)kv_page(p.sp, p.src_user, page) * p.sp.page_stride +
+                       (int64_t)g * REC + (is_v ? CODES + EXPS : 0);
+  if (is_v) {
+    for (int i = tid; i < CODES / 16; i += 256) codes[i] = reinterpret_cast<const v4u*>(rec)[i];
+    __syncthreads();
+  }
+  const uint8_t* lds = reinterpret_cast<const uint8_t*>(codes);
+#pragma unroll
+  for (int k = 0; k < kKvPage * UPR / 256; ++k) {
+    const int u = tid + 256 * k, t = u / UPR, d0 = (u % UPR) * 8;
+    if (t < a || t >= b) continue;
+    uint32_t w = 0;
+    int e;
+    if (is_v) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w |= (uint32_t)((lds[mx_v_byte(t, d0 + i)] >> (4 * (t & 1))) & 15) << (4 * i);
+      e = rec[CODES + mx_v_exp<HD>(t, d0 / kMxBlock)];
+    } else {
+      w = *reinterpret_cast<const uint32_t*>(rec + mx_k_byte<HD>(t, d0));
+      e = rec[CODES + mx_k_exp(t, d0 / kMxBlock)];
+    }
+    const float scale = __uint_as_float((uint32_t)e << 23);
+    if (p.to_pages) {
+      const h2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1),
+               x2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
+      uint16_t* dst = reinterpret_cast<uint16_t*>((is_v ? p.dv : p.dk) + blockIdx.z * p.dst_layer) +
+                      kv_offset(p.dp, p.dst_user, g, page * kKvPage + t, HD) + d0;
+      *reinterpret_cast<v4u*>(dst) = v4u{__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1),
+                                         __builtin_bit_cast(uint32_t, x2), __builtin_bit_cast(uint32_t, x3)};
+      continue;
+    }
+    const f2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1),
+             x2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
+    float* dst = reinterpret_cast<float*>(is_v ? p.dv : p.dk) +
+                 ((int64_t)(page * kKvPage + t - p.pos0) * p.nkv + g) * HD + d0;
+    if (p.wide) {
+      __builtin_nontemporal_store(v4f{x0.x, x0.y, x1.x, x1.y}, reinterpret_cast<v4f*>(dst));
+      __builtin_nontemporal_store(v4f{x2.x, x2.y, x3.x, x3.y}, reinterpret_cast<v4f*>(dst) + 1);
+    } else {
+      dst[0] = x0.x; dst[1] = x0.y; dst[2] = x1.x; dst[3] = x1.y;
+      dst[4] = x2.x; dst[5] = x2.y; dst[6] = x3.x; dst[7] = x3.y;
+    }
+  }
+}
+
+struct CopyParams {
+  CacheRef dst, src;
+  int dst_user, src_user, pos0, n;
+};
+
+// Workgroup (page, KV head, layer) of an MXFP4 copy: the dwords of the record, of
+// which only what belongs to positions [a, b) is replaced.
+template <int HD>
+__global__ __launch_bounds__(256) void mx_copy_kernel(const CopyParams p) {
+  constexpr int REC = mx_record(HD), CODES = mx_codes(HD), EXPS = mx_exps(HD);
+  const int page = p.pos0 / kKvPage + blockIdx.x, g = blockIdx.y;
+  const int a = max(p.pos0 - page * kKvPage, 0), b = min(p.pos0 + p.n - page * kKvPage, kKvPage);
+  auto record = [&](const CacheRef& c, int user) {
+    return c.k + blockIdx.z * c.layer_bytes + (int64_t)kv_page(c.pages, user, page) * c.pages.page_stride + (int64_t)g * REC;
+  };
+  const uint8_t* src = record(p.src, p.src_user);
+  uint8_t* dst = record(p.dst, p.dst_user);
+  if (a == 0 && b == kKvPage) {
+    for (int i = threadIdx.x; i < REC / 16; i += 256) reinterpret_cast<v4u*>(dst)[i] = reinterpret_cast<const v4u*>(src)[i];
+    return;
+  }
+  auto in = [&](int t) { return t >= a && t < b; };
+  for (int i = threadIdx.x; i < REC / 4; i += 256) {
+    const int is_v = i * 4 >= CODES + EXPS, at = i * 4 - (is_v ? CODES + EXPS : 0);
+    uint32_t mask = 0;
+    if (at < CODES) {
+      if (is_v) {  // 8 positions of one d
+        const int grp = (at >> 8) & 3, s = (at >> 2) & 1;
+        for (int j = 0; j < 8; ++j)
+          if (in(16 * (2 * s + j / 4) + 4 * grp + j % 4)) mask |= 15u << (4 * j);
+      } else {  // 8 values of one position
+        const int tile = HD == 128 ? at >> 10 : 2 * (at >> 10) + ((at >> 3) & 1);
+        if (in(16 * tile + ((at >> 4) & 15))) mask = ~0u;
+      }
+    } else {  // the exponents of 4 positions
+      const int w = at - CODES;
+      for (int j = 0; j < 4; ++j) {
+        const int t = is_v ? 16 * ((w >> 2) & 3) + 4 * ((w >> 4) / (HD / kMxBlock)) + j : 16 * j + ((w >> 2) & 15);
+        if (in(t)) mask |= 255u << (8 * j);
+      }
+    }
+    if (!mask) continue;
+    const uint32_t v = reinterpret_cast<const uint32_t*>(src)[i];
+    uint32_t* out = reinterpret_cast<uint32_t*>(dst) + i;
+    *out = mask == ~0u ? v : (*out & ~mask) | (v & mask);
+  }
+}
+
+// fp16 to fp16: 16 bytes a thread, K and V of every layer in grid.y.
+__global__ __launch_bounds__(256) void f16_copy_kernel(const CopyParams p, int64_t first, uint32_t total) {
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= total) return;
+  const int hd = p.src.hd, nkv = p.src.nkv;
+  const uint32_t row = i / (uint32_t)(hd / 8), d = (i - row * (uint32_t)(hd / 8)) * 8;
+  const uint32_t t = row / (uint32_t)nkv, g = row - t * (uint32_t)nkv;
+  const int pos = p.pos0 + (int)(first + t);
+  const int64_t layer = blockIdx.y >> 1;
+  const uint8_t* src = (blockIdx.y & 1 ? p.src.v : p.src.k) + layer * p.src.layer_bytes;
+  uint8_t* dst = (blockIdx.y & 1 ? p.dst.v : p.dst.k) + layer * p.dst.layer_bytes;
+  *reinterpret_cast<v4u*>(dst + 2 * (kv_offset(p.dst.pages, p.dst_user, (int)g, pos, hd) + d)) =
+      *reinterpret_cast<const v4u*>(src + 2 * (kv_offset(p.src.pages, p.src_user, (int)g, pos, hd) + d));
+}
+
+__global__ __launch_bounds__(256) void page_copy_kernel(const CacheRef c, const PageCopies u, int64_t page_bytes) {
+  const int arrays = c.mx ? 1 : 2;
+  const int64_t layer = blockIdx.y / arrays;
+  uint8_t* base = (blockIdx.y % arrays ? c.v : c.k) + layer * c.layer_bytes;
+  const v4u* src = reinterpret_cast<const v4u*>(base + (int64_t)u.src[blockIdx.z] * page_bytes);
+  v4u* dst = reinterpret_cast<v4u*>(base + (int64_t)u.dst[blockIdx.z] * page_bytes);
+  for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < page_bytes / 16; i += (int64_t)gridDim.x * 256) dst[i] = src[i];
+}
+
+__global__ void table_share_kernel(int* table, int src, int dst, int n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) table[dst + i] = table[src + i];
+}
+
+// ------------------------------------------------------------------ launchers
+static bool aligned16(const void* a, const void* b) { return (((uintptr_t)a | (uintptr_t)b) & 15) == 0; }
+static unsigned pages_spanned(int pos0, int n) { return (unsigned)((pos0 + n - 1) / kKvPage - pos0 / kKvPage + 1); }
+
+static hipError_t encode(const MxEncodeParams& p, int hd, int layers, hipStream_t s) {
+  const dim3 grid(pages_spanned(p.pos0, p.n), 2 * p.nkv, layers);
+  if (hd == 128) hipLaunchKernelGGL(mx_encode_kernel<128>, grid, dim3(256), 0, s, p);
+  else if (hd == 64) hipLaunchKernelGGL(mx_encode_kernel<64>, grid, dim3(256), 0, s, p);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+static hipError_t decode(const MxDecodeParams& p, int hd, int layers, hipStream_t s) {
+  const dim3 grid(pages_spanned(p.pos0, p.n), 2 * p.nkv, layers);
+  if (hd == 128) hipLaunchKernelGGL(mx_decode_kernel<128>, grid, dim3(256), 0, s, p);
+  else if (hd == 64) hipLaunchKernelGGL(mx_decode_kernel<64>, grid, dim3(256), 0, s, p);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_write(const CacheRef& c, int user, int pos0, const void* src_k, const void* src_v, int src_type,
+                           int n, int* err_flag, hipStream_t s) {
+  MxEncodeParams p{};
+  p.dst = c.k;
+  p.dp = c.pages;
+  p.dst_user = user;
+  p.sk = src_k;
+  p.sv = src_v;
+  p.src_type = src_type;
+  p.wide = aligned16(src_k, src_v);
+  p.pos0 = pos0;
+  p.n = n;
+  p.nkv = c.nkv;
+  p.err_flag = err_flag;
+  return encode(p, c.hd, 1, s);
+}
+
+hipError_t launch_mx_read(const CacheRef& c, int user, int pos0, float* dst_k, float* dst_v, int n, hipStream_t s) {
+  MxDecodeParams p{};
+  p.src = c.k;
+  p.sp = c.pages;
+  p.src_user = user;
+  p.dk = reinterpret_cast<uint8_t*>(dst_k);
+  p.dv = reinterpret_cast<uint8_t*>(dst_v);
+  p.wide = aligned16(dst_k, dst_v);
+  p.pos0 = pos0;
+  p.n = n;
+  p.nkv = c.nkv;
+  return decode(p, c.hd, 1, s);
+}
+
+hipError_t launch_cache_copy(const CacheRef& dst, int dst_user, const CacheRef& src, int src_user, int pos0, int n,
+                             int layers, int* err_flag, hipStream_t s) {
+  if (n <= 0) return hipSuccess;
+  if (dst.hd != src.hd || dst.nkv != src.nkv) return hipErrorInvalidValue;
+  if (dst.mx && !src.mx) {
+    MxEncodeParams p{};
+    p.dst = dst.k;
+    p.dp = dst.pages;
+    p.dst_user = dst_user;
+    p.dst_layer = dst.layer_bytes;
+    p.sk = src.k;
+    p.sv = src.v;
+    p.src_type = kPagesF16;
+    p.sp = src.pages;
+    p.src_user = src_user;
+    p.src_layer = src.layer_bytes;
+    p.pos0 = pos0;
+    p.n = n;
+    p.nkv = src.nkv;
+    p.err_flag = err_flag;
+    return encode(p, src.hd, layers, s);
+  }
+  if (src.mx && !dst.mx) {
+    MxDecodeParams p{};
+    p.src = src.k;
+    p.sp = src.pages;
+    p.src_user = src_user;
+    p.src_layer = src.layer_bytes;
+    p.dk = dst.k;
+    p.dv = dst.v;
+    p.to_pages = 1;
+    p.dp = dst.pages;
+    p.dst_user = dst_user;
+    p.dst_layer = dst.layer_bytes;
+    p.pos0 = pos0;
+    p.n = n;
+    p.nkv = src.nkv;
+    return decode(p, src.hd, layers, s);
+  }
+  const CopyParams p{dst, src, dst_user, src_user, pos0, n};
+  if (src.mx) {
+    const dim3 grid(pages_spanned(pos0, n), src.nkv, layers);
+    if (src.hd == 128) hipLaunchKernelGGL(mx_copy_kernel<128>, grid, dim3(256), 0, s, p);
+    else if (src.hd == 64) hipLaunchKernelGGL(mx_copy_kernel<64>, grid, dim3(256), 0, s, p);
+    else return hipErrorInvalidValue;
+    return hipGetLastError();
+  }
+  // In pieces whose values a 32-bit index holds.
+  const int64_t piece = std::max<int64_t>(1, (1LL << 30) / ((int64_t)src.nkv * src.hd));
+  for (int64_t p0 = 0; p0 < n; p0 += piece) {
+    const uint32_t total = (uint32_t)(std::min<int64_t>(piece, n - p0) * src.nkv * (src.hd / 8));
+    hipLaunchKernelGGL(f16_copy_kernel, dim3((total + 255) / 256, 2 * layers), dim3(256), 0, s, p, p0, total);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_page_copies(const CacheRef& c, const PageCopies& u, int layers, hipStream_t s) {
+  if (u.n < 1 || u.n > kPageCopyBatch) return hipErrorInvalidValue;
+  const int64_t bytes = c.pages.page_stride * (c.mx ? 1 : 2);
+  const unsigned wgs = (unsigned)std::min<int64_t>((bytes / 16 + 1023) / 1024, 64);
+  hipLaunchKernelGGL(page_copy_kernel, dim3(wgs, layers * (c.mx ? 1 : 2), u.n), dim3(256), 0, s, c, u, bytes);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_table_share(int* table, int src, int dst, int n, hipStream_t s) {
+  hipLaunchKernelGGL(table_share_kernel, dim3((n + 255) / 256), dim3(256), 0, s, table, src, dst, n);
+  return hipGetLastError();
+}
+
+}  // namespace kf

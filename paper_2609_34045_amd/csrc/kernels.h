@@ -59,6 +59,67 @@ __device__ __forceinline__ int64_t kv_offset(const KvPages& kp, int user, int g,
   return (int64_t)kv_page(kp, user, t / kKvPage) * kp.page_stride + ((int64_t)g * kKvPage + t % kKvPage) * hd;
 }
 
+// MXFP4 caches (KF_KV_MXFP4).  A page holds one record per KV head, K codes, K
+// exponents, V codes, V exponents; KvPages::page_stride counts bytes there.  A
+// block of kMxBlock values along the head has one exponent e in [kMxExpMin,
+// kMxExpMax], stored as e + 127, and E2M1 codes: value = 2^e times 0, 0.5, 1, 1.5,
+// 2, 3, 4 or 6 with a sign.  With that range every stored value is an fp16 number.
+// Codes and exponents lie in the order in which the attention's lanes take them
+// (mx_* below), so that each of its loads is 16 contiguous bytes a lane.
+constexpr int kMxBlock = 32;
+constexpr int kMxExpMin = -23, kMxExpMax = 13;
+__host__ __device__ constexpr int mx_codes(int hd) { return kKvPage * hd / 2; }           // bytes, K or V
+__host__ __device__ constexpr int mx_exps(int hd) { return kKvPage * hd / kMxBlock; }     // bytes, K or V
+__host__ __device__ constexpr int mx_record(int hd) { return 2 * (mx_codes(hd) + mx_exps(hd)); }
+// Position t of the page as a matrix-core operand sees it: tile t / 16, and within
+// it row t % 16 of K; for V, 16-lane group (t / 4) % 4 and element t % 4.
+// Byte of the K code of (t, d); its nibble is d % 2.  A lane (row, group) takes hd / 4 consecutive d.
+template <int HD>
+__host__ __device__ constexpr int mx_k_byte(int t, int d) {
+  const int tile = t / 16, row = t % 16, grp = d / (HD / 4), x = d % (HD / 4);
+  return HD == 128 ? (tile * 64 + grp * 16 + row) * 16 + x / 2
+                   : ((tile / 2) * 64 + grp * 16 + row) * 16 + (tile % 2) * 8 + x / 2;
+}
+// Byte of the exponent of K block blk at t.
+__host__ __device__ constexpr int mx_k_exp(int t, int blk) { return (blk * 16 + t % 16) * 4 + t / 16; }
+// Byte of the V code of (t, d); its nibble is t % 2.  A lane (d % 16, group) takes its 16 positions of two 16-wide d tiles.
+__host__ __device__ constexpr int mx_v_byte(int t, int d) {
+  const int dt = d / 16;
+  return ((dt / 2) * 64 + ((t / 4) % 4) * 16 + d % 16) * 16 + (dt % 2) * 8 + (t / 16) * 2 + (t % 4) / 2;
+}
+// Byte of the exponent of V block blk at t.
+template <int HD>
+__host__ __device__ constexpr int mx_v_exp(int t, int blk) {
+  return (((t / 4) % 4) * (HD / kMxBlock) + blk) * 16 + (t / 16) * 4 + t % 4;
+}
+
+// 8 of a block's values, the other 24 in the 3 lanes beside (lanes 4 k .. 4 k + 3 hold a
+// block): their E2M1 codes, and the block's exponent.  A NaN is stored as 0, an infinity as
+// the largest magnitude; both, and what fp16 rounds to infinity, are noted in `bad`.
+__device__ __forceinline__ uint32_t mx_encode8(const float (&x)[8], int& e, bool& bad) {
+  float h[8], top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    h[i] = (float)(_Float16)x[i];
+    bad |= !(__builtin_fabsf(h[i]) <= 65504.0f);
+    if (h[i] != h[i]) h[i] = 0.f;
+    top = fmaxf(top, __builtin_fabsf(h[i]));
+  }
+  // over the four lanes, by two quad permutes
+  top = fmaxf(top, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, top), 0xB1, 0xf, 0xf, false)));
+  top = fmaxf(top, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, top), 0x4E, 0xf, 0xf, false)));
+  // adding half a unit of the one kept mantissa bit carries into the exponent where the rounding does
+  e = (int)((__builtin_bit_cast(uint32_t, top) + 0x200000u) >> 23) - 127 - 2;
+  e = e < kMxExpMin ? kMxExpMin : e > kMxExpMax ? kMxExpMax : e;
+  const float scale = __builtin_bit_cast(float, (uint32_t)(e + 127) << 23), most = 6.0f * scale;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) h[i] = fminf(fmaxf(h[i], -most), most);
+  uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, h[0], h[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, h[2], h[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, h[4], h[5], scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, h[6], h[7], scale, 3);
+}
+
 // Optional per-launch marker around each kernel (instrumentation hook of the runtime).
 struct Tracer {
   void* ctx = nullptr;
@@ -199,5 +260,33 @@ struct KvTableUpdate {
   int val[kKvTableBatch];
 };
 hipError_t launch_kv_table_update(int* table, const KvTableUpdate& u, hipStream_t s);
+// table[dst + i] = table[src + i] for i < n: a user that shares another's pages.
+hipError_t launch_kv_table_share(int* table, int src, int dst, int n, hipStream_t s);
+
+// A cache as the copying kernels see it (cache.hip): fp16 K and V arrays, or one array of MXFP4 records at k.
+struct CacheRef {
+  uint8_t* k;
+  uint8_t* v;           // fp16 caches only
+  KvPages pages;
+  int64_t layer_bytes;  // of k (and, alike, v)
+  int mx;
+  int nkv, hd;
+};
+// As launch_kv_write / launch_kv_read, for one layer (c.k: its base) of an MXFP4 cache.  A value is rounded to fp16
+// first, so that an MXFP4 cache holds the same whether a position was written, appended or copied from an fp16 cache.
+hipError_t launch_mx_write(const CacheRef& c, int user, int pos0, const void* src_k, const void* src_v, int src_type,
+                           int n, int* err_flag, hipStream_t s);
+hipError_t launch_mx_read(const CacheRef& c, int user, int pos0, float* dst_k, float* dst_v, int n, hipStream_t s);
+// Positions [pos0, pos0 + n) of src_user to the same ones of dst_user, in every one of `layers` layers.
+hipError_t launch_cache_copy(const CacheRef& dst, int dst_user, const CacheRef& src, int src_user, int pos0, int n,
+                             int layers, int* err_flag, hipStream_t s);
+// Whole pages src[i] to dst[i] for i < n (n <= kPageCopyBatch), in every layer.
+constexpr int kPageCopyBatch = 32;
+struct PageCopies {
+  int n;
+  int src[kPageCopyBatch];
+  int dst[kPageCopyBatch];
+};
+hipError_t launch_page_copies(const CacheRef& c, const PageCopies& u, int layers, hipStream_t s);
 
 }  // namespace kf

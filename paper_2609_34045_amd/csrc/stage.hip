@@ -185,55 +185,123 @@ struct kf_kv {
   std::vector<int> host_table; // mirror of the table (-1: not held)
   std::vector<int> held;       // pages each user holds
   std::vector<int> free_pages; // the pool's free pages (paged caches only), next page last
-  uint16_t *k = nullptr, *v = nullptr;
+  std::vector<int> refs;       // users that hold each page (paged caches only); a page of several is copied before a write
+  kf_kv_type type = KF_KV_F16;
+  uint16_t *k = nullptr, *v = nullptr;  // KF_KV_MXFP4: the records at k, no v, and strides in bytes
+  int64_t bytes = 0;                    // device bytes of everything here
   float *rcos = nullptr, *rsin = nullptr;
   float *part_acc = nullptr, *part_ml = nullptr;
   int64_t page_stride, layer_stride;  // elements
   std::vector<int> len;
   KvPages pages() const { return KvPages{table, ppu, page_stride}; }
+  bool mx() const { return type == KF_KV_MXFP4; }
+  CacheRef ref() const {
+    return CacheRef{(uint8_t*)k, (uint8_t*)v, pages(), layer_stride * (mx() ? 1 : 2), mx(), st->cfg.n_kv_heads, st->cfg.head_dim};
+  }
+  CacheRef layer_ref(int layer) const {
+    CacheRef c = ref();
+    const int64_t off = (layer - st->lo) * c.layer_bytes;
+    c.k += off;
+    if (c.v) c.v += off;
+    return c;
+  }
+  int layers() const { return st->hi - st->lo; }
 };
 
 static int pages_for(int64_t len) { return (int)((len + kKvPage - 1) / kKvPage); }
 
-// Lend each of the (distinct) `users` the pages it needs to hold `upto[i]`
-// positions, or change nothing and fail when the pool is short.  New table
-// entries are written on the stage's stream before any later work there reads them.
-static kf_status kv_grant(kf_kv* kv, int n, const int* users, const int64_t* upto) {
+// The page of `user` that holds position `pos`, if other users hold it too; else -1.
+static int shared_page(const kf_kv* kv, int user, int64_t pos) {
+  const int pg = (int)(pos / kKvPage);
+  if (!kv->table || pg >= kv->held[user]) return -1;
+  const int id = kv->host_table[(size_t)user * kv->ppu + pg];
+  return kv->refs[id] > 1 ? id : -1;
+}
+
+namespace kf {
+// Pages that appending to the (distinct) users takes beyond their growth: copies of shared pages.
+// The last of a page's users writes to it in place.
+int kv_append_copies(const kf_kv* kv, int n, const int* users) {
+  int copies = 0;
+  for (int i = 0; i < n; ++i) {
+    const int id = shared_page(kv, users[i], kv->len[users[i]]);
+    if (id < 0) continue;
+    int before = 0;
+    for (int j = 0; j < i; ++j) before += shared_page(kv, users[j], kv->len[users[j]]) == id;
+    copies += before < kv->refs[id] - 1;
+  }
+  return copies;
+}
+}  // namespace kf
+
+// Before a write of positions [from[i], upto[i]) of each of the (distinct) `users`
+// (several users only where each writes one position): lend it the pages it needs to
+// hold upto[i] positions and give it copies of its own of the pages to be written
+// that other users hold too, or change nothing and fail when the pool is short.
+// Copies and new table entries are written on the stage's stream before any later
+// work there reads them.
+static kf_status kv_grant(kf_kv* kv, int n, const int* users, const int64_t* from, const int64_t* upto) {
   if (!kv->table) return KF_OK;  // reserved cache: every page is held from the start
   int64_t want = 0;
   for (int i = 0; i < n; ++i) {
     const int need = pages_for(upto[i]) - kv->held[users[i]];
     if (need > 0) want += need;
+    if (n == 1)
+      for (int64_t p = from[i]; p < upto[i]; p = (p / kKvPage + 1) * kKvPage) want += shared_page(kv, users[i], p) >= 0;
   }
+  if (n > 1) want += kv_append_copies(kv, n, users);
   if (want > (int64_t)kv->free_pages.size())
     return fail(KF_ENOMEM, "KV pool: %lld more pages needed, %zu free of %d", (long long)want, kv->free_pages.size(),
                 kv->n_pages);
+  hipStream_t st = kv->st->stream;
   KvTableUpdate up{};
+  PageCopies cp{};
+  auto flush = [&]() {
+    if (cp.n) KF_HIP(launch_page_copies(kv->ref(), cp, kv->layers(), st), "page copies");
+    if (up.n) KF_HIP(launch_kv_table_update(kv->table, up, st), "page table update");
+    cp.n = up.n = 0;
+    return KF_OK;
+  };
+  auto take = [&](int u, int pg) {
+    const int id = kv->free_pages.back();
+    kv->free_pages.pop_back();
+    kv->refs[id] = 1;
+    kv->host_table[(size_t)u * kv->ppu + pg] = id;
+    up.idx[up.n] = u * kv->ppu + pg;
+    up.val[up.n++] = id;
+    return id;
+  };
   for (int i = 0; i < n; ++i) {
     const int u = users[i];
+    for (int64_t p = from[i]; p < upto[i]; p = (p / kKvPage + 1) * kKvPage) {
+      const int old = shared_page(kv, u, p);
+      if (old < 0) continue;
+      kv->refs[old]--;
+      cp.src[cp.n] = old;
+      cp.dst[cp.n++] = take(u, (int)(p / kKvPage));
+      if (up.n == kKvTableBatch || cp.n == kPageCopyBatch) {
+        const kf_status e = flush();
+        if (e != KF_OK) return e;
+      }
+    }
     for (int pg = kv->held[u]; pg < pages_for(upto[i]); ++pg) {
-      const int id = kv->free_pages.back();
-      kv->free_pages.pop_back();
-      kv->host_table[(size_t)u * kv->ppu + pg] = id;
-      up.idx[up.n] = u * kv->ppu + pg;
-      up.val[up.n] = id;
-      if (++up.n == kKvTableBatch) {
-        KF_HIP(launch_kv_table_update(kv->table, up, kv->st->stream), "page table update");
-        up.n = 0;
+      take(u, pg);
+      if (up.n == kKvTableBatch) {
+        const kf_status e = flush();
+        if (e != KF_OK) return e;
       }
     }
     if (pages_for(upto[i]) > kv->held[u]) kv->held[u] = pages_for(upto[i]);
   }
-  if (up.n) KF_HIP(launch_kv_table_update(kv->table, up, kv->st->stream), "page table update");
-  return KF_OK;
+  return flush();
 }
 
-// Return a user's pages past the first `keep` to the pool (paged caches).
+// Return a user's pages past the first `keep`, and to the pool those that no other user holds (paged caches).
 static void kv_release(kf_kv* kv, int u, int keep) {
   if (!kv->table) return;
   for (int pg = kv->held[u] - 1; pg >= keep; --pg) {
     int& id = kv->host_table[(size_t)u * kv->ppu + pg];
-    kv->free_pages.push_back(id);
+    if (--kv->refs[id] == 0) kv->free_pages.push_back(id);
     id = -1;
   }
   if (kv->held[u] > keep) kv->held[u] = keep;
@@ -642,7 +710,8 @@ kf_status kf_stage_get_flags(const kf_stage* s, int32_t* flags) {
 
 // ------------------------------------------------------------------ KV cache
 // n_pages == 0: a reserved cache (every user's pages in user order); else a pool of n_pages.
-static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_t n_pages, kf_kv** out) {
+static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_t n_pages, kf_kv_type type,
+                           kf_kv** out) {
   if (!out) return fail(KF_EINVAL, "out is NULL");
   *out = nullptr;
   if (!s) return fail(KF_EINVAL, "stage is NULL");
@@ -661,25 +730,28 @@ static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int3
   kv->max_split = max_split_for(max_ctx);
   kv->ppu = ppu;
   kv->n_pages = paged ? n_pages : max_users * ppu;
-  kv->page_stride = (int64_t)c.n_kv_heads * kKvPage * c.head_dim;
+  kv->type = type;
+  kv->page_stride = kv->mx() ? (int64_t)c.n_kv_heads * mx_record(c.head_dim) : (int64_t)c.n_kv_heads * kKvPage * c.head_dim;
   kv->layer_stride = kv->page_stride * kv->n_pages;
   kv->len.assign(max_users, 0);
   kv->held.assign(max_users, paged ? 0 : ppu);
   if (paged) {
     kv->host_table.assign((size_t)max_users * ppu, -1);
+    kv->refs.assign(n_pages, 0);
     kv->free_pages.reserve(n_pages);
     for (int i = n_pages - 1; i >= 0; --i) kv->free_pages.push_back(i);  // page 0 lent first
   }
-  const int64_t cache = kv->layer_stride * nl * 2;
+  const int64_t cache = kv->layer_stride * nl * (kv->mx() ? 1 : 2);
   const int64_t half = c.head_dim / 2;
   const int64_t rope = (int64_t)max_ctx * half * 4;
   const int64_t pacc = (int64_t)kMaxBatch * c.n_q_heads * kv->max_split * c.head_dim * 4;
   const int64_t pml = (int64_t)kMaxBatch * c.n_q_heads * kv->max_split * 2 * 4;
   const int64_t tab = paged ? (int64_t)max_users * ppu * 4 : 0;
   char* mem[7] = {nullptr};
-  const int64_t sz[7] = {cache, cache, rope, rope, pacc, pml, tab};
+  const int64_t sz[7] = {cache, kv->mx() ? 0 : cache, rope, rope, pacc, pml, tab};
   for (int i = 0; i < 7; ++i) {
     if (sz[i] == 0) continue;
+    kv->bytes += sz[i];
     if (hipMalloc((void**)&mem[i], sz[i]) != hipSuccess) {
       hipGetLastError();
       for (int j = 0; j < i; ++j)
@@ -706,7 +778,7 @@ static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int3
     }
   }
   hipError_t e = hipMemset(kv->k, 0, cache);
-  if (e == hipSuccess) e = hipMemset(kv->v, 0, cache);
+  if (e == hipSuccess && kv->v) e = hipMemset(kv->v, 0, cache);
   if (e == hipSuccess && kv->table) e = hipMemset(kv->table, 0, tab);
   if (e == hipSuccess) e = hipMemcpy(kv->rcos, tc.data(), rope, hipMemcpyHostToDevice);
   if (e == hipSuccess) e = hipMemcpy(kv->rsin, ts.data(), rope, hipMemcpyHostToDevice);
@@ -722,7 +794,7 @@ static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int3
 }
 
 kf_status kf_kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, kf_kv** out) {
-  return kv_create(s, max_users, max_ctx, 0, out);
+  return kv_create(s, max_users, max_ctx, 0, KF_KV_F16, out);
 }
 
 kf_status kf_kv_create_paged(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_t n_pages, kf_kv** out) {
@@ -730,7 +802,22 @@ kf_status kf_kv_create_paged(kf_stage* s, int32_t max_users, int32_t max_ctx, in
     if (out) *out = nullptr;
     return fail(KF_EINVAL, "n_pages %d < 1", n_pages);
   }
-  return kv_create(s, max_users, max_ctx, n_pages, out);
+  return kv_create(s, max_users, max_ctx, n_pages, KF_KV_F16, out);
+}
+
+kf_status kf_kv_create_typed(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_t n_pages, kf_kv_type type,
+                             kf_kv** out) {
+  if (out) *out = nullptr;
+  if (n_pages < 0) return fail(KF_EINVAL, "n_pages %d < 0", n_pages);
+  if (type != KF_KV_F16 && type != KF_KV_MXFP4) return fail(KF_EINVAL, "cache type %d", (int)type);
+  return kv_create(s, max_users, max_ctx, n_pages, type, out);
+}
+
+kf_status kf_kv_format(const kf_kv* kv, kf_kv_type* type, int64_t* bytes) {
+  if (!kv) return fail(KF_EINVAL, "kv is NULL");
+  if (type) *type = kv->type;
+  if (bytes) *bytes = kv->bytes;
+  return KF_OK;
 }
 
 kf_status kf_kv_pages(const kf_kv* kv, int32_t* total, int32_t* free_pages) {
@@ -771,7 +858,7 @@ kf_status kf_kv_set_len(kf_kv* kv, int32_t user, int32_t len) {
   if (user < 0 || user >= kv->max_users) return fail(KF_EINVAL, "user %d outside [0, %d)", user, kv->max_users);
   if (len < 0 || len > kv->max_ctx) return fail(KF_ERANGE, "length %d outside [0, %d]", len, kv->max_ctx);
   const int64_t upto = len;
-  kf_status st = kv_grant(kv, 1, &user, &upto);
+  kf_status st = kv_grant(kv, 1, &user, &upto, &upto);  // nothing is written
   if (st != KF_OK) return st;
   kv_release(kv, user, pages_for(len));
   kv->len[user] = len;
@@ -796,9 +883,14 @@ kf_status kf_kv_write(kf_kv* kv, int32_t layer, int32_t user, int32_t pos0, int3
   if (!k_dev || !v_dev) return fail(KF_EINVAL, "NULL source");
   if (dtype != KF_F32 && dtype != KF_BF16 && dtype != KF_F16) return fail(KF_EINVAL, "dtype");
   const kf_model_config& c = kv->st->cfg;
-  const int64_t upto = (int64_t)pos0 + n;
-  st = kv_grant(kv, 1, &user, &upto);
+  const int64_t from = pos0, upto = from + n;
+  st = kv_grant(kv, 1, &user, &from, &upto);
   if (st != KF_OK) return st;
+  if (kv->mx()) {
+    KF_HIP(launch_mx_write(kv->layer_ref(layer), user, pos0, k_dev, v_dev, (int)dtype, n, kv->st->err_flag, kv->st->stream),
+           "kv_write launch");
+    return KF_OK;
+  }
   const int64_t off = (layer - kv->st->lo) * kv->layer_stride;
   KF_HIP(launch_kv_write(kv->k + off, kv->v + off, kv->pages(), user, pos0, k_dev, v_dev, (int)dtype, n,
                          c.n_kv_heads, c.head_dim, kv->st->stream),
@@ -817,10 +909,68 @@ kf_status kf_kv_read(const kf_kv* kv, int32_t layer, int32_t user, int32_t pos0,
   if ((int64_t)pos0 + n > (int64_t)kv->held[user] * kKvPage)
     return fail(KF_ERANGE, "positions up to %d of user %d are not in the cache (it holds %d pages)", pos0 + n, user,
                 kv->held[user]);
+  if (kv->mx()) {
+    KF_HIP(launch_mx_read(kv->layer_ref(layer), user, pos0, k_dev, v_dev, n, kv->st->stream), "kv_read launch");
+    return KF_OK;
+  }
   const int64_t off = (layer - kv->st->lo) * kv->layer_stride;
   KF_HIP(launch_kv_read(kv->k + off, kv->v + off, kv->pages(), user, pos0, k_dev, v_dev, n, c.n_kv_heads, c.head_dim,
                         kv->st->stream),
          "kv_read launch");
+  return KF_OK;
+}
+
+kf_status kf_kv_copy(kf_kv* dst, int32_t dst_user, const kf_kv* src, int32_t src_user, int32_t pos0, int32_t n) {
+  if (!dst || !src) return fail(KF_EINVAL, "cache is NULL");
+  if (dst->st != src->st) return fail(KF_EINVAL, "the caches belong to different stages");
+  kf_status st = kv_slice_check(src, src->st->lo, src_user, pos0, n);
+  if (st != KF_OK) return st;
+  st = kv_slice_check(dst, dst->st->lo, dst_user, pos0, n);
+  if (st != KF_OK) return st;
+  if (dst == src && dst_user == src_user) return fail(KF_EINVAL, "user %d copied to itself", src_user);
+  if (n == 0) return KF_OK;
+  if ((int64_t)pos0 + n > (int64_t)src->held[src_user] * kKvPage)
+    return fail(KF_ERANGE, "positions up to %d of user %d are not in the cache (it holds %d pages)", pos0 + n, src_user,
+                src->held[src_user]);
+  const int64_t from = pos0, upto = from + n;
+  st = kv_grant(dst, 1, &dst_user, &from, &upto);
+  if (st != KF_OK) return st;
+  KF_HIP(launch_cache_copy(dst->ref(), dst_user, src->ref(), src_user, pos0, n, dst->layers(), dst->st->err_flag,
+                           dst->st->stream),
+         "kv_copy launch");
+  return KF_OK;
+}
+
+kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n) {
+  if (!kv) return fail(KF_EINVAL, "kv is NULL");
+  for (int u : {src_user, dst_user})
+    if (u < 0 || u >= kv->max_users) return fail(KF_EINVAL, "user %d outside [0, %d)", u, kv->max_users);
+  if (src_user == dst_user) return fail(KF_EINVAL, "user %d forked to itself", src_user);
+  if (n < 0) return fail(KF_EINVAL, "negative count");
+  if (n > kv->len[src_user]) return fail(KF_ERANGE, "%d positions of user %d, which holds %d", n, src_user, kv->len[src_user]);
+  hipStream_t st = kv->st->stream;
+  if (!kv->table) {
+    KF_HIP(launch_cache_copy(kv->ref(), dst_user, kv->ref(), src_user, 0, n, kv->layers(), kv->st->err_flag, st),
+           "kv_fork launch");
+    kv->len[dst_user] = n;
+    return KF_OK;
+  }
+  // The pages are shared; whoever writes to one first takes a copy (kv_grant).
+  // Those that the destination shares already need no new entry.
+  const int pages = pages_for(n);
+  int same = 0;
+  const int *from = &kv->host_table[(size_t)src_user * kv->ppu], *to = &kv->host_table[(size_t)dst_user * kv->ppu];
+  while (same < pages && same < kv->held[dst_user] && from[same] == to[same]) ++same;
+  kv_release(kv, dst_user, same);
+  for (int pg = same; pg < pages; ++pg) {
+    kv->host_table[(size_t)dst_user * kv->ppu + pg] = from[pg];
+    kv->refs[from[pg]]++;
+  }
+  kv->held[dst_user] = pages;
+  if (pages > same)
+    KF_HIP(launch_kv_table_share(kv->table, src_user * kv->ppu + same, dst_user * kv->ppu + same, pages - same, st),
+           "page table update");
+  kv->len[dst_user] = n;
   return KF_OK;
 }
 
@@ -881,6 +1031,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
                           const int32_t* tokens_dev, const void* hidden_in_dev, void* hidden_out_dev, kf_dtype io) {
   if (!s || !kv) return fail(KF_EINVAL, "stage or kv is NULL");
   if (kv->st != s) return fail(KF_EINVAL, "kv belongs to another stage");
+  if (kv->mx()) return fail(KF_EUNSUPPORTED, "an MXFP4 cache is written and read by kf_kv_* calls only");
   if (batch < 1 || batch > kMaxBatch) return fail(KF_EINVAL, "batch %d outside [1, %d]", batch, kMaxBatch);
   if (!users || !positions) return fail(KF_EINVAL, "users / positions is NULL");
   if ((tokens_dev == nullptr) == (hidden_in_dev == nullptr))
@@ -909,9 +1060,12 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
   if (batch > 1) attn_split_mfma(c.n_kv_heads, total_len, max_len, kv->max_split, s->n_cu, &split, &n_split);
   else attn_split(c.n_kv_heads, total_len, max_len, kv->max_split, &split, &n_split);
   if (split % kAttnMfmaAlign) return fail(KF_EINVAL, "split of %d keys breaks the attention kernel's alignment", split);
-  int64_t upto[kMaxBatch];
-  for (int b = 0; b < batch; ++b) upto[b] = (int64_t)positions[b] + 1;
-  const kf_status gst = kv_grant(kv, batch, users, upto);
+  int64_t from[kMaxBatch], upto[kMaxBatch];
+  for (int b = 0; b < batch; ++b) {
+    from[b] = positions[b];
+    upto[b] = from[b] + 1;
+  }
+  const kf_status gst = kv_grant(kv, batch, users, from, upto);
   if (gst != KF_OK) return gst;
   s->kept_rows = 0;  // the residual rows change from here on; set again when the step completes
 
@@ -1218,6 +1372,7 @@ static kf_status prefill_impl(kf_stage* s, kf_kv* kv, int32_t user, int32_t pos0
                               bool no_alloc) {
   if (!s || !kv) return fail(KF_EINVAL, "stage or kv is NULL");
   if (kv->st != s) return fail(KF_EINVAL, "kv belongs to another stage");
+  if (kv->mx()) return fail(KF_EUNSUPPORTED, "an MXFP4 cache is written and read by kf_kv_* calls only");
   if (n < 1) return fail(KF_EINVAL, "n_tokens must be >= 1");
   if (user < 0 || user >= kv->max_users) return fail(KF_EINVAL, "user %d outside [0, %d)", user, kv->max_users);
   if ((tokens_dev == nullptr) == (hidden_in_dev == nullptr))
@@ -1259,8 +1414,8 @@ static kf_status prefill_impl(kf_stage* s, kf_kv* kv, int32_t user, int32_t pos0
     if (e == hipErrorOutOfMemory) return fail(KF_ENOMEM, "device allocation of the prefill workspace");
     KF_HIP(e, "prefill workspace");
   }
-  const int64_t upto = (int64_t)pos0 + n;
-  const kf_status gst = kv_grant(kv, 1, &user, &upto);
+  const int64_t from = pos0, upto = from + n;
+  const kf_status gst = kv_grant(kv, 1, &user, &from, &upto);
   if (gst != KF_OK) return gst;
   const Tracer tr = no_alloc ? Tracer{} : s->tracer();  // event records may create events
   for (int l = s->lo; l < s->hi; ++l) {

@@ -32,7 +32,8 @@ EXPORTS = ("kf_abi_version", "kf_last_error", "kf_stage_bytes", "kf_stage_init",
            "kf_kv_write", "kf_kv_read", "kf_stage_decode", "kf_stage_prefill", "kf_head_logits", "kf_head_argmax",
            "kf_stage_profile", "kf_stage_profile_read", "kf_stage_describe", "kf_kv_describe",
            "kf_kv_create_paged", "kf_kv_pages", "kf_stage_set_flags", "kf_stage_get_flags",
-           "kf_stage_prefill_noalloc")
+           "kf_stage_prefill_noalloc", "kf_kv_create_typed", "kf_kv_format", "kf_kv_copy", "kf_kv_fork")
+KV_TYPES = {"f16": 0, "mxfp4": 1}  # kf_kv_type
 PREFILL_SCRATCH_BYTES = 144 << 20  # KF_PREFILL_SCRATCH_BYTES: the no-allocation prefill's workspace limit
 KF_STAGE_ORDERED = 1  # batch-1 decode adds the heads' output projections in a fixed order
 
@@ -106,6 +107,10 @@ def load_library(path: str = LIB_PATH):
         "kf_stage_describe": (I32, [P, ctypes.POINTER(ModelConfig), I32P, I32P, I32P, ctypes.POINTER(VP), I32P]),
         "kf_kv_describe": (I32, [P, ctypes.POINTER(P), I32P, I32P]),
         "kf_kv_create_paged": (I32, [P, I32, I32, I32, ctypes.POINTER(P)]),
+        "kf_kv_create_typed": (I32, [P, I32, I32, I32, I32, ctypes.POINTER(P)]),
+        "kf_kv_format": (I32, [P, I32P, I64P]),
+        "kf_kv_copy": (I32, [P, I32, P, I32, I32, I32]),
+        "kf_kv_fork": (I32, [P, I32, I32, I32]),
         "kf_kv_pages": (I32, [P, I32P, I32P]),
         "kf_stage_set_flags": (I32, [P, I32]),
         "kf_stage_get_flags": (I32, [P, I32P]),
@@ -262,9 +267,10 @@ class Stage:
                 out[name] = (n.value, t.value)
         return out
 
-    def kv(self, max_users: int, max_ctx: int, pages: int | None = None) -> "KV":
-        """A KV cache; with ``pages`` a paged cache of that many 64-position pages shared by the users."""
-        return KV(self, max_users, max_ctx, pages)
+    def kv(self, max_users: int, max_ctx: int, pages: int | None = None, dtype: str = "f16") -> "KV":
+        """A KV cache of a type of KV_TYPES; with ``pages`` a paged cache of that many 64-position pages shared by
+        the users."""
+        return KV(self, max_users, max_ctx, pages, dtype)
 
     # -- compute
     def decode(self, kv: "KV", users, positions, tokens=None, hidden=None, out=None, keep: bool = False):
@@ -351,11 +357,18 @@ class Stage:
 class KV:
     """A KV reservation of ``max_users`` users x ``max_ctx`` positions for every layer of a stage."""
 
-    def __init__(self, stage: Stage, max_users: int, max_ctx: int, pages: int | None = None):
+    def __init__(self, stage: Stage, max_users: int, max_ctx: int, pages: int | None = None, dtype: str = "f16"):
+        if dtype not in KV_TYPES:
+            raise ValueError(f"cache dtype must be one of {sorted(KV_TYPES)}, not {dtype!r}")
         self.stage, self.max_users, self.max_ctx = stage, max_users, max_ctx
         self._lib = stage._lib
         h = ctypes.c_void_p()
-        if pages is None:
+        if dtype != "f16":
+            if pages is not None and pages < 1:
+                raise ValueError(f"pages {pages} < 1")
+            _check(self._lib.kf_kv_create_typed(stage.handle, max_users, max_ctx, pages or 0, KV_TYPES[dtype],
+                                                ctypes.byref(h)), "kf_kv_create_typed")
+        elif pages is None:
             _check(self._lib.kf_kv_create(stage.handle, max_users, max_ctx, ctypes.byref(h)), "kf_kv_create")
         else:
             _check(self._lib.kf_kv_create_paged(stage.handle, max_users, max_ctx, pages, ctypes.byref(h)),
@@ -386,6 +399,21 @@ class KV:
         t, f = ctypes.c_int32(), ctypes.c_int32()
         _check(self._lib.kf_kv_pages(self.handle, ctypes.byref(t), ctypes.byref(f)), "kf_kv_pages")
         return t.value, f.value
+
+    def format(self):
+        """(type, device bytes) of the cache: a key of KV_TYPES, and all that it holds."""
+        t, b = ctypes.c_int32(), ctypes.c_int64()
+        _check(self._lib.kf_kv_format(self.handle, ctypes.byref(t), ctypes.byref(b)), "kf_kv_format")
+        return {v: k for k, v in KV_TYPES.items()}[t.value], b.value
+
+    def copy(self, src: "KV", src_user: int, dst_user: int, pos0: int, n: int):
+        """Copy positions [pos0, pos0 + n) of ``src_user`` in ``src`` (this cache or another of the stage) to
+        ``dst_user`` here, in every layer (kf_kv_copy)."""
+        _check(self._lib.kf_kv_copy(self.handle, dst_user, src.handle, src_user, pos0, n), "kf_kv_copy")
+
+    def fork(self, src_user: int, dst_user: int, n: int | None = None):
+        """``dst_user`` continues from the first ``n`` (default: all) positions of ``src_user`` (kf_kv_fork)."""
+        _check(self._lib.kf_kv_fork(self.handle, src_user, dst_user, self.len(src_user) if n is None else n), "kf_kv_fork")
 
     def describe(self) -> dict:
         owner, mu, mc = ctypes.c_void_p(), ctypes.c_int32(), ctypes.c_int32()

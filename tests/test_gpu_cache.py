@@ -1,0 +1,293 @@
+"""Caches of both types: what they hold, copies between them, and users that share pages."""
+
+import numpy as np
+import pytest
+
+import synth
+from tests import mx_ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    if not t.cuda.is_available():
+        pytest.skip("no GPU")
+    return t
+
+
+@pytest.fixture(scope="module")
+def st():
+    from paper_2609_34045_amd import stage
+    return stage
+
+
+def bare_stage(st, nkv, hd, layers=1, group=1):
+    """A stage whose weights are all zero: only its caches are used."""
+    shape = synth.ModelShape(layers, 64, nkv * group, nkv, hd, 64, 0)
+    layer = {k: np.zeros(shape.tensor_shape(k), np.uint16) for k in shape.layer_kinds()}
+    return st.Stage(shape, 0, layers, lambda l: layer)
+
+
+def rows(seed, n, nkv, hd, scale=1.0):
+    return np.random.default_rng(seed).normal(size=(n, nkv, hd)).astype(np.float32) * np.float32(scale)
+
+
+def held(x, dtype):
+    with np.errstate(over="ignore"):
+        return mx_ref.stored(x) if dtype == "mxfp4" else x.astype(np.float16).astype(np.float64)
+
+
+def host(pair):
+    return [t.cpu().numpy().astype(np.float64) for t in pair]
+
+
+def check(kv, layer, user, pos0, k, v, what=""):
+    got = host(kv.read(layer, user, pos0, len(k)))
+    for name, g, w in (("k", got[0], k), ("v", got[1], v)):
+        assert np.array_equal(g, w), (what, name, np.argwhere(g != w)[:4].tolist())
+
+
+@pytest.mark.parametrize("io", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("hd,nkv,pos0,n,paged", [(128, 2, 0, 1, False), (64, 1, 63, 2, True), (128, 3, 5, 64, True),
+                                                 (64, 3, 1, 200, False), (128, 1, 130, 61, False), (64, 2, 64, 64, True)])
+def test_mxfp4_holds_the_nearest_values(torch, st, io, hd, nkv, pos0, n, paged):
+    """Written positions come back as the format's roundings, exactly, for every source type and alignment of positions
+    to pages, bytes and nibbles; positions beside them stay as they were."""
+    g = bare_stage(st, nkv, hd, layers=2)
+    ctx = pos0 + n + 70
+    kv = g.kv(2, ctx, 2 * ((ctx + 63) // 64) if paged else None, dtype="mxfp4")
+    old = [rows(7 + i, ctx, nkv, hd) for i in range(2)]
+    kv.write(1, 1, 0, *(torch.from_numpy(x).cuda() for x in old))
+    new = [torch.from_numpy(rows(3 + i, n, nkv, hd, 10.0 ** (i - 1))).to(getattr(torch, io)).cuda() for i in range(2)]
+    kv.write(1, 1, pos0, *new)
+    want = [held(x, "mxfp4") for x in old]
+    for w, x in zip(want, new):
+        w[pos0:pos0 + n] = held(x.float().cpu().numpy(), "mxfp4")
+    check(kv, 1, 1, 0, *want)
+    check(kv, 1, 1, pos0, *(w[pos0:pos0 + n] for w in want))
+    g.sync()
+    kv.close()
+    g.close()
+
+
+def test_every_block_magnitude_and_ties(torch, st):
+    """Blocks whose largest value runs over every fp16 exponent, at mantissas on both sides of the one that moves the
+    shared exponent, with values on the middles between elements; zeros; and rows at odd addresses."""
+    g = bare_stage(st, 1, 64)
+    n = 41 * 7
+    x = np.zeros((n, 1, 64), np.float32)
+    with np.errstate(over="ignore"):
+        for i, e in enumerate(range(-25, 16)):
+            for j, m in enumerate((1.0, 1.25, 1.5, 1.7490234375, 1.75, 1.7509765625, 1.9990234375)):
+                r = x[7 * i + j, 0]
+                r[0], r[32] = m * 2.0 ** e, -m * 2.0 ** e
+                r[1:17] = np.arange(16) / 16 * 2.0 ** e * 1.75
+                r[33:62] = -np.arange(29) / 32 * 2.0 ** e
+    x = np.clip(x, -65504, 65504)
+    kv = g.kv(1, n, dtype="mxfp4")
+    flat = torch.zeros(2 * x.size + 3, device="cuda")
+    k, v = (flat[1 + i * x.size:1 + (i + 1) * x.size].view(n, 1, 64) for i in range(2))  # not 16-byte aligned
+    k.copy_(torch.from_numpy(x))
+    v.copy_(torch.from_numpy(-x[::-1].copy()))
+    kv.write(0, 0, 0, k, v)
+    check(kv, 0, 0, 0, mx_ref.stored(x), mx_ref.stored(-x[::-1]))
+    g.sync()
+    kv.close()
+    g.close()
+
+
+def test_values_that_do_not_fit(torch, st):
+    """Infinities and what fp16 rounds to one are stored as 49152, NaN as 0, with the range error; the other blocks of
+    the row are as without them."""
+    g = bare_stage(st, 1, 128)
+    kv = g.kv(1, 64, dtype="mxfp4")
+    k, v = rows(1, 3, 1, 128), rows(2, 3, 1, 128)
+    kv.write(0, 0, 0, torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda())
+    g.sync()
+    k[0, 0, 5], k[1, 0, 40], v[2, 0, 127], v[1, 0, 0] = np.inf, np.nan, -70000.0, 60000.0
+    kv.write(0, 0, 0, torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda())
+    got = host(kv.read(0, 0, 0, 3))
+    want = [mx_ref.stored(x) for x in (k, v)]
+    assert want[0][0, 0, 5] == 49152 and want[0][1, 0, 40] == 0 and want[1][2, 0, 127] == -49152 and want[1][1, 0, 0] == 49152
+    assert all(np.array_equal(a, b) for a, b in zip(got, want))
+    with pytest.raises(st.KFError) as e:
+        g.sync()
+    assert e.value.status == 3
+    v[1, 0, 0] = 49152  # a finite value past the largest element raises nothing
+    kv.write(0, 0, 0, torch.from_numpy(rows(1, 3, 1, 128)).cuda(), torch.from_numpy(np.abs(v).clip(0, 65504)).cuda())
+    g.sync()
+    kv.close()
+    g.close()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("src,dst", [("f16", "mxfp4"), ("mxfp4", "f16"), ("mxfp4", "mxfp4"), ("f16", "f16")])
+@pytest.mark.parametrize("pos0,n,paged", [(0, 1, False), (3, 130, True), (65, 62, False), (64, 128, True), (17, 0, False)])
+def test_copies_between_caches(torch, st, hd, src, dst, pos0, n, paged):
+    """A copy holds what writing the source's values would have, in every layer, and leaves every other position."""
+    nkv, layers, ctx = 2, 2, 260
+    g = bare_stage(st, nkv, hd, layers)
+    a = g.kv(2, ctx, None if paged else 10, dtype=src)
+    b = g.kv(3, ctx, 14 if paged else None, dtype=dst)
+    x, y = ([[rows(100 * s + 10 * l + i, ctx, nkv, hd) for i in range(2)] for l in range(layers)] for s in (1, 2))
+    for l in range(layers):
+        a.write(l, 1, 0, *(torch.from_numpy(t).cuda() for t in x[l]))
+        b.write(l, 2, 0, *(torch.from_numpy(t).cuda() for t in y[l]))
+    b.copy(a, 1, 2, pos0, n)
+    assert b.len(2) == 0  # lengths stay
+    for l in range(layers):
+        want = [held(t, dst) for t in y[l]]
+        for w, t in zip(want, x[l]):
+            w[pos0:pos0 + n] = held(held(t, src)[pos0:pos0 + n], dst)
+        check(b, l, 2, 0, *want, what=f"layer {l}")
+        check(a, l, 1, 0, *(held(t, src) for t in x[l]), what="source")
+    g.sync()
+    a.close()
+    b.close()
+    g.close()
+
+
+def test_copy_within_a_cache_and_refusals(torch, st):
+    g, other = bare_stage(st, 1, 64), bare_stage(st, 1, 64)
+    kv, far = g.kv(3, 100, 4, dtype="mxfp4"), other.kv(1, 100)
+    x = [rows(i, 70, 1, 64) for i in range(2)]
+    kv.write(0, 0, 0, *(torch.from_numpy(t).cuda() for t in x))
+    kv.copy(kv, 0, 1, 0, 70)
+    check(kv, 0, 1, 0, *(held(t, "mxfp4") for t in x))
+    assert kv.pages() == (4, 0)
+
+    def refused(status, call):
+        with pytest.raises(st.KFError) as e:
+            call()
+        assert e.value.status == status
+    refused(2, lambda: kv.copy(kv, 0, 2, 0, 1))      # no page left
+    refused(1, lambda: kv.copy(kv, 0, 0, 0, 1))      # onto itself
+    refused(1, lambda: kv.copy(kv, 3, 0, 0, 1))
+    refused(1, lambda: kv.copy(kv, 0, -1, 0, 1))
+    refused(1, lambda: kv.copy(kv, 0, 1, -1, 1))
+    refused(3, lambda: kv.copy(kv, 0, 1, 60, 41))    # past max_ctx
+    refused(3, lambda: kv.copy(kv, 2, 1, 0, 1))      # the source holds no page
+    refused(1, lambda: kv.copy(far, 0, 0, 0, 1))     # another stage's cache
+    refused(1, lambda: kv.fork(0, 0, 0))
+    refused(1, lambda: kv.fork(0, 3, 0))
+    refused(1, lambda: kv.fork(-1, 0, 0))
+    refused(1, lambda: kv.fork(0, 1, -1))
+    refused(3, lambda: kv.fork(0, 1, 1))             # the source's length is 0
+    assert kv.pages() == (4, 0)
+    g.sync()
+    kv.close()
+    far.close()
+    g.close()
+    other.close()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "mxfp4"])
+@pytest.mark.parametrize("hd,n", [(64, 130), (128, 1), (128, 128), (64, 63)])
+def test_reserved_fork_copies(torch, st, dtype, hd, n):
+    g = bare_stage(st, 2, hd, layers=2)
+    kv = g.kv(2, 200, dtype=dtype)
+    x = [[rows(10 * l + i, 150, 2, hd) for i in range(2)] for l in range(2)]
+    for l in range(2):
+        kv.write(l, 1, 0, *(torch.from_numpy(t).cuda() for t in x[l]))
+    kv.set_len(1, 150)
+    kv.fork(1, 0, n)
+    assert (kv.len(0), kv.len(1)) == (n, 150) and kv.pages()[1] == -1
+    for l in range(2):
+        check(kv, l, 0, 0, *(held(t, dtype)[:n] for t in x[l]))
+    kv.write(0, 0, 0, *(torch.from_numpy(t[1:2]).cuda() for t in x[1]))  # its own positions from here on
+    check(kv, 0, 1, 0, *(held(t, dtype) for t in x[0]))
+    kv.fork(1, 0)
+    assert kv.len(0) == 150
+    g.sync()
+    kv.close()
+    g.close()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "mxfp4"])
+def test_forks_share_pages_until_a_write(torch, st, dtype):
+    """Three users of one prompt take its pages once; each write copies the page it touches for the writer alone (the
+    last holder writes in place), and pages come back with their last user."""
+    hd, nkv, layers = 128, 2, 2
+    g = bare_stage(st, nkv, hd, layers)
+    kv = g.kv(4, 400, 9, dtype=dtype)
+    x = [[rows(10 * l + i, 300, nkv, hd) for i in range(2)] for l in range(layers)]
+    new = [[rows(50 + 10 * u + i, 2, nkv, hd) for i in range(2)] for u in range(3)]
+    for l in range(layers):
+        kv.write(l, 0, 0, *(torch.from_numpy(t[:150]).cuda() for t in x[l]))
+    kv.set_len(0, 150)  # 3 pages, the last one part full
+    kv.fork(0, 1)
+    kv.fork(0, 2, 149)
+    assert kv.pages() == (9, 6) and [kv.len(u) for u in range(4)] == [150, 150, 149, 0]
+    base = [[held(t, dtype) for t in x[l]] for l in range(layers)]
+    for u in (0, 1, 2):
+        for l in range(layers):
+            check(kv, l, u, 0, *(t[:149] for t in base[l]))
+    # one position appended for each, in every layer: two copies, then the third user owns the page alone
+    for u, free in ((1, 5), (2, 4), (0, 4)):
+        for l in range(layers):
+            kv.write(l, u, kv.len(u), *(torch.from_numpy(t[:1]).cuda() for t in new[u]))
+        kv.set_len(u, kv.len(u) + 1)
+        assert kv.pages() == (9, free), u
+    for u, n in ((0, 150), (1, 150), (2, 149)):
+        for l in range(layers):
+            want = [np.concatenate([t[:n], held(c[:1], dtype)]) for t, c in zip(base[l], new[u])]
+            check(kv, l, u, 0, *want, what=f"user {u}")
+    # a write over the first, shared page in the middle of a prompt
+    kv.write(0, 2, 10, *(torch.from_numpy(t).cuda() for t in new[2]))
+    assert kv.pages() == (9, 3)
+    check(kv, 0, 0, 10, *(t[10:12] for t in base[0]))
+    check(kv, 0, 2, 10, *(held(t, dtype) for t in new[2]))
+    check(kv, 1, 2, 0, *(t[:149] for t in base[1]))  # the copy took every layer along
+    # giving back: the prompt's pages stay while any user holds them
+    kv.set_len(0, 0)
+    assert kv.pages() == (9, 4)
+    check(kv, 0, 1, 0, *(t[:150] for t in base[0]))
+    kv.set_len(1, 70)   # a shorter user: its pages past 70 come back where it held them alone
+    assert kv.pages() == (9, 5)
+    kv.fork(1, 0)
+    kv.fork(1, 2)       # in place of what user 2 held: pages 0 (its own), 1 (shared with user 1), 2 (its own)
+    assert kv.pages() == (9, 7) and kv.len(2) == 70
+    for u in (0, 1, 2):
+        check(kv, 0, u, 0, *(t[:70] for t in base[0]))
+    for u in (0, 1, 2):
+        kv.set_len(u, 0)
+    assert kv.pages() == (9, 9)
+    g.sync()
+    kv.close()
+    g.close()
+
+
+def test_a_short_pool_refuses_a_write_to_a_shared_page(torch, st):
+    g = bare_stage(st, 1, 64)
+    kv = g.kv(3, 200, 2, dtype="mxfp4")
+    x = [rows(i, 100, 1, 64) for i in range(2)]
+    on = lambda a: [torch.from_numpy(t).cuda() for t in a]  # noqa: E731
+    kv.write(0, 0, 0, *on(x))
+    kv.set_len(0, 100)
+    kv.fork(0, 1)
+    assert kv.pages() == (2, 0)
+    with pytest.raises(st.KFError) as e:
+        kv.write(0, 1, 100, *on([t[:1] for t in x]))
+    assert e.value.status == 2 and kv.pages() == (2, 0) and kv.len(1) == 100
+    check(kv, 0, 0, 0, *(held(t, "mxfp4") for t in x))
+    kv.set_len(0, 64)  # user 1 now holds the second page alone and writes in place
+    kv.write(0, 1, 100, *on([t[:1] for t in x]))
+    check(kv, 0, 1, 0, *(np.concatenate([held(t, "mxfp4"), held(t[:1], "mxfp4")]) for t in x))
+    g.sync()
+    kv.close()
+    g.close()
+
+
+def test_format_and_bytes(torch, st):
+    g = bare_stage(st, 2, 128, layers=3)
+    a, b = g.kv(2, 1000), g.kv(2, 1000, dtype="mxfp4")
+    assert a.format()[0] == "f16" and b.format()[0] == "mxfp4"
+    pages = 3 * 2 * 16 * 2 * 64 * 128  # layers, users, pages each, heads, positions, values
+    both = a.format()[1] - 2 * 2 * pages, b.format()[1] - 2 * pages * 17 // 32
+    assert 0 < both[0] <= both[1]  # tables and workspaces: an MXFP4 cache may keep more
+    assert b.describe()["max_ctx"] == 1000
+    a.close()
+    b.close()
+    g.close()
