@@ -50,7 +50,7 @@ extern "C" {
                             5: a head stage's decode may keep its output rows (hidden_out_dev NULL)
                                for kf_head_logits / kf_head_argmax with hidden_dev NULL.
                             Calls added since leave the others as they are: kf_kv_create_typed,
-                            kf_kv_format, kf_kv_copy, kf_kv_fork */
+                            kf_kv_format, kf_kv_copy, kf_kv_fork, kf_kv_attend */
 #define KF_KV_PAGE 64     /* positions per KV cache page */
 #define KF_MAX_BATCH 4
 
@@ -230,7 +230,9 @@ kf_status kf_kv_create_paged(kf_stage* stage, int32_t max_users, int32_t max_ctx
  * become that.  Every stored value is an fp16 number.  Infinities and what fp16 rounds
  * to one are stored as 49152, a NaN as 0, and all three raise the stage's range
  * error (KF_ERANGE from kf_stage_sync).
- * kf_stage_decode and kf_stage_prefill take KF_KV_F16 caches only (else KF_EUNSUPPORTED).  KF_EINVAL for a negative n_pages or an unknown type.
+ * Every call takes caches of both types.  Decode attends to the new position as it is
+ * stored.  Prefill attends through fp16 pages of one user and layer that an MXFP4 cache keeps
+ * beside its own (max_ctx positions).  KF_EINVAL for a negative n_pages or an unknown type.
  */
 typedef enum { KF_KV_F16 = 0, KF_KV_MXFP4 = 1 } kf_kv_type;
 kf_status kf_kv_create_typed(kf_stage* stage, int32_t max_users, int32_t max_ctx, int32_t n_pages, kf_kv_type type,
@@ -294,6 +296,22 @@ kf_status kf_kv_copy(kf_kv* dst, int32_t dst_user, const kf_kv* src, int32_t src
  * above src_user's length.
  */
 kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n);
+
+/*
+ * Attention of given queries over cached positions of one held layer, as a decode step
+ * attends: out[b][h] = softmax(q[b][h] . K^T / sqrt(hd)) V over positions [0, lens[b]) of
+ * users[b], query head h reading KV head h / (nq / nkv).
+ *   rows : 1..KF_MAX_BATCH; users may repeat (several queries of one user, or users
+ *          that share pages); lens[b] 0 gives a row of zeros
+ *   q_dev : [rows, nq, hd] rotated queries in io (KF_F32, KF_BF16 or KF_F16), 16-byte aligned
+ *   out_dev : [rows, nq, hd] in io; may be q_dev
+ * Over an MXFP4 cache the products take queries and probabilities in two parts each (16 and more
+ * bits) and fp32 sums; over an fp16 cache they are rounded to fp16, as in a decode step.  A query head
+ * that holds a NaN gives NaN.  KF_ERANGE for lens[b] beyond max_ctx or the pages the user holds.
+ * Changes nothing in the cache.  Enqueued on the stage's stream.
+ */
+kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* users, const int32_t* lens,
+                       const void* q_dev, kf_dtype io, void* out_dev);
 
 /*
  * Forward one token for each of `batch` (1..KF_MAX_BATCH) users (decode): the

@@ -1,0 +1,418 @@
+// Attention over an MXFP4 cache for one query row of each of up to four users, the
+// append of a decode step's keys and values to such a cache, and the call that
+// attends with given queries (kf_kv_attend) over caches of both types.
+//
+//   out_h = sum_t p_t v_t / sum_t p_t,  p_t = 2^(s_t - m),  s_t = q_h . k_t log2(e) / sqrt(hd)
+//
+// over the first len positions, a running maximum m per query head, 32-bit sums.
+// A workgroup (split, KV head, row) takes whole pages of 64 positions for all G
+// query heads of the KV head, so that each cached byte is read once per KV head
+// and row; its waves take the split's pages in turn and keep states of their own
+// until the end.  A lane loads a page's codes and exponents straight into the
+// registers it computes from (kernels.h gives the order), the next page while one
+// is computed: nothing passes through LDS, and no wave waits for another.
+//
+// Scores: S = K Q^T on 16x16x32 fp16 MFMAs, K decoded by the convert instruction
+// that takes two E2M1 codes and the block's power of two (exact in fp16).  The 16
+// columns of a tile hold 8 query heads twice, as two fp16 parts of each query
+// value (columns 0-7 the rounded value, 8-15 what rounding left), so that a score
+// is as exact as 22-bit queries give it at no more products than one part would
+// take.  P V: O^T = V^T P^T on bf16 MFMAs.  V's exponents differ by position,
+// which is the reduction's index there, so they multiply the probabilities:
+// bf16 has fp32's exponent range, and the same two halves of the columns hold the
+// two parts of a probability.  The score tile's lane layout is the P^T operand's.
+#include <cmath>
+
+#include "kernels.h"
+
+namespace kf {
+
+namespace {
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float ror8(float v) {  // the lane 8 apart within each row of 16
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float groups_max(float x) {  // over the four 16-lane groups
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float groups_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ __forceinline__ float exponent(uint32_t w, int byte) {  // 2^e of a stored exponent
+  return __uint_as_float(((w >> (8 * byte)) & 255u) << 23);
+}
+
+// 8 consecutive values of a query row.
+__device__ __forceinline__ void load_q8(const void* q, int type, int64_t at, float (&f)[8]) {
+  if (type == 0) {
+    const v4f* p = reinterpret_cast<const v4f*>(reinterpret_cast<const float*>(q) + at);
+    const v4f a = p[0], b = p[1];
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    return;
+  }
+  const v4u w = *reinterpret_cast<const v4u*>(reinterpret_cast<const uint16_t*>(q) + at);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint16_t h = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+    f[i] = type == 1 ? __uint_as_float((uint32_t)h << 16) : (float)__builtin_bit_cast(_Float16, h);
+  }
+}
+// An output value in fp32, bf16 or fp16 (nearest even).
+__device__ __forceinline__ void store_out(void* out, int type, int64_t at, float v) {
+  if (type == 0) reinterpret_cast<float*>(out)[at] = v;
+  else if (type == 1) reinterpret_cast<__bf16*>(out)[at] = (__bf16)v;
+  else reinterpret_cast<_Float16*>(out)[at] = (_Float16)v;
+}
+
+constexpr int kWaves = 4;
+// The maximum moves only when a page's exceeds it by this much (log2 units); probabilities stay
+// below 2^8, which neither bf16 nor the fp32 sums mind, and the rescaling of O is rare.
+constexpr float kLazyMax = 8.0f;
+
+template <int HD>
+struct MxPage {
+  v4u k[HD / 32], v[HD / 32];
+  uint32_t ks;
+  v4u vs[HD / 32];
+};
+}  // namespace
+
+template <int HD>
+__global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnParams p) {
+  constexpr int NS = HD / 32, NT = HD / 16, NB = HD / kMxBlock;
+  constexpr int CODES = mx_codes(HD), EXPS = mx_exps(HD), REC = mx_record(HD);
+  constexpr int SROW = HD + 4;  // a head's row of a wave's state in LDS
+  __shared__ __attribute__((aligned(16))) float state[kWaves][8 * SROW];
+  __shared__ float state_m[kWaves][8], state_l[kWaves][8];
+
+  const int split = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = p.a.nq / p.a.nkv, hq0 = g * G;
+  const int col = lane & 15, grp = lane >> 4, head = col & 7;
+  const bool low = col >= 8;  // this lane's column holds the low parts
+
+  const int len = p.a.len[b], u = p.a.users[b];
+  const int page0 = split * (p.a.split / kKvPage);
+  const int pages = min(p.a.split / kKvPage, (len + kKvPage - 1) / kKvPage - page0);
+  auto put = [&](int h, int d, float v, float m, float l) {
+    if (p.out) {
+      store_out(p.out, p.io, ((int64_t)b * p.a.nq + hq0 + h) * HD + d, len ? v / l : 0.f);
+      return;
+    }
+    const int64_t row = ((int64_t)b * p.a.nq + hq0 + h) * p.a.max_split + split;
+    p.a.part_acc[row * HD + d] = v;
+    if (d == 0) {
+      p.a.part_ml[row * 2] = m;
+      p.a.part_ml[row * 2 + 1] = l;
+    }
+  };
+  if (pages <= 0) {  // a trailing split of a shorter row, or a row without positions
+    for (int e = tid; e < G * HD; e += 64 * kWaves) put(e / HD, e % HD, 0.f, -INFINITY, 0.f);
+    return;
+  }
+
+  // A split has at most kAttnMaxSplit / kKvPage pages: lane i holds the id of page i.
+  int pid = 0;
+  if (lane < pages) pid = kv_page(p.a.kv, u, page0 + lane);
+  const uint8_t* heads = p.rec + (int64_t)g * REC;
+  auto load = [&](MxPage<HD>& pg, int i) {
+    const uint8_t* rec = heads + (int64_t)__builtin_amdgcn_readlane(pid, i) * p.a.kv.page_stride;
+#pragma unroll
+    for (int j = 0; j < HD / 32; ++j) pg.k[j] = *reinterpret_cast<const v4u*>(rec + j * 1024 + lane * 16);
+    pg.ks = *reinterpret_cast<const uint32_t*>(rec + CODES + ((HD == 128 ? grp : grp / 2) * 16 + col) * 4);
+#pragma unroll
+    for (int j = 0; j < HD / 32; ++j)
+      pg.v[j] = *reinterpret_cast<const v4u*>(rec + CODES + EXPS + j * 1024 + lane * 16);
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      pg.vs[j] = *reinterpret_cast<const v4u*>(rec + 2 * CODES + EXPS + (grp * NB + j) * 16);
+  };
+  MxPage<HD> even, odd;
+  if (wave < pages) load(even, wave);
+
+  // The query operand: step s, d = grp hd/4 + 8 s .. + 7 of this column's head, in log2
+  // units and scaled by a power of two that puts its largest value near 2^10, so that the
+  // fp16 parts neither overflow nor lose bits below the normal range.
+  h8 qf[NS];
+  float unscale;
+  {
+    float f[NS][8], top = 0.f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      load_q8(p.q, p.q_type, ((int64_t)b * p.a.nq + hq0 + min(head, G - 1)) * HD + grp * (HD / 4) + 8 * s, f[s]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        f[s][j] *= p.a.scale_log2;
+        top = fmaxf(top, __builtin_fabsf(f[s][j]));
+      }
+    }
+    top = groups_max(top);
+    const int e = top > 0.f && top < INFINITY ? min(max(10 - ilogbf(top), -100), 100) : 0;
+    unscale = ldexpf(1.0f, -e);
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float x = ldexpf(f[s][j], e);
+        const _Float16 hi = (_Float16)x;
+        qf[s][j] = head >= G ? (_Float16)0.f : low ? (_Float16)(x - (float)hi) : hi;
+      }
+  }
+
+  v4f o[NT];  // O^T tile t: lane holds d = 16 t + 4 grp + r of its column's part
+#pragma unroll
+  for (int t = 0; t < NT; ++t) o[t] = v4f{0.f, 0.f, 0.f, 0.f};
+  float m_run = -INFINITY, l_run = 0.f;
+
+  auto compute = [&](const MxPage<HD>& pg, int i) {
+    v4f sc[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const float scale = exponent(pg.ks, t);
+      sc[t] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const uint32_t w = HD == 128 ? pg.k[t][s] : pg.k[t / 2][(t % 2) * 2 + s];
+        const v4u kf = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0)),
+                        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1)),
+                        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2)),
+                        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3))};
+        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, kf), qf[s], sc[t], 0, 0, 0);
+      }
+    }
+    const int left = len - (page0 + i) * kKvPage;  // positions of the page
+    float mb = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float x = (sc[t][r] + ror8(sc[t][r])) * unscale;
+        if (16 * t + 4 * grp + r >= left) x = -INFINITY;
+        sc[t][r] = x;
+        mb = fmaxf(mb, x);
+      }
+    mb = groups_max(mb);
+    const float m_new = mb > m_run + kLazyMax ? mb : m_run;
+    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);  // 0 while m_run is -inf
+    float part[4][4], ls = 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float x = __builtin_amdgcn_exp2f(sc[t][r] - m_new);
+        ls += x;
+        const float hi = (float)(__bf16)x;
+        part[t][r] = low ? x - hi : hi;
+      }
+    l_run = l_run * alpha + ls;
+    m_run = m_new;
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o[t] *= alpha;
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) {
+        b8 pf;  // scaling by a power of two is exact, so the parts round here as they would unscaled
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pf[j] = (__bf16)(part[2 * s + j / 4][j % 4] * exponent(pg.vs[blk][2 * s + j / 4], j % 4));
+#pragma unroll
+        for (int t = 2 * blk; t < 2 * blk + 2; ++t) {
+          const uint32_t w = pg.v[t / 2][(t % 2) * 2 + s];
+          const v4u vf = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0)),
+                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1)),
+                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2)),
+                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3))};
+          o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, vf), pf, o[t], 0, 0, 0);
+        }
+      }
+    }
+  };
+  for (int i = wave; i < pages; i += 2 * kWaves) {
+    if (i + kWaves < pages) load(odd, i + kWaves);
+    compute(even, i);
+    if (i + 2 * kWaves < pages) load(even, i + 2 * kWaves);
+    if (i + kWaves < pages) compute(odd, i + kWaves);
+  }
+  l_run = groups_sum(l_run);
+
+  // The waves' states meet in LDS; the two parts of a column are one head.
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    v4f x;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] = o[t][r] + ror8(o[t][r]);
+    if (!low) *reinterpret_cast<v4f*>(&state[wave][head * SROW + 16 * t + 4 * grp]) = x;
+  }
+  if (lane < 8) {
+    state_m[wave][lane] = m_run;
+    state_l[wave][lane] = l_run;
+  }
+  __syncthreads();
+  for (int e = tid; e < G * HD; e += 64 * kWaves) {
+    const int h = e / HD, d = e % HD;
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, state_m[w][h]);
+    float v = 0.f, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      // M is -inf only where every score was NaN (a query that is not finite): the sums stay NaN
+      const float f = M == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(state_m[w][h] - M);
+      v += f * state[w][h * SROW + d];
+      l += f * state_l[w][h];
+    }
+    put(h, d, v, M, l);
+  }
+}
+
+// Merge of a row's split partials into the output of kf_kv_attend; a row without
+// positions gives zeros.  Workgroup (head, row); wave w sums every fourth split.
+template <int HD>
+__global__ __launch_bounds__(256) void attend_merge_kernel(const MxAttnParams p) {
+  constexpr int DPL = HD / 64;
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t r0 = ((int64_t)b * p.a.nq + h) * p.a.max_split;
+  const float* ml = p.a.part_ml + r0 * 2;
+  const float* acc = p.a.part_acc + r0 * HD + lane * DPL;
+  __shared__ float red[4][HD], red_l[4];
+  float M = -INFINITY;
+  for (int s = lane; s < p.a.n_split; s += 64) M = fmaxf(M, ml[2 * s]);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+  float v[DPL] = {}, l = 0.f;
+  for (int s = wave; s < p.a.n_split; s += 4) {
+    const float f = M == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml[2 * s] - M);
+    l += f * ml[2 * s + 1];
+#pragma unroll
+    for (int i = 0; i < DPL; ++i) v[i] += f * acc[(int64_t)s * HD + i];
+  }
+#pragma unroll
+  for (int i = 0; i < DPL; ++i) red[wave][lane * DPL + i] = v[i];
+  if (lane == 0) red_l[wave] = l;
+  __syncthreads();
+  if (tid < HD) {
+    const float x = (red[0][tid] + red[1][tid]) + (red[2][tid] + red[3][tid]);
+    l = (red_l[0] + red_l[1]) + (red_l[2] + red_l[3]);
+    store_out(p.out, p.io, ((int64_t)b * p.a.nq + h) * HD + tid, p.a.len[b] ? x / l : 0.f);
+  }
+}
+
+// The new key and value of each row of a decode step, to its position of an MXFP4
+// cache.  hd / 8 lanes hold a head, 8 values each.  In blocks with per-head norms
+// the keys come raw and are normalised and rotated here, and so are the queries, in
+// place.
+__global__ __launch_bounds__(256) void mx_append_kernel(const MxAppendParams p) {
+  const int hd = p.hd, per = hd / 8, i = blockIdx.x * 256 + threadIdx.x;
+  const int item = i / per, d0 = (i % per) * 8;
+  const int nq = p.gq ? p.nq : 0, heads = nq + 2 * p.nkv;  // queries, keys, values
+  const int b = item / heads, h = item % heads;
+  if (b >= p.batch) return;  // whole heads: a head's lanes leave together
+  const int g = h < nq ? 0 : (h - nq) % p.nkv;
+  const bool is_v = h >= nq + p.nkv;
+  float* src = h < nq ? p.q + ((int64_t)b * p.nq + h) * hd : (is_v ? p.v : p.k) + ((int64_t)b * p.nkv + g) * hd;
+  float x[8];
+  load_q8(src, 0, d0, x);
+  if (p.gq && !is_v) {
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss += x[j] * x[j];
+    for (int o = 1; o < per; o <<= 1) ss += __shfl_xor(ss, o);
+    const float rs = 1.0f / sqrtf(ss / (float)hd + p.eps);
+    float gain[8];
+    load_q8(h < nq ? p.gq : p.gk, 1, d0, gain);
+    const int i0 = d0 % (hd / 2);
+    const float sign = d0 < hd / 2 ? -1.f : 1.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] *= rs * gain[j];
+    float y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float other = __shfl_xor(x[j], per / 2);
+      const int64_t at = (int64_t)p.pos[b] * (hd / 2) + i0 + j;
+      y[j] = x[j] * p.rope_cos[at] + sign * other * p.rope_sin[at];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = y[j];
+    if (h < nq) {
+      reinterpret_cast<v4f*>(src + d0)[0] = v4f{x[0], x[1], x[2], x[3]};
+      reinterpret_cast<v4f*>(src + d0)[1] = v4f{x[4], x[5], x[6], x[7]};
+      return;
+    }
+  }
+  bool bad = false;
+  int e;
+  const uint32_t w = mx_encode8(x, e, bad);
+  raise_err(p.err_flag, bad, kErrF16Range);
+  const int t = p.pos[b] % kKvPage;
+  const int codes = mx_codes(hd), exps = mx_exps(hd);
+  uint8_t* rec = p.rec + (int64_t)kv_page(p.kv, p.users[b], p.pos[b] / kKvPage) * p.kv.page_stride +
+                 (int64_t)g * mx_record(hd) + (is_v ? codes + exps : 0);
+  const int blk = d0 / kMxBlock;
+  if (!is_v) {
+    *reinterpret_cast<uint32_t*>(rec + (hd == 128 ? mx_k_byte<128>(t, d0) : mx_k_byte<64>(t, d0))) = w;
+    if (d0 % kMxBlock == 0) rec[codes + mx_k_exp(t, blk)] = (uint8_t)(e + 127);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {  // the other nibble of each byte is a neighbouring position's
+    uint8_t* at = rec + mx_v_byte(t, d0 + j);
+    const uint32_t c = (w >> (4 * j)) & 15u;
+    *at = (uint8_t)(t & 1 ? (*at & 0x0f) | (c << 4) : (*at & 0xf0) | c);
+  }
+  if (d0 % kMxBlock == 0) rec[codes + (hd == 128 ? mx_v_exp<128>(t, blk) : mx_v_exp<64>(t, blk))] = (uint8_t)(e + 127);
+}
+
+__global__ void rows_to_f32_kernel(const void* src, int type, float* dst, int n8) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= n8) return;
+  float f[8];
+  load_q8(src, type, (int64_t)i * 8, f);
+  reinterpret_cast<v4f*>(dst)[2 * i] = v4f{f[0], f[1], f[2], f[3]};
+  reinterpret_cast<v4f*>(dst)[2 * i + 1] = v4f{f[4], f[5], f[6], f[7]};
+}
+
+// ------------------------------------------------------------------ launchers
+hipError_t launch_attn_mx(const MxAttnParams& p, int batch, hipStream_t s) {
+  if (p.a.nq % p.a.nkv || p.a.nq / p.a.nkv > 8 || p.a.split % kKvPage || p.a.split > kAttnMaxSplit) return hipErrorInvalidValue;
+  const dim3 grid(p.a.n_split, p.a.nkv, batch);
+  if (p.a.hd == 128) hipLaunchKernelGGL(attn_mx_kernel<128>, grid, dim3(64 * kWaves), 0, s, p);
+  else if (p.a.hd == 64) hipLaunchKernelGGL(attn_mx_kernel<64>, grid, dim3(64 * kWaves), 0, s, p);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+hipError_t launch_attend_merge(const MxAttnParams& p, int batch, hipStream_t s) {
+  const dim3 grid(p.a.nq, batch);
+  if (p.a.hd == 128) hipLaunchKernelGGL(attend_merge_kernel<128>, grid, dim3(256), 0, s, p);
+  else if (p.a.hd == 64) hipLaunchKernelGGL(attend_merge_kernel<64>, grid, dim3(256), 0, s, p);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_append(const MxAppendParams& p, hipStream_t s) {
+  const int lanes = p.batch * ((p.gq ? p.nq : 0) + 2 * p.nkv) * (p.hd / 8);
+  hipLaunchKernelGGL(mx_append_kernel, dim3((lanes + 255) / 256), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_rows_to_f32(const void* src, int type, float* dst, int n, hipStream_t s) {
+  hipLaunchKernelGGL(rows_to_f32_kernel, dim3((n / 8 + 255) / 256), dim3(256), 0, s, src, type, dst, n / 8);
+  return hipGetLastError();
+}
+
+}  // namespace kf

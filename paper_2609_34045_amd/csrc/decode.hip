@@ -241,11 +241,19 @@ __device__ __forceinline__ void gemv_epilogue(const GemvParams& p, int wg, const
           float* q = p.q + (int64_t)b * p.nq * hd + head * hd;
           q[i] = z1;
           q[i + half] = z2;
+        } else if (p.k32) {
+          float* k = p.k32 + ((int64_t)b * p.nkv + head - p.nq) * hd;
+          k[i] = z1;
+          k[i + half] = z2;
         } else {
           uint16_t* k = p.kc + kv_offset(p.kv, p.users[b], head - p.nq, pos, hd);
           k[i] = f16_checked(z1, bad);
           k[i + half] = f16_checked(z2, bad);
         }
+      } else if (p.v32) {
+        float* v = p.v32 + ((int64_t)b * p.nkv + head - p.nq - p.nkv) * hd;
+        v[i] = y1;
+        v[i + half] = y2;
       } else {
         uint16_t* v = p.vc + kv_offset(p.kv, p.users[b], head - p.nq - p.nkv, pos, hd);
         v[i] = f16_checked(y1, bad);

@@ -172,6 +172,9 @@ struct GemvParams {
   // ([B][nkv][hd] fp32) as projected (after the attention RMSNorm), without
   // RoPE; the decode attention finishes both.  v goes to the cache as usual.
   float* kraw;
+  // MXFP4 caches: k (rotated; raw in kraw when that is set) and v go here instead of the
+  // cache, [B][nkv][hd] fp32; launch_mx_append stores them.
+  float *k32, *v32;
 
   // kEpiSwiGLU
   float* act;          // [B][N] with N = F: fp32, or fp16 when act16 is set
@@ -225,7 +228,38 @@ struct AttnParams {
   int* err_flag;          // sticky error bits: kErrF16Range for an fp16 store out of range
 };
 
+// Attention over an MXFP4 cache (attend.hip): a's queries and cache pointers are not
+// used, its KvPages count bytes, its splits are whole pages.  With `out` set (one split, or
+// the merge) the result goes there; else the partials go to a's arrays, as the fp16 kernel's do.
+struct MxAttnParams {
+  AttnParams a;
+  const uint8_t* rec;  // layer base
+  const void* q;       // [B][nq][hd] rotated queries of q_type (the kf_dtype values)
+  int q_type;
+  void* out;           // [B][nq][hd] of type io, or NULL
+  int io;
+};
+// A decode step's new keys and values into an MXFP4 cache.
+struct MxAppendParams {
+  uint8_t* rec;  // layer base
+  KvPages kv;
+  float* q;      // [B][nq][hd]: normalised and rotated in place when gq is set
+  float *k, *v;  // [B][nkv][hd]; k rotated, or raw when gq is set
+  const uint16_t *gq, *gk;  // per-head norm gains [hd] bf16, or NULL
+  const float *rope_cos, *rope_sin;
+  float eps;
+  int nq, nkv, hd, batch;
+  int users[kMaxBatch];
+  int pos[kMaxBatch];
+  int* err_flag;
+};
+
 // Launchers (return hipGetLastError() of the launch).
+hipError_t launch_attn_mx(const MxAttnParams& p, int batch, hipStream_t s);
+// p.out from the partials of either cache type's attention.
+hipError_t launch_attend_merge(const MxAttnParams& p, int batch, hipStream_t s);
+hipError_t launch_mx_append(const MxAppendParams& p, hipStream_t s);
+hipError_t launch_rows_to_f32(const void* src, int type, float* dst, int n, hipStream_t s);
 int gemv_grid(int epi, int rows_per_wg, const GemvParams& p);
 hipError_t launch_gemv(int epi, int rows_per_wg, int chunks_in_flight, bool norm, const GemvParams& p, hipStream_t s);
 // The same launch with the stage input (p.src or p.tokens) as its input rows.

@@ -25,6 +25,10 @@ struct PrefillLayer {
   const uint16_t *g_qn, *g_kn;  // per-head q / k norm gains (qk_norm blocks), else NULL
   uint16_t* kc;  // K cache of this layer (fp16 bits), pages as in KvPages
   uint16_t* vc;
+  // MXFP4 caches: the layer (mx.k NULL: none) and the user whose positions it holds; kc and vc are then
+  // fp16 pages of one user that the chunk works on.
+  CacheRef mx;
+  int mx_user;
   void* out;     // hidden output after this layer (last layer only), else NULL
   int out_bf16;
   // The stage's input (first layer only; exactly one set): hidden rows, fp32 or bf16, or token ids, rows of embed

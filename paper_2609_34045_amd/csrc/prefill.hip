@@ -995,6 +995,13 @@ hipError_t prefill_layer(PrefillWorkspace& ws, const PrefillArgs& a, const Prefi
   if (e != hipSuccess) return e;
   tr.begin(ROPE);
   e = launch_rope_kv(ws, a, l);
+  // An MXFP4 cache takes the chunk's keys and values from the fp16 pages, which then
+  // get all positions as the cache holds them.
+  if (e == hipSuccess && l.mx.k) {
+    const CacheRef pages{(uint8_t*)l.kc, (uint8_t*)l.vc, a.kv, 0, 0, a.nkv, a.hd};
+    e = launch_cache_copy(l.mx, l.mx_user, pages, a.user, a.pos0, T, 1, a.err_flag, s);
+    if (e == hipSuccess) e = launch_cache_copy(pages, a.user, l.mx, l.mx_user, 0, a.pos0 + T, 1, a.err_flag, s);
+  }
   tr.end(ROPE);
   if (e != hipSuccess) return e;
   const float sl2 = (float)(1.4426950408889634 / std::sqrt((double)a.hd));

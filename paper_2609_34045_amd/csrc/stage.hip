@@ -191,6 +191,10 @@ struct kf_kv {
   int64_t bytes = 0;                    // device bytes of everything here
   float *rcos = nullptr, *rsin = nullptr;
   float *part_acc = nullptr, *part_ml = nullptr;
+  // KF_KV_MXFP4: a decode step's new keys and values, [kMaxBatch][nkv][hd] fp32 each; and one layer of
+  // one user's positions in fp16 pages, which the prefill's attention reads
+  float* append = nullptr;
+  uint16_t *f16_k = nullptr, *f16_v = nullptr;
   int64_t page_stride, layer_stride;  // elements
   std::vector<int> len;
   KvPages pages() const { return KvPages{table, ppu, page_stride}; }
@@ -747,9 +751,12 @@ static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int3
   const int64_t pacc = (int64_t)kMaxBatch * c.n_q_heads * kv->max_split * c.head_dim * 4;
   const int64_t pml = (int64_t)kMaxBatch * c.n_q_heads * kv->max_split * 2 * 4;
   const int64_t tab = paged ? (int64_t)max_users * ppu * 4 : 0;
-  char* mem[7] = {nullptr};
-  const int64_t sz[7] = {cache, kv->mx() ? 0 : cache, rope, rope, pacc, pml, tab};
-  for (int i = 0; i < 7; ++i) {
+  const int64_t app = kv->mx() ? 2LL * kMaxBatch * c.n_kv_heads * c.head_dim * 4 : 0;
+  const int64_t f16 = kv->mx() ? (int64_t)ppu * kKvPage * c.n_kv_heads * c.head_dim * 2 : 0;
+  constexpr int kMem = 10;
+  char* mem[kMem] = {nullptr};
+  const int64_t sz[kMem] = {cache, kv->mx() ? 0 : cache, rope, rope, pacc, pml, tab, app, f16, f16};
+  for (int i = 0; i < kMem; ++i) {
     if (sz[i] == 0) continue;
     kv->bytes += sz[i];
     if (hipMalloc((void**)&mem[i], sz[i]) != hipSuccess) {
@@ -767,6 +774,9 @@ static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int3
   kv->part_acc = (float*)mem[4];
   kv->part_ml = (float*)mem[5];
   kv->table = (int*)mem[6];
+  kv->append = (float*)mem[7];
+  kv->f16_k = (uint16_t*)mem[8];
+  kv->f16_v = (uint16_t*)mem[9];
   // RoPE table from float64 angles: pos * theta^(-2i/hd).
   std::vector<float> tc((size_t)max_ctx * half), ts((size_t)max_ctx * half);
   for (int64_t i = 0; i < half; ++i) {
@@ -779,12 +789,14 @@ static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int3
   }
   hipError_t e = hipMemset(kv->k, 0, cache);
   if (e == hipSuccess && kv->v) e = hipMemset(kv->v, 0, cache);
+  if (e == hipSuccess && f16) e = hipMemset(kv->f16_k, 0, f16);
+  if (e == hipSuccess && f16) e = hipMemset(kv->f16_v, 0, f16);
   if (e == hipSuccess && kv->table) e = hipMemset(kv->table, 0, tab);
   if (e == hipSuccess) e = hipMemcpy(kv->rcos, tc.data(), rope, hipMemcpyHostToDevice);
   if (e == hipSuccess) e = hipMemcpy(kv->rsin, ts.data(), rope, hipMemcpyHostToDevice);
   if (e != hipSuccess) {
-    for (int j = 0; j < 7; ++j)
-      if (mem[j]) hipFree(mem[j]);
+    for (char* m : mem)
+      if (m) hipFree(m);
     delete kv;
     return fail(KF_EDEVICE, "KV init: %s", hipGetErrorString(e));
   }
@@ -830,7 +842,7 @@ kf_status kf_kv_pages(const kf_kv* kv, int32_t* total, int32_t* free_pages) {
 kf_status kf_kv_destroy(kf_kv* kv) {
   if (!kv) return fail(KF_EINVAL, "kv is NULL");
   hipStreamSynchronize(kv->st->stream);
-  void* mem[7] = {kv->k, kv->v, kv->rcos, kv->rsin, kv->part_acc, kv->part_ml, kv->table};
+  void* mem[] = {kv->k, kv->v, kv->rcos, kv->rsin, kv->part_acc, kv->part_ml, kv->table, kv->append, kv->f16_k, kv->f16_v};
   for (void* m : mem)
     if (m) hipFree(m);
   kv->st->live_kv--;
@@ -1027,11 +1039,127 @@ static void attn_split_mfma(int nkv, int64_t total_len, int max_len, int max_spl
   *n_split = (max_len + sp - 1) / sp;
 }
 
+// Pages per workgroup of the attention over MXFP4 caches: about two workgroups a CU over the batch's
+// pages, a page for each of a workgroup's waves at least.
+static void attn_split_mx(int nkv, int64_t total_pages, int max_len, int max_split, int n_cu, int* split, int* n_split) {
+  const int64_t wgs = 2LL * n_cu, most = kAttnMaxSplit / kKvPage;
+  const int pages = pages_for(max_len);
+  int64_t sp = (total_pages * nkv + wgs - 1) / wgs;
+  if (sp < 4) sp = 4;
+  const int64_t need = (pages + max_split - 1) / max_split;
+  if (sp < need) sp = need;
+  if (sp > most) sp = most;
+  *split = (int)sp * kKvPage;
+  *n_split = pages ? (int)((pages + sp - 1) / sp) : 1;
+}
+
+// A decode step's attention over an MXFP4 cache, for which the QKV launch g left the new keys and
+// values in kv->append (and raw keys of qk_norm blocks in s->kraw).
+static hipError_t attn_mx(kf_stage* s, kf_kv* kv, const LayerW& L, const AttnParams& a, const GemvParams& g, int layer,
+                          hipStream_t st) {
+  const kf_model_config& c = s->cfg;
+  MxAppendParams n{};
+  n.rec = kv->layer_ref(layer).k;
+  n.kv = a.kv;
+  n.q = s->q;
+  n.k = c.qk_norm ? s->kraw : g.k32;
+  n.v = g.v32;
+  n.gq = L.g_qn;
+  n.gk = L.g_kn;
+  n.rope_cos = kv->rcos;
+  n.rope_sin = kv->rsin;
+  n.eps = c.rms_eps;
+  n.nq = c.n_q_heads;
+  n.nkv = c.n_kv_heads;
+  n.hd = c.head_dim;
+  n.batch = g.batch;
+  n.err_flag = s->err_flag;
+  for (int b = 0; b < g.batch; ++b) {
+    n.users[b] = g.users[b];
+    n.pos[b] = g.pos[b];
+  }
+  const hipError_t e = launch_mx_append(n, st);
+  if (e != hipSuccess) return e;
+  MxAttnParams p{};
+  p.a = a;
+  p.rec = n.rec;
+  p.q = s->q;
+  return launch_attn_mx(p, g.batch, st);
+}
+
+kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* users, const int32_t* lens,
+                       const void* q_dev, kf_dtype io, void* out_dev) {
+  if (!kv) return fail(KF_EINVAL, "kv is NULL");
+  if (rows < 1 || rows > kMaxBatch) return fail(KF_EINVAL, "rows %d outside [1, %d]", rows, kMaxBatch);
+  if (!users || !lens) return fail(KF_EINVAL, "users / lens is NULL");
+  if (!q_dev || !out_dev) return fail(KF_EINVAL, "queries / output is NULL");
+  if (io != KF_F32 && io != KF_BF16 && io != KF_F16) return fail(KF_EINVAL, "io dtype");
+  if ((uintptr_t)q_dev % 16) return fail(KF_EINVAL, "the queries are not 16-byte aligned");
+  int max_len = 0;
+  int64_t total_len = 0, total_pages = 0;
+  for (int b = 0; b < rows; ++b) {
+    const kf_status st = kv_slice_check(kv, layer, users[b], 0, lens[b]);
+    if (st != KF_OK) return st;
+    if (lens[b] > (int64_t)kv->held[users[b]] * kKvPage)
+      return fail(KF_ERANGE, "positions up to %d of user %d are not in the cache (it holds %d pages)", lens[b], users[b],
+                  kv->held[users[b]]);
+    if (lens[b] > max_len) max_len = lens[b];
+    total_len += lens[b];
+    total_pages += pages_for(lens[b]);
+  }
+  kf_stage* s = kv->st;
+  const kf_model_config& c = s->cfg;
+  const CacheRef ref = kv->layer_ref(layer);
+  MxAttnParams p{};
+  AttnParams& a = p.a;
+  a.part_acc = kv->part_acc;
+  a.part_ml = kv->part_ml;
+  a.kv = kv->pages();
+  a.nq = c.n_q_heads;
+  a.nkv = c.n_kv_heads;
+  a.hd = c.head_dim;
+  a.max_split = kv->max_split;
+  a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c.head_dim));
+  a.err_flag = s->err_flag;
+  for (int b = 0; b < rows; ++b) {
+    a.users[b] = users[b];
+    a.len[b] = lens[b];
+  }
+  p.io = io;
+  const Tracer tr = s->tracer();
+  tr.begin(KF_K_ATTN);
+  hipError_t e = hipSuccess;
+  if (kv->mx()) {
+    attn_split_mx(c.n_kv_heads, total_pages, max_len, kv->max_split, s->n_cu, &a.split, &a.n_split);
+    p.rec = ref.k;
+    p.q = q_dev;
+    p.q_type = io;
+    p.out = a.n_split == 1 ? out_dev : nullptr;
+    e = launch_attn_mx(p, rows, s->stream);
+  } else {
+    attn_split_mfma(c.n_kv_heads, total_len, max_len > 0 ? max_len : 1, kv->max_split, s->n_cu, &a.split, &a.n_split);
+    a.q = reinterpret_cast<const float*>(q_dev);
+    if (io != KF_F32) {  // the fp16 kernel takes fp32 queries
+      e = launch_rows_to_f32(q_dev, io, s->q, rows * c.n_q_heads * c.head_dim, s->stream);
+      a.q = s->q;
+    }
+    a.kc = (uint16_t*)ref.k;
+    a.vc = (uint16_t*)ref.v;
+    if (e == hipSuccess) e = launch_attn_decode(a, rows, s->stream);
+  }
+  if (e == hipSuccess && !p.out) {
+    p.out = out_dev;
+    e = launch_attend_merge(p, rows, s->stream);
+  }
+  tr.end(KF_K_ATTN);
+  KF_HIP(e, "attention launch");
+  return KF_OK;
+}
+
 kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* users, const int32_t* positions,
                           const int32_t* tokens_dev, const void* hidden_in_dev, void* hidden_out_dev, kf_dtype io) {
   if (!s || !kv) return fail(KF_EINVAL, "stage or kv is NULL");
   if (kv->st != s) return fail(KF_EINVAL, "kv belongs to another stage");
-  if (kv->mx()) return fail(KF_EUNSUPPORTED, "an MXFP4 cache is written and read by kf_kv_* calls only");
   if (batch < 1 || batch > kMaxBatch) return fail(KF_EINVAL, "batch %d outside [1, %d]", batch, kMaxBatch);
   if (!users || !positions) return fail(KF_EINVAL, "users / positions is NULL");
   if ((tokens_dev == nullptr) == (hidden_in_dev == nullptr))
@@ -1041,7 +1169,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     return fail(KF_EINVAL, "hidden output is NULL (only a stage that holds the head may keep its rows)");
   if (io != KF_F32 && io != KF_BF16) return fail(KF_EINVAL, "io dtype");
   int max_len = 0;
-  int64_t total_len = 0;
+  int64_t total_len = 0, total_pages = 0;
   for (int b = 0; b < batch; ++b) {
     const int u = users[b], p = positions[b];
     if (u < 0 || u >= kv->max_users) return fail(KF_EINVAL, "users[%d] = %d outside [0, %d)", b, u, kv->max_users);
@@ -1051,13 +1179,15 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     if (p >= kv->max_ctx) return fail(KF_ERANGE, "position %d beyond max_ctx %d", p, kv->max_ctx);
     if (p + 1 > max_len) max_len = p + 1;
     total_len += p + 1;
+    total_pages += pages_for(p + 1);
   }
   const kf_model_config& c = s->cfg;
   const int H = c.hidden, hd = c.head_dim;
   hipStream_t st = s->stream;
 
   int split, n_split;
-  if (batch > 1) attn_split_mfma(c.n_kv_heads, total_len, max_len, kv->max_split, s->n_cu, &split, &n_split);
+  if (kv->mx()) attn_split_mx(c.n_kv_heads, total_pages, max_len, kv->max_split, s->n_cu, &split, &n_split);
+  else if (batch > 1) attn_split_mfma(c.n_kv_heads, total_len, max_len, kv->max_split, s->n_cu, &split, &n_split);
   else attn_split(c.n_kv_heads, total_len, max_len, kv->max_split, &split, &n_split);
   if (split % kAttnMfmaAlign) return fail(KF_EINVAL, "split of %d keys breaks the attention kernel's alignment", split);
   int64_t from[kMaxBatch], upto[kMaxBatch];
@@ -1096,6 +1226,10 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     g.rope_cos = kv->rcos;
     g.rope_sin = kv->rsin;
     g.kraw = s->kraw;  // set for qk_norm blocks: q and k are normalised and rotated below
+    if (kv->mx()) {
+      g.k32 = kv->append;
+      g.v32 = kv->append + (int64_t)kMaxBatch * c.n_kv_heads * hd;
+    }
     g.err_flag = s->err_flag;
     for (int b = 0; b < kMaxBatch; ++b) {
       g.users[b] = b < batch ? users[b] : 0;
@@ -1147,7 +1281,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     }
     {
       tr.begin(KF_K_ATTN);
-      const hipError_t le = launch_attn_decode(a, batch, st);
+      const hipError_t le = kv->mx() ? attn_mx(s, kv, L, a, g, l, st) : launch_attn_decode(a, batch, st);
       tr.end(KF_K_ATTN);
       KF_HIP(le, "attention launch");
     }
@@ -1372,7 +1506,6 @@ static kf_status prefill_impl(kf_stage* s, kf_kv* kv, int32_t user, int32_t pos0
                               bool no_alloc) {
   if (!s || !kv) return fail(KF_EINVAL, "stage or kv is NULL");
   if (kv->st != s) return fail(KF_EINVAL, "kv belongs to another stage");
-  if (kv->mx()) return fail(KF_EUNSUPPORTED, "an MXFP4 cache is written and read by kf_kv_* calls only");
   if (n < 1) return fail(KF_EINVAL, "n_tokens must be >= 1");
   if (user < 0 || user >= kv->max_users) return fail(KF_EINVAL, "user %d outside [0, %d)", user, kv->max_users);
   if ((tokens_dev == nullptr) == (hidden_in_dev == nullptr))
@@ -1418,6 +1551,10 @@ static kf_status prefill_impl(kf_stage* s, kf_kv* kv, int32_t user, int32_t pos0
   const kf_status gst = kv_grant(kv, 1, &user, &from, &upto);
   if (gst != KF_OK) return gst;
   const Tracer tr = no_alloc ? Tracer{} : s->tracer();  // event records may create events
+  if (kv->mx()) {  // the chunk works on one layer's positions in fp16 pages (prefill_layer brings them there)
+    pa.kv = KvPages{nullptr, kv->ppu, (int64_t)c.n_kv_heads * kKvPage * c.head_dim};
+    pa.user = 0;
+  }
   for (int l = s->lo; l < s->hi; ++l) {
     const LayerW& L = s->layers[l - s->lo];
     const int64_t loff = (l - s->lo) * kv->layer_stride;
@@ -1431,8 +1568,15 @@ static kf_status prefill_impl(kf_stage* s, kf_kv* kv, int32_t user, int32_t pos0
     pl.g_mlp = L.mlp_gain();
     pl.g_qn = L.g_qn;
     pl.g_kn = L.g_kn;
-    pl.kc = kv->k + loff;
-    pl.vc = kv->v + loff;
+    if (kv->mx()) {
+      pl.kc = kv->f16_k;
+      pl.vc = kv->f16_v;
+      pl.mx = kv->layer_ref(l);
+      pl.mx_user = user;
+    } else {
+      pl.kc = kv->k + loff;
+      pl.vc = kv->v + loff;
+    }
     if (l == s->lo) {  // the first layer's norm reads the stage's input and starts the residual stream
       pl.src = hidden_in_dev;
       pl.src_bf16 = io == KF_BF16;

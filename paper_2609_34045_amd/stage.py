@@ -32,7 +32,8 @@ EXPORTS = ("kf_abi_version", "kf_last_error", "kf_stage_bytes", "kf_stage_init",
            "kf_kv_write", "kf_kv_read", "kf_stage_decode", "kf_stage_prefill", "kf_head_logits", "kf_head_argmax",
            "kf_stage_profile", "kf_stage_profile_read", "kf_stage_describe", "kf_kv_describe",
            "kf_kv_create_paged", "kf_kv_pages", "kf_stage_set_flags", "kf_stage_get_flags",
-           "kf_stage_prefill_noalloc", "kf_kv_create_typed", "kf_kv_format", "kf_kv_copy", "kf_kv_fork")
+           "kf_stage_prefill_noalloc", "kf_kv_create_typed", "kf_kv_format", "kf_kv_copy", "kf_kv_fork",
+           "kf_kv_attend")
 KV_TYPES = {"f16": 0, "mxfp4": 1}  # kf_kv_type
 PREFILL_SCRATCH_BYTES = 144 << 20  # KF_PREFILL_SCRATCH_BYTES: the no-allocation prefill's workspace limit
 KF_STAGE_ORDERED = 1  # batch-1 decode adds the heads' output projections in a fixed order
@@ -111,6 +112,7 @@ def load_library(path: str = LIB_PATH):
         "kf_kv_format": (I32, [P, I32P, I64P]),
         "kf_kv_copy": (I32, [P, I32, P, I32, I32, I32]),
         "kf_kv_fork": (I32, [P, I32, I32, I32]),
+        "kf_kv_attend": (I32, [P, I32, I32, I32P, I32P, VP, I32, VP]),
         "kf_kv_pages": (I32, [P, I32P, I32P]),
         "kf_stage_set_flags": (I32, [P, I32]),
         "kf_stage_get_flags": (I32, [P, I32P]),
@@ -414,6 +416,29 @@ class KV:
     def fork(self, src_user: int, dst_user: int, n: int | None = None):
         """``dst_user`` continues from the first ``n`` (default: all) positions of ``src_user`` (kf_kv_fork)."""
         _check(self._lib.kf_kv_fork(self.handle, src_user, dst_user, self.len(src_user) if n is None else n), "kf_kv_fork")
+
+    def attend(self, layer: int, users, lens, q, out=None):
+        """Attention of queries ``q`` ([rows, nq, hd] or [rows, nq * hd]; float32, bfloat16 or float16) over the first
+        ``lens[b]`` positions of ``users[b]`` in one layer (kf_kv_attend); the result has q's shape and type."""
+        import torch
+        n, s = len(users), self.stage.shape
+        if len(lens) != n:
+            raise ValueError("users and lens differ in length")
+        _require_device(q, "q")
+        if q.dtype not in (torch.float32, torch.bfloat16, torch.float16):
+            raise TypeError(f"q must be float32, bfloat16 or float16, not {q.dtype}")
+        io = {torch.float32: KF_F32, torch.bfloat16: KF_BF16, torch.float16: KF_F16}[q.dtype]
+        if tuple(q.shape) not in ((n, s.n_q_heads, s.head_dim), (n, s.n_q_heads * s.head_dim)):
+            raise ValueError(f"q of shape {tuple(q.shape)} for {n} rows of {s.n_q_heads} heads of {s.head_dim}")
+        if out is None:
+            out = torch.empty_like(q)
+        else:
+            _require_device(out, "out")
+            if out.dtype != q.dtype or out.shape != q.shape:
+                raise ValueError("out must have the shape and type of q")
+        u, t = (ctypes.c_int32 * max(n, 1))(*users), (ctypes.c_int32 * max(n, 1))(*lens)
+        _check(self._lib.kf_kv_attend(self.handle, layer, n, u, t, _ptr(q), io, _ptr(out)), "kf_kv_attend")
+        return out
 
     def describe(self) -> dict:
         owner, mu, mc = ctypes.c_void_p(), ctypes.c_int32(), ctypes.c_int32()

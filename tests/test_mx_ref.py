@@ -48,5 +48,6 @@ def test_refusals_before_touching_the_device():
     assert lib.kf_kv_format(None, None, None) == 1
     assert lib.kf_kv_copy(None, 0, None, 0, 0, 1) == 1
     assert lib.kf_kv_fork(None, 0, 1, 0) == 1
+    assert lib.kf_kv_attend(None, 0, 1, None, None, None, 0, None) == 1
     with pytest.raises(ValueError, match="dtype"):
         stage.KV(None, 1, 64, dtype="int4")
