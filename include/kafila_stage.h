@@ -50,7 +50,8 @@ extern "C" {
                             5: a head stage's decode may keep its output rows (hidden_out_dev NULL)
                                for kf_head_logits / kf_head_argmax with hidden_dev NULL.
                             Calls added since leave the others as they are: kf_kv_create_typed,
-                            kf_kv_format, kf_kv_copy, kf_kv_fork, kf_kv_attend */
+                            kf_kv_format, kf_kv_copy, kf_kv_fork, kf_kv_attend,
+                            kf_head_logprobs, kf_logits_logprobs */
 #define KF_KV_PAGE 64     /* positions per KV cache page */
 #define KF_MAX_BATCH 4
 
@@ -161,12 +162,13 @@ kf_status kf_stage_set_stream(kf_stage* stage, void* hip_stream);
  * Wait for all enqueued work; KF_EDEVICE (with the HIP error text) if any of it failed.
  * Then reports, and clears, the stage's sticky data errors raised by enqueued work:
  *   KF_EINVAL : a token id given to decode or prefill was outside [0, vocab); that row's
- *               hidden state was set to NaN;
+ *               hidden state was set to NaN (a target's log probability alike);
  *   KF_ERANGE : a value the stage holds in fp16 (keys and values in the cache, and the
  *               fp16 activations: from batch 2 the decode residual copy, SwiGLU output and
  *               merged attention output; in prefill the normalised rows, queries, attention
  *               output and SwiGLU output) reached 65520 in magnitude and was stored as
- *               infinity; or a logit was NaN (skipped by the argmax; see kf_head_argmax).
+ *               infinity; or a logit was NaN (skipped by the argmax and the log probabilities; see
+ *               kf_head_argmax and kf_head_logprobs).
  * The message (kf_last_error) names every condition that occurred.
  */
 kf_status kf_stage_sync(kf_stage* stage);
@@ -410,6 +412,39 @@ kf_status kf_head_argmax(kf_stage* stage, int32_t rows, const void* hidden_dev, 
                          int32_t* token_dev, float* max_logit_dev);
 
 /*
+ * Log probabilities instead of logits or an argmax: what scoring a prompt, sampling with
+ * alternatives or a beam search takes from the head.  rows, hidden_dev and dtype as
+ * for kf_head_logits (any rows; hidden_dev NULL: the kept rows).
+ *   targets_dev int32 [rows], logprob_dev fp32 [rows] : both or neither.  logprob =
+ *       z_t - ln sum e^z of the row's logits z; a target of -1 (padding) gives 0, any
+ *       other id outside [0, vocab) NaN and the stage's token error
+ *   entropy_dev fp32 [rows] or NULL : -sum p ln p, in nats
+ *   n_top in [0, KF_MAX_TOP], top_ids_dev int32 and top_logprobs_dev fp32 [rows, n_top] :
+ *       the most probable tokens, largest first, the lower id first among equal logits
+ * A logit of -inf is masked: probability 0 and never an alternative; where a row has
+ * fewer than n_top others the rest are -1 with -inf.  A row with nothing left gives
+ * -inf for its target and entropy 0.  A NaN or +inf logit is left out and raises
+ * the NaN-logit error (a target there gives NaN).
+ * The logits of up to 256 rows stay in a workspace of the stage (4 rows for calls of up
+ * to 4, 64 up to 64), allocated by the first call that needs it and kept; KF_ENOMEM
+ * where not even 4 rows can be had, which includes a first call under graph capture.
+ * Vocabularies up to 2^20 (else KF_EUNSUPPORTED).  Head stages only (else KF_ESTATE).
+ */
+#define KF_MAX_TOP 32
+kf_status kf_head_logprobs(kf_stage* stage, int32_t rows, const void* hidden_dev, kf_dtype dtype,
+                           const int32_t* targets_dev, float* logprob_dev, float* entropy_dev, int32_t n_top,
+                           int32_t* top_ids_dev, float* top_logprobs_dev);
+
+/*
+ * The same of logits that the caller holds (after masking or a temperature of its own):
+ * logits_dev fp32 [rows] rows of `vocab` values, `stride` values apart.  Any stage;
+ * the logits may be of another vocabulary than the stage's.
+ */
+kf_status kf_logits_logprobs(kf_stage* stage, int32_t rows, int32_t vocab, int64_t stride, const float* logits_dev,
+                             const int32_t* targets_dev, float* logprob_dev, float* entropy_dev, int32_t n_top,
+                             int32_t* top_ids_dev, float* top_logprobs_dev);
+
+/*
  * Per-kernel timing (instrumentation).  The paper's sessions record predicted and
  * measured cost per stage (Section VI); this records, per kernel class, the HIP-event
  * time of every launch the stage enqueues while recording is on.
@@ -440,9 +475,10 @@ typedef enum {
   KF_K_PF_STORE = 15,  /* prefill: hidden output store */
   KF_K_QKNORM = 16,    /* kept for numbering: the decode per-head q/k RMSNorm + RoPE of qk_norm blocks
                           now runs inside the attention launch (KF_K_ATTN); nothing records here */
-  KF_K_COUNT = 17
+  KF_K_LOGPROB = 17,   /* head: log probabilities of logits */
+  KF_K_COUNT = 18
 } kf_kernel_class;
-#define KF_K_ALL 0x1ffff
+#define KF_K_ALL 0x3ffff
 
 kf_status kf_stage_profile(kf_stage* stage, int32_t mask);
 kf_status kf_stage_profile_read(kf_stage* stage, int32_t kernel_class, int64_t* launches, double* total_ms);

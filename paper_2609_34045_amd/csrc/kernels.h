@@ -297,6 +297,30 @@ hipError_t launch_kv_table_update(int* table, const KvTableUpdate& u, hipStream_
 // table[dst + i] = table[src + i] for i < n: a user that shares another's pages.
 hipError_t launch_kv_table_share(int* table, int src, int dst, int n, hipStream_t s);
 
+// Log probabilities of rows of logits (logprob.hip).
+constexpr int kMaxTop = 32;
+constexpr int kMaxLogprobVocab = 1 << 20;
+constexpr int kLogprobRows = 32768;  // rows of one launch
+struct LogprobParams {
+  const float* logits;  // [rows][stride]
+  int64_t stride;
+  int vocab;
+  const int32_t* targets;  // [rows] or NULL
+  float* logprob;          // [rows], with targets
+  float* entropy;          // [rows] or NULL
+  int top;
+  int32_t* top_ids;        // [rows][top]
+  float* top_logprobs;
+  int* err_flag;
+  // set by the launcher: partial results of rows of several chunks
+  int chunks;
+  unsigned long long* part_keys;  // [rows][chunks][top]
+  float* part_sums;               // [rows][chunks][4]
+};
+int logprob_chunks(int rows, int vocab);
+int64_t logprob_part_bytes(int rows, int vocab, int top);  // workspace of a launch (not used where logprob_chunks is 1)
+hipError_t launch_logprobs(LogprobParams p, int rows, char* part, hipStream_t s);
+
 // A cache as the copying kernels see it (cache.hip): fp16 K and V arrays, or one array of MXFP4 records at k.
 struct CacheRef {
   uint8_t* k;

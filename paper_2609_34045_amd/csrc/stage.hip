@@ -2,6 +2,7 @@
 // device memory (weights, KV cache, workspaces) and the per-step kernel sequence.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -109,6 +110,15 @@ struct LayerW {
   const uint16_t* mlp_gain() const { return mlp_fold ? nullptr : g_mlp; }
 };
 
+// A workspace grown to the most a call needed.  What it grew out of stays until the stage ends: a captured
+// graph may hold its address.  Each is at least twice the one before, so that all take less than twice the last.
+struct Grown {
+  char* mem = nullptr;
+  int64_t cap = 0;
+  char* all[48] = {};
+  int n = 0;
+};
+
 struct kf_stage {
   kf_model_config cfg;
   int lo, hi, has_head;
@@ -132,6 +142,8 @@ struct kf_stage {
   // logits of many rows (head_reserve): a chunk's rows as matrix operands
   uint16_t* head_a = nullptr;
   double* head_scale = nullptr;   // and, kHeadScaleBytes, what brings the rows back
+  // log probabilities: partial results, and the logits of a chunk of rows (grow_kept)
+  Grown lp_part, lp_logits;
   int lm_wg = 0;       // capacity of the argmax partials per batch row
   int lm_wg_used = 0;  // partials per row written by the last LM-head launch
   int kept_rows = 0;   // rows the last decode kept for the head (called without hidden output), else 0
@@ -655,6 +667,8 @@ kf_status kf_stage_destroy(kf_stage* s) {
   if (s->arena) hipFree(s->arena);
   if (s->ws) hipFree(s->ws);
   if (s->head_a) hipFree(s->head_a);
+  for (Grown* g : {&s->lp_part, &s->lp_logits})
+    for (int i = 0; i < g->n; ++i) hipFree(g->all[i]);
   prefill_free(s->pf);
   for (hipEvent_t e : s->ev) hipEventDestroy(e);
   delete s;
@@ -689,7 +703,7 @@ kf_status kf_stage_sync(kf_stage* s) {
     int zero = 0;
     KF_HIP(hipMemcpy(s->err_flag, &zero, 4, hipMemcpyHostToDevice), "error flag clear");
     std::string msg;
-    if (flag & kErrToken) msg += "a token id was outside [0, vocab) (its hidden row was set to NaN); ";
+    if (flag & kErrToken) msg += "a token id was outside [0, vocab) (its hidden row or log probability was set to NaN); ";
     if (flag & kErrF16Range)
       msg += "an activation, key or value held in fp16 reached 65520 in magnitude (stored as infinity); ";
     if (flag & kErrNaNLogit) msg += "a logit was NaN (skipped by the argmax; a row of NaN logits gave token -1); ";
@@ -1493,6 +1507,127 @@ kf_status kf_head_argmax(kf_stage* s, int32_t rows, const void* hidden, kf_dtype
   const hipError_t e = launch_argmax_final(s->part_val, s->part_idx, s->lm_wg_used, rows, token, max_logit, s->stream);
   tr.end(KF_K_ARGMAX);
   KF_HIP(e, "argmax launch");
+  return KF_OK;
+}
+
+// ------------------------------------------------------------------ log probabilities
+// At least `bytes` at g.mem, kept from call to call; false where they cannot be had: no device
+// memory left, or the stream is being captured.
+static bool grow_kept(kf_stage* s, Grown& g, int64_t bytes) {
+  if (bytes <= g.cap) return true;
+  if (g.n == (int)(sizeof g.all / sizeof g.all[0])) return false;
+  bytes = std::max(bytes, 2 * g.cap);
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s->stream, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone) {
+    (void)hipGetLastError();
+    return false;
+  }
+  // Relaxed: the allocation leaves captures of other threads alone.
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+  (void)hipThreadExchangeStreamCaptureMode(&mode);
+  char* fresh = nullptr;
+  const hipError_t e = hipMalloc((void**)&fresh, bytes);
+  (void)hipThreadExchangeStreamCaptureMode(&mode);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return false;
+  }
+  g.mem = g.all[g.n++] = fresh;
+  g.cap = bytes;
+  return true;
+}
+
+static kf_status logprob_check(int rows, int64_t vocab, const int32_t* targets, const float* logprob,
+                               const float* entropy, int n_top, const int32_t* top_ids, const float* top_logprobs) {
+  if (rows < 1) return fail(KF_EINVAL, "rows must be >= 1");
+  if (vocab > kMaxLogprobVocab) return fail(KF_EUNSUPPORTED, "vocabulary %lld above %d", (long long)vocab, kMaxLogprobVocab);
+  if ((targets == nullptr) != (logprob == nullptr)) return fail(KF_EINVAL, "targets and their log probabilities go together");
+  if (n_top < 0 || n_top > kMaxTop) return fail(KF_EINVAL, "n_top %d outside [0, %d]", n_top, kMaxTop);
+  if (n_top > 0 && (!top_ids || !top_logprobs)) return fail(KF_EINVAL, "NULL output of the alternatives");
+  if (!logprob && !entropy && n_top == 0) return fail(KF_EINVAL, "no output asked for");
+  return KF_OK;
+}
+
+// Rows [0, rows) of logits in as few launches as they go in.
+static kf_status logprob_launch(kf_stage* s, int rows, const LogprobParams& all) {
+  for (int r0 = 0; r0 < rows; r0 += kLogprobRows) {
+    const int n = rows - r0 < kLogprobRows ? rows - r0 : kLogprobRows;
+    LogprobParams p = all;
+    p.logits += r0 * p.stride;
+    if (p.targets) p.targets += r0, p.logprob += r0;
+    if (p.entropy) p.entropy += r0;
+    if (p.top) p.top_ids += (int64_t)r0 * p.top, p.top_logprobs += (int64_t)r0 * p.top;
+    if (logprob_chunks(n, p.vocab) > 1 &&
+        !grow_kept(s, s->lp_part, logprob_part_bytes(n, p.vocab, kMaxTop)))
+      return fail(KF_ENOMEM, "workspace of the log probabilities (%lld bytes; a first call may not be captured)",
+                  (long long)logprob_part_bytes(n, p.vocab, kMaxTop));
+    const Tracer tr = s->tracer();
+    tr.begin(KF_K_LOGPROB);
+    const hipError_t e = launch_logprobs(p, n, s->lp_part.mem, s->stream);
+    tr.end(KF_K_LOGPROB);
+    KF_HIP(e, "log probabilities launch");
+  }
+  return KF_OK;
+}
+
+kf_status kf_logits_logprobs(kf_stage* s, int32_t rows, int32_t vocab, int64_t stride, const float* logits,
+                             const int32_t* targets, float* logprob, float* entropy, int32_t n_top, int32_t* top_ids,
+                             float* top_logprobs) {
+  if (!s) return fail(KF_EINVAL, "stage is NULL");
+  if (vocab < 1) return fail(KF_EINVAL, "vocab must be >= 1");
+  if (stride < vocab) return fail(KF_EINVAL, "row stride %lld below the row's %d logits", (long long)stride, vocab);
+  const kf_status st = logprob_check(rows, vocab, targets, logprob, entropy, n_top, top_ids, top_logprobs);
+  if (st != KF_OK) return st;
+  if (!logits) return fail(KF_EINVAL, "logits is NULL");
+  LogprobParams p{};
+  p.logits = logits;
+  p.stride = stride;
+  p.vocab = vocab;
+  p.targets = targets;
+  p.logprob = logprob;
+  p.entropy = entropy;
+  p.top = n_top;
+  p.top_ids = top_ids;
+  p.top_logprobs = top_logprobs;
+  p.err_flag = s->err_flag;
+  return logprob_launch(s, rows, p);
+}
+
+kf_status kf_head_logprobs(kf_stage* s, int32_t rows, const void* hidden, kf_dtype dtype, const int32_t* targets,
+                           float* logprob, float* entropy, int32_t n_top, int32_t* top_ids, float* top_logprobs) {
+  kf_status st = head_common(s, rows, hidden, dtype);
+  if (st != KF_OK) return st;
+  const kf_model_config& c = s->cfg;
+  st = logprob_check(rows, c.vocab, targets, logprob, entropy, n_top, top_ids, top_logprobs);
+  if (st != KF_OK) return st;
+  // The logits of a chunk stay in the stage (a chunk of 8B-shaped ones, 131 MB, in the last-level
+  // cache); where there is no memory for a larger chunk the rows go through what is held.
+  const int64_t row_bytes = (int64_t)c.vocab * 4;
+  const int chunk = rows <= kMaxBatch ? kMaxBatch : rows <= 64 ? 64 : kHeadChunk;
+  if (!grow_kept(s, s->lp_logits, chunk * row_bytes) && !grow_kept(s, s->lp_logits, kMaxBatch * row_bytes))
+    return fail(KF_ENOMEM, "workspace of the log probabilities (%lld bytes; a first call may not be captured)",
+                (long long)(kMaxBatch * row_bytes));
+  const int held = (int)std::min<int64_t>(chunk, s->lp_logits.cap / row_bytes);
+  for (int r0 = 0; r0 < rows; r0 += held) {
+    const int n = rows - r0 < held ? rows - r0 : held;
+    const char* in = (const char*)hidden;
+    st = kf_head_logits(s, n, hidden ? in + (int64_t)r0 * c.hidden * (dtype == KF_BF16 ? 2 : 4) : nullptr, dtype,
+                        (float*)s->lp_logits.mem);
+    if (st != KF_OK) return st;
+    LogprobParams p{};
+    p.logits = (const float*)s->lp_logits.mem;
+    p.stride = c.vocab;
+    p.vocab = c.vocab;
+    p.targets = targets ? targets + r0 : nullptr;
+    p.logprob = logprob ? logprob + r0 : nullptr;
+    p.entropy = entropy ? entropy + r0 : nullptr;
+    p.top = n_top;
+    p.top_ids = n_top ? top_ids + (int64_t)r0 * n_top : nullptr;
+    p.top_logprobs = n_top ? top_logprobs + (int64_t)r0 * n_top : nullptr;
+    p.err_flag = s->err_flag;
+    st = logprob_launch(s, n, p);
+    if (st != KF_OK) return st;
+  }
   return KF_OK;
 }
 

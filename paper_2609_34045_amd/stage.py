@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -33,14 +34,23 @@ EXPORTS = ("kf_abi_version", "kf_last_error", "kf_stage_bytes", "kf_stage_init",
            "kf_stage_profile", "kf_stage_profile_read", "kf_stage_describe", "kf_kv_describe",
            "kf_kv_create_paged", "kf_kv_pages", "kf_stage_set_flags", "kf_stage_get_flags",
            "kf_stage_prefill_noalloc", "kf_kv_create_typed", "kf_kv_format", "kf_kv_copy", "kf_kv_fork",
-           "kf_kv_attend")
+           "kf_kv_attend", "kf_head_logprobs", "kf_logits_logprobs")
 KV_TYPES = {"f16": 0, "mxfp4": 1}  # kf_kv_type
 PREFILL_SCRATCH_BYTES = 144 << 20  # KF_PREFILL_SCRATCH_BYTES: the no-allocation prefill's workspace limit
 KF_STAGE_ORDERED = 1  # batch-1 decode adds the heads' output projections in a fixed order
 
 # kf_kernel_class
 KERNEL_CLASSES = ("prep", "qkv", "attn", "oproj", "gateup", "down", "lmhead", "argmax", "pf_norm", "pf_qkv", "pf_rope",
-                  "pf_attn", "pf_oproj", "pf_gateup", "pf_down", "pf_store", "qknorm")
+                  "pf_attn", "pf_oproj", "pf_gateup", "pf_down", "pf_store", "qknorm", "logprob")
+MAX_TOP = 32  # KF_MAX_TOP
+
+
+class LogProbs(NamedTuple):
+    """Log probabilities of rows (kf_head_logprobs); None for what was not asked for."""
+    logprob: object       # [rows] float32: the given tokens'
+    entropy: object       # [rows] float32, nats
+    top_ids: object       # [rows, top] int32, most probable first
+    top_logprobs: object  # [rows, top] float32
 
 
 class KFError(RuntimeError):
@@ -112,6 +122,8 @@ def load_library(path: str = LIB_PATH):
         "kf_kv_format": (I32, [P, I32P, I64P]),
         "kf_kv_copy": (I32, [P, I32, P, I32, I32, I32]),
         "kf_kv_fork": (I32, [P, I32, I32, I32]),
+        "kf_head_logprobs": (I32, [P, I32, VP, I32, VP, VP, VP, I32, VP, VP]),
+        "kf_logits_logprobs": (I32, [P, I32, I32, I64, VP, VP, VP, VP, I32, VP, VP]),
         "kf_kv_attend": (I32, [P, I32, I32, I32P, I32P, VP, I32, VP]),
         "kf_kv_pages": (I32, [P, I32P, I32P]),
         "kf_stage_set_flags": (I32, [P, I32]),
@@ -354,6 +366,40 @@ class Stage:
         mx = torch.empty((n,), dtype=torch.float32, device=dev) if with_max else None
         _check(self._lib.kf_head_argmax(self.handle, n, _ptr(hidden), dt, _ptr(tok), _ptr(mx)), "kf_head_argmax")
         return (tok, mx) if with_max else tok
+
+    def _logprobs(self, call, name, n, dev, targets, top, entropy) -> LogProbs:
+        import torch
+        if targets is not None:
+            _require_device(targets, "targets")
+            if targets.dtype != torch.int32:
+                raise TypeError("targets must be int32")
+            if tuple(targets.shape) != (n,):
+                raise ValueError(f"targets of shape {tuple(targets.shape)} for {n} rows")
+        lp = torch.empty((n,), dtype=torch.float32, device=dev) if targets is not None else None
+        en = torch.empty((n,), dtype=torch.float32, device=dev) if entropy else None
+        ids = torch.empty((n, top), dtype=torch.int32, device=dev) if top > 0 else None
+        tl = torch.empty((n, top), dtype=torch.float32, device=dev) if top > 0 else None
+        _check(call(_ptr(targets), _ptr(lp), _ptr(en), int(top), _ptr(ids), _ptr(tl)), name)
+        return LogProbs(lp, en, ids, tl)
+
+    def head_logprobs(self, hidden, targets=None, top: int = 0, entropy: bool = True, rows: int | None = None) -> LogProbs:
+        """Log probabilities of ``targets`` (int32 [rows]), entropy and ``top`` alternatives of each hidden row
+        (kf_head_logprobs); hidden None with ``rows``: the rows the last decode kept."""
+        n, dt, dev = self._head_rows(hidden, rows)
+        return self._logprobs(lambda *a: self._lib.kf_head_logprobs(self.handle, n, _ptr(hidden), dt, *a),
+                              "kf_head_logprobs", n, dev, targets, top, entropy)
+
+    def logits_logprobs(self, logits, targets=None, top: int = 0, entropy: bool = True) -> LogProbs:
+        """The same of float32 logits [rows, V] (kf_logits_logprobs); rows may lie further apart than V."""
+        import torch
+        if not logits.is_cuda or logits.dtype != torch.float32 or logits.dim() != 2:
+            raise TypeError("logits must be a float32 device tensor [rows, V]")
+        n, v = logits.shape
+        stride = logits.stride(0) if n > 1 else max(v, 1)
+        if v > 1 and logits.stride(1) != 1 or stride < v:
+            raise ValueError("a row's logits must be contiguous, and rows apart")
+        return self._logprobs(lambda *a: self._lib.kf_logits_logprobs(self.handle, n, v, stride, _ptr(logits), *a),
+                              "kf_logits_logprobs", n, logits.device, targets, top, entropy)
 
 
 class KV:
