@@ -223,7 +223,7 @@ kf_status kf_kv_create_paged(kf_stage* stage, int32_t max_users, int32_t max_ctx
 
 /*
  * A cache of a given type: KF_KV_F16 as kf_kv_create (n_pages 0) and kf_kv_create_paged
- * (n_pages >= 1) make it, or KF_KV_MXFP4, reserved or paged alike, which takes 17/64 of the bytes.
+ * (n_pages >= 1) make it, or KF_KV_MXFP4, reserved or paged alike, which takes 35/128 of the bytes.
  * An MXFP4 cache holds each head vector of a key or value in blocks of 32 consecutive
  * values: E2M1 elements (0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign), rounded to
  * nearest even, times one power of two 2^e.  A value x is rounded to fp16 first; e is
@@ -307,7 +307,7 @@ kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n);
  *          that share pages); lens[b] 0 gives a row of zeros
  *   q_dev : [rows, nq, hd] rotated queries in io (KF_F32, KF_BF16 or KF_F16), 16-byte aligned
  *   out_dev : [rows, nq, hd] in io; may be q_dev
- * Over an MXFP4 cache the products take queries and probabilities in two parts each (16 and more
+ * Over an MXFP4 cache the products take queries and probabilities in two fp16 parts each (22
  * bits) and fp32 sums; over an fp16 cache they are rounded to fp16, as in a decode step.  A query head
  * that holds a NaN gives NaN.  KF_ERANGE for lens[b] beyond max_ctx or the pages the user holds.
  * Changes nothing in the cache.  Enqueued on the stage's stream.

@@ -17,10 +17,9 @@
 // columns of a tile hold 8 query heads twice, as two fp16 parts of each query
 // value (columns 0-7 the rounded value, 8-15 what rounding left), so that a score
 // is as exact as 22-bit queries give it at no more products than one part would
-// take.  P V: O^T = V^T P^T on bf16 MFMAs.  V's exponents differ by position,
-// which is the reduction's index there, so they multiply the probabilities:
-// bf16 has fp32's exponent range, and the same two halves of the columns hold the
-// two parts of a probability.  The score tile's lane layout is the P^T operand's.
+// take.  P V: O^T = V^T P^T alike, V decoded and multiplied by its positions' scales
+// two at a time, the two halves of the columns holding the two parts of a
+// probability.  The score tile's lane layout is the P^T operand's.
 #include <cmath>
 
 #include "kernels.h"
@@ -32,8 +31,7 @@ typedef unsigned v4u __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-typedef __bf16 b8 __attribute__((ext_vector_type(8)));
-typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float ror8(float v) {  // the lane 8 apart within each row of 16
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, false));
@@ -50,7 +48,7 @@ __device__ __forceinline__ float groups_sum(float x) {
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
-__device__ __forceinline__ float exponent(uint32_t w, int byte) {  // 2^e of a stored exponent
+__device__ __forceinline__ float exponent(uint32_t w, int byte) {  // 2^e of a stored K exponent
   return __uint_as_float(((w >> (8 * byte)) & 255u) << 23);
 }
 
@@ -78,22 +76,34 @@ __device__ __forceinline__ void store_out(void* out, int type, int64_t at, float
 }
 
 constexpr int kWaves = 4;
-// The maximum moves only when a page's exceeds it by this much (log2 units); probabilities stay
-// below 2^8, which neither bf16 nor the fp32 sums mind, and the rescaling of O is rare.
-constexpr float kLazyMax = 8.0f;
+constexpr int kMostPages = kMxMaxSplit / kKvPage;
+static_assert(kMostPages <= 64, "a lane holds the id of one page of the split");
+// Probabilities are taken relative to 2^-kShift of a maximum that moves only when a page's exceeds it by
+// kLazyMax (log2 units): the largest lies in [2^kShift, 2^(kShift + kLazyMax)], where its two fp16 parts hold
+// 22 bits and those of small ones the bits above 2^-(25 + kShift) of it, and O is rarely rescaled.
+constexpr float kShift = 4.0f, kLazyMax = 8.0f;
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {  // two fp16, nearest even
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, h2));
+}
+// The parts of a pair: the rounded values in lanes of keep 0, what rounding left in lanes of keep 1.
+__device__ __forceinline__ uint32_t part2(float a, float b, float keep) {
+  const h2 hi = __builtin_convertvector(f2{a, b}, h2);
+  return pack2(__builtin_fmaf(-keep, (float)hi.x, a), __builtin_fmaf(-keep, (float)hi.y, b));
+}
 
 template <int HD>
 struct MxPage {
   v4u k[HD / 32], v[HD / 32];
   uint32_t ks;
-  v4u vs[HD / 32];
+  v4u vs[HD / 16];
 };
 }  // namespace
 
 template <int HD>
 __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnParams p) {
   constexpr int NS = HD / 32, NT = HD / 16, NB = HD / kMxBlock;
-  constexpr int CODES = mx_codes(HD), EXPS = mx_exps(HD), REC = mx_record(HD);
+  constexpr int CODES = mx_codes(HD), REC = mx_record(HD), V = mx_v(HD);
   constexpr int SROW = HD + 4;  // a head's row of a wave's state in LDS
   __shared__ __attribute__((aligned(16))) float state[kWaves][8 * SROW];
   __shared__ float state_m[kWaves][8], state_l[kWaves][8];
@@ -102,7 +112,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = p.a.nq / p.a.nkv, hq0 = g * G;
   const int col = lane & 15, grp = lane >> 4, head = col & 7;
-  const bool low = col >= 8;  // this lane's column holds the low parts
+  const float keep = col >= 8 ? 1.0f : 0.0f;  // this lane's column holds the low parts
 
   const int len = p.a.len[b], u = p.a.users[b];
   const int page0 = split * (p.a.split / kKvPage);
@@ -124,9 +134,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
     return;
   }
 
-  // A split has at most kAttnMaxSplit / kKvPage pages: lane i holds the id of page i.
+  // Lane i holds the id of the split's page i.
   int pid = 0;
   if (lane < pages) pid = kv_page(p.a.kv, u, page0 + lane);
+  // The query operand, step s: d = grp hd/4 + 8 s .. + 7 of this column's head (columns past G repeat
+  // the last one, and are not read).
+  float f[NS][8];
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+    load_q8(p.q, p.q_type, ((int64_t)b * p.a.nq + hq0 + min(head, G - 1)) * HD + grp * (HD / 4) + 8 * s, f[s]);
   const uint8_t* heads = p.rec + (int64_t)g * REC;
   auto load = [&](MxPage<HD>& pg, int i) {
     const uint8_t* rec = heads + (int64_t)__builtin_amdgcn_readlane(pid, i) * p.a.kv.page_stride;
@@ -134,42 +150,33 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
     for (int j = 0; j < HD / 32; ++j) pg.k[j] = *reinterpret_cast<const v4u*>(rec + j * 1024 + lane * 16);
     pg.ks = *reinterpret_cast<const uint32_t*>(rec + CODES + ((HD == 128 ? grp : grp / 2) * 16 + col) * 4);
 #pragma unroll
-    for (int j = 0; j < HD / 32; ++j)
-      pg.v[j] = *reinterpret_cast<const v4u*>(rec + CODES + EXPS + j * 1024 + lane * 16);
+    for (int j = 0; j < HD / 32; ++j) pg.v[j] = *reinterpret_cast<const v4u*>(rec + V + j * 1024 + lane * 16);
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
-      pg.vs[j] = *reinterpret_cast<const v4u*>(rec + 2 * CODES + EXPS + (grp * NB + j) * 16);
+    for (int j = 0; j < 2 * NB; ++j) pg.vs[j] = *reinterpret_cast<const v4u*>(rec + V + CODES + grp * NB * 32 + j * 16);
   };
   MxPage<HD> even, odd;
   if (wave < pages) load(even, wave);
 
-  // The query operand: step s, d = grp hd/4 + 8 s .. + 7 of this column's head, in log2
-  // units and scaled by a power of two that puts its largest value near 2^10, so that the
-  // fp16 parts neither overflow nor lose bits below the normal range.
+  // In log2 units, times a power of two that puts the row's largest value near 2^10, so that the fp16
+  // parts neither overflow nor lose bits below the normal range.
   h8 qf[NS];
   float unscale;
   {
-    float f[NS][8], top = 0.f;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      load_q8(p.q, p.q_type, ((int64_t)b * p.a.nq + hq0 + min(head, G - 1)) * HD + grp * (HD / 4) + 8 * s, f[s]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        f[s][j] *= p.a.scale_log2;
-        top = fmaxf(top, __builtin_fabsf(f[s][j]));
-      }
-    }
-    top = groups_max(top);
-    const int e = top > 0.f && top < INFINITY ? min(max(10 - ilogbf(top), -100), 100) : 0;
-    unscale = ldexpf(1.0f, -e);
+    float top = 0.f;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float x = ldexpf(f[s][j], e);
-        const _Float16 hi = (_Float16)x;
-        qf[s][j] = head >= G ? (_Float16)0.f : low ? (_Float16)(x - (float)hi) : hi;
-      }
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, __builtin_fabsf(f[s][j]));
+    const int e = min(max((int)(__float_as_uint(groups_max(top)) >> 23) - 127, -90), 110);
+    unscale = __uint_as_float((uint32_t)(127 - 13 + e) << 23);
+    const float scale = p.a.scale_log2 * __uint_as_float((uint32_t)(127 + 13 - e) << 23);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[s][j] *= scale;
+      qf[s] = __builtin_bit_cast(h8, v4u{part2(f[s][0], f[s][1], keep), part2(f[s][2], f[s][3], keep),
+                                         part2(f[s][4], f[s][5], keep), part2(f[s][6], f[s][7], keep)});
+    }
   }
 
   v4f o[NT];  // O^T tile t: lane holds d = 16 t + 4 grp + r of its column's part
@@ -193,30 +200,33 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
         sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, kf), qf[s], sc[t], 0, 0, 0);
       }
     }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sc[t][r] += ror8(sc[t][r]);
     const int left = len - (page0 + i) * kKvPage;  // positions of the page
+    if (left < kKvPage) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (16 * t + 4 * grp + r >= left) sc[t][r] = -INFINITY;
+    }
     float mb = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float x = (sc[t][r] + ror8(sc[t][r])) * unscale;
-        if (16 * t + 4 * grp + r >= left) x = -INFINITY;
-        sc[t][r] = x;
-        mb = fmaxf(mb, x);
-      }
-    mb = groups_max(mb);
+    for (int t = 0; t < 4; ++t) mb = fmaxf(mb, fmaxf(fmaxf(sc[t][0], sc[t][1]), fmaxf(sc[t][2], sc[t][3])));
+    mb = groups_max(mb) * unscale - kShift;
     const float m_new = mb > m_run + kLazyMax ? mb : m_run;
     const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);  // 0 while m_run is -inf
-    float part[4][4], ls = 0.f;
+    float ls = 0.f;
+    uint32_t pw[8];  // pair k: positions 16 (k / 2) + 4 grp + 2 (k % 2), and the next
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float x = __builtin_amdgcn_exp2f(sc[t][r] - m_new);
-        ls += x;
-        const float hi = (float)(__bf16)x;
-        part[t][r] = low ? x - hi : hi;
-      }
+    for (int k = 0; k < 8; ++k) {
+      const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][2 * (k % 2)], unscale, -m_new));
+      const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][2 * (k % 2) + 1], unscale, -m_new));
+      ls += x + y;
+      pw[k] = part2(x, y, keep);
+    }
     l_run = l_run * alpha + ls;
     m_run = m_new;
     if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {
@@ -225,20 +235,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
+      const h8 pf = __builtin_bit_cast(h8, v4u{pw[4 * s], pw[4 * s + 1], pw[4 * s + 2], pw[4 * s + 3]});
 #pragma unroll
-      for (int blk = 0; blk < NB; ++blk) {
-        b8 pf;  // scaling by a power of two is exact, so the parts round here as they would unscaled
-#pragma unroll
-        for (int j = 0; j < 8; ++j) pf[j] = (__bf16)(part[2 * s + j / 4][j % 4] * exponent(pg.vs[blk][2 * s + j / 4], j % 4));
-#pragma unroll
-        for (int t = 2 * blk; t < 2 * blk + 2; ++t) {
-          const uint32_t w = pg.v[t / 2][(t % 2) * 2 + s];
-          const v4u vf = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0)),
-                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1)),
-                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2)),
-                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3))};
-          o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, vf), pf, o[t], 0, 0, 0);
-        }
+      for (int t = 0; t < NT; ++t) {
+        const uint32_t w = pg.v[t / 2][(t % 2) * 2 + s];
+        const h8 vs = __builtin_bit_cast(h8, pg.vs[2 * (t / 2) + s]);
+        const h2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0) * __builtin_shufflevector(vs, vs, 0, 1),
+                 v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1) * __builtin_shufflevector(vs, vs, 2, 3),
+                 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2) * __builtin_shufflevector(vs, vs, 4, 5),
+                 v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3) * __builtin_shufflevector(vs, vs, 6, 7);
+        const v4u vf = {__builtin_bit_cast(uint32_t, v0), __builtin_bit_cast(uint32_t, v1), __builtin_bit_cast(uint32_t, v2),
+                        __builtin_bit_cast(uint32_t, v3)};
+        o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, vf), pf, o[t], 0, 0, 0);
       }
     }
   };
@@ -256,7 +264,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
     v4f x;
 #pragma unroll
     for (int r = 0; r < 4; ++r) x[r] = o[t][r] + ror8(o[t][r]);
-    if (!low) *reinterpret_cast<v4f*>(&state[wave][head * SROW + 16 * t + 4 * grp]) = x;
+    if (col < 8) *reinterpret_cast<v4f*>(&state[wave][head * SROW + 16 * t + 4 * grp]) = x;
   }
   if (lane < 8) {
     state_m[wave][lane] = m_run;
@@ -281,29 +289,56 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
 }
 
 // Merge of a row's split partials into the output of kf_kv_attend; a row without
-// positions gives zeros.  Workgroup (head, row); wave w sums every fourth split.
+// positions gives zeros.  Workgroup (head, row): the splits' weights at once, in LDS, then each
+// wave sums every fourth split, eight loads in flight.
 template <int HD>
 __global__ __launch_bounds__(256) void attend_merge_kernel(const MxAttnParams p) {
-  constexpr int DPL = HD / 64;
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int DPL = HD / 64, PRE = 8;
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ns = p.a.n_split;
   const int64_t r0 = ((int64_t)b * p.a.nq + h) * p.a.max_split;
   const float* ml = p.a.part_ml + r0 * 2;
   const float* acc = p.a.part_acc + r0 * HD + lane * DPL;
-  __shared__ float red[4][HD], red_l[4];
+  __shared__ float weight[kAttnMaxSplitCount];
+  __shared__ float red[4][HD], red_m[4], red_l[4];
+  // The wave's first splits are asked for with the maxima; past the last split it is read again, at weight 0.
+  float pre[PRE][DPL];
+#pragma unroll
+  for (int k = 0; k < PRE; ++k)
+#pragma unroll
+    for (int i = 0; i < DPL; ++i) pre[k][i] = acc[(int64_t)min(wave + 4 * k, ns - 1) * HD + i];
   float M = -INFINITY;
-  for (int s = lane; s < p.a.n_split; s += 64) M = fmaxf(M, ml[2 * s]);
+  for (int s = tid; s < ns; s += 256) M = fmaxf(M, ml[2 * s]);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-  float v[DPL] = {}, l = 0.f;
-  for (int s = wave; s < p.a.n_split; s += 4) {
+  if (lane == 0) red_m[wave] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
+  float l = 0.f;
+  for (int s = tid; s < ns; s += 256) {
+    // M is -inf where no split saw a key, or where every score was NaN: those sums stay NaN
     const float f = M == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml[2 * s] - M);
+    weight[s] = f;
     l += f * ml[2 * s + 1];
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) l += __shfl_xor(l, o);
+  if (lane == 0) red_l[wave] = l;
+  __syncthreads();
+  float v[DPL] = {};
+#pragma unroll
+  for (int k = 0; k < PRE; ++k) {
+    const float f = wave + 4 * k < ns ? weight[wave + 4 * k] : 0.f;
+#pragma unroll
+    for (int i = 0; i < DPL; ++i) v[i] += f * pre[k][i];
+  }
+#pragma unroll 8
+  for (int s = wave + 4 * PRE; s < ns; s += 4) {
+    const float f = weight[s];
 #pragma unroll
     for (int i = 0; i < DPL; ++i) v[i] += f * acc[(int64_t)s * HD + i];
   }
 #pragma unroll
   for (int i = 0; i < DPL; ++i) red[wave][lane * DPL + i] = v[i];
-  if (lane == 0) red_l[wave] = l;
   __syncthreads();
   if (tid < HD) {
     const float x = (red[0][tid] + red[1][tid]) + (red[2][tid] + red[3][tid]);
@@ -359,9 +394,9 @@ __global__ __launch_bounds__(256) void mx_append_kernel(const MxAppendParams p) 
   const uint32_t w = mx_encode8(x, e, bad);
   raise_err(p.err_flag, bad, kErrF16Range);
   const int t = p.pos[b] % kKvPage;
-  const int codes = mx_codes(hd), exps = mx_exps(hd);
+  const int codes = mx_codes(hd);
   uint8_t* rec = p.rec + (int64_t)kv_page(p.kv, p.users[b], p.pos[b] / kKvPage) * p.kv.page_stride +
-                 (int64_t)g * mx_record(hd) + (is_v ? codes + exps : 0);
+                 (int64_t)g * mx_record(hd) + (is_v ? mx_v(hd) : 0);
   const int blk = d0 / kMxBlock;
   if (!is_v) {
     *reinterpret_cast<uint32_t*>(rec + (hd == 128 ? mx_k_byte<128>(t, d0) : mx_k_byte<64>(t, d0))) = w;
@@ -374,7 +409,8 @@ __global__ __launch_bounds__(256) void mx_append_kernel(const MxAppendParams p) 
     const uint32_t c = (w >> (4 * j)) & 15u;
     *at = (uint8_t)(t & 1 ? (*at & 0x0f) | (c << 4) : (*at & 0xf0) | c);
   }
-  if (d0 % kMxBlock == 0) rec[codes + (hd == 128 ? mx_v_exp<128>(t, blk) : mx_v_exp<64>(t, blk))] = (uint8_t)(e + 127);
+  if (d0 % kMxBlock == 0)
+    reinterpret_cast<uint16_t*>(rec + codes)[hd == 128 ? mx_v_exp<128>(t, blk) : mx_v_exp<64>(t, blk)] = mx_v_scale(e);
 }
 
 __global__ void rows_to_f32_kernel(const void* src, int type, float* dst, int n8) {
@@ -388,7 +424,7 @@ __global__ void rows_to_f32_kernel(const void* src, int type, float* dst, int n8
 
 // ------------------------------------------------------------------ launchers
 hipError_t launch_attn_mx(const MxAttnParams& p, int batch, hipStream_t s) {
-  if (p.a.nq % p.a.nkv || p.a.nq / p.a.nkv > 8 || p.a.split % kKvPage || p.a.split > kAttnMaxSplit) return hipErrorInvalidValue;
+  if (p.a.nq % p.a.nkv || p.a.nq / p.a.nkv > 8 || p.a.split % kKvPage || p.a.split > kMxMaxSplit) return hipErrorInvalidValue;
   const dim3 grid(p.a.n_split, p.a.nkv, batch);
   if (p.a.hd == 128) hipLaunchKernelGGL(attn_mx_kernel<128>, grid, dim3(64 * kWaves), 0, s, p);
   else if (p.a.hd == 64) hipLaunchKernelGGL(attn_mx_kernel<64>, grid, dim3(64 * kWaves), 0, s, p);

@@ -81,12 +81,12 @@ struct MxEncodeParams {
 template <int HD>
 __global__ __launch_bounds__(256) void mx_encode_kernel(const MxEncodeParams p) {
   constexpr int UPR = HD / 8;  // 8-value units per position
-  constexpr int REC = mx_record(HD), CODES = mx_codes(HD), EXPS = mx_exps(HD);
+  constexpr int REC = mx_record(HD), CODES = mx_codes(HD);
   __shared__ uint32_t codes[kKvPage * UPR];
   const int page = p.pos0 / kKvPage + blockIdx.x, g = blockIdx.y >> 1, is_v = blockIdx.y & 1, tid = threadIdx.x;
   const int a = max(p.pos0 - page * kKvPage, 0), b = min(p.pos0 + p.n - page * kKvPage, kKvPage);
   uint8_t* rec = p.dst + blockIdx.z * p.dst_layer + (int64_t)kv_page(p.dp, p.dst_user, page) * p.dp.page_stride +
-                 (int64_t)g * REC + (is_v ? CODES + EXPS : 0);
+                 (int64_t)g * REC + (is_v ? mx_v(HD) : 0);
   const void* src = is_v ? p.sv : p.sk;
   bool bad = false;
   // Every load goes out before the first is used.
@@ -116,7 +116,10 @@ __global__ __launch_bounds__(256) void mx_encode_kernel(const MxEncodeParams p) 
     } else {
       codes[u] = w;
     }
-    if (live && u % 4 == 0) rec[CODES + (is_v ? mx_v_exp<HD>(t, d0 / kMxBlock) : mx_k_exp(t, d0 / kMxBlock))] = (uint8_t)(e + 127);
+    if (live && u % 4 == 0) {
+      if (is_v) reinterpret_cast<uint16_t*>(rec + CODES)[mx_v_exp<HD>(t, d0 / kMxBlock)] = mx_v_scale(e);
+      else rec[CODES + mx_k_exp(t, d0 / kMxBlock)] = (uint8_t)(e + 127);
+    }
   }
   raise_err(p.err_flag, bad, kErrF16Range);
   if (!is_v) return;
@@ -158,12 +161,12 @@ struct MxDecodeParams {
 template <int HD>
 __global__ __launch_bounds__(256) void mx_decode_kernel(const MxDecodeParams p) {
   constexpr int UPR = HD / 8;
-  constexpr int REC = mx_record(HD), CODES = mx_codes(HD), EXPS = mx_exps(HD);
+  constexpr int REC = mx_record(HD), CODES = mx_codes(HD);
   __shared__ v4u codes[CODES / 16];
   const int page = p.pos0 / kKvPage + blockIdx.x, g = blockIdx.y >> 1, is_v = blockIdx.y & 1, tid = threadIdx.x;
   const int a = max(p.pos0 - page * kKvPage, 0), b = min(p.pos0 + p.n - page * kKvPage, kKvPage);
   const uint8_t* rec = p.src + blockIdx.z * p.src_layer + (int64_t)kv_page(p.sp, p.src_user, page) * p.sp.page_stride +
-                       (int64_t)g * REC + (is_v ? CODES + EXPS : 0);
+                       (int64_t)g * REC + (is_v ? mx_v(HD) : 0);
   if (is_v) {
     for (int i = tid; i < CODES / 16; i += 256) codes[i] = reinterpret_cast<const v4u*>(rec)[i];
     __syncthreads();
@@ -174,16 +177,15 @@ __global__ __launch_bounds__(256) void mx_decode_kernel(const MxDecodeParams p) 
     const int u = tid + 256 * k, t = u / UPR, d0 = (u % UPR) * 8;
     if (t < a || t >= b) continue;
     uint32_t w = 0;
-    int e;
+    float scale;
     if (is_v) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) w |= (uint32_t)((lds[mx_v_byte(t, d0 + i)] >> (4 * (t & 1))) & 15) << (4 * i);
-      e = rec[CODES + mx_v_exp<HD>(t, d0 / kMxBlock)];
+      scale = (float)reinterpret_cast<const _Float16*>(rec + CODES)[mx_v_exp<HD>(t, d0 / kMxBlock)];
     } else {
       w = *reinterpret_cast<const uint32_t*>(rec + mx_k_byte<HD>(t, d0));
-      e = rec[CODES + mx_k_exp(t, d0 / kMxBlock)];
+      scale = __uint_as_float((uint32_t)rec[CODES + mx_k_exp(t, d0 / kMxBlock)] << 23);
     }
-    const float scale = __uint_as_float((uint32_t)e << 23);
     if (p.to_pages) {
       const h2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1),
                x2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
@@ -216,7 +218,7 @@ struct CopyParams {
 // which only what belongs to positions [a, b) is replaced.
 template <int HD>
 __global__ __launch_bounds__(256) void mx_copy_kernel(const CopyParams p) {
-  constexpr int REC = mx_record(HD), CODES = mx_codes(HD), EXPS = mx_exps(HD);
+  constexpr int REC = mx_record(HD), CODES = mx_codes(HD);
   const int page = p.pos0 / kKvPage + blockIdx.x, g = blockIdx.y;
   const int a = max(p.pos0 - page * kKvPage, 0), b = min(p.pos0 + p.n - page * kKvPage, kKvPage);
   auto record = [&](const CacheRef& c, int user) {
@@ -230,7 +232,7 @@ __global__ __launch_bounds__(256) void mx_copy_kernel(const CopyParams p) {
   }
   auto in = [&](int t) { return t >= a && t < b; };
   for (int i = threadIdx.x; i < REC / 4; i += 256) {
-    const int is_v = i * 4 >= CODES + EXPS, at = i * 4 - (is_v ? CODES + EXPS : 0);
+    const int is_v = i * 4 >= mx_v(HD), at = i * 4 - (is_v ? mx_v(HD) : 0);
     uint32_t mask = 0;
     if (at < CODES) {
       if (is_v) {  // 8 positions of one d
@@ -241,12 +243,13 @@ __global__ __launch_bounds__(256) void mx_copy_kernel(const CopyParams p) {
         const int tile = HD == 128 ? at >> 10 : 2 * (at >> 10) + ((at >> 3) & 1);
         if (in(16 * tile + ((at >> 4) & 15))) mask = ~0u;
       }
+    } else if (is_v) {  // the scales of 2 positions
+      const int w = (at - CODES) / 2, t = 16 * ((w >> 2) & 3) + 4 * ((w >> 4) / (HD / kMxBlock)) + w % 4;
+      if (in(t)) mask |= 0xffffu;
+      if (in(t + 1)) mask |= 0xffff0000u;
     } else {  // the exponents of 4 positions
-      const int w = at - CODES;
-      for (int j = 0; j < 4; ++j) {
-        const int t = is_v ? 16 * ((w >> 2) & 3) + 4 * ((w >> 4) / (HD / kMxBlock)) + j : 16 * j + ((w >> 2) & 15);
-        if (in(t)) mask |= 255u << (8 * j);
-      }
+      for (int j = 0; j < 4; ++j)
+        if (in(16 * j + (((at - CODES) >> 2) & 15))) mask |= 255u << (8 * j);
     }
     if (!mask) continue;
     const uint32_t v = reinterpret_cast<const uint32_t*>(src)[i];

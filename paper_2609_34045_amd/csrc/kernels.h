@@ -62,15 +62,20 @@ __device__ __forceinline__ int64_t kv_offset(const KvPages& kp, int user, int g,
 // MXFP4 caches (KF_KV_MXFP4).  A page holds one record per KV head, K codes, K
 // exponents, V codes, V exponents; KvPages::page_stride counts bytes there.  A
 // block of kMxBlock values along the head has one exponent e in [kMxExpMin,
-// kMxExpMax], stored as e + 127, and E2M1 codes: value = 2^e times 0, 0.5, 1, 1.5,
-// 2, 3, 4 or 6 with a sign.  With that range every stored value is an fp16 number.
+// kMxExpMax] and E2M1 codes: value = 2^e times 0, 0.5, 1, 1.5, 2, 3, 4 or 6 with a
+// sign.  With that range every stored value is an fp16 number.  K's exponents are bytes
+// e + 127, of which the convert instruction's fp32 scale is made by a shift.  V's are
+// 2^e in fp16: a register of V operands holds two positions, so the products with their
+// two scales are one packed instruction where the pair lies ready (1/32 more bytes, a third
+// fewer instructions in the attention's loop than with bytes that each lane expands).
 // Codes and exponents lie in the order in which the attention's lanes take them
 // (mx_* below), so that each of its loads is 16 contiguous bytes a lane.
 constexpr int kMxBlock = 32;
 constexpr int kMxExpMin = -23, kMxExpMax = 13;
 __host__ __device__ constexpr int mx_codes(int hd) { return kKvPage * hd / 2; }           // bytes, K or V
-__host__ __device__ constexpr int mx_exps(int hd) { return kKvPage * hd / kMxBlock; }     // bytes, K or V
-__host__ __device__ constexpr int mx_record(int hd) { return 2 * (mx_codes(hd) + mx_exps(hd)); }
+__host__ __device__ constexpr int mx_exps(int hd) { return kKvPage * hd / kMxBlock; }     // exponents, K or V
+__host__ __device__ constexpr int mx_v(int hd) { return mx_codes(hd) + mx_exps(hd); }     // byte where V begins
+__host__ __device__ constexpr int mx_record(int hd) { return mx_v(hd) + mx_codes(hd) + 2 * mx_exps(hd); }
 // Position t of the page as a matrix-core operand sees it: tile t / 16, and within
 // it row t % 16 of K; for V, 16-lane group (t / 4) % 4 and element t % 4.
 // Byte of the K code of (t, d); its nibble is d % 2.  A lane (row, group) takes hd / 4 consecutive d.
@@ -87,10 +92,13 @@ __host__ __device__ constexpr int mx_v_byte(int t, int d) {
   const int dt = d / 16;
   return ((dt / 2) * 64 + ((t / 4) % 4) * 16 + d % 16) * 16 + (dt % 2) * 8 + (t / 16) * 2 + (t % 4) / 2;
 }
-// Byte of the exponent of V block blk at t.
+// Index of the scale (fp16) of V block blk at t.
 template <int HD>
 __host__ __device__ constexpr int mx_v_exp(int t, int blk) {
   return (((t / 4) % 4) * (HD / kMxBlock) + blk) * 16 + (t / 16) * 4 + t % 4;
+}
+__device__ __forceinline__ uint16_t mx_v_scale(int e) {  // 2^e
+  return (uint16_t)(e >= -14 ? (e + 15) << 10 : 1 << (e + 24));
 }
 
 // 8 of a block's values, the other 24 in the 3 lanes beside (lanes 4 k .. 4 k + 3 hold a
@@ -231,6 +239,7 @@ struct AttnParams {
 // Attention over an MXFP4 cache (attend.hip): a's queries and cache pointers are not
 // used, its KvPages count bytes, its splits are whole pages.  With `out` set (one split, or
 // the merge) the result goes there; else the partials go to a's arrays, as the fp16 kernel's do.
+constexpr int kMxMaxSplit = 4096;  // keys per workgroup, upper bound
 struct MxAttnParams {
   AttnParams a;
   const uint8_t* rec;  // layer base

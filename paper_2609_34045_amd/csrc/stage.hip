@@ -1056,7 +1056,7 @@ static void attn_split_mfma(int nkv, int64_t total_len, int max_len, int max_spl
 // Pages per workgroup of the attention over MXFP4 caches: about two workgroups a CU over the batch's
 // pages, a page for each of a workgroup's waves at least.
 static void attn_split_mx(int nkv, int64_t total_pages, int max_len, int max_split, int n_cu, int* split, int* n_split) {
-  const int64_t wgs = 2LL * n_cu, most = kAttnMaxSplit / kKvPage;
+  const int64_t wgs = 2LL * n_cu, most = kMxMaxSplit / kKvPage;
   const int pages = pages_for(max_len);
   int64_t sp = (total_pages * nkv + wgs - 1) / wgs;
   if (sp < 4) sp = 4;
