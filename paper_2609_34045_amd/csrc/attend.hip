@@ -101,15 +101,17 @@ struct MxPage {
 }  // namespace
 
 template <int HD>
-__global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnParams p) {
+__global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const MxAttnParams p) {
   constexpr int NS = HD / 32, NT = HD / 16, NB = HD / kMxBlock;
   constexpr int CODES = mx_codes(HD), REC = mx_record(HD), V = mx_v(HD);
   constexpr int SROW = HD + 4;  // a head's row of a wave's state in LDS
   __shared__ __attribute__((aligned(16))) float state[kWaves][8 * SROW];
   __shared__ float state_m[kWaves][8], state_l[kWaves][8];
 
-  const int split = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // grid.x: the splits of row 0, then of row 1, ..
+  int split = blockIdx.x, b = 0;
+  for (; b < kMaxBatch - 1 && split >= p.a.row_splits[b]; ++b) split -= p.a.row_splits[b];
+  const int g = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = p.a.nq / p.a.nkv, hq0 = g * G;
   const int col = lane & 15, grp = lane >> 4, head = col & 7;
   const float keep = col >= 8 ? 1.0f : 0.0f;  // this lane's column holds the low parts
@@ -129,7 +131,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
       p.a.part_ml[row * 2 + 1] = l;
     }
   };
-  if (pages <= 0) {  // a trailing split of a shorter row, or a row without positions
+  if (pages <= 0) {  // a row without positions
     for (int e = tid; e < G * HD; e += 64 * kWaves) put(e / HD, e % HD, 0.f, -INFINITY, 0.f);
     return;
   }
@@ -137,32 +139,36 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
   // Lane i holds the id of the split's page i.
   int pid = 0;
   if (lane < pages) pid = kv_page(p.a.kv, u, page0 + lane);
-  // The query operand, step s: d = grp hd/4 + 8 s .. + 7 of this column's head (columns past G repeat
-  // the last one, and are not read).
-  float f[NS][8];
-#pragma unroll
-  for (int s = 0; s < NS; ++s)
-    load_q8(p.q, p.q_type, ((int64_t)b * p.a.nq + hq0 + min(head, G - 1)) * HD + grp * (HD / 4) + 8 * s, f[s]);
   const uint8_t* heads = p.rec + (int64_t)g * REC;
-  auto load = [&](MxPage<HD>& pg, int i) {
-    const uint8_t* rec = heads + (int64_t)__builtin_amdgcn_readlane(pid, i) * p.a.kv.page_stride;
+  MxPage<HD> pg;
+  auto record = [&](int i) { return heads + (int64_t)__builtin_amdgcn_readlane(pid, i) * p.a.kv.page_stride; };
+  auto load_k = [&](const uint8_t* rec) {
 #pragma unroll
     for (int j = 0; j < HD / 32; ++j) pg.k[j] = *reinterpret_cast<const v4u*>(rec + j * 1024 + lane * 16);
     pg.ks = *reinterpret_cast<const uint32_t*>(rec + CODES + ((HD == 128 ? grp : grp / 2) * 16 + col) * 4);
+  };
+  auto load_v = [&](const uint8_t* rec) {
 #pragma unroll
     for (int j = 0; j < HD / 32; ++j) pg.v[j] = *reinterpret_cast<const v4u*>(rec + V + j * 1024 + lane * 16);
 #pragma unroll
     for (int j = 0; j < 2 * NB; ++j) pg.vs[j] = *reinterpret_cast<const v4u*>(rec + V + CODES + grp * NB * 32 + j * 16);
   };
-  MxPage<HD> even, odd;
-  if (wave < pages) load(even, wave);
+  if (wave < pages) {
+    load_k(record(wave));
+    load_v(record(wave));
+  }
 
+  // The query operand, step s: d = grp hd/4 + 8 s .. + 7 of this column's head (columns past G repeat the
+  // last one, and are not read).  Asked for after the page, so that one wait covers both.
   // In log2 units, times a power of two that puts the row's largest value near 2^10, so that the fp16
   // parts neither overflow nor lose bits below the normal range.
   h8 qf[NS];
   float unscale;
   {
-    float top = 0.f;
+    float f[NS][8], top = 0.f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+      load_q8(p.q, p.q_type, ((int64_t)b * p.a.nq + hq0 + min(head, G - 1)) * HD + grp * (HD / 4) + 8 * s, f[s]);
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -184,7 +190,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
   for (int t = 0; t < NT; ++t) o[t] = v4f{0.f, 0.f, 0.f, 0.f};
   float m_run = -INFINITY, l_run = 0.f;
 
-  auto compute = [&](const MxPage<HD>& pg, int i) {
+  for (int i = wave; i < pages; i += kWaves) {
+    const bool more = i + kWaves < pages;
+    const uint8_t* next = record(more ? i + kWaves : i);
     v4f sc[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -200,6 +208,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
         sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, kf), qf[s], sc[t], 0, 0, 0);
       }
     }
+    if (more) load_k(next);  // K's registers are free from here on, V's after the last product
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -249,12 +258,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
         o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, vf), pf, o[t], 0, 0, 0);
       }
     }
-  };
-  for (int i = wave; i < pages; i += 2 * kWaves) {
-    if (i + kWaves < pages) load(odd, i + kWaves);
-    compute(even, i);
-    if (i + 2 * kWaves < pages) load(even, i + 2 * kWaves);
-    if (i + kWaves < pages) compute(odd, i + kWaves);
+    if (more) load_v(next);
   }
   l_run = groups_sum(l_run);
 
@@ -294,7 +298,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_mx_kernel(const MxAttnPar
 template <int HD>
 __global__ __launch_bounds__(256) void attend_merge_kernel(const MxAttnParams p) {
   constexpr int DPL = HD / 64, PRE = 8;
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ns = p.a.n_split;
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ns = p.a.row_splits[b];
   const int64_t r0 = ((int64_t)b * p.a.nq + h) * p.a.max_split;
   const float* ml = p.a.part_ml + r0 * 2;
   const float* acc = p.a.part_acc + r0 * HD + lane * DPL;
@@ -425,7 +429,12 @@ __global__ void rows_to_f32_kernel(const void* src, int type, float* dst, int n8
 // ------------------------------------------------------------------ launchers
 hipError_t launch_attn_mx(const MxAttnParams& p, int batch, hipStream_t s) {
   if (p.a.nq % p.a.nkv || p.a.nq / p.a.nkv > 8 || p.a.split % kKvPage || p.a.split > kMxMaxSplit) return hipErrorInvalidValue;
-  const dim3 grid(p.a.n_split, p.a.nkv, batch);
+  int splits = 0;
+  for (int b = 0; b < batch; ++b) {
+    if (p.a.row_splits[b] < 1 || p.a.row_splits[b] > p.a.max_split) return hipErrorInvalidValue;
+    splits += p.a.row_splits[b];
+  }
+  const dim3 grid(splits, p.a.nkv);
   if (p.a.hd == 128) hipLaunchKernelGGL(attn_mx_kernel<128>, grid, dim3(64 * kWaves), 0, s, p);
   else if (p.a.hd == 64) hipLaunchKernelGGL(attn_mx_kernel<64>, grid, dim3(64 * kWaves), 0, s, p);
   else return hipErrorInvalidValue;

@@ -73,7 +73,8 @@ struct MxEncodeParams {
   int* err_flag;
 };
 
-// Workgroup (page, K or V of one KV head, layer): encodes the page's positions that
+// Workgroup (K or V of one KV head, page, layer), neighbouring workgroups taking the heads of the
+// same positions, whose rows lie side by side in the source: encodes the page's positions that
 // lie in [pos0, pos0 + n) and leaves the others as they are.  Four lanes hold a
 // block, 8 values each.  K codes go out as they are made (8 codes are 4 bytes of a
 // row); V codes, whose bytes hold neighbouring positions, meet in LDS first.  One
@@ -83,15 +84,15 @@ __global__ __launch_bounds__(256) void mx_encode_kernel(const MxEncodeParams p) 
   constexpr int UPR = HD / 8;  // 8-value units per position
   constexpr int REC = mx_record(HD), CODES = mx_codes(HD);
   __shared__ uint32_t codes[kKvPage * UPR];
-  const int page = p.pos0 / kKvPage + blockIdx.x, g = blockIdx.y >> 1, is_v = blockIdx.y & 1, tid = threadIdx.x;
+  const int page = p.pos0 / kKvPage + blockIdx.y, g = blockIdx.x >> 1, is_v = blockIdx.x & 1, tid = threadIdx.x;
   const int a = max(p.pos0 - page * kKvPage, 0), b = min(p.pos0 + p.n - page * kKvPage, kKvPage);
-  uint8_t* rec = p.dst + blockIdx.z * p.dst_layer + (int64_t)kv_page(p.dp, p.dst_user, page) * p.dp.page_stride +
-                 (int64_t)g * REC + (is_v ? mx_v(HD) : 0);
   const void* src = is_v ? p.sv : p.sk;
   bool bad = false;
   // Every load goes out before the first is used.
   constexpr int NU = kKvPage * UPR / 256;
+  constexpr int NW = CODES / 4 / 256;
   float f[NU][8];
+  uint32_t old[NW];  // the V codes of a page that is written in part
 #pragma unroll
   for (int k = 0; k < NU; ++k) {
     const int u = tid + 256 * k, t = u / UPR, d0 = (u % UPR) * 8;
@@ -104,6 +105,13 @@ __global__ __launch_bounds__(256) void mx_encode_kernel(const MxEncodeParams p) 
     } else {
       load8(src, p.src_type, ((int64_t)(page * kKvPage + t - p.pos0) * p.nkv + g) * HD + d0, p.wide, f[k]);
     }
+  }
+  uint8_t* rec = p.dst + blockIdx.z * p.dst_layer + (int64_t)kv_page(p.dp, p.dst_user, page) * p.dp.page_stride +
+                 (int64_t)g * REC + (is_v ? mx_v(HD) : 0);
+  const bool whole = a == 0 && b == kKvPage;
+  if (is_v && !whole) {
+#pragma unroll
+    for (int k = 0; k < NW; ++k) old[k] = reinterpret_cast<const uint32_t*>(rec)[tid + 256 * k];
   }
 #pragma unroll
   for (int k = 0; k < NU; ++k) {
@@ -126,7 +134,7 @@ __global__ __launch_bounds__(256) void mx_encode_kernel(const MxEncodeParams p) 
   __syncthreads();
   const uint8_t* lds = reinterpret_cast<const uint8_t*>(codes);
 #pragma unroll
-  for (int k = 0; k < CODES / 4 / 256; ++k) {
+  for (int k = 0; k < NW; ++k) {
     const int w = tid + 256 * k;  // dword of the V codes: 8 positions of one d
     const int s = w & 1, d = (2 * (w >> 8) + ((w >> 1) & 1)) * 16 + ((w >> 2) & 15), grp = (w >> 6) & 3;
     uint32_t v = 0, mask = 0;
@@ -137,8 +145,8 @@ __global__ __launch_bounds__(256) void mx_encode_kernel(const MxEncodeParams p) 
       if (t >= a && t < b) mask |= 15u << (4 * j);
     }
     uint32_t* out = reinterpret_cast<uint32_t*>(rec) + w;
-    if (mask == ~0u) *out = v;
-    else if (mask) *out = (*out & ~mask) | (v & mask);
+    if (whole) *out = v;
+    else if (mask) *out = (old[k] & ~mask) | (v & mask);
   }
 }
 
@@ -147,8 +155,7 @@ struct MxDecodeParams {
   KvPages sp;
   int src_user;
   int64_t src_layer;
-  uint8_t *dk, *dv;  // fp32 rows [n][nkv][hd], or (to_pages) fp16 pages
-  int to_pages;
+  uint8_t *dk, *dv;  // fp32 rows [n][nkv][hd], or fp16 pages
   int wide;  // rows: dk and dv are 16-byte aligned
   KvPages dp;
   int dst_user;
@@ -157,54 +164,62 @@ struct MxDecodeParams {
 };
 
 // The way back, exactly: workgroups as above.  V codes pass through LDS, where each
-// thread collects the nibbles of its 8 values.
-template <int HD>
+// thread collects the nibbles of its values.  A thread stores 16 bytes, beside its
+// neighbours': 4 values of fp32 rows, 8 of fp16 pages.
+template <int HD, bool PAGES>
 __global__ __launch_bounds__(256) void mx_decode_kernel(const MxDecodeParams p) {
-  constexpr int UPR = HD / 8;
+  constexpr int VPU = PAGES ? 8 : 4, UPR = HD / VPU;  // values per unit, units per position
   constexpr int REC = mx_record(HD), CODES = mx_codes(HD);
   __shared__ v4u codes[CODES / 16];
-  const int page = p.pos0 / kKvPage + blockIdx.x, g = blockIdx.y >> 1, is_v = blockIdx.y & 1, tid = threadIdx.x;
+  const int page = p.pos0 / kKvPage + blockIdx.y, g = blockIdx.x >> 1, is_v = blockIdx.x & 1, tid = threadIdx.x;
   const int a = max(p.pos0 - page * kKvPage, 0), b = min(p.pos0 + p.n - page * kKvPage, kKvPage);
   const uint8_t* rec = p.src + blockIdx.z * p.src_layer + (int64_t)kv_page(p.sp, p.src_user, page) * p.sp.page_stride +
                        (int64_t)g * REC + (is_v ? mx_v(HD) : 0);
+  constexpr int NU = kKvPage * UPR / 256;
+  uint32_t kw[NU];
+  float scale[NU];
   if (is_v) {
     for (int i = tid; i < CODES / 16; i += 256) codes[i] = reinterpret_cast<const v4u*>(rec)[i];
-    __syncthreads();
   }
+#pragma unroll
+  for (int k = 0; k < NU; ++k) {
+    const int u = tid + 256 * k, t = u / UPR, d0 = (u % UPR) * VPU;
+    if (is_v) {
+      scale[k] = (float)reinterpret_cast<const _Float16*>(rec + CODES)[mx_v_exp<HD>(t, d0 / kMxBlock)];
+    } else {
+      const uint8_t* at = rec + mx_k_byte<HD>(t, d0);
+      kw[k] = PAGES ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
+      scale[k] = __uint_as_float((uint32_t)rec[CODES + mx_k_exp(t, d0 / kMxBlock)] << 23);
+    }
+  }
+  if (is_v) __syncthreads();
   const uint8_t* lds = reinterpret_cast<const uint8_t*>(codes);
 #pragma unroll
-  for (int k = 0; k < kKvPage * UPR / 256; ++k) {
-    const int u = tid + 256 * k, t = u / UPR, d0 = (u % UPR) * 8;
+  for (int k = 0; k < NU; ++k) {
+    const int u = tid + 256 * k, t = u / UPR, d0 = (u % UPR) * VPU;
     if (t < a || t >= b) continue;
     uint32_t w = 0;
-    float scale;
     if (is_v) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w |= (uint32_t)((lds[mx_v_byte(t, d0 + i)] >> (4 * (t & 1))) & 15) << (4 * i);
-      scale = (float)reinterpret_cast<const _Float16*>(rec + CODES)[mx_v_exp<HD>(t, d0 / kMxBlock)];
+      for (int i = 0; i < VPU; ++i) w |= (uint32_t)((lds[mx_v_byte(t, d0 + i)] >> (4 * (t & 1))) & 15) << (4 * i);
     } else {
-      w = *reinterpret_cast<const uint32_t*>(rec + mx_k_byte<HD>(t, d0));
-      scale = __uint_as_float((uint32_t)rec[CODES + mx_k_exp(t, d0 / kMxBlock)] << 23);
+      w = kw[k];
     }
-    if (p.to_pages) {
-      const h2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1),
-               x2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
+    if constexpr (PAGES) {
+      const h2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale[k], 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale[k], 1),
+               x2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale[k], 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale[k], 3);
       uint16_t* dst = reinterpret_cast<uint16_t*>((is_v ? p.dv : p.dk) + blockIdx.z * p.dst_layer) +
                       kv_offset(p.dp, p.dst_user, g, page * kKvPage + t, HD) + d0;
       *reinterpret_cast<v4u*>(dst) = v4u{__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1),
                                          __builtin_bit_cast(uint32_t, x2), __builtin_bit_cast(uint32_t, x3)};
-      continue;
-    }
-    const f2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1),
-             x2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
-    float* dst = reinterpret_cast<float*>(is_v ? p.dv : p.dk) +
-                 ((int64_t)(page * kKvPage + t - p.pos0) * p.nkv + g) * HD + d0;
-    if (p.wide) {
-      __builtin_nontemporal_store(v4f{x0.x, x0.y, x1.x, x1.y}, reinterpret_cast<v4f*>(dst));
-      __builtin_nontemporal_store(v4f{x2.x, x2.y, x3.x, x3.y}, reinterpret_cast<v4f*>(dst) + 1);
     } else {
-      dst[0] = x0.x; dst[1] = x0.y; dst[2] = x1.x; dst[3] = x1.y;
-      dst[4] = x2.x; dst[5] = x2.y; dst[6] = x3.x; dst[7] = x3.y;
+      const f2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale[k], 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale[k], 1);
+      float* dst = reinterpret_cast<float*>(is_v ? p.dv : p.dk) + ((int64_t)(page * kKvPage + t - p.pos0) * p.nkv + g) * HD + d0;
+      if (p.wide) {
+        __builtin_nontemporal_store(v4f{x0.x, x0.y, x1.x, x1.y}, reinterpret_cast<v4f*>(dst));
+      } else {
+        dst[0] = x0.x; dst[1] = x0.y; dst[2] = x1.x; dst[3] = x1.y;
+      }
     }
   }
 }
@@ -292,16 +307,17 @@ static bool aligned16(const void* a, const void* b) { return (((uintptr_t)a | (u
 static unsigned pages_spanned(int pos0, int n) { return (unsigned)((pos0 + n - 1) / kKvPage - pos0 / kKvPage + 1); }
 
 static hipError_t encode(const MxEncodeParams& p, int hd, int layers, hipStream_t s) {
-  const dim3 grid(pages_spanned(p.pos0, p.n), 2 * p.nkv, layers);
+  const dim3 grid(2 * p.nkv, pages_spanned(p.pos0, p.n), layers);
   if (hd == 128) hipLaunchKernelGGL(mx_encode_kernel<128>, grid, dim3(256), 0, s, p);
   else if (hd == 64) hipLaunchKernelGGL(mx_encode_kernel<64>, grid, dim3(256), 0, s, p);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
+template <bool PAGES>
 static hipError_t decode(const MxDecodeParams& p, int hd, int layers, hipStream_t s) {
-  const dim3 grid(pages_spanned(p.pos0, p.n), 2 * p.nkv, layers);
-  if (hd == 128) hipLaunchKernelGGL(mx_decode_kernel<128>, grid, dim3(256), 0, s, p);
-  else if (hd == 64) hipLaunchKernelGGL(mx_decode_kernel<64>, grid, dim3(256), 0, s, p);
+  const dim3 grid(2 * p.nkv, pages_spanned(p.pos0, p.n), layers);
+  if (hd == 128) hipLaunchKernelGGL((mx_decode_kernel<128, PAGES>), grid, dim3(256), 0, s, p);
+  else if (hd == 64) hipLaunchKernelGGL((mx_decode_kernel<64, PAGES>), grid, dim3(256), 0, s, p);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
@@ -334,7 +350,7 @@ hipError_t launch_mx_read(const CacheRef& c, int user, int pos0, float* dst_k, f
   p.pos0 = pos0;
   p.n = n;
   p.nkv = c.nkv;
-  return decode(p, c.hd, 1, s);
+  return decode<false>(p, c.hd, 1, s);
 }
 
 hipError_t launch_cache_copy(const CacheRef& dst, int dst_user, const CacheRef& src, int src_user, int pos0, int n,
@@ -367,14 +383,13 @@ hipError_t launch_cache_copy(const CacheRef& dst, int dst_user, const CacheRef& 
     p.src_layer = src.layer_bytes;
     p.dk = dst.k;
     p.dv = dst.v;
-    p.to_pages = 1;
     p.dp = dst.pages;
     p.dst_user = dst_user;
     p.dst_layer = dst.layer_bytes;
     p.pos0 = pos0;
     p.n = n;
     p.nkv = src.nkv;
-    return decode(p, src.hd, layers, s);
+    return decode<true>(p, src.hd, layers, s);
   }
   const CopyParams p{dst, src, dst_user, src_user, pos0, n};
   if (src.mx) {

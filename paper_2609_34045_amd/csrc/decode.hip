@@ -959,7 +959,7 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(const AttnParams a, uin
                                                          float* __restrict__ o32) {
   constexpr int DPL = HD / 64;
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int ns = a.n_split;
+  const int ns = a.row_splits[b];
   const int64_t r0 = ((int64_t)b * a.nq + h) * a.max_split;
   const float* ml = a.part_ml + r0 * 2;
   const float* acc = a.part_acc + r0 * HD + lane * DPL;

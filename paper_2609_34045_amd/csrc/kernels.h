@@ -216,7 +216,8 @@ struct AttnParams {
   KvPages kv;
   int nq, nkv, hd;
   int split;           // keys per workgroup
-  int n_split;         // workgroups per (row, kv head)
+  int n_split;         // workgroups per (row, kv head): the most of any row
+  int row_splits[kMaxBatch];  // partials of each row; the fp16 kernel writes n_split for every row
   int max_split;       // allocated split capacity
   float scale_log2;    // log2(e) / sqrt(hd)
   int users[kMaxBatch];
@@ -237,8 +238,9 @@ struct AttnParams {
 };
 
 // Attention over an MXFP4 cache (attend.hip): a's queries and cache pointers are not
-// used, its KvPages count bytes, its splits are whole pages.  With `out` set (one split, or
-// the merge) the result goes there; else the partials go to a's arrays, as the fp16 kernel's do.
+// used, its KvPages count bytes, its splits are whole pages, and rows have as many as they
+// need (row_splits, 1 at least).  With `out` set (one split a row, or the merge) the result goes
+// there; else the partials go to a's arrays, as the fp16 kernel's do.
 constexpr int kMxMaxSplit = 4096;  // keys per workgroup, upper bound
 struct MxAttnParams {
   AttnParams a;

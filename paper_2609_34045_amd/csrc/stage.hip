@@ -1053,18 +1053,33 @@ static void attn_split_mfma(int nkv, int64_t total_len, int max_len, int max_spl
   *n_split = (max_len + sp - 1) / sp;
 }
 
-// Pages per workgroup of the attention over MXFP4 caches: about two workgroups a CU over the batch's
-// pages, a page for each of a workgroup's waves at least.
-static void attn_split_mx(int nkv, int64_t total_pages, int max_len, int max_split, int n_cu, int* split, int* n_split) {
-  const int64_t wgs = 2LL * n_cu, most = kMxMaxSplit / kKvPage;
-  const int pages = pages_for(max_len);
-  int64_t sp = (total_pages * nkv + wgs - 1) / wgs;
-  if (sp < 4) sp = 4;
-  const int64_t need = (pages + max_split - 1) / max_split;
-  if (sp < need) sp = need;
-  if (sp > most) sp = most;
-  *split = (int)sp * kKvPage;
-  *n_split = pages ? (int)((pages + sp - 1) / sp) : 1;
+#ifndef KF_MX_WGS
+#define KF_MX_WGS(n_cu) (2 * (n_cu))
+#endif
+#ifndef KF_MX_MIN_PAGES
+#define KF_MX_MIN_PAGES 4
+#endif
+// Pages per workgroup of the attention over MXFP4 caches: two workgroups a CU over the batch's
+// pages (three fit; with two to three, and with four and six, the 70B shape's two rows of 131072 and 100001
+// positions took 55.0, 58 to 61, 63 and 61 us, the 8B shape's four rows of 1024 to 32768 19.0, 20.5, 21 and
+// 23.5), and a page for each of a workgroup's waves at least.  Each row has as many splits as its pages need,
+// and one where it has none.
+static void attn_split_mx(int nkv, int rows, const int* lens, int max_split, int n_cu, AttnParams& a) {
+  int64_t total = 0, longest = 0;
+  for (int b = 0; b < rows; ++b) {
+    total += pages_for(lens[b]);
+    longest = std::max<int64_t>(longest, pages_for(lens[b]));
+  }
+  const int64_t wgs = KF_MX_WGS(n_cu);
+  int64_t sp = std::max<int64_t>((total * nkv + wgs - 1) / wgs, KF_MX_MIN_PAGES);
+  sp = std::max(sp, (longest + max_split - 1) / max_split);
+  sp = std::min<int64_t>(sp, kMxMaxSplit / kKvPage);
+  a.split = (int)sp * kKvPage;
+  a.n_split = 1;
+  for (int b = 0; b < rows; ++b) {
+    a.row_splits[b] = std::max(1, (int)((pages_for(lens[b]) + sp - 1) / sp));
+    a.n_split = std::max(a.n_split, a.row_splits[b]);
+  }
 }
 
 // A decode step's attention over an MXFP4 cache, for which the QKV launch g left the new keys and
@@ -1110,7 +1125,7 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
   if (io != KF_F32 && io != KF_BF16 && io != KF_F16) return fail(KF_EINVAL, "io dtype");
   if ((uintptr_t)q_dev % 16) return fail(KF_EINVAL, "the queries are not 16-byte aligned");
   int max_len = 0;
-  int64_t total_len = 0, total_pages = 0;
+  int64_t total_len = 0;
   for (int b = 0; b < rows; ++b) {
     const kf_status st = kv_slice_check(kv, layer, users[b], 0, lens[b]);
     if (st != KF_OK) return st;
@@ -1119,7 +1134,6 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
                   kv->held[users[b]]);
     if (lens[b] > max_len) max_len = lens[b];
     total_len += lens[b];
-    total_pages += pages_for(lens[b]);
   }
   kf_stage* s = kv->st;
   const kf_model_config& c = s->cfg;
@@ -1144,7 +1158,7 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
   tr.begin(KF_K_ATTN);
   hipError_t e = hipSuccess;
   if (kv->mx()) {
-    attn_split_mx(c.n_kv_heads, total_pages, max_len, kv->max_split, s->n_cu, &a.split, &a.n_split);
+    attn_split_mx(c.n_kv_heads, rows, lens, kv->max_split, s->n_cu, a);
     p.rec = ref.k;
     p.q = q_dev;
     p.q_type = io;
@@ -1152,6 +1166,7 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
     e = launch_attn_mx(p, rows, s->stream);
   } else {
     attn_split_mfma(c.n_kv_heads, total_len, max_len > 0 ? max_len : 1, kv->max_split, s->n_cu, &a.split, &a.n_split);
+    for (int b = 0; b < rows; ++b) a.row_splits[b] = a.n_split;
     a.q = reinterpret_cast<const float*>(q_dev);
     if (io != KF_F32) {  // the fp16 kernel takes fp32 queries
       e = launch_rows_to_f32(q_dev, io, s->q, rows * c.n_q_heads * c.head_dim, s->stream);
@@ -1183,7 +1198,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     return fail(KF_EINVAL, "hidden output is NULL (only a stage that holds the head may keep its rows)");
   if (io != KF_F32 && io != KF_BF16) return fail(KF_EINVAL, "io dtype");
   int max_len = 0;
-  int64_t total_len = 0, total_pages = 0;
+  int64_t total_len = 0;
   for (int b = 0; b < batch; ++b) {
     const int u = users[b], p = positions[b];
     if (u < 0 || u >= kv->max_users) return fail(KF_EINVAL, "users[%d] = %d outside [0, %d)", b, u, kv->max_users);
@@ -1193,15 +1208,13 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     if (p >= kv->max_ctx) return fail(KF_ERANGE, "position %d beyond max_ctx %d", p, kv->max_ctx);
     if (p + 1 > max_len) max_len = p + 1;
     total_len += p + 1;
-    total_pages += pages_for(p + 1);
   }
   const kf_model_config& c = s->cfg;
   const int H = c.hidden, hd = c.head_dim;
   hipStream_t st = s->stream;
 
   int split, n_split;
-  if (kv->mx()) attn_split_mx(c.n_kv_heads, total_pages, max_len, kv->max_split, s->n_cu, &split, &n_split);
-  else if (batch > 1) attn_split_mfma(c.n_kv_heads, total_len, max_len, kv->max_split, s->n_cu, &split, &n_split);
+  if (batch > 1) attn_split_mfma(c.n_kv_heads, total_len, max_len, kv->max_split, s->n_cu, &split, &n_split);
   else attn_split(c.n_kv_heads, total_len, max_len, kv->max_split, &split, &n_split);
   if (split % kAttnMfmaAlign) return fail(KF_EINVAL, "split of %d keys breaks the attention kernel's alignment", split);
   int64_t from[kMaxBatch], upto[kMaxBatch];
@@ -1286,6 +1299,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     a.hd = hd;
     a.split = split;
     a.n_split = n_split;
+    for (int b = 0; b < batch; ++b) a.row_splits[b] = n_split;
     a.max_split = kv->max_split;
     a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)hd));
     a.err_flag = s->err_flag;
@@ -1293,6 +1307,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
       a.users[b] = b < batch ? users[b] : 0;
       a.len[b] = b < batch ? positions[b] + 1 : 0;
     }
+    if (kv->mx()) attn_split_mx(c.n_kv_heads, batch, a.len, kv->max_split, s->n_cu, a);
     {
       tr.begin(KF_K_ATTN);
       const hipError_t le = kv->mx() ? attn_mx(s, kv, L, a, g, l, st) : launch_attn_decode(a, batch, st);
