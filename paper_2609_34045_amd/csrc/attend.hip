@@ -83,13 +83,10 @@ static_assert(kMostPages <= 64, "a lane holds the id of one page of the split");
 // 22 bits and those of small ones the bits above 2^-(25 + kShift) of it, and O is rarely rescaled.
 constexpr float kShift = 4.0f, kLazyMax = 8.0f;
 
-__device__ __forceinline__ uint32_t pack2(float a, float b) {  // two fp16, nearest even
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, h2));
-}
 // The parts of a pair: the rounded values in lanes of keep 0, what rounding left in lanes of keep 1.
 __device__ __forceinline__ uint32_t part2(float a, float b, float keep) {
   const h2 hi = __builtin_convertvector(f2{a, b}, h2);
-  return pack2(__builtin_fmaf(-keep, (float)hi.x, a), __builtin_fmaf(-keep, (float)hi.y, b));
+  return f16_pair(__builtin_fmaf(-keep, (float)hi.x, a), __builtin_fmaf(-keep, (float)hi.y, b));
 }
 
 template <int HD>
@@ -395,7 +392,8 @@ __global__ __launch_bounds__(256) void mx_append_kernel(const MxAppendParams p) 
   }
   bool bad = false;
   int e;
-  const uint32_t w = mx_encode8(x, e, bad);
+  uint32_t pairs[4] = {f16_pair(x[0], x[1]), f16_pair(x[2], x[3]), f16_pair(x[4], x[5]), f16_pair(x[6], x[7])};
+  const uint32_t w = mx_encode8(pairs, e, bad);
   raise_err(p.err_flag, bad, kErrF16Range);
   const int t = p.pos[b] % kKvPage;
   const int codes = mx_codes(hd);

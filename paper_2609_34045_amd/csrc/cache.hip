@@ -22,39 +22,59 @@ typedef float f2 __attribute__((ext_vector_type(2)));
 
 enum : int { kRowsF32 = 0, kRowsBF16 = 1, kRowsF16 = 2, kPagesF16 = 3 };  // the first three are kf_dtype values
 
-template <int CTRL>
-__device__ __forceinline__ float dpp_f(float v) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
-}
-
-// 8 consecutive values of a row as fp32; `wide`: at is 16-byte aligned.
-__device__ __forceinline__ void load8(const void* base, int type, int64_t at, bool wide, float (&f)[8]) {
+// 8 consecutive values of a row as fp16 pairs; `wide`: at is 16-byte aligned.
+__device__ __forceinline__ void load8(const void* base, int type, int64_t at, bool wide, uint32_t (&x)[4]) {
   if (type == kRowsF32) {
     const float* p = reinterpret_cast<const float*>(base) + at;
+    v4f a, b;
     if (wide) {
-      const v4f a = __builtin_nontemporal_load(reinterpret_cast<const v4f*>(p));
-      const v4f b = __builtin_nontemporal_load(reinterpret_cast<const v4f*>(p) + 1);
-      f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-      f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+      a = __builtin_nontemporal_load(reinterpret_cast<const v4f*>(p));
+      b = __builtin_nontemporal_load(reinterpret_cast<const v4f*>(p) + 1);
     } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = p[i];
+      a = v4f{p[0], p[1], p[2], p[3]};
+      b = v4f{p[4], p[5], p[6], p[7]};
     }
+    x[0] = f16_pair(a.x, a.y);
+    x[1] = f16_pair(a.z, a.w);
+    x[2] = f16_pair(b.x, b.y);
+    x[3] = f16_pair(b.z, b.w);
     return;
   }
   const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + at;
-  uint16_t h[8];
   if (wide) {
     const v4u w = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+    for (int i = 0; i < 4; ++i) x[i] = w[i];
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = p[i];
+    for (int i = 0; i < 4; ++i) x[i] = p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
+  }
+  if (type != kRowsBF16) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = f16_pair(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u));
+}
+
+// Nibble i of word j to nibble j of word i, of 8 words.
+__device__ __forceinline__ void transpose_nibbles(uint32_t (&r)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t a = r[j], b = r[j + 4];
+    r[j] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+    r[j + 4] = __builtin_amdgcn_perm(b, a, 0x07060302u);
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    f[i] = type == kRowsBF16 ? __uint_as_float((uint32_t)h[i] << 16) : (float)__builtin_bit_cast(_Float16, h[i]);
+  for (int k = 0; k < 4; ++k) {
+    const int j = k < 2 ? k : k + 2;
+    const uint32_t a = r[j], b = r[j + 2];
+    r[j] = __builtin_amdgcn_perm(b, a, 0x06020400u);
+    r[j + 2] = __builtin_amdgcn_perm(b, a, 0x07030501u);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    const uint32_t a = r[j], b = r[j + 1];
+    r[j] = (a & 0x0f0f0f0fu) | (b & 0x0f0f0f0fu) << 4;
+    r[j + 1] = (a >> 4 & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);
+  }
 }
 }  // namespace
 
@@ -77,13 +97,13 @@ struct MxEncodeParams {
 // same positions, whose rows lie side by side in the source: encodes the page's positions that
 // lie in [pos0, pos0 + n) and leaves the others as they are.  Four lanes hold a
 // block, 8 values each.  K codes go out as they are made (8 codes are 4 bytes of a
-// row); V codes, whose bytes hold neighbouring positions, meet in LDS first.  One
-// workgroup owns all of a head's page, so no byte has two writers.
+// row); V codes, whose words hold 8 positions of one d, are exchanged through LDS, 8 x 8 at a
+// time.  One workgroup owns all of a head's page, so no byte has two writers.
 template <int HD>
 __global__ __launch_bounds__(256) void mx_encode_kernel(const MxEncodeParams p) {
   constexpr int UPR = HD / 8;  // 8-value units per position
   constexpr int REC = mx_record(HD), CODES = mx_codes(HD);
-  __shared__ uint32_t codes[kKvPage * UPR];
+  __shared__ uint32_t codes[kKvPage * UPR], turned[CODES / 4];
   const int page = p.pos0 / kKvPage + blockIdx.y, g = blockIdx.x >> 1, is_v = blockIdx.x & 1, tid = threadIdx.x;
   const int a = max(p.pos0 - page * kKvPage, 0), b = min(p.pos0 + p.n - page * kKvPage, kKvPage);
   const void* src = is_v ? p.sv : p.sk;
@@ -91,19 +111,19 @@ __global__ __launch_bounds__(256) void mx_encode_kernel(const MxEncodeParams p) 
   // Every load goes out before the first is used.
   constexpr int NU = kKvPage * UPR / 256;
   constexpr int NW = CODES / 4 / 256;
-  float f[NU][8];
+  uint32_t x[NU][4];
   uint32_t old[NW];  // the V codes of a page that is written in part
 #pragma unroll
   for (int k = 0; k < NU; ++k) {
     const int u = tid + 256 * k, t = u / UPR, d0 = (u % UPR) * 8;
     if (t < a || t >= b) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[k][i] = 0.f;
+      for (int i = 0; i < 4; ++i) x[k][i] = 0;
     } else if (p.src_type == kPagesF16) {
       const char* base = reinterpret_cast<const char*>(src) + blockIdx.z * p.src_layer;
-      load8(base, kRowsF16, kv_offset(p.sp, p.src_user, g, page * kKvPage + t, HD) + d0, true, f[k]);
+      load8(base, kRowsF16, kv_offset(p.sp, p.src_user, g, page * kKvPage + t, HD) + d0, true, x[k]);
     } else {
-      load8(src, p.src_type, ((int64_t)(page * kKvPage + t - p.pos0) * p.nkv + g) * HD + d0, p.wide, f[k]);
+      load8(src, p.src_type, ((int64_t)(page * kKvPage + t - p.pos0) * p.nkv + g) * HD + d0, p.wide, x[k]);
     }
   }
   uint8_t* rec = p.dst + blockIdx.z * p.dst_layer + (int64_t)kv_page(p.dp, p.dst_user, page) * p.dp.page_stride +
@@ -117,7 +137,7 @@ __global__ __launch_bounds__(256) void mx_encode_kernel(const MxEncodeParams p) 
   for (int k = 0; k < NU; ++k) {
     const int u = tid + 256 * k, t = u / UPR, d0 = (u % UPR) * 8;
     int e;
-    const uint32_t w = mx_encode8(f[k], e, bad);
+    const uint32_t w = mx_encode8(x[k], e, bad);
     const bool live = t >= a && t < b;
     if (!is_v) {
       if (live) *reinterpret_cast<uint32_t*>(rec + mx_k_byte<HD>(t, d0)) = w;
@@ -132,21 +152,31 @@ __global__ __launch_bounds__(256) void mx_encode_kernel(const MxEncodeParams p) 
   raise_err(p.err_flag, bad, kErrF16Range);
   if (!is_v) return;
   __syncthreads();
-  const uint8_t* lds = reinterpret_cast<const uint8_t*>(codes);
+  if (tid < CODES / 32) {  // positions 16 (2 s + j / 4) + 4 grp + j % 4 of 8 values
+    const int c = tid % UPR, s = (tid / UPR) & 1, grp = tid / (2 * UPR), d0 = 8 * c;
+    uint32_t r[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = codes[(16 * (2 * s + j / 4) + 4 * grp + j % 4) * UPR + c];
+    transpose_nibbles(r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) turned[mx_v_byte(32 * s + 4 * grp, d0 + i) / 4] = r[i];
+  }
+  __syncthreads();
 #pragma unroll
   for (int k = 0; k < NW; ++k) {
     const int w = tid + 256 * k;  // dword of the V codes: 8 positions of one d
-    const int s = w & 1, d = (2 * (w >> 8) + ((w >> 1) & 1)) * 16 + ((w >> 2) & 15), grp = (w >> 6) & 3;
-    uint32_t v = 0, mask = 0;
+    uint32_t* out = reinterpret_cast<uint32_t*>(rec) + w;
+    if (whole) {
+      *out = turned[w];
+      continue;
+    }
+    uint32_t mask = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int t = 16 * (2 * s + j / 4) + 4 * grp + j % 4;
-      v |= (uint32_t)((lds[t * (HD / 2) + d / 2] >> (4 * (d & 1))) & 15) << (4 * j);
+      const int t = 16 * (2 * (w & 1) + j / 4) + 4 * ((w >> 6) & 3) + j % 4;
       if (t >= a && t < b) mask |= 15u << (4 * j);
     }
-    uint32_t* out = reinterpret_cast<uint32_t*>(rec) + w;
-    if (whole) *out = v;
-    else if (mask) *out = (old[k] & ~mask) | (v & mask);
+    if (mask) *out = (old[k] & ~mask) | (turned[w] & mask);
   }
 }
 

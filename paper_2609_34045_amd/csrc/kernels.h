@@ -101,31 +101,48 @@ __device__ __forceinline__ uint16_t mx_v_scale(int e) {  // 2^e
   return (uint16_t)(e >= -14 ? (e + 15) << 10 : 1 << (e + 24));
 }
 
-// 8 of a block's values, the other 24 in the 3 lanes beside (lanes 4 k .. 4 k + 3 hold a
-// block): their E2M1 codes, and the block's exponent.  A NaN is stored as 0, an infinity as
-// the largest magnitude; both, and what fp16 rounds to infinity, are noted in `bad`.
-__device__ __forceinline__ uint32_t mx_encode8(const float (&x)[8], int& e, bool& bad) {
-  float h[8], top = 0.f;
+// Two fp32 values as packed fp16 bits (nearest even; what fp16 cannot hold becomes infinite).
+__device__ __forceinline__ uint32_t f16_pair(float a, float b) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, h2));
+}
+// 8 of a block's values as fp16 pairs, the other 24 in the 3 lanes beside (lanes 4 k .. 4 k + 3
+// hold a block): their E2M1 codes, and the block's exponent.  A NaN is stored as 0, an infinity as the
+// largest magnitude; both are noted in `bad`.  The convert instruction rounds to nearest even
+// and saturates at 6.
+__device__ __forceinline__ uint32_t mx_encode8(uint32_t (&x)[4], int& e, bool& bad) {
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  typedef uint16_t u2 __attribute__((ext_vector_type(2)));
+  auto most = [&]() {  // of the magnitudes' bits, whose order is the values'
+    u2 m = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    h[i] = (float)(_Float16)x[i];
-    bad |= !(__builtin_fabsf(h[i]) <= 65504.0f);
-    if (h[i] != h[i]) h[i] = 0.f;
-    top = fmaxf(top, __builtin_fabsf(h[i]));
+    for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u2, x[i] & 0x7fff7fffu));
+    return (uint32_t)(m.x > m.y ? m.x : m.y);
+  };
+  uint32_t top = most();
+  if (top >= 0x7c00u) {
+    bad = true;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t h = (x[i / 2] >> (16 * (i % 2))) & 0xffffu, a = h & 0x7fffu;
+      const uint32_t v = a > 0x7c00u ? 0u : a == 0x7c00u ? h - 1u : h;  // infinity - 1 is 65504
+      x[i / 2] = i % 2 ? (x[i / 2] & 0xffffu) | v << 16 : (x[i / 2] & 0xffff0000u) | v;
+    }
+    top = most();
   }
   // over the four lanes, by two quad permutes
-  top = fmaxf(top, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, top), 0xB1, 0xf, 0xf, false)));
-  top = fmaxf(top, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, top), 0x4E, 0xf, 0xf, false)));
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, false));
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, false));
   // adding half a unit of the one kept mantissa bit carries into the exponent where the rounding does
-  e = (int)((__builtin_bit_cast(uint32_t, top) + 0x200000u) >> 23) - 127 - 2;
+  const float t = (float)__builtin_bit_cast(_Float16, (uint16_t)top);
+  e = (int)((__builtin_bit_cast(uint32_t, t) + 0x200000u) >> 23) - 127 - 2;
   e = e < kMxExpMin ? kMxExpMin : e > kMxExpMax ? kMxExpMax : e;
-  const float scale = __builtin_bit_cast(float, (uint32_t)(e + 127) << 23), most = 6.0f * scale;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) h[i] = fminf(fmaxf(h[i], -most), most);
-  uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, h[0], h[1], scale, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, h[2], h[3], scale, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, h[4], h[5], scale, 2);
-  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, h[6], h[7], scale, 3);
+  const float scale = __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
+  uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(0u, __builtin_bit_cast(h2, x[0]), scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(h2, x[1]), scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(h2, x[2]), scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(w, __builtin_bit_cast(h2, x[3]), scale, 3);
 }
 
 // Optional per-launch marker around each kernel (instrumentation hook of the runtime).
