@@ -6,13 +6,15 @@
 //
 // One pass over the logits, which bounds it (4 bytes a value).  A workgroup takes a
 // chunk of a row into registers: maximum, then the two sums, then the chunk's k
-// largest.  A key orders values and, among equals, puts the lower index first, so
-// that keys are distinct: (order-preserving bits of z, ~index).  The k-th largest of
-// a wave's 64 per-lane maxima is a lower bound of the chunk's k-th largest key (k
-// keys reach it), at most k lanes of each wave hold keys that reach the largest of the four
-// waves' bounds, and these few candidates are ranked by counting.  A second, small launch
-// joins a row's chunks: sums rescaled to the row's maximum, and k rounds of the
-// largest head of the chunks' sorted lists.  Rows of one chunk need no second launch.
+// largest.  Those: a value T that k of a wave's 64 per-lane maxima reach is a lower
+// bound of the k-th largest, found by a search over its upper bits whose steps are one
+// compare and a count of its lanes; the values that reach the largest of the four waves'
+// bounds, about a hundredth of a chunk for k = 20, go to LDS and are ranked by counting.  Keys
+// order values and, among equals, put the lower index first, so that they are distinct:
+// (order-preserving bits of z, ~index).  Where equal values make the candidates too many, the
+// bound is taken over keys, which at most k lanes of each wave reach.  A second, small
+// launch joins a row's chunks: sums rescaled to the row's maximum, and k rounds of
+// the largest head of the chunks' sorted lists.  Rows of one chunk need no second launch.
 #include <cmath>
 
 #include "kernels.h"
@@ -25,30 +27,49 @@ typedef unsigned long long u64;
 
 constexpr int kT = 256;  // threads
 
-// 0 for a masked (-inf) or refused logit, else its key.
+// The order of values as that of unsigned numbers; -0 and 0 are equal.
+__device__ __forceinline__ uint32_t order_of(float z) {
+  const uint32_t b = __float_as_uint(z + 0.0f);
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of_order(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
+// 0 for a masked (-inf) logit, else its key.
 __device__ __forceinline__ u64 key_of(float z, int index) {
-  if (z == -INFINITY) return 0;
-  const uint32_t b = __float_as_uint(z + 0.0f);  // -0 and 0 are equal
-  const uint32_t o = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-  return (u64)o << 32 | (uint32_t)~index;
+  return z == -INFINITY ? 0 : (u64)order_of(z) << 32 | (uint32_t)~index;
 }
-__device__ __forceinline__ float value_of(u64 key) {
-  const uint32_t o = (uint32_t)(key >> 32);
-  return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
-}
+__device__ __forceinline__ float value_of(u64 key) { return value_of_order((uint32_t)(key >> 32)); }
 __device__ __forceinline__ u64 lane_key(u64 key, int lane) {
   return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), lane) << 32 |
          (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)key, lane);
 }
+// Over the wave, result in every lane: quad permutes and row mirrors within 16 lanes, then the 16-lane groups.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false);
+}
+template <class F>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t v, F f) {
+  v = f(v, dpp<0xB1>(v));
+  v = f(v, dpp<0x4E>(v));
+  v = f(v, dpp<0x141>(v));
+  v = f(v, dpp<0x140>(v));
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = f(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return f(b[0], b[1]);
+}
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  return wave_reduce(v, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
+  return __uint_as_float(wave_reduce(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
 }
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+  return __uint_as_float(wave_reduce(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
 }
 __device__ __forceinline__ float block_max(float v, float* lds) {
   v = wave_max(v);
@@ -100,9 +121,11 @@ __device__ __forceinline__ void finish_row(const LogprobParams& p, int row, floa
 // Chunk blockIdx.x of row blockIdx.y: VPT values a thread.
 template <int VPT>
 __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p) {
-  __shared__ float red[4];
-  __shared__ u64 bound[4], cand[4 * kMaxTop * VPT], best[kMaxTop];
-  __shared__ int n_cand;
+  constexpr int kSeg = kMaxTop * VPT;  // candidates of a wave
+  __shared__ float red[4], red_s[4], red_w[4];
+  __shared__ u64 cand[4][kSeg], best[kMaxTop], key_bound[4];
+  __shared__ uint32_t bound[4];
+  __shared__ int count[4];
   const int row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int c0 = blockIdx.x * kT * VPT;
   const float* z = p.logits + row * p.stride;
@@ -120,18 +143,34 @@ __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p
       for (int i = 0; i < 4; ++i) v[4 * j + i] = at + i < p.vocab ? z[at + i] : -INFINITY;
     }
   }
+  float mine = v[0];  // the lane's largest
   bool bad = false;
-  float m = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    if (!(v[i] < INFINITY)) {  // NaN or +inf: skipped, and reported
-      v[i] = -INFINITY;
-      bad = true;
+  for (int i = 0; i < VPT; i += 2) {
+    bad |= __builtin_isunordered(v[i], v[i + 1]);
+    mine = fmaxf(mine, fmaxf(v[i], v[i + 1]));
+  }
+  bad |= mine == INFINITY;
+  if (bad) {  // NaN or +inf: skipped, and reported
+    mine = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      if (!(v[i] < INFINITY)) v[i] = -INFINITY;
+      mine = fmaxf(mine, v[i]);
     }
-    m = fmaxf(m, v[i]);
   }
   raise_err(p.err_flag, bad, kErrNaNLogit);
-  m = block_max(m, red);
+  if (p.top) {  // the bound, as far as sign, exponent and 8 bits of the mantissa give it
+    uint32_t least = 0;
+    const uint32_t o = order_of(mine);
+    for (int bit = 31; bit >= 15; --bit) {
+      const uint32_t t = least | 1u << bit;
+      if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(o >= t)) >= p.top) least = t;
+    }
+    if (lane == 0) bound[wave] = least;
+    if (tid < kMaxTop) best[tid] = 0;
+  }
+  const float m = block_max(mine, red);
   float s = 0.f, w = 0.f;
   if (m != -INFINITY) {
 #pragma unroll
@@ -142,39 +181,67 @@ __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p
       w += e * x;
     }
   }
-  s = block_sum(s, red);
-  w = block_sum(w, red);
-
+  s = wave_sum(s);
+  w = wave_sum(w);
+  if (lane == 0) {
+    red_s[wave] = s;
+    red_w[wave] = w;
+  }
+  int n = 0;  // this wave's candidates
   if (p.top) {
-    u64 mine = 0;
+    // no lower than the lowest finite value, so that masked values are no candidates
+    const uint32_t least = max(max(max(bound[0], bound[1]), max(bound[2], bound[3])), order_of(-__FLT_MAX__));
+    const float t = value_of_order(least);
+    if (__builtin_amdgcn_ballot_w64(mine >= t)) {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const u64 k = key_of(v[i], c0 + 4 * (kT * (i / 4) + tid) + i % 4);
-      mine = k > mine ? k : mine;
+      for (int i = 0; i < VPT; ++i) {
+        const u64 hit = __builtin_amdgcn_ballot_w64(v[i] >= t);
+        if (!hit) continue;
+        const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
+        if (v[i] >= t && at < kSeg) cand[wave][at] = key_of(v[i], c0 + 4 * (kT * (i / 4) + tid) + i % 4);
+        n += __builtin_popcountll(hit);
+      }
     }
-    int rank = 0;
-    for (int l = 0; l < 64; ++l) rank += lane_key(mine, l) > mine;
-    const u64 at = __builtin_amdgcn_ballot_w64(rank == p.top - 1 && mine != 0);
-    if (lane == 0) bound[wave] = at ? lane_key(mine, __builtin_ctzll(at)) : 0;
-    if (tid == 0) n_cand = 0;
-    if (tid < kMaxTop) best[tid] = 0;
-    __syncthreads();
-    u64 least = 1;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) least = bound[i] > least ? bound[i] : least;
-    if (mine >= least) {
+    if (lane == 0) count[wave] = n;
+  }
+  __syncthreads();
+  s = (red_s[0] + red_s[1]) + (red_s[2] + red_s[3]);
+  w = (red_w[0] + red_w[1]) + (red_w[2] + red_w[3]);
+  if (p.top) {
+    if (max(max(count[0], count[1]), max(count[2], count[3])) > kSeg) {  // the bound over keys instead
+      u64 k0 = 0;
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
         const u64 k = key_of(v[i], c0 + 4 * (kT * (i / 4) + tid) + i % 4);
-        if (k >= least) cand[atomicAdd(&n_cand, 1)] = k;
+        k0 = k > k0 ? k : k0;
       }
+      int rank = 0;
+      for (int l = 0; l < 64; ++l) rank += lane_key(k0, l) > k0;
+      const u64 at = __builtin_amdgcn_ballot_w64(rank == p.top - 1 && k0 != 0);
+      __syncthreads();  // every count has been read
+      if (lane == 0) key_bound[wave] = at ? lane_key(k0, __builtin_ctzll(at)) : 1;
+      __syncthreads();
+      u64 least = key_bound[0];
+#pragma unroll
+      for (int i = 1; i < 4; ++i) least = key_bound[i] > least ? key_bound[i] : least;
+      n = 0;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        const u64 k = key_of(v[i], c0 + 4 * (kT * (i / 4) + tid) + i % 4);
+        const u64 hit = __builtin_amdgcn_ballot_w64(k >= least);
+        const int pos = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
+        if (k >= least) cand[wave][pos] = k;  // at most top lanes of a wave: kMaxTop VPT keys
+        n += __builtin_popcountll(hit);
+      }
+      if (lane == 0) count[wave] = n;
+      __syncthreads();
     }
-    __syncthreads();
-    const int n = n_cand;  // at most top lanes of each wave reach the bound: 4 top VPT keys
-    for (int c = tid; c < n; c += kT) {
-      const u64 k = cand[c];
+    for (int c = lane; c < n; c += 64) {
+      const u64 k = cand[wave][c];
       int r = 0;
-      for (int i = 0; i < n; ++i) r += cand[i] > k;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        for (int i = 0; i < count[q]; ++i) r += cand[q][i] > k;
       if (r < p.top) best[r] = k;
     }
     __syncthreads();
@@ -217,26 +284,14 @@ __global__ __launch_bounds__(kT) void logprob_join_kernel(const LogprobParams p)
     u64 h0 = top && tid < n ? l0[0] : 0, h1 = top && tid + 64 < n ? l1[0] : 0;
     for (int r = 0; r < top; ++r) {
       const u64 mine = h0 > h1 ? h0 : h1;
-      // the largest value, then among its lanes (one, but for equal values) the largest key
-      uint32_t hi = (uint32_t)(mine >> 32);
-#pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) {
-        const uint32_t other = __shfl_xor(hi, o);
-        hi = other > hi ? other : hi;
-      }
-      u64 lanes = __builtin_amdgcn_ballot_w64((uint32_t)(mine >> 32) == hi), k = 0;
-      int who = 0;
-      while (lanes) {
-        const int l = __builtin_ctzll(lanes);
-        lanes &= lanes - 1;
-        const u64 c = lane_key(mine, l);
-        if (c >= k) {
-          k = c;
-          who = l;
-        }
-      }
+      // the largest value, then the largest key of its lanes (one, but for equal values)
+      const uint32_t hi = wave_max_u32((uint32_t)(mine >> 32));
+      const u64 lanes = __builtin_amdgcn_ballot_w64((uint32_t)(mine >> 32) == hi);
+      uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, __builtin_ctzll(lanes));
+      if (lanes & (lanes - 1)) lo = wave_max_u32((uint32_t)(mine >> 32) == hi ? (uint32_t)mine : 0);
+      const u64 k = (u64)hi << 32 | lo;
       if (tid == 0) best[r] = k;
-      if (tid == who && k) {
+      if (mine == k && k) {
         if (h0 == k) h0 = ++at0 < top ? l0[at0] : 0;
         else h1 = ++at1 < top ? l1[at1] : 0;
       }
@@ -247,9 +302,10 @@ __global__ __launch_bounds__(kT) void logprob_join_kernel(const LogprobParams p)
 }
 
 // Values per thread: chunks of 8192 values where they fill the chip (two workgroups a
-// CU) or cover a row at once, else of 2048.
+// CU) or cover a row that 2048 do not at once, else of 2048.
 static int values_per_thread(int rows, int vocab) {
   const int64_t large = (vocab + 8191) / 8192;
+  if (vocab <= 2048) return 8;
   return large == 1 || rows * large >= 512 || (vocab + 2047) / 2048 > 128 ? 32 : 8;
 }
 
