@@ -6,15 +6,16 @@
 //
 // One pass over the logits, which bounds it (4 bytes a value).  A workgroup takes a
 // chunk of a row into registers: maximum, then the two sums, then the chunk's k
-// largest.  Those: a value T that k of a wave's 64 per-lane maxima reach is a lower
-// bound of the k-th largest, found by a search over its upper bits whose steps are one
-// compare and a count of its lanes; the values that reach the largest of the four waves'
-// bounds, about a hundredth of a chunk for k = 20, go to LDS and are ranked by counting.  Keys
-// order values and, among equals, put the lower index first, so that they are distinct:
-// (order-preserving bits of z, ~index).  Where equal values make the candidates too many, the
-// bound is taken over keys, which at most k lanes of each wave reach.  A second, small
-// launch joins a row's chunks: sums rescaled to the row's maximum, and k rounds of
-// the largest head of the chunks' sorted lists.  Rows of one chunk need no second launch.
+// largest.  Those: a value that k of a wave's 64 per-lane maxima reach is a lower bound of
+// the k-th largest, and so is one that a quarter of k reach in each of the four waves (the
+// closer one where the large values are spread, as they mostly are).  Both are found by a search
+// over their upper bits whose steps are one compare and a count of its lanes.  The values that
+// reach the larger bound, some 30 of 8192 for k = 20, go to LDS and are ranked by counting.
+// Keys order values and, among equals, put the lower index first, so that they are
+// distinct: (order-preserving bits of z, ~index).  Where equal values make the
+// candidates too many the k largest keys are taken one by one.  A second, small launch joins
+// a row's chunks: sums rescaled to the row's maximum, and k rounds of the largest head of the
+// chunks' sorted lists.  Rows of one chunk need no second launch.
 #include <cmath>
 
 #include "kernels.h"
@@ -38,10 +39,6 @@ __device__ __forceinline__ u64 key_of(float z, int index) {
   return z == -INFINITY ? 0 : (u64)order_of(z) << 32 | (uint32_t)~index;
 }
 __device__ __forceinline__ float value_of(u64 key) { return value_of_order((uint32_t)(key >> 32)); }
-__device__ __forceinline__ u64 lane_key(u64 key, int lane) {
-  return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), lane) << 32 |
-         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)key, lane);
-}
 // Over the wave, result in every lane: quad permutes and row mirrors within 16 lanes, then the 16-lane groups.
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t v) {
@@ -121,10 +118,10 @@ __device__ __forceinline__ void finish_row(const LogprobParams& p, int row, floa
 // Chunk blockIdx.x of row blockIdx.y: VPT values a thread.
 template <int VPT>
 __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p) {
-  constexpr int kSeg = kMaxTop * VPT;  // candidates of a wave
+  constexpr int kSeg = 256;  // candidates of a wave
   __shared__ float red[4], red_s[4], red_w[4];
-  __shared__ u64 cand[4][kSeg], best[kMaxTop], key_bound[4];
-  __shared__ uint32_t bound[4];
+  __shared__ u64 cand[4][kSeg], best[kMaxTop], round[2][4];
+  __shared__ uint32_t bound[4], quarter[4];
   __shared__ int count[4];
   const int row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int c0 = blockIdx.x * kT * VPT;
@@ -160,14 +157,18 @@ __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p
     }
   }
   raise_err(p.err_flag, bad, kErrNaNLogit);
-  if (p.top) {  // the bound, as far as sign, exponent and 8 bits of the mantissa give it
-    uint32_t least = 0;
+  if (p.top) {  // the bounds, as far as sign, exponent and 8 bits of the mantissa give them
+    uint32_t all = 0, part = 0;
     const uint32_t o = order_of(mine);
     for (int bit = 31; bit >= 15; --bit) {
-      const uint32_t t = least | 1u << bit;
-      if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(o >= t)) >= p.top) least = t;
+      const uint32_t t = all | 1u << bit, q = part | 1u << bit;
+      if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(o >= t)) >= p.top) all = t;
+      if (4 * __builtin_popcountll(__builtin_amdgcn_ballot_w64(o >= q)) >= p.top) part = q;
     }
-    if (lane == 0) bound[wave] = least;
+    if (lane == 0) {
+      bound[wave] = all;
+      quarter[wave] = part;
+    }
     if (tid < kMaxTop) best[tid] = 0;
   }
   const float m = block_max(mine, red);
@@ -190,7 +191,8 @@ __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p
   int n = 0;  // this wave's candidates
   if (p.top) {
     // no lower than the lowest finite value, so that masked values are no candidates
-    const uint32_t least = max(max(max(bound[0], bound[1]), max(bound[2], bound[3])), order_of(-__FLT_MAX__));
+    const uint32_t least = max(max(max(bound[0], bound[1]), max(bound[2], bound[3])),
+                               max(min(min(quarter[0], quarter[1]), min(quarter[2], quarter[3])), order_of(-__FLT_MAX__)));
     const float t = value_of_order(least);
     if (__builtin_amdgcn_ballot_w64(mine >= t)) {
 #pragma unroll
@@ -208,43 +210,40 @@ __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p
   s = (red_s[0] + red_s[1]) + (red_s[2] + red_s[3]);
   w = (red_w[0] + red_w[1]) + (red_w[2] + red_w[3]);
   if (p.top) {
-    if (max(max(count[0], count[1]), max(count[2], count[3])) > kSeg) {  // the bound over keys instead
-      u64 k0 = 0;
+    if (max(max(count[0], count[1]), max(count[2], count[3])) > kSeg) {
+      u64 k0 = ~0ull;  // the last key taken, then the lane's largest below it
+      for (int r = 0; r < p.top; ++r) {
+        u64 next = 0;
+        if (r == 0 || k0 == best[r - 1]) {  // the lane whose key was taken, and at first every lane
 #pragma unroll
-      for (int i = 0; i < VPT; ++i) {
-        const u64 k = key_of(v[i], c0 + 4 * (kT * (i / 4) + tid) + i % 4);
-        k0 = k > k0 ? k : k0;
+          for (int i = 0; i < VPT; ++i) {
+            const u64 k = key_of(v[i], c0 + 4 * (kT * (i / 4) + tid) + i % 4);
+            next = k < k0 && k > next ? k : next;
+          }
+          k0 = next;
+        }
+        const uint32_t hi = wave_max_u32((uint32_t)(k0 >> 32));
+        const uint32_t lo = wave_max_u32((uint32_t)(k0 >> 32) == hi ? (uint32_t)k0 : 0);
+        if (lane == 0) round[r & 1][wave] = (u64)hi << 32 | lo;
+        __syncthreads();
+        if (tid == 0) {
+          const u64* q = round[r & 1];
+          const u64 x = q[0] > q[1] ? q[0] : q[1], y = q[2] > q[3] ? q[2] : q[3];
+          best[r] = x > y ? x : y;
+        }
+        __syncthreads();
       }
-      int rank = 0;
-      for (int l = 0; l < 64; ++l) rank += lane_key(k0, l) > k0;
-      const u64 at = __builtin_amdgcn_ballot_w64(rank == p.top - 1 && k0 != 0);
-      __syncthreads();  // every count has been read
-      if (lane == 0) key_bound[wave] = at ? lane_key(k0, __builtin_ctzll(at)) : 1;
-      __syncthreads();
-      u64 least = key_bound[0];
+    } else {
+      for (int c = lane; c < n; c += 64) {
+        const u64 k = cand[wave][c];
+        int r = 0;
 #pragma unroll
-      for (int i = 1; i < 4; ++i) least = key_bound[i] > least ? key_bound[i] : least;
-      n = 0;
-#pragma unroll
-      for (int i = 0; i < VPT; ++i) {
-        const u64 k = key_of(v[i], c0 + 4 * (kT * (i / 4) + tid) + i % 4);
-        const u64 hit = __builtin_amdgcn_ballot_w64(k >= least);
-        const int pos = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
-        if (k >= least) cand[wave][pos] = k;  // at most top lanes of a wave: kMaxTop VPT keys
-        n += __builtin_popcountll(hit);
+        for (int q = 0; q < 4; ++q)
+          for (int i = 0; i < count[q]; ++i) r += cand[q][i] > k;
+        if (r < p.top) best[r] = k;
       }
-      if (lane == 0) count[wave] = n;
       __syncthreads();
     }
-    for (int c = lane; c < n; c += 64) {
-      const u64 k = cand[wave][c];
-      int r = 0;
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        for (int i = 0; i < count[q]; ++i) r += cand[q][i] > k;
-      if (r < p.top) best[r] = k;
-    }
-    __syncthreads();
   }
   if (gridDim.x == 1) {
     finish_row(p, row, m, s, w, best);
