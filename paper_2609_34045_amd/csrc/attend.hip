@@ -165,7 +165,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const MxAttnPar
     float f[NS][8], top = 0.f;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
-      load_q8(p.q, p.q_type, ((int64_t)b * p.a.nq + hq0 + min(head, G - 1)) * HD + grp * (HD / 4) + 8 * s, f[s]);
+      load_q8(p.q, p.a.q_type, ((int64_t)b * p.a.nq + hq0 + min(head, G - 1)) * HD + grp * (HD / 4) + 8 * s, f[s]);
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -415,15 +415,6 @@ __global__ __launch_bounds__(256) void mx_append_kernel(const MxAppendParams p) 
     reinterpret_cast<uint16_t*>(rec + codes)[hd == 128 ? mx_v_exp<128>(t, blk) : mx_v_exp<64>(t, blk)] = mx_v_scale(e);
 }
 
-__global__ void rows_to_f32_kernel(const void* src, int type, float* dst, int n8) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= n8) return;
-  float f[8];
-  load_q8(src, type, (int64_t)i * 8, f);
-  reinterpret_cast<v4f*>(dst)[2 * i] = v4f{f[0], f[1], f[2], f[3]};
-  reinterpret_cast<v4f*>(dst)[2 * i + 1] = v4f{f[4], f[5], f[6], f[7]};
-}
-
 // ------------------------------------------------------------------ launchers
 hipError_t launch_attn_mx(const MxAttnParams& p, int batch, hipStream_t s) {
   if (p.a.nq % p.a.nkv || p.a.nq / p.a.nkv > 8 || p.a.split % kKvPage || p.a.split > kMxMaxSplit) return hipErrorInvalidValue;
@@ -450,11 +441,6 @@ hipError_t launch_attend_merge(const MxAttnParams& p, int batch, hipStream_t s) 
 hipError_t launch_mx_append(const MxAppendParams& p, hipStream_t s) {
   const int lanes = p.batch * ((p.gq ? p.nq : 0) + 2 * p.nkv) * (p.hd / 8);
   hipLaunchKernelGGL(mx_append_kernel, dim3((lanes + 255) / 256), dim3(256), 0, s, p);
-  return hipGetLastError();
-}
-
-hipError_t launch_rows_to_f32(const void* src, int type, float* dst, int n, hipStream_t s) {
-  hipLaunchKernelGGL(rows_to_f32_kernel, dim3((n / 8 + 255) / 256), dim3(256), 0, s, src, type, dst, n / 8);
   return hipGetLastError();
 }
 

@@ -318,7 +318,9 @@ __global__ __launch_bounds__(256) void f16_copy_kernel(const CopyParams p, int64
       *reinterpret_cast<const v4u*>(src + 2 * (kv_offset(p.src.pages, p.src_user, (int)g, pos, hd) + d));
 }
 
-__global__ __launch_bounds__(256) void page_copy_kernel(const CacheRef c, const PageCopies u, int64_t page_bytes) {
+__global__ __launch_bounds__(256) void page_copy_kernel(const CacheRef c, const PageCopies u, int64_t page_bytes, int* table,
+                                                        const KvTableUpdate t) {
+  if (blockIdx.x + blockIdx.y + blockIdx.z == 0 && (int)threadIdx.x < t.n) table[t.idx[threadIdx.x]] = t.val[threadIdx.x];
   const int arrays = c.mx ? 1 : 2;
   const int64_t layer = blockIdx.y / arrays;
   uint8_t* base = (blockIdx.y % arrays ? c.v : c.k) + layer * c.layer_bytes;
@@ -438,11 +440,12 @@ hipError_t launch_cache_copy(const CacheRef& dst, int dst_user, const CacheRef& 
   return hipGetLastError();
 }
 
-hipError_t launch_page_copies(const CacheRef& c, const PageCopies& u, int layers, hipStream_t s) {
+hipError_t launch_page_copies(const CacheRef& c, const PageCopies& u, int layers, int* table, const KvTableUpdate& t,
+                              hipStream_t s) {
   if (u.n < 1 || u.n > kPageCopyBatch) return hipErrorInvalidValue;
   const int64_t bytes = c.pages.page_stride * (c.mx ? 1 : 2);
   const unsigned wgs = (unsigned)std::min<int64_t>((bytes / 16 + 1023) / 1024, 64);
-  hipLaunchKernelGGL(page_copy_kernel, dim3(wgs, layers * (c.mx ? 1 : 2), u.n), dim3(256), 0, s, c, u, bytes);
+  hipLaunchKernelGGL(page_copy_kernel, dim3(wgs, layers * (c.mx ? 1 : 2), u.n), dim3(256), 0, s, c, u, bytes, table, t);
   return hipGetLastError();
 }
 

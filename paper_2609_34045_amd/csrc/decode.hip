@@ -643,7 +643,8 @@ __device__ __forceinline__ void dk_read_vt(uint32_t base, const int (&off)[NT], 
 #define KF_ATTN_LAZY 8.0f
 #endif
 
-template <int HD, int NW>
+// QT: the queries' type, as AttnParams::q_type has it.
+template <int HD, int NW, int QT>
 __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_kernel(const AttnParams p) {
   constexpr int KB = 16;             // keys per block
   constexpr int ROWB = HD * 2;       // bytes per key row
@@ -673,12 +674,22 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
   v4f qlo[NS], qhi[NS];
   {
     const bool hv = hn < G;
-    const float* qr = p.q + (int64_t)b * p.nq * HD + (int64_t)(hq0 + (hv ? hn : 0)) * HD;
+    const int64_t row = (int64_t)b * p.nq * HD + (int64_t)(hq0 + (hv ? hn : 0)) * HD;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      const v4f* src = reinterpret_cast<const v4f*>(qr + 32 * s + 8 * q4);
-      qlo[s] = src[0];
-      qhi[s] = src[1];
+      const int64_t at = row + 32 * s + 8 * q4;
+      if constexpr (QT == 0) {
+        const v4f* src = reinterpret_cast<const v4f*>(p.q + at);
+        qlo[s] = src[0];
+        qhi[s] = src[1];
+      } else {
+        const v4u w = *reinterpret_cast<const v4u*>(reinterpret_cast<const uint16_t*>(p.q) + at);
+        float f[8];
+        if (QT == 1) bf16x8(w, f);
+        else f16x8(w, f);
+        qlo[s] = v4f{f[0], f[1], f[2], f[3]};
+        qhi[s] = v4f{f[4], f[5], f[6], f[7]};
+      }
     }
   }
   asm volatile("" ::: "memory");  // the query loads go out before the exit test below
@@ -1436,14 +1447,20 @@ hipError_t launch_gemv(int epi, int R, int U, bool norm, const GemvParams& p, hi
 
 hipError_t launch_attn_decode(const AttnParams& p, int batch, hipStream_t s) {
   if (p.nq % p.nkv || p.nq / p.nkv > 16) return hipErrorInvalidValue;  // query slots of one MFMA column block
-  const dim3 grid(p.n_split, p.nkv, batch);
-  if (p.hd == 128)
-    hipLaunchKernelGGL((attn_decode_mfma_kernel<128, kAttnMfmaWaves>), grid, dim3(64 * kAttnMfmaWaves), 0, s, p);
-  else if (p.hd == 64)
-    hipLaunchKernelGGL((attn_decode_mfma_kernel<64, kAttnMfmaWaves>), grid, dim3(64 * kAttnMfmaWaves), 0, s, p);
-  else
-    return hipErrorInvalidValue;
-  return hipGetLastError();
+  const dim3 grid(p.n_split, p.nkv, batch), block(64 * kAttnMfmaWaves);
+  auto launch = [&](auto type) {
+    constexpr int QT = decltype(type)::value;
+    if (p.hd == 128) hipLaunchKernelGGL((attn_decode_mfma_kernel<128, kAttnMfmaWaves, QT>), grid, block, 0, s, p);
+    else if (p.hd == 64) hipLaunchKernelGGL((attn_decode_mfma_kernel<64, kAttnMfmaWaves, QT>), grid, block, 0, s, p);
+    else return hipErrorInvalidValue;
+    return hipGetLastError();
+  };
+  switch (p.q_type) {
+    case 0: return launch(std::integral_constant<int, 0>{});
+    case 1: return launch(std::integral_constant<int, 1>{});
+    case 2: return launch(std::integral_constant<int, 2>{});
+    default: return hipErrorInvalidValue;
+  }
 }
 
 template <int HD>

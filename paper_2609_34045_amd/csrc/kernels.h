@@ -226,6 +226,7 @@ struct GemvParams {
 
 struct AttnParams {
   const float* q;      // [B][nq*hd] rotated queries
+  int q_type;          // their type, 0 fp32, 1 bf16, 2 fp16 (the kf_dtype values); fp32 in a decode step
   uint16_t* kc;        // layer base (fp16 bits), pages as in KvPages (written only for the new key of qk-norm blocks)
   const uint16_t* vc;
   float* part_acc;     // [B][nq][max_split][hd]
@@ -262,8 +263,7 @@ constexpr int kMxMaxSplit = 4096;  // keys per workgroup, upper bound
 struct MxAttnParams {
   AttnParams a;
   const uint8_t* rec;  // layer base
-  const void* q;       // [B][nq][hd] rotated queries of q_type (the kf_dtype values)
-  int q_type;
+  const void* q;       // [B][nq][hd] rotated queries of type a.q_type
   void* out;           // [B][nq][hd] of type io, or NULL
   int io;
 };
@@ -287,7 +287,6 @@ hipError_t launch_attn_mx(const MxAttnParams& p, int batch, hipStream_t s);
 // p.out from the partials of either cache type's attention.
 hipError_t launch_attend_merge(const MxAttnParams& p, int batch, hipStream_t s);
 hipError_t launch_mx_append(const MxAppendParams& p, hipStream_t s);
-hipError_t launch_rows_to_f32(const void* src, int type, float* dst, int n, hipStream_t s);
 int gemv_grid(int epi, int rows_per_wg, const GemvParams& p);
 hipError_t launch_gemv(int epi, int rows_per_wg, int chunks_in_flight, bool norm, const GemvParams& p, hipStream_t s);
 // The same launch with the stage input (p.src or p.tokens) as its input rows.
@@ -366,13 +365,14 @@ hipError_t launch_mx_read(const CacheRef& c, int user, int pos0, float* dst_k, f
 // Positions [pos0, pos0 + n) of src_user to the same ones of dst_user, in every one of `layers` layers.
 hipError_t launch_cache_copy(const CacheRef& dst, int dst_user, const CacheRef& src, int src_user, int pos0, int n,
                              int layers, int* err_flag, hipStream_t s);
-// Whole pages src[i] to dst[i] for i < n (n <= kPageCopyBatch), in every layer.
+// Whole pages src[i] to dst[i] for i < n (n <= kPageCopyBatch), in every layer, and the table entries in u.
 constexpr int kPageCopyBatch = 32;
 struct PageCopies {
   int n;
   int src[kPageCopyBatch];
   int dst[kPageCopyBatch];
 };
-hipError_t launch_page_copies(const CacheRef& c, const PageCopies& u, int layers, hipStream_t s);
+hipError_t launch_page_copies(const CacheRef& c, const PageCopies& copies, int layers, int* table,
+                              const KvTableUpdate& u, hipStream_t s);
 
 }  // namespace kf

@@ -273,8 +273,8 @@ static kf_status kv_grant(kf_kv* kv, int n, const int* users, const int64_t* fro
   KvTableUpdate up{};
   PageCopies cp{};
   auto flush = [&]() {
-    if (cp.n) KF_HIP(launch_page_copies(kv->ref(), cp, kv->layers(), st), "page copies");
-    if (up.n) KF_HIP(launch_kv_table_update(kv->table, up, st), "page table update");
+    if (cp.n) KF_HIP(launch_page_copies(kv->ref(), cp, kv->layers(), kv->table, up, st), "page copies");
+    else if (up.n) KF_HIP(launch_kv_table_update(kv->table, up, st), "page table update");
     cp.n = up.n = 0;
     return KF_OK;
   };
@@ -1154,6 +1154,7 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
     a.len[b] = lens[b];
   }
   p.io = io;
+  a.q_type = io;
   const Tracer tr = s->tracer();
   tr.begin(KF_K_ATTN);
   hipError_t e = hipSuccess;
@@ -1161,20 +1162,15 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
     attn_split_mx(c.n_kv_heads, rows, lens, kv->max_split, s->n_cu, a);
     p.rec = ref.k;
     p.q = q_dev;
-    p.q_type = io;
     p.out = a.n_split == 1 ? out_dev : nullptr;
     e = launch_attn_mx(p, rows, s->stream);
   } else {
     attn_split_mfma(c.n_kv_heads, total_len, max_len > 0 ? max_len : 1, kv->max_split, s->n_cu, &a.split, &a.n_split);
     for (int b = 0; b < rows; ++b) a.row_splits[b] = a.n_split;
     a.q = reinterpret_cast<const float*>(q_dev);
-    if (io != KF_F32) {  // the fp16 kernel takes fp32 queries
-      e = launch_rows_to_f32(q_dev, io, s->q, rows * c.n_q_heads * c.head_dim, s->stream);
-      a.q = s->q;
-    }
     a.kc = (uint16_t*)ref.k;
     a.vc = (uint16_t*)ref.v;
-    if (e == hipSuccess) e = launch_attn_decode(a, rows, s->stream);
+    e = launch_attn_decode(a, rows, s->stream);
   }
   if (e == hipSuccess && !p.out) {
     p.out = out_dev;

@@ -145,7 +145,7 @@ def _check(status: int, where: str):
 def _ptr(t):
     if t is None:
         return None
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _io_dtype(t) -> int:
