@@ -220,7 +220,10 @@ __device__ __forceinline__ void gemv_epilogue(const GemvParams& p, int wg, const
   bool bad = false;  // an fp16 store out of range
   float rs[B];
 #pragma unroll
-  for (int b = 0; b < B; ++b) rs[b] = NORM ? 1.0f / sqrtf(fin[R * B + b] / (float)p.K + p.eps) : 1.0f;
+  for (int b = 0; b < B; ++b) {
+    const float eps = EPI == kEpiLMHead && p.eps_rows ? p.eps_rows[b] : p.eps;
+    rs[b] = NORM ? 1.0f / sqrtf(fin[R * B + b] / (float)p.K + eps) : 1.0f;
+  }
 
   if (EPI == kEpiQKV) {
     if (tid < (R / 2) * B) {

@@ -218,6 +218,7 @@ struct GemvParams {
   int* err_flag;           // sticky error bits (kErrToken, kErrF16Range, kErrNaNLogit); every launch sets it
 
   // kEpiLMHead
+  const float* eps_rows;  // [B] or NULL: eps of each row, for input rows that were scaled (launch_rows_to_f16)
   float* logits;       // optional [B][N]
   float* part_val;     // [B][n_wg]
   int* part_idx;       // [B][n_wg]
@@ -344,6 +345,10 @@ struct LogprobParams {
   unsigned long long* part_keys;  // [rows][chunks][top]
   float* part_sums;               // [rows][chunks][4]
 };
+// x16 = x 2^e of up to kMaxBatch bf16 rows [rows][K] and eps_rows = eps 4^e, with e so that a row's largest
+// value lies in [2^14, 2^15): what RMSNorm with that eps makes of x16 and of x is the same.  Every value above 2^-29 of
+// the row's largest is exact.
+hipError_t launch_rows_to_f16(const uint16_t* x, int rows, int K, float eps, uint16_t* x16, float* eps_rows, hipStream_t s);
 int logprob_chunks(int rows, int vocab);
 int64_t logprob_part_bytes(int rows, int vocab, int top);  // workspace of a launch (not used where logprob_chunks is 1)
 hipError_t launch_logprobs(LogprobParams p, int rows, char* part, hipStream_t s);

@@ -24,6 +24,7 @@ namespace kf {
 
 namespace {
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef unsigned long long u64;
 
 constexpr int kT = 256;  // threads
@@ -300,12 +301,63 @@ __global__ __launch_bounds__(kT) void logprob_join_kernel(const LogprobParams p)
   finish_row(p, row, M, S, W, best);
 }
 
+// Row blockIdx.x, bound by its latency: a thread's values wait in registers (rows of up to 32768; longer ones are
+// read again).  K is a multiple of 64.
+constexpr int kRowThreads = 512;
+__global__ __launch_bounds__(kRowThreads) void rows_to_f16_kernel(const uint16_t* x, int K, float eps, uint16_t* x16, float* eps_rows) {
+  constexpr int kHeld = 8;  // 16-byte pieces
+  __shared__ uint32_t red[kRowThreads / 64];
+  const int tid = threadIdx.x, n = K / 8;
+  const v4u* src = reinterpret_cast<const v4u*>(x + (int64_t)blockIdx.x * K);
+  v4u* dst = reinterpret_cast<v4u*>(x16 + (int64_t)blockIdx.x * K);
+  v4u v[kHeld];
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const int i = tid + kRowThreads * j;
+    v[j] = i < n ? src[i] : v4u{0u, 0u, 0u, 0u};
+  }
+  uint32_t top = 0;  // the magnitudes' bits, in the upper half
+  auto seen = [&](const v4u& w) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7fff0000u, (w[i] & 0x7fffu) << 16));
+  };
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) seen(v[j]);
+  for (int i = tid + kRowThreads * kHeld; i < n; i += kRowThreads) seen(src[i]);
+  top = wave_max_u32(top);
+  if ((tid & 63) == 0) red[tid / 64] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kRowThreads / 64; ++w) top = max(top, red[w]);
+  const float most = __uint_as_float(top);
+  int e = top && most < INFINITY ? 14 - ilogbf(most) : 0;
+  if (eps > 0.f) e = min(e, (126 - ilogbf(eps)) / 2);  // eps 4^e stays finite: smaller rows are nothing beside it
+  if (tid == 0) eps_rows[blockIdx.x] = ldexpf(eps, 2 * e);
+  auto scaled = [&](v4u w) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = f16_pair(ldexpf(__uint_as_float(w[i] << 16), e), ldexpf(__uint_as_float(w[i] & 0xffff0000u), e));
+    return w;
+  };
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const int i = tid + kRowThreads * j;
+    if (i < n) dst[i] = scaled(v[j]);
+  }
+  for (int i = tid + kRowThreads * kHeld; i < n; i += kRowThreads) dst[i] = scaled(src[i]);
+}
+
 // Values per thread: chunks of 8192 values where they fill the chip (two workgroups a
 // CU) or cover a row that 2048 do not at once, else of 2048.
 static int values_per_thread(int rows, int vocab) {
   const int64_t large = (vocab + 8191) / 8192;
   if (vocab <= 2048) return 8;
   return large == 1 || rows * large >= 512 || (vocab + 2047) / 2048 > 128 ? 32 : 8;
+}
+
+hipError_t launch_rows_to_f16(const uint16_t* x, int rows, int K, float eps, uint16_t* x16, float* eps_rows, hipStream_t s) {
+  hipLaunchKernelGGL(rows_to_f16_kernel, dim3(rows), dim3(kRowThreads), 0, s, x, K, eps, x16, eps_rows);
+  return hipGetLastError();
 }
 
 int logprob_chunks(int rows, int vocab) {

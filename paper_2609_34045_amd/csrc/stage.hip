@@ -1412,7 +1412,9 @@ static kf_status head_common(kf_stage* s, int rows, const void* hidden, kf_dtype
   return KF_OK;
 }
 
-static kf_status head_launch(kf_stage* s, int rows, const void* hidden, kf_dtype dtype, float* logits) {
+// hidden NULL: the kept rows, or with rows16 the caller's as launch_rows_to_f16 left them.
+static kf_status head_launch(kf_stage* s, int rows, const void* hidden, kf_dtype dtype, float* logits,
+                             const uint16_t* rows16 = nullptr, const float* eps_rows = nullptr) {
   const kf_model_config& c = s->cfg;
   const Tracer tr = s->tracer();
   GemvParams g{};
@@ -1426,6 +1428,8 @@ static kf_status head_launch(kf_stage* s, int rows, const void* hidden, kf_dtype
     g.in = rows > 1 ? reinterpret_cast<const float*>(s->x16) : s->x;
     g.in16 = rows > 1;
   }
+  if (rows16) g.in = reinterpret_cast<const float*>(rows16);
+  g.eps_rows = eps_rows;
   g.K = c.hidden;
   g.N = c.vocab;
   g.logits = logits;
@@ -1613,20 +1617,30 @@ kf_status kf_head_logprobs(kf_stage* s, int32_t rows, const void* hidden, kf_dty
   if (st != KF_OK) return st;
   // The logits of a chunk stay in the stage (a chunk of 8B-shaped ones, 131 MB, in the last-level
   // cache); where there is no memory for a larger chunk the rows go through what is held.
-  const int64_t row_bytes = (int64_t)c.vocab * 4;
+  const int64_t row_bytes = (int64_t)c.vocab * 4, rows16 = align256((int64_t)kMaxBatch * c.hidden * 2), front = rows16 + 256;
   const int chunk = rows <= kMaxBatch ? kMaxBatch : rows <= 64 ? 64 : kHeadChunk;
-  if (!grow_kept(s, s->lp_logits, chunk * row_bytes) && !grow_kept(s, s->lp_logits, kMaxBatch * row_bytes))
+  if (!grow_kept(s, s->lp_logits, front + chunk * row_bytes) && !grow_kept(s, s->lp_logits, front + kMaxBatch * row_bytes))
     return fail(KF_ENOMEM, "workspace of the log probabilities (%lld bytes; a first call may not be captured)",
-                (long long)(kMaxBatch * row_bytes));
-  const int held = (int)std::min<int64_t>(chunk, s->lp_logits.cap / row_bytes);
+                (long long)(front + kMaxBatch * row_bytes));
+  const int held = (int)std::min<int64_t>(chunk, (s->lp_logits.cap - front) / row_bytes);
+  float* z = (float*)(s->lp_logits.mem + front);
   for (int r0 = 0; r0 < rows; r0 += held) {
     const int n = rows - r0 < held ? rows - r0 : held;
     const char* in = (const char*)hidden;
-    st = kf_head_logits(s, n, hidden ? in + (int64_t)r0 * c.hidden * (dtype == KF_BF16 ? 2 : 4) : nullptr, dtype,
-                        (float*)s->lp_logits.mem);
+    if (hidden) in += (int64_t)r0 * c.hidden * (dtype == KF_BF16 ? 2 : 4);
+    if (hidden && dtype == KF_BF16 && n > 1 && n <= kMaxBatch && s->head_fold) {
+      // Two to four bf16 rows go as fp16 ones, through the launch that kept rows take, which multiplies
+      // pairs (8B-shaped head, 4 rows: 187 us from bf16 rows, 154 so with the scaling's launch).
+      uint16_t* x16 = (uint16_t*)s->lp_logits.mem;
+      float* eps = (float*)(s->lp_logits.mem + rows16);
+      KF_HIP(launch_rows_to_f16((const uint16_t*)in, n, c.hidden, c.rms_eps, x16, eps, s->stream), "head rows launch");
+      st = head_launch(s, n, nullptr, dtype, z, x16, eps);
+    } else {
+      st = kf_head_logits(s, n, in, dtype, z);
+    }
     if (st != KF_OK) return st;
     LogprobParams p{};
-    p.logits = (const float*)s->lp_logits.mem;
+    p.logits = z;
     p.stride = c.vocab;
     p.vocab = c.vocab;
     p.targets = targets ? targets + r0 : nullptr;
