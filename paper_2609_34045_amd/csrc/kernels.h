@@ -333,6 +333,7 @@ struct LogprobParams {
   const float* logits;  // [rows][stride]
   int64_t stride;
   int vocab;
+  const float* row_scale;  // [rows] or NULL: the logits are these times what is stored
   const int32_t* targets;  // [rows] or NULL
   float* logprob;          // [rows], with targets
   float* entropy;          // [rows] or NULL
@@ -345,10 +346,11 @@ struct LogprobParams {
   unsigned long long* part_keys;  // [rows][chunks][top]
   float* part_sums;               // [rows][chunks][4]
 };
-// x16 = x 2^e of up to kMaxBatch bf16 rows [rows][K] and eps_rows = eps 4^e, with e so that a row's largest
-// value lies in [2^14, 2^15): what RMSNorm with that eps makes of x16 and of x is the same.  Every value above 2^-29 of
-// the row's largest is exact.
-hipError_t launch_rows_to_f16(const uint16_t* x, int rows, int K, float eps, uint16_t* x16, float* eps_rows, hipStream_t s);
+// x16 = x 2^e of bf16 rows [rows][K], with e so that a row's largest value lies in [2^14, 2^15): every value above
+// 2^-29 of the row's largest is exact.  What RMSNorm multiplies x16 by is row_scale = 1 / sqrt(mean x16^2 + eps 4^e);
+// eps_rows = eps 4^e.  Either may be NULL.
+hipError_t launch_rows_to_f16(const uint16_t* x, int rows, int K, float eps, uint16_t* x16, float* eps_rows,
+                              float* row_scale, hipStream_t s);
 int logprob_chunks(int rows, int vocab);
 int64_t logprob_part_bytes(int rows, int vocab, int top);  // workspace of a launch (not used where logprob_chunks is 1)
 hipError_t launch_logprobs(LogprobParams p, int rows, char* part, hipStream_t s);

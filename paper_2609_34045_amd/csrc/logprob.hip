@@ -102,7 +102,7 @@ __device__ __forceinline__ void finish_row(const LogprobParams& p, int row, floa
         v = __builtin_nanf("");
         raise_err(p.err_flag, true, kErrToken);
       } else {
-        const float z = p.logits[row * p.stride + t];
+        const float z = p.logits[row * p.stride + t] * (p.row_scale ? p.row_scale[row] : 1.0f);
         v = z == -INFINITY ? z : z != z || z == INFINITY ? __builtin_nanf("") : some ? (z - M) - ls : z;
       }
       p.logprob[row] = v;
@@ -140,6 +140,11 @@ __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[4 * j + i] = at + i < p.vocab ? z[at + i] : -INFINITY;
     }
+  }
+  if (p.row_scale) {
+    const float scale = p.row_scale[row];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) v[i] = v[i] == -INFINITY ? v[i] : v[i] * scale;  // (past the row's end: -inf stays)
   }
   float mine = v[0];  // the lane's largest
   bool bad = false;
@@ -304,9 +309,11 @@ __global__ __launch_bounds__(kT) void logprob_join_kernel(const LogprobParams p)
 // Row blockIdx.x, bound by its latency: a thread's values wait in registers (rows of up to 32768; longer ones are
 // read again).  K is a multiple of 64.
 constexpr int kRowThreads = 512;
-__global__ __launch_bounds__(kRowThreads) void rows_to_f16_kernel(const uint16_t* x, int K, float eps, uint16_t* x16, float* eps_rows) {
+__global__ __launch_bounds__(kRowThreads) void rows_to_f16_kernel(const uint16_t* x, int K, float eps, uint16_t* x16, float* eps_rows,
+                                                                 float* row_scale) {
   constexpr int kHeld = 8;  // 16-byte pieces
   __shared__ uint32_t red[kRowThreads / 64];
+  __shared__ float red_s[kRowThreads / 64];
   const int tid = threadIdx.x, n = K / 8;
   const v4u* src = reinterpret_cast<const v4u*>(x + (int64_t)blockIdx.x * K);
   v4u* dst = reinterpret_cast<v4u*>(x16 + (int64_t)blockIdx.x * K);
@@ -332,11 +339,14 @@ __global__ __launch_bounds__(kRowThreads) void rows_to_f16_kernel(const uint16_t
   const float most = __uint_as_float(top);
   int e = top && most < INFINITY ? 14 - ilogbf(most) : 0;
   if (eps > 0.f) e = min(e, (126 - ilogbf(eps)) / 2);  // eps 4^e stays finite: smaller rows are nothing beside it
-  if (tid == 0) eps_rows[blockIdx.x] = ldexpf(eps, 2 * e);
+  float ss = 0.f;
   auto scaled = [&](v4u w) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = f16_pair(ldexpf(__uint_as_float(w[i] << 16), e), ldexpf(__uint_as_float(w[i] & 0xffff0000u), e));
+    for (int i = 0; i < 4; ++i) {
+      const float a = ldexpf(__uint_as_float(w[i] << 16), e), b = ldexpf(__uint_as_float(w[i] & 0xffff0000u), e);
+      ss += a * a + b * b;
+      w[i] = f16_pair(a, b);
+    }
     return w;
   };
 #pragma unroll
@@ -345,6 +355,17 @@ __global__ __launch_bounds__(kRowThreads) void rows_to_f16_kernel(const uint16_t
     if (i < n) dst[i] = scaled(v[j]);
   }
   for (int i = tid + kRowThreads * kHeld; i < n; i += kRowThreads) dst[i] = scaled(src[i]);
+  const float eps_row = ldexpf(eps, 2 * e);
+  if (tid == 0 && eps_rows) eps_rows[blockIdx.x] = eps_row;
+  if (!row_scale) return;
+  ss = wave_sum(ss);
+  if ((tid & 63) == 0) red_s[tid / 64] = ss;
+  __syncthreads();
+  if (tid == 0) {
+    ss = 0.f;
+    for (int w = 0; w < kRowThreads / 64; ++w) ss += red_s[w];
+    row_scale[blockIdx.x] = 1.0f / sqrtf(ss / (float)K + eps_row);
+  }
 }
 
 // Values per thread: chunks of 8192 values where they fill the chip (two workgroups a
@@ -355,8 +376,9 @@ static int values_per_thread(int rows, int vocab) {
   return large == 1 || rows * large >= 512 || (vocab + 2047) / 2048 > 128 ? 32 : 8;
 }
 
-hipError_t launch_rows_to_f16(const uint16_t* x, int rows, int K, float eps, uint16_t* x16, float* eps_rows, hipStream_t s) {
-  hipLaunchKernelGGL(rows_to_f16_kernel, dim3(rows), dim3(kRowThreads), 0, s, x, K, eps, x16, eps_rows);
+hipError_t launch_rows_to_f16(const uint16_t* x, int rows, int K, float eps, uint16_t* x16, float* eps_rows,
+                              float* row_scale, hipStream_t s) {
+  hipLaunchKernelGGL(rows_to_f16_kernel, dim3(rows), dim3(kRowThreads), 0, s, x, K, eps, x16, eps_rows, row_scale);
   return hipGetLastError();
 }
 

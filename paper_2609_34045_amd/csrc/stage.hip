@@ -1617,30 +1617,45 @@ kf_status kf_head_logprobs(kf_stage* s, int32_t rows, const void* hidden, kf_dty
   if (st != KF_OK) return st;
   // The logits of a chunk stay in the stage (a chunk of 8B-shaped ones, 131 MB, in the last-level
   // cache); where there is no memory for a larger chunk the rows go through what is held.
-  const int64_t row_bytes = (int64_t)c.vocab * 4, rows16 = align256((int64_t)kMaxBatch * c.hidden * 2), front = rows16 + 256;
+  const int64_t row_bytes = (int64_t)c.vocab * 4, rows16 = align256((int64_t)kHeadChunk * c.hidden * 2),
+                front = rows16 + align256(kHeadChunk * 4);
   const int chunk = rows <= kMaxBatch ? kMaxBatch : rows <= 64 ? 64 : kHeadChunk;
   if (!grow_kept(s, s->lp_logits, front + chunk * row_bytes) && !grow_kept(s, s->lp_logits, front + kMaxBatch * row_bytes))
     return fail(KF_ENOMEM, "workspace of the log probabilities (%lld bytes; a first call may not be captured)",
                 (long long)(front + kMaxBatch * row_bytes));
   const int held = (int)std::min<int64_t>(chunk, (s->lp_logits.cap - front) / row_bytes);
   float* z = (float*)(s->lp_logits.mem + front);
+  uint16_t* x16 = (uint16_t*)s->lp_logits.mem;
+  float* per_row = (float*)(s->lp_logits.mem + rows16);
   for (int r0 = 0; r0 < rows; r0 += held) {
     const int n = rows - r0 < held ? rows - r0 : held;
     const char* in = (const char*)hidden;
     if (hidden) in += (int64_t)r0 * c.hidden * (dtype == KF_BF16 ? 2 : 4);
-    if (hidden && dtype == KF_BF16 && n > 1 && n <= kMaxBatch && s->head_fold) {
-      // Two to four bf16 rows go as fp16 ones, through the launch that kept rows take, which multiplies
-      // pairs (8B-shaped head, 4 rows: 187 us from bf16 rows, 154 so with the scaling's launch).
-      uint16_t* x16 = (uint16_t*)s->lp_logits.mem;
-      float* eps = (float*)(s->lp_logits.mem + rows16);
-      KF_HIP(launch_rows_to_f16((const uint16_t*)in, n, c.hidden, c.rms_eps, x16, eps, s->stream), "head rows launch");
-      st = head_launch(s, n, nullptr, dtype, z, x16, eps);
+    LogprobParams p{};
+    p.logits = z;
+    // bf16 rows go as fp16 ones where the matrix holds the gain: two to four through the launch that kept
+    // rows take, which multiplies pairs (8B-shaped head, 4 rows: 187 us from bf16 rows, 152 so), and more as a
+    // plain product on the matrix cores.  Its sums are one fp32 chain over K, where the logits' launch keeps
+    // what each of its shorter ones rounds off: 4e-7 of a logit instead of 1e-7, far below a log probability's
+    // own rounding, and tiles twice as wide fit the registers (200 rows: 368 us, 274 so).
+    const bool as16 = hidden && dtype == KF_BF16 && n > 1 && s->head_fold;
+    if (as16 && n <= kMaxBatch) {
+      KF_HIP(launch_rows_to_f16((const uint16_t*)in, n, c.hidden, c.rms_eps, x16, per_row, nullptr, s->stream), "head rows launch");
+      st = head_launch(s, n, nullptr, dtype, z, x16, per_row);
+    } else if (as16) {
+      const Tracer tr = s->tracer();
+      tr.begin(KF_K_LMHEAD);
+      hipError_t e = launch_rows_to_f16((const uint16_t*)in, n, c.hidden, c.rms_eps, x16, nullptr, per_row, s->stream);
+      if (e == hipSuccess)
+        e = launch_gemm(kGemmPartialF32, gemm_plan(kGemmPartialF32, n, c.vocab, c.hidden, (int64_t)n * c.vocab), x16, s->lm_head,
+                        nullptr, n, c.vocab, c.hidden, z, nullptr, s->err_flag, s->stream);
+      tr.end(KF_K_LMHEAD);
+      KF_HIP(e, "head product launch");
+      p.row_scale = per_row;
     } else {
       st = kf_head_logits(s, n, in, dtype, z);
     }
     if (st != KF_OK) return st;
-    LogprobParams p{};
-    p.logits = z;
     p.stride = c.vocab;
     p.vocab = c.vocab;
     p.targets = targets ? targets + r0 : nullptr;

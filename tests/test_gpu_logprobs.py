@@ -157,7 +157,7 @@ def test_hidden_rows_as_their_logits(torch, st, rows, io):
 
 
 def test_bf16_rows_of_any_size(torch, st):
-    """Two to four bf16 rows, from far below eps to the type's largest and with values of every size in a row, against
+    """Bf16 rows, few and many, from far below eps to the type's largest and with values of every size in a row, against
     64-bit sums over the stored matrix; a row of zeros, and a NaN that stays in its row."""
     shape, head, g = head_stage(st, 320, 5000, 95, lambda h: h["final_norm"].fill(0x3F80))  # gains of one
     x = synth.hidden_states(95, synth.STREAM_DECODE_HIDDEN, 0, 8, 320)
@@ -172,20 +172,21 @@ def test_bf16_rows_of_any_size(torch, st):
     xd = x.float().cpu().numpy().astype(np.float64)
     z = xd / np.sqrt((xd * xd).mean(1, keepdims=True) + np.float64(np.float32(shape.rms_eps))) @ w.T
     t = torch.arange(8, dtype=torch.int32, device="cuda")
-    for rows in ([0, 1, 2, 3], [4, 5], [6, 7, 2]):
+    for rows in ([0, 1, 2, 3], [4, 5], [6, 7, 2], [0, 1, 2, 3, 4, 5, 6, 7], [7] * 40 + [6, 3, 0, 1]):
         r = g.head_logprobs(x[rows].contiguous(), t[rows].contiguous(), top=5)
         lp, h, ids, alt = reference(z[rows], np.array(rows), 5)
-        # logits of up to 2^-24 sqrt(K) of their terms' sum off, below 2^-19 of the largest
+        # a logit is a chain of K / 16 roundings, each 2^-24 of a partial sum of the size of the largest: below 2^-19 of it
         far = 2.0 ** -17 + 2.0 ** -18 * np.abs(z[rows]).max(1)
         close(r.logprob, lp, far + 2.0 ** -23 * np.abs(lp), "logprob")
         close(r.top_logprobs, alt, far[:, None] + 2.0 ** -23 * np.abs(alt), "alternatives")
         close(r.entropy, h, 2.0 ** -17 * 15 + 2.0 ** -23 * 196 + 15 * far, "entropy")
     g.sync()
     x[1, 3] = float("nan")
-    r = g.head_logprobs(x[:3].contiguous(), top=5)
-    assert (r.top_ids[1] == -1).all() and (r.top_ids[[0, 2]] >= 0).all()
-    with pytest.raises(st.KFError):
-        g.sync()
+    for rows in (3, 8):
+        r = g.head_logprobs(x[:rows].contiguous(), top=5)
+        assert (r.top_ids[1] == -1).all() and (r.top_ids[[0, *range(2, rows)]] >= 0).all()
+        with pytest.raises(st.KFError):
+            g.sync()
     g.close()
 
 
