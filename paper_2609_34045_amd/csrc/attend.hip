@@ -107,7 +107,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const MxAttnPar
 
   // grid.x: the splits of row 0, then of row 1, ..
   int split = blockIdx.x, b = 0;
-  for (; b < kMaxBatch - 1 && split >= p.a.row_splits[b]; ++b) split -= p.a.row_splits[b];
+  for (; b < kMaxBatch - 1 && split >= p.rows.n[b]; ++b) split -= p.rows.n[b];
   const int g = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = p.a.nq / p.a.nkv, hq0 = g * G;
   const int col = lane & 15, grp = lane >> 4, head = col & 7;
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const MxAttnPar
     float f[NS][8], top = 0.f;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
-      load_q8(p.q, p.a.q_type, ((int64_t)b * p.a.nq + hq0 + min(head, G - 1)) * HD + grp * (HD / 4) + 8 * s, f[s]);
+      load_q8(p.q, p.q_type, ((int64_t)b * p.a.nq + hq0 + min(head, G - 1)) * HD + grp * (HD / 4) + 8 * s, f[s]);
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const MxAttnPar
 template <int HD>
 __global__ __launch_bounds__(256) void attend_merge_kernel(const MxAttnParams p) {
   constexpr int DPL = HD / 64, PRE = 8;
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ns = p.a.row_splits[b];
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ns = p.rows.n[b];
   const int64_t r0 = ((int64_t)b * p.a.nq + h) * p.a.max_split;
   const float* ml = p.a.part_ml + r0 * 2;
   const float* acc = p.a.part_acc + r0 * HD + lane * DPL;
@@ -360,9 +360,15 @@ __global__ __launch_bounds__(256) void mx_append_kernel(const MxAppendParams p) 
   if (b >= p.batch) return;  // whole heads: a head's lanes leave together
   const int g = h < nq ? 0 : (h - nq) % p.nkv;
   const bool is_v = h >= nq + p.nkv;
-  float* src = h < nq ? p.q + ((int64_t)b * p.nq + h) * hd : (is_v ? p.v : p.k) + ((int64_t)b * p.nkv + g) * hd;
+  const int t = p.pos[b] % kKvPage;
   float x[8];
-  load_q8(src, 0, d0, x);
+  if (h < nq) {
+    load_q8(p.q, 0, ((int64_t)b * p.nq + h) * hd + d0, x);
+  } else if (p.gq && !is_v) {
+    load_q8(p.kraw, 0, ((int64_t)b * p.nkv + g) * hd + d0, x);
+  } else {
+    load_q8(is_v ? p.v16 : p.k16, 2, (((int64_t)b * p.nkv + g) * kKvPage + t) * hd + d0, x);
+  }
   if (p.gq && !is_v) {
     float ss = 0.f;
 #pragma unroll
@@ -385,8 +391,9 @@ __global__ __launch_bounds__(256) void mx_append_kernel(const MxAppendParams p) 
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = y[j];
     if (h < nq) {
-      reinterpret_cast<v4f*>(src + d0)[0] = v4f{x[0], x[1], x[2], x[3]};
-      reinterpret_cast<v4f*>(src + d0)[1] = v4f{x[4], x[5], x[6], x[7]};
+      v4f* q = reinterpret_cast<v4f*>(p.q + ((int64_t)b * p.nq + h) * hd + d0);
+      q[0] = v4f{x[0], x[1], x[2], x[3]};
+      q[1] = v4f{x[4], x[5], x[6], x[7]};
       return;
     }
   }
@@ -395,7 +402,6 @@ __global__ __launch_bounds__(256) void mx_append_kernel(const MxAppendParams p) 
   uint32_t pairs[4] = {f16_pair(x[0], x[1]), f16_pair(x[2], x[3]), f16_pair(x[4], x[5]), f16_pair(x[6], x[7])};
   const uint32_t w = mx_encode8(pairs, e, bad);
   raise_err(p.err_flag, bad, kErrF16Range);
-  const int t = p.pos[b] % kKvPage;
   const int codes = mx_codes(hd);
   uint8_t* rec = p.rec + (int64_t)kv_page(p.kv, p.users[b], p.pos[b] / kKvPage) * p.kv.page_stride +
                  (int64_t)g * mx_record(hd) + (is_v ? mx_v(hd) : 0);
@@ -420,8 +426,8 @@ hipError_t launch_attn_mx(const MxAttnParams& p, int batch, hipStream_t s) {
   if (p.a.nq % p.a.nkv || p.a.nq / p.a.nkv > 8 || p.a.split % kKvPage || p.a.split > kMxMaxSplit) return hipErrorInvalidValue;
   int splits = 0;
   for (int b = 0; b < batch; ++b) {
-    if (p.a.row_splits[b] < 1 || p.a.row_splits[b] > p.a.max_split) return hipErrorInvalidValue;
-    splits += p.a.row_splits[b];
+    if (p.rows.n[b] < 1 || p.rows.n[b] > p.a.max_split) return hipErrorInvalidValue;
+    splits += p.rows.n[b];
   }
   const dim3 grid(splits, p.a.nkv);
   if (p.a.hd == 128) hipLaunchKernelGGL(attn_mx_kernel<128>, grid, dim3(64 * kWaves), 0, s, p);

@@ -221,7 +221,7 @@ __device__ __forceinline__ void gemv_epilogue(const GemvParams& p, int wg, const
   float rs[B];
 #pragma unroll
   for (int b = 0; b < B; ++b) {
-    const float eps = EPI == kEpiLMHead && p.eps_rows ? p.eps_rows[b] : p.eps;
+    const float eps = EPI == kEpiLMHead && R == kHeadRowsKept && p.eps_rows ? p.eps_rows[b] : p.eps;
     rs[b] = NORM ? 1.0f / sqrtf(fin[R * B + b] / (float)p.K + eps) : 1.0f;
   }
 
@@ -244,19 +244,11 @@ __device__ __forceinline__ void gemv_epilogue(const GemvParams& p, int wg, const
           float* q = p.q + (int64_t)b * p.nq * hd + head * hd;
           q[i] = z1;
           q[i + half] = z2;
-        } else if (p.k32) {
-          float* k = p.k32 + ((int64_t)b * p.nkv + head - p.nq) * hd;
-          k[i] = z1;
-          k[i + half] = z2;
         } else {
           uint16_t* k = p.kc + kv_offset(p.kv, p.users[b], head - p.nq, pos, hd);
           k[i] = f16_checked(z1, bad);
           k[i + half] = f16_checked(z2, bad);
         }
-      } else if (p.v32) {
-        float* v = p.v32 + ((int64_t)b * p.nkv + head - p.nq - p.nkv) * hd;
-        v[i] = y1;
-        v[i + half] = y2;
       } else {
         uint16_t* v = p.vc + kv_offset(p.kv, p.users[b], head - p.nq - p.nkv, pos, hd);
         v[i] = f16_checked(y1, bad);
@@ -646,7 +638,7 @@ __device__ __forceinline__ void dk_read_vt(uint32_t base, const int (&off)[NT], 
 #define KF_ATTN_LAZY 8.0f
 #endif
 
-// QT: the queries' type, as AttnParams::q_type has it.
+// QT: the queries' type (0 fp32, as in a decode step, 1 bf16, 2 fp16).
 template <int HD, int NW, int QT>
 __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_kernel(const AttnParams p) {
   constexpr int KB = 16;             // keys per block
@@ -968,12 +960,13 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
 // fourth split's vector (independent loads) and the four sums are combined.  The
 // result goes out for the output projection's GEMV: in fp16 (o16, batch > 1) or
 // fp32 (o32, the batch-1 launch sequence that adds the heads in a fixed order).
-template <int HD>
+// EACH: the rows' numbers of splits differ (rows), else all have n_split.
+template <int HD, bool EACH>
 __global__ __launch_bounds__(256) void attn_merge_kernel(const AttnParams a, uint16_t* __restrict__ o16,
-                                                         float* __restrict__ o32) {
+                                                         float* __restrict__ o32, const RowSplits rows) {
   constexpr int DPL = HD / 64;
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int ns = a.row_splits[b];
+  const int ns = EACH ? rows.n[b] : a.n_split;
   const int64_t r0 = ((int64_t)b * a.nq + h) * a.max_split;
   const float* ml = a.part_ml + r0 * 2;
   const float* acc = a.part_acc + r0 * HD + lane * DPL;
@@ -1448,7 +1441,7 @@ hipError_t launch_gemv(int epi, int R, int U, bool norm, const GemvParams& p, hi
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_attn_decode(const AttnParams& p, int batch, hipStream_t s) {
+hipError_t launch_attn_decode(const AttnParams& p, int batch, hipStream_t s, int q_type) {
   if (p.nq % p.nkv || p.nq / p.nkv > 16) return hipErrorInvalidValue;  // query slots of one MFMA column block
   const dim3 grid(p.n_split, p.nkv, batch), block(64 * kAttnMfmaWaves);
   auto launch = [&](auto type) {
@@ -1458,7 +1451,7 @@ hipError_t launch_attn_decode(const AttnParams& p, int batch, hipStream_t s) {
     else return hipErrorInvalidValue;
     return hipGetLastError();
   };
-  switch (p.q_type) {
+  switch (q_type) {
     case 0: return launch(std::integral_constant<int, 0>{});
     case 1: return launch(std::integral_constant<int, 1>{});
     case 2: return launch(std::integral_constant<int, 2>{});
@@ -1479,11 +1472,15 @@ static hipError_t oproj_dispatch(const AttnParams& a, const uint16_t* w, float* 
   return hipGetLastError();
 }
 
-hipError_t launch_attn_merge(const AttnParams& a, uint16_t* o16, float* o32, int batch, hipStream_t s) {
+hipError_t launch_attn_merge(const AttnParams& a, const RowSplits* rows, uint16_t* o16, float* o32, int batch,
+                             hipStream_t s) {
   if (batch < 1 || batch > kMaxBatch || (o16 == nullptr) == (o32 == nullptr)) return hipErrorInvalidValue;
   const dim3 grid(a.nq, batch);
-  if (a.hd == 128) hipLaunchKernelGGL(attn_merge_kernel<128>, grid, dim3(256), 0, s, a, o16, o32);
-  else if (a.hd == 64) hipLaunchKernelGGL(attn_merge_kernel<64>, grid, dim3(256), 0, s, a, o16, o32);
+  const RowSplits n = rows ? *rows : RowSplits{};
+  if (a.hd == 128 && rows) hipLaunchKernelGGL((attn_merge_kernel<128, true>), grid, dim3(256), 0, s, a, o16, o32, n);
+  else if (a.hd == 128) hipLaunchKernelGGL((attn_merge_kernel<128, false>), grid, dim3(256), 0, s, a, o16, o32, n);
+  else if (a.hd == 64 && rows) hipLaunchKernelGGL((attn_merge_kernel<64, true>), grid, dim3(256), 0, s, a, o16, o32, n);
+  else if (a.hd == 64) hipLaunchKernelGGL((attn_merge_kernel<64, false>), grid, dim3(256), 0, s, a, o16, o32, n);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }

@@ -14,6 +14,7 @@ constexpr int kAttnMaxSplit = 1024; // keys per split-KV workgroup, upper bound
 // slower: every workgroup repeats its head's merge of the split partials).
 constexpr int kOprojRows = 256;
 constexpr int kAttnMaxSplitCount = 1024;  // split-KV workgroups per (row, KV head), upper bound
+constexpr int kHeadRowsKept = 12;  // rows of the LM head per workgroup, for fp16 input rows of batch 2-4
 // Decode attention on the matrix cores: workgroups of kAttnMfmaWaves waves over
 // splits of any multiple of kAttnMfmaAlign keys (16-key blocks, one page or
 // less each).
@@ -197,9 +198,6 @@ struct GemvParams {
   // ([B][nkv][hd] fp32) as projected (after the attention RMSNorm), without
   // RoPE; the decode attention finishes both.  v goes to the cache as usual.
   float* kraw;
-  // MXFP4 caches: k (rotated; raw in kraw when that is set) and v go here instead of the
-  // cache, [B][nkv][hd] fp32; launch_mx_append stores them.
-  float *k32, *v32;
 
   // kEpiSwiGLU
   float* act;          // [B][N] with N = F: fp32, or fp16 when act16 is set
@@ -218,16 +216,15 @@ struct GemvParams {
   int* err_flag;           // sticky error bits (kErrToken, kErrF16Range, kErrNaNLogit); every launch sets it
 
   // kEpiLMHead
-  const float* eps_rows;  // [B] or NULL: eps of each row, for input rows that were scaled (launch_rows_to_f16)
   float* logits;       // optional [B][N]
   float* part_val;     // [B][n_wg]
   int* part_idx;       // [B][n_wg]
   int n_wg;
+  const float* eps_rows;  // [B] or NULL: eps of each row, for input rows that were scaled (launch_rows_to_f16)
 };
 
 struct AttnParams {
   const float* q;      // [B][nq*hd] rotated queries
-  int q_type;          // their type, 0 fp32, 1 bf16, 2 fp16 (the kf_dtype values); fp32 in a decode step
   uint16_t* kc;        // layer base (fp16 bits), pages as in KvPages (written only for the new key of qk-norm blocks)
   const uint16_t* vc;
   float* part_acc;     // [B][nq][max_split][hd]
@@ -236,7 +233,6 @@ struct AttnParams {
   int nq, nkv, hd;
   int split;           // keys per workgroup
   int n_split;         // workgroups per (row, kv head): the most of any row
-  int row_splits[kMaxBatch];  // partials of each row; the fp16 kernel writes n_split for every row
   int max_split;       // allocated split capacity
   float scale_log2;    // log2(e) / sqrt(hd)
   int users[kMaxBatch];
@@ -258,13 +254,18 @@ struct AttnParams {
 
 // Attention over an MXFP4 cache (attend.hip): a's queries and cache pointers are not
 // used, its KvPages count bytes, its splits are whole pages, and rows have as many as they
-// need (row_splits, 1 at least).  With `out` set (one split a row, or the merge) the result goes
+// need (1 at least).  With `out` set (one split a row, or the merge) the result goes
 // there; else the partials go to a's arrays, as the fp16 kernel's do.
 constexpr int kMxMaxSplit = 4096;  // keys per workgroup, upper bound
+struct RowSplits {
+  int n[kMaxBatch];  // partials of each row
+};
 struct MxAttnParams {
   AttnParams a;
+  RowSplits rows;
   const uint8_t* rec;  // layer base
-  const void* q;       // [B][nq][hd] rotated queries of type a.q_type
+  const void* q;       // [B][nq][hd] rotated queries
+  int q_type;          // and their type, 0 fp32, 1 bf16, 2 fp16 (the kf_dtype values)
   void* out;           // [B][nq][hd] of type io, or NULL
   int io;
 };
@@ -273,7 +274,9 @@ struct MxAppendParams {
   uint8_t* rec;  // layer base
   KvPages kv;
   float* q;      // [B][nq][hd]: normalised and rotated in place when gq is set
-  float *k, *v;  // [B][nkv][hd]; k rotated, or raw when gq is set
+  // row b's key (rotated) and value, as the QKV launch left them: fp16 page b, at the position's slot
+  const uint16_t *k16, *v16;
+  const float* kraw;  // [B][nkv][hd]: the raw keys instead, when gq is set
   const uint16_t *gq, *gk;  // per-head norm gains [hd] bf16, or NULL
   const float *rope_cos, *rope_sin;
   float eps;
@@ -293,10 +296,11 @@ hipError_t launch_gemv(int epi, int rows_per_wg, int chunks_in_flight, bool norm
 // The same launch with the stage input (p.src or p.tokens) as its input rows.
 hipError_t launch_gemv_src(int epi, int rows_per_wg, int chunks_in_flight, bool norm, const GemvParams& p,
                            hipStream_t s);
-hipError_t launch_attn_decode(const AttnParams& p, int batch, hipStream_t s);
+hipError_t launch_attn_decode(const AttnParams& p, int batch, hipStream_t s, int q_type = 0);  // q of a kf_dtype
 // Head h of row b merged from the attention partials in p, to o16[b][h*hd:(h+1)*hd]
 // (fp16) or, with o16 NULL, to o32[b][h*hd:(h+1)*hd] (fp32).
-hipError_t launch_attn_merge(const AttnParams& p, uint16_t* o16, float* o32, int batch, hipStream_t s);
+// rows: how many partials each row has, or NULL for p.n_split.
+hipError_t launch_attn_merge(const AttnParams& p, const RowSplits* rows, uint16_t* o16, float* o32, int batch, hipStream_t s);
 // x[b][0:N) += W_o o_b with o_b merged from the attention partials in p (W_o [N][nq*hd] fp16).
 hipError_t launch_oproj_heads(const AttnParams& p, const uint16_t* w, float* x, int N, int batch, hipStream_t s);
 hipError_t launch_argmax_final(const float* part_val, const int* part_idx, int n_wg, int rows, int32_t* token,

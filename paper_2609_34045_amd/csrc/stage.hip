@@ -28,9 +28,8 @@ constexpr int kQkvRowsBatch1 = 4;  // the batch-1 QKV launch takes 4-row workgro
 // The LM head on the rows a decode kept (fp16, batch 2-4) takes 12-row
 // workgroups: each reads its input rows once for all its weight rows, so these
 // move two thirds of the 8-row launch's input bytes per weight byte (8B-shaped
-// head stage at batch 4: 153.5 -> 152.2 us, V = 128256 = 12 x 10688).  The
-// caller's fp32 or bf16 rows keep 8-row workgroups.
-constexpr int kHeadRowsKept = 12;
+// head stage at batch 4: 153.5 -> 152.2 us, V = 128256 = 12 x 10688): kHeadRowsKept.
+// The caller's fp32 or bf16 rows keep 8-row workgroups.
 
 // Rows per workgroup of a residual GEMV with n output rows: 8, unless that
 // leaves the grid a fraction of a round over the compute units and 4 rows do
@@ -203,9 +202,14 @@ struct kf_kv {
   int64_t bytes = 0;                    // device bytes of everything here
   float *rcos = nullptr, *rsin = nullptr;
   float *part_acc = nullptr, *part_ml = nullptr;
-  // KF_KV_MXFP4: a decode step's new keys and values, [kMaxBatch][nkv][hd] fp32 each; and one layer of
-  // one user's positions in fp16 pages, which the prefill's attention reads
-  float* append = nullptr;
+  // KF_KV_MXFP4: a decode step's new keys and values, which the QKV launch leaves in fp16 as in an fp16
+  // cache, row b's in page b (append_table gives that page for every position); and one layer of one user's
+  // positions in fp16 pages, which the prefill's attention reads
+  uint16_t* append = nullptr;  // kMaxBatch pages of K, then of V
+  int* append_table = nullptr; // [kMaxBatch][ppu]
+  KvPages append_pages() const {
+    return KvPages{append_table, ppu, (int64_t)st->cfg.n_kv_heads * kKvPage * st->cfg.head_dim};
+  }
   uint16_t *f16_k = nullptr, *f16_v = nullptr;
   int64_t page_stride, layer_stride;  // elements
   std::vector<int> len;
@@ -765,11 +769,12 @@ static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int3
   const int64_t pacc = (int64_t)kMaxBatch * c.n_q_heads * kv->max_split * c.head_dim * 4;
   const int64_t pml = (int64_t)kMaxBatch * c.n_q_heads * kv->max_split * 2 * 4;
   const int64_t tab = paged ? (int64_t)max_users * ppu * 4 : 0;
-  const int64_t app = kv->mx() ? 2LL * kMaxBatch * c.n_kv_heads * c.head_dim * 4 : 0;
+  const int64_t app = kv->mx() ? 2LL * kMaxBatch * c.n_kv_heads * kKvPage * c.head_dim * 2 : 0;
+  const int64_t app_tab = kv->mx() ? (int64_t)kMaxBatch * ppu * 4 : 0;
   const int64_t f16 = kv->mx() ? (int64_t)ppu * kKvPage * c.n_kv_heads * c.head_dim * 2 : 0;
-  constexpr int kMem = 10;
+  constexpr int kMem = 11;
   char* mem[kMem] = {nullptr};
-  const int64_t sz[kMem] = {cache, kv->mx() ? 0 : cache, rope, rope, pacc, pml, tab, app, f16, f16};
+  const int64_t sz[kMem] = {cache, kv->mx() ? 0 : cache, rope, rope, pacc, pml, tab, app, f16, f16, app_tab};
   for (int i = 0; i < kMem; ++i) {
     if (sz[i] == 0) continue;
     kv->bytes += sz[i];
@@ -788,7 +793,8 @@ static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int3
   kv->part_acc = (float*)mem[4];
   kv->part_ml = (float*)mem[5];
   kv->table = (int*)mem[6];
-  kv->append = (float*)mem[7];
+  kv->append = (uint16_t*)mem[7];
+  kv->append_table = (int*)mem[10];
   kv->f16_k = (uint16_t*)mem[8];
   kv->f16_v = (uint16_t*)mem[9];
   // RoPE table from float64 angles: pos * theta^(-2i/hd).
@@ -805,6 +811,11 @@ static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int3
   if (e == hipSuccess && kv->v) e = hipMemset(kv->v, 0, cache);
   if (e == hipSuccess && f16) e = hipMemset(kv->f16_k, 0, f16);
   if (e == hipSuccess && f16) e = hipMemset(kv->f16_v, 0, f16);
+  if (e == hipSuccess && app_tab) {
+    std::vector<int> t((size_t)kMaxBatch * ppu);
+    for (size_t i = 0; i < t.size(); ++i) t[i] = (int)(i / ppu);
+    e = hipMemcpy(kv->append_table, t.data(), app_tab, hipMemcpyHostToDevice);
+  }
   if (e == hipSuccess && kv->table) e = hipMemset(kv->table, 0, tab);
   if (e == hipSuccess) e = hipMemcpy(kv->rcos, tc.data(), rope, hipMemcpyHostToDevice);
   if (e == hipSuccess) e = hipMemcpy(kv->rsin, ts.data(), rope, hipMemcpyHostToDevice);
@@ -856,7 +867,7 @@ kf_status kf_kv_pages(const kf_kv* kv, int32_t* total, int32_t* free_pages) {
 kf_status kf_kv_destroy(kf_kv* kv) {
   if (!kv) return fail(KF_EINVAL, "kv is NULL");
   hipStreamSynchronize(kv->st->stream);
-  void* mem[] = {kv->k, kv->v, kv->rcos, kv->rsin, kv->part_acc, kv->part_ml, kv->table, kv->append, kv->f16_k, kv->f16_v};
+  void* mem[] = {kv->k, kv->v, kv->rcos, kv->rsin, kv->part_acc, kv->part_ml, kv->table, kv->append, kv->append_table, kv->f16_k, kv->f16_v};
   for (void* m : mem)
     if (m) hipFree(m);
   kv->st->live_kv--;
@@ -1064,7 +1075,7 @@ static void attn_split_mfma(int nkv, int64_t total_len, int max_len, int max_spl
 // positions took 55.0, 58 to 61, 63 and 61 us, the 8B shape's four rows of 1024 to 32768 19.0, 20.5, 21 and
 // 23.5), and a page for each of a workgroup's waves at least.  Each row has as many splits as its pages need,
 // and one where it has none.
-static void attn_split_mx(int nkv, int rows, const int* lens, int max_split, int n_cu, AttnParams& a) {
+static void attn_split_mx(int nkv, int rows, const int* lens, int max_split, int n_cu, AttnParams& a, RowSplits& of) {
   int64_t total = 0, longest = 0;
   for (int b = 0; b < rows; ++b) {
     total += pages_for(lens[b]);
@@ -1077,22 +1088,23 @@ static void attn_split_mx(int nkv, int rows, const int* lens, int max_split, int
   a.split = (int)sp * kKvPage;
   a.n_split = 1;
   for (int b = 0; b < rows; ++b) {
-    a.row_splits[b] = std::max(1, (int)((pages_for(lens[b]) + sp - 1) / sp));
-    a.n_split = std::max(a.n_split, a.row_splits[b]);
+    of.n[b] = std::max(1, (int)((pages_for(lens[b]) + sp - 1) / sp));
+    a.n_split = std::max(a.n_split, of.n[b]);
   }
 }
 
 // A decode step's attention over an MXFP4 cache, for which the QKV launch g left the new keys and
 // values in kv->append (and raw keys of qk_norm blocks in s->kraw).
-static hipError_t attn_mx(kf_stage* s, kf_kv* kv, const LayerW& L, const AttnParams& a, const GemvParams& g, int layer,
-                          hipStream_t st) {
+static hipError_t attn_mx(kf_stage* s, kf_kv* kv, const LayerW& L, const AttnParams& a, const GemvParams& g,
+                          const RowSplits& rows, const int32_t* users, int layer, hipStream_t st) {
   const kf_model_config& c = s->cfg;
   MxAppendParams n{};
   n.rec = kv->layer_ref(layer).k;
   n.kv = a.kv;
   n.q = s->q;
-  n.k = c.qk_norm ? s->kraw : g.k32;
-  n.v = g.v32;
+  n.k16 = g.kc;
+  n.v16 = g.vc;
+  n.kraw = s->kraw;
   n.gq = L.g_qn;
   n.gk = L.g_kn;
   n.rope_cos = kv->rcos;
@@ -1104,13 +1116,14 @@ static hipError_t attn_mx(kf_stage* s, kf_kv* kv, const LayerW& L, const AttnPar
   n.batch = g.batch;
   n.err_flag = s->err_flag;
   for (int b = 0; b < g.batch; ++b) {
-    n.users[b] = g.users[b];
+    n.users[b] = users[b];
     n.pos[b] = g.pos[b];
   }
   const hipError_t e = launch_mx_append(n, st);
   if (e != hipSuccess) return e;
   MxAttnParams p{};
   p.a = a;
+  p.rows = rows;
   p.rec = n.rec;
   p.q = s->q;
   return launch_attn_mx(p, g.batch, st);
@@ -1154,23 +1167,23 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
     a.len[b] = lens[b];
   }
   p.io = io;
-  a.q_type = io;
   const Tracer tr = s->tracer();
   tr.begin(KF_K_ATTN);
   hipError_t e = hipSuccess;
   if (kv->mx()) {
-    attn_split_mx(c.n_kv_heads, rows, lens, kv->max_split, s->n_cu, a);
+    attn_split_mx(c.n_kv_heads, rows, lens, kv->max_split, s->n_cu, a, p.rows);
     p.rec = ref.k;
     p.q = q_dev;
+    p.q_type = io;
     p.out = a.n_split == 1 ? out_dev : nullptr;
     e = launch_attn_mx(p, rows, s->stream);
   } else {
     attn_split_mfma(c.n_kv_heads, total_len, max_len > 0 ? max_len : 1, kv->max_split, s->n_cu, &a.split, &a.n_split);
-    for (int b = 0; b < rows; ++b) a.row_splits[b] = a.n_split;
+    for (int b = 0; b < rows; ++b) p.rows.n[b] = a.n_split;
     a.q = reinterpret_cast<const float*>(q_dev);
     a.kc = (uint16_t*)ref.k;
     a.vc = (uint16_t*)ref.v;
-    e = launch_attn_decode(a, rows, s->stream);
+    e = launch_attn_decode(a, rows, s->stream, io);
   }
   if (e == hipSuccess && !p.out) {
     p.out = out_dev;
@@ -1249,14 +1262,16 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     g.rope_cos = kv->rcos;
     g.rope_sin = kv->rsin;
     g.kraw = s->kraw;  // set for qk_norm blocks: q and k are normalised and rotated below
-    if (kv->mx()) {
-      g.k32 = kv->append;
-      g.v32 = kv->append + (int64_t)kMaxBatch * c.n_kv_heads * hd;
-    }
     g.err_flag = s->err_flag;
     for (int b = 0; b < kMaxBatch; ++b) {
       g.users[b] = b < batch ? users[b] : 0;
       g.pos[b] = b < batch ? positions[b] : 0;
+    }
+    if (kv->mx()) {  // kept in fp16 for attn_mx, which stores them
+      g.kv = kv->append_pages();
+      g.kc = kv->append;
+      g.vc = kv->append + kMaxBatch * g.kv.page_stride;
+      for (int b = 0; b < batch; ++b) g.users[b] = b;
     }
     hipError_t le;
     tr.begin(KF_K_QKV);
@@ -1295,7 +1310,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     a.hd = hd;
     a.split = split;
     a.n_split = n_split;
-    for (int b = 0; b < batch; ++b) a.row_splits[b] = n_split;
+    RowSplits rows{};  // MXFP4 caches
     a.max_split = kv->max_split;
     a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)hd));
     a.err_flag = s->err_flag;
@@ -1303,10 +1318,10 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
       a.users[b] = b < batch ? users[b] : 0;
       a.len[b] = b < batch ? positions[b] + 1 : 0;
     }
-    if (kv->mx()) attn_split_mx(c.n_kv_heads, batch, a.len, kv->max_split, s->n_cu, a);
+    if (kv->mx()) attn_split_mx(c.n_kv_heads, batch, a.len, kv->max_split, s->n_cu, a, rows);
     {
       tr.begin(KF_K_ATTN);
-      const hipError_t le = kv->mx() ? attn_mx(s, kv, L, a, g, l, st) : launch_attn_decode(a, batch, st);
+      const hipError_t le = kv->mx() ? attn_mx(s, kv, L, a, g, rows, users, l, st) : launch_attn_decode(a, batch, st);
       tr.end(KF_K_ATTN);
       KF_HIP(le, "attention launch");
     }
@@ -1325,8 +1340,8 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
       // rows in fp32 would crowd the vector cache the weights stream through);
       // at batch 1 the merged output and the residual stay fp32.
       tr.begin(KF_K_OPROJ);
-      hipError_t le = batch > 1 ? launch_attn_merge(a, s->o16, nullptr, batch, st)
-                                : launch_attn_merge(a, nullptr, s->o32, batch, st);
+      hipError_t le = batch > 1 ? launch_attn_merge(a, kv->mx() ? &rows : nullptr, s->o16, nullptr, batch, st)
+                                : launch_attn_merge(a, kv->mx() ? &rows : nullptr, nullptr, s->o32, batch, st);
       if (le == hipSuccess) {
         GemvParams op{};
         op.batch = batch;
