@@ -40,6 +40,11 @@ __device__ __forceinline__ u64 key_of(float z, int index) {
   return z == -INFINITY ? 0 : (u64)order_of(z) << 32 | (uint32_t)~index;
 }
 __device__ __forceinline__ float value_of(u64 key) { return value_of_order((uint32_t)(key >> 32)); }
+// (fmaxf would quieten each operand first; NaN are looked for apart)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(a), "v"(b), "v"(c));
+  return a;
+}
 // Over the wave, result in every lane: quad permutes and row mirrors within 16 lanes, then the 16-lane groups.
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t v) {
@@ -151,7 +156,7 @@ __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p
 #pragma unroll
   for (int i = 0; i < VPT; i += 2) {
     bad |= __builtin_isunordered(v[i], v[i + 1]);
-    mine = fmaxf(mine, fmaxf(v[i], v[i + 1]));
+    mine = max3(mine, v[i], v[i + 1]);
   }
   bad |= mine == INFINITY;
   if (bad) {  // NaN or +inf: skipped, and reported
@@ -221,9 +226,12 @@ __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p
       for (int r = 0; r < p.top; ++r) {
         u64 next = 0;
         if (r == 0 || k0 == best[r - 1]) {  // the lane whose key was taken, and at first every lane
-#pragma unroll
+          // (read again: from the registers the loop would be unrolled, at the cost of a wave per SIMD)
           for (int i = 0; i < VPT; ++i) {
-            const u64 k = key_of(v[i], c0 + 4 * (kT * (i / 4) + tid) + i % 4);
+            const int at = c0 + 4 * (kT * (i / 4) + tid) + i % 4;
+            float x = at < p.vocab ? z[at] : -INFINITY;
+            if (p.row_scale && at < p.vocab) x *= p.row_scale[row];
+            const u64 k = key_of(x < INFINITY ? x : -INFINITY, at);
             next = k < k0 && k > next ? k : next;
           }
           k0 = next;
