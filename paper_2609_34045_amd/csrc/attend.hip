@@ -1,6 +1,6 @@
-// Attention over an MXFP4 cache for one query row of each of up to four users, the
-// append of a decode step's keys and values to such a cache, and the call that
-// attends with given queries (kf_kv_attend) over caches of both types.
+// Attention over an MXFP4 cache for one query row of each of up to four users: with
+// given queries (kf_kv_attend), and in a decode step, whose new keys and values it
+// appends; and the merge of kf_kv_attend's splits, of caches of both types.
 //
 //   out_h = sum_t p_t v_t / sum_t p_t,  p_t = 2^(s_t - m),  s_t = q_h . k_t log2(e) / sqrt(hd)
 //
@@ -21,6 +21,7 @@
 // two at a time, the two halves of the columns holding the two parts of a
 // probability.  The score tile's lane layout is the P^T operand's.
 #include <cmath>
+#include <type_traits>
 
 #include "kernels.h"
 
@@ -95,10 +96,91 @@ struct MxPage {
   uint32_t ks;
   v4u vs[HD / 16];
 };
+
+// x[s][j] of d = grp hd/4 + 8 s + j, normalised (gains `gain`) and rotated to position pos; the RoPE partner
+// d +- hd/2 lies in the lane 32 apart.
+template <int HD>
+__device__ __forceinline__ void norm_rope(const MxStepParams& p, float (&x)[HD / 32][8], int grp, int pos) {
+  float ss = 0.f;
+#pragma unroll
+  for (int s = 0; s < HD / 32; ++s)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss += x[s][j] * x[s][j];
+  const float rs = 1.0f / sqrtf(groups_sum(ss) / (float)HD + p.eps);
+  const float sign = grp < 2 ? -1.0f : 1.0f;
+#pragma unroll
+  for (int s = 0; s < HD / 32; ++s) {
+    const int d0 = grp * (HD / 4) + 8 * s;
+    float gain[8], c[8], sn[8];
+    load_q8(p.gq, 1, d0, gain);
+    load_q8(p.rope_cos, 0, (int64_t)pos * (HD / 2) + d0 % (HD / 2), c);
+    load_q8(p.rope_sin, 0, (int64_t)pos * (HD / 2) + d0 % (HD / 2), sn);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float a = x[s][j] * (rs * gain[j]);
+      x[s][j] = a * c[j] + sign * __shfl_xor(a, 32) * sn[j];
+    }
+  }
+}
+
+// Row b's new key or value of KV head g to its position of the cache, by lanes 0 .. hd/8 - 1 of a wave, 8 values each.
+template <int HD>
+__device__ __forceinline__ void append(const MxStepParams& p, int b, int g, bool is_v, int lane) {
+  constexpr int PER = HD / 8;
+  if (lane >= PER) return;
+  const int pos = p.a.len[b] - 1, t = pos % kKvPage, d0 = 8 * lane, blk = d0 / kMxBlock;
+  uint8_t* rec = p.cache + (int64_t)kv_page(p.a.kv, p.a.users[b], pos / kKvPage) * p.a.kv.page_stride + (int64_t)g * mx_record(HD) +
+                 (is_v ? mx_v(HD) : 0);
+  uint8_t old[8];
+  if (is_v) {  // the other nibble of each byte is a neighbouring position's
+#pragma unroll
+    for (int j = 0; j < 8; ++j) old[j] = rec[mx_v_byte(t, d0 + j)];
+  }
+  float x[8];
+  if (!is_v && p.gk) {  // raw: its norm and RoPE are due
+    load_q8(p.kraw, 0, ((int64_t)b * p.a.nkv + g) * HD + d0, x);
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss += x[j] * x[j];
+    for (int o = 1; o < PER; o <<= 1) ss += __shfl_xor(ss, o);
+    const float rs = 1.0f / sqrtf(ss / (float)HD + p.eps);
+    float gain[8], c[8], sn[8];
+    load_q8(p.gk, 1, d0, gain);
+    load_q8(p.rope_cos, 0, (int64_t)pos * (HD / 2) + d0 % (HD / 2), c);
+    load_q8(p.rope_sin, 0, (int64_t)pos * (HD / 2) + d0 % (HD / 2), sn);
+    const float sign = d0 < HD / 2 ? -1.f : 1.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float a = x[j] * (rs * gain[j]);
+      x[j] = a * c[j] + sign * __shfl_xor(a, PER / 2) * sn[j];
+    }
+  } else {
+    load_q8(is_v ? p.v16 : p.k16, 2, (((int64_t)b * p.a.nkv + g) * kKvPage + t) * HD + d0, x);
+  }
+  uint32_t pairs[4] = {f16_pair(x[0], x[1]), f16_pair(x[2], x[3]), f16_pair(x[4], x[5]), f16_pair(x[6], x[7])};
+  bool bad = false;
+  int e;
+  const uint32_t w = mx_encode8(pairs, e, bad);
+  raise_err(p.a.err_flag, bad, kErrF16Range);
+  if (!is_v) {
+    *reinterpret_cast<uint32_t*>(rec + mx_k_byte<HD>(t, d0)) = w;
+    if (lane % 4 == 0) rec[mx_codes(HD) + mx_k_exp(t, blk)] = (uint8_t)(e + 127);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t c = (w >> (4 * j)) & 15u;
+    rec[mx_v_byte(t, d0 + j)] = (uint8_t)(t & 1 ? (old[j] & 0x0f) | (c << 4) : (old[j] & 0xf0) | c);
+  }
+  if (lane % 4 == 0) reinterpret_cast<uint16_t*>(rec + mx_codes(HD))[mx_v_exp<HD>(t, blk)] = mx_v_scale(e);
+}
 }  // namespace
 
-template <int HD>
-__global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const MxAttnParams p) {
+// P is MxAttnParams, or MxStepParams for a decode step: the workgroup whose split ends in the row's new position
+// stores its key and value first (a launch of its own for that cost 5 us a layer).
+template <int HD, class P>
+__global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const P p) {
+  constexpr bool STEP = std::is_same<P, MxStepParams>::value;
   constexpr int NS = HD / 32, NT = HD / 16, NB = HD / kMxBlock;
   constexpr int CODES = mx_codes(HD), REC = mx_record(HD), V = mx_v(HD);
   constexpr int SROW = HD + 4;  // a head's row of a wave's state in LDS
@@ -131,6 +213,16 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const MxAttnPar
   if (pages <= 0) {  // a row without positions
     for (int e = tid; e < G * HD; e += 64 * kWaves) put(e / HD, e % HD, 0.f, -INFINITY, 0.f);
     return;
+  }
+
+  if constexpr (STEP) {
+    if (page0 + pages == (len + kKvPage - 1) / kKvPage) {
+      if (wave < 2) append<HD>(p, b, g, wave == 1, lane);
+      // one workgroup reads the page, and its loads follow: the waves' stores are waited for, and no other CU has its lines
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    }
   }
 
   // Lane i holds the id of the split's page i.
@@ -166,6 +258,9 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const MxAttnPar
 #pragma unroll
     for (int s = 0; s < NS; ++s)
       load_q8(p.q, p.q_type, ((int64_t)b * p.a.nq + hq0 + min(head, G - 1)) * HD + grp * (HD / 4) + 8 * s, f[s]);
+    if constexpr (STEP) {
+      if (p.gq) norm_rope<HD>(p, f, grp, len - 1);
+    }
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -348,81 +443,9 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(const MxAttnParams p)
   }
 }
 
-// The new key and value of each row of a decode step, to its position of an MXFP4
-// cache.  hd / 8 lanes hold a head, 8 values each.  In blocks with per-head norms
-// the keys come raw and are normalised and rotated here, and so are the queries, in
-// place.
-__global__ __launch_bounds__(256) void mx_append_kernel(const MxAppendParams p) {
-  const int hd = p.hd, per = hd / 8, i = blockIdx.x * 256 + threadIdx.x;
-  const int item = i / per, d0 = (i % per) * 8;
-  const int nq = p.gq ? p.nq : 0, heads = nq + 2 * p.nkv;  // queries, keys, values
-  const int b = item / heads, h = item % heads;
-  if (b >= p.batch) return;  // whole heads: a head's lanes leave together
-  const int g = h < nq ? 0 : (h - nq) % p.nkv;
-  const bool is_v = h >= nq + p.nkv;
-  const int t = p.pos[b] % kKvPage;
-  float x[8];
-  if (h < nq) {
-    load_q8(p.q, 0, ((int64_t)b * p.nq + h) * hd + d0, x);
-  } else if (p.gq && !is_v) {
-    load_q8(p.kraw, 0, ((int64_t)b * p.nkv + g) * hd + d0, x);
-  } else {
-    load_q8(is_v ? p.v16 : p.k16, 2, (((int64_t)b * p.nkv + g) * kKvPage + t) * hd + d0, x);
-  }
-  if (p.gq && !is_v) {
-    float ss = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) ss += x[j] * x[j];
-    for (int o = 1; o < per; o <<= 1) ss += __shfl_xor(ss, o);
-    const float rs = 1.0f / sqrtf(ss / (float)hd + p.eps);
-    float gain[8];
-    load_q8(h < nq ? p.gq : p.gk, 1, d0, gain);
-    const int i0 = d0 % (hd / 2);
-    const float sign = d0 < hd / 2 ? -1.f : 1.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] *= rs * gain[j];
-    float y[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float other = __shfl_xor(x[j], per / 2);
-      const int64_t at = (int64_t)p.pos[b] * (hd / 2) + i0 + j;
-      y[j] = x[j] * p.rope_cos[at] + sign * other * p.rope_sin[at];
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = y[j];
-    if (h < nq) {
-      v4f* q = reinterpret_cast<v4f*>(p.q + ((int64_t)b * p.nq + h) * hd + d0);
-      q[0] = v4f{x[0], x[1], x[2], x[3]};
-      q[1] = v4f{x[4], x[5], x[6], x[7]};
-      return;
-    }
-  }
-  bool bad = false;
-  int e;
-  uint32_t pairs[4] = {f16_pair(x[0], x[1]), f16_pair(x[2], x[3]), f16_pair(x[4], x[5]), f16_pair(x[6], x[7])};
-  const uint32_t w = mx_encode8(pairs, e, bad);
-  raise_err(p.err_flag, bad, kErrF16Range);
-  const int codes = mx_codes(hd);
-  uint8_t* rec = p.rec + (int64_t)kv_page(p.kv, p.users[b], p.pos[b] / kKvPage) * p.kv.page_stride +
-                 (int64_t)g * mx_record(hd) + (is_v ? mx_v(hd) : 0);
-  const int blk = d0 / kMxBlock;
-  if (!is_v) {
-    *reinterpret_cast<uint32_t*>(rec + (hd == 128 ? mx_k_byte<128>(t, d0) : mx_k_byte<64>(t, d0))) = w;
-    if (d0 % kMxBlock == 0) rec[codes + mx_k_exp(t, blk)] = (uint8_t)(e + 127);
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {  // the other nibble of each byte is a neighbouring position's
-    uint8_t* at = rec + mx_v_byte(t, d0 + j);
-    const uint32_t c = (w >> (4 * j)) & 15u;
-    *at = (uint8_t)(t & 1 ? (*at & 0x0f) | (c << 4) : (*at & 0xf0) | c);
-  }
-  if (d0 % kMxBlock == 0)
-    reinterpret_cast<uint16_t*>(rec + codes)[hd == 128 ? mx_v_exp<128>(t, blk) : mx_v_exp<64>(t, blk)] = mx_v_scale(e);
-}
-
 // ------------------------------------------------------------------ launchers
-hipError_t launch_attn_mx(const MxAttnParams& p, int batch, hipStream_t s) {
+template <class P>
+static hipError_t attn_mx(const P& p, int batch, hipStream_t s) {
   if (p.a.nq % p.a.nkv || p.a.nq / p.a.nkv > 8 || p.a.split % kKvPage || p.a.split > kMxMaxSplit) return hipErrorInvalidValue;
   int splits = 0;
   for (int b = 0; b < batch; ++b) {
@@ -430,23 +453,19 @@ hipError_t launch_attn_mx(const MxAttnParams& p, int batch, hipStream_t s) {
     splits += p.rows.n[b];
   }
   const dim3 grid(splits, p.a.nkv);
-  if (p.a.hd == 128) hipLaunchKernelGGL(attn_mx_kernel<128>, grid, dim3(64 * kWaves), 0, s, p);
-  else if (p.a.hd == 64) hipLaunchKernelGGL(attn_mx_kernel<64>, grid, dim3(64 * kWaves), 0, s, p);
+  if (p.a.hd == 128) hipLaunchKernelGGL((attn_mx_kernel<128, P>), grid, dim3(64 * kWaves), 0, s, p);
+  else if (p.a.hd == 64) hipLaunchKernelGGL((attn_mx_kernel<64, P>), grid, dim3(64 * kWaves), 0, s, p);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
+hipError_t launch_attn_mx(const MxAttnParams& p, int batch, hipStream_t s) { return attn_mx(p, batch, s); }
+hipError_t launch_attn_mx_step(const MxStepParams& p, int batch, hipStream_t s) { return attn_mx(p, batch, s); }
 
 hipError_t launch_attend_merge(const MxAttnParams& p, int batch, hipStream_t s) {
   const dim3 grid(p.a.nq, batch);
   if (p.a.hd == 128) hipLaunchKernelGGL(attend_merge_kernel<128>, grid, dim3(256), 0, s, p);
   else if (p.a.hd == 64) hipLaunchKernelGGL(attend_merge_kernel<64>, grid, dim3(256), 0, s, p);
   else return hipErrorInvalidValue;
-  return hipGetLastError();
-}
-
-hipError_t launch_mx_append(const MxAppendParams& p, hipStream_t s) {
-  const int lanes = p.batch * ((p.gq ? p.nq : 0) + 2 * p.nkv) * (p.hd / 8);
-  hipLaunchKernelGGL(mx_append_kernel, dim3((lanes + 255) / 256), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

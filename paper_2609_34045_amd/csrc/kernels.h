@@ -269,28 +269,22 @@ struct MxAttnParams {
   void* out;           // [B][nq][hd] of type io, or NULL
   int io;
 };
-// A decode step's new keys and values into an MXFP4 cache.
-struct MxAppendParams {
-  uint8_t* rec;  // layer base
-  KvPages kv;
-  float* q;      // [B][nq][hd]: normalised and rotated in place when gq is set
+// The same in a decode step, which appends each row's new key and value at its last position (a.len - 1).
+struct MxStepParams : MxAttnParams {  // q: fp32; normalised and rotated here when gq is set
+  uint8_t* cache;  // = rec
   // row b's key (rotated) and value, as the QKV launch left them: fp16 page b, at the position's slot
   const uint16_t *k16, *v16;
-  const float* kraw;  // [B][nkv][hd]: the raw keys instead, when gq is set
+  const float* kraw;        // [B][nkv][hd]: the raw keys instead, when gk is set
   const uint16_t *gq, *gk;  // per-head norm gains [hd] bf16, or NULL
   const float *rope_cos, *rope_sin;
   float eps;
-  int nq, nkv, hd, batch;
-  int users[kMaxBatch];
-  int pos[kMaxBatch];
-  int* err_flag;
 };
 
 // Launchers (return hipGetLastError() of the launch).
 hipError_t launch_attn_mx(const MxAttnParams& p, int batch, hipStream_t s);
 // p.out from the partials of either cache type's attention.
 hipError_t launch_attend_merge(const MxAttnParams& p, int batch, hipStream_t s);
-hipError_t launch_mx_append(const MxAppendParams& p, hipStream_t s);
+hipError_t launch_attn_mx_step(const MxStepParams& p, int batch, hipStream_t s);
 int gemv_grid(int epi, int rows_per_wg, const GemvParams& p);
 hipError_t launch_gemv(int epi, int rows_per_wg, int chunks_in_flight, bool norm, const GemvParams& p, hipStream_t s);
 // The same launch with the stage input (p.src or p.tokens) as its input rows.

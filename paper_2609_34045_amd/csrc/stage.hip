@@ -1094,39 +1094,22 @@ static void attn_split_mx(int nkv, int rows, const int* lens, int max_split, int
 }
 
 // A decode step's attention over an MXFP4 cache, for which the QKV launch g left the new keys and
-// values in kv->append (and raw keys of qk_norm blocks in s->kraw).
-static hipError_t attn_mx(kf_stage* s, kf_kv* kv, const LayerW& L, const AttnParams& a, const GemvParams& g,
-                          const RowSplits& rows, const int32_t* users, int layer, hipStream_t st) {
-  const kf_model_config& c = s->cfg;
-  MxAppendParams n{};
-  n.rec = kv->layer_ref(layer).k;
-  n.kv = a.kv;
-  n.q = s->q;
-  n.k16 = g.kc;
-  n.v16 = g.vc;
-  n.kraw = s->kraw;
-  n.gq = L.g_qn;
-  n.gk = L.g_kn;
-  n.rope_cos = kv->rcos;
-  n.rope_sin = kv->rsin;
-  n.eps = c.rms_eps;
-  n.nq = c.n_q_heads;
-  n.nkv = c.n_kv_heads;
-  n.hd = c.head_dim;
-  n.batch = g.batch;
-  n.err_flag = s->err_flag;
-  for (int b = 0; b < g.batch; ++b) {
-    n.users[b] = users[b];
-    n.pos[b] = g.pos[b];
-  }
-  const hipError_t e = launch_mx_append(n, st);
-  if (e != hipSuccess) return e;
-  MxAttnParams p{};
+// values in kv->append (and raw queries and keys of qk_norm blocks in s->q and s->kraw).
+static hipError_t attn_mx(kf_stage* s, kf_kv* kv, const AttnParams& a, const RowSplits& rows, const GemvParams& g, int layer) {
+  MxStepParams p{};
   p.a = a;
   p.rows = rows;
-  p.rec = n.rec;
+  p.rec = p.cache = kv->layer_ref(layer).k;
   p.q = s->q;
-  return launch_attn_mx(p, g.batch, st);
+  p.k16 = g.kc;
+  p.v16 = g.vc;
+  p.kraw = s->kraw;
+  p.gq = a.gq;
+  p.gk = a.gk;
+  p.rope_cos = kv->rcos;
+  p.rope_sin = kv->rsin;
+  p.eps = s->cfg.rms_eps;
+  return launch_attn_mx_step(p, g.batch, s->stream);
 }
 
 kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* users, const int32_t* lens,
@@ -1321,7 +1304,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     if (kv->mx()) attn_split_mx(c.n_kv_heads, batch, a.len, kv->max_split, s->n_cu, a, rows);
     {
       tr.begin(KF_K_ATTN);
-      const hipError_t le = kv->mx() ? attn_mx(s, kv, L, a, g, rows, users, l, st) : launch_attn_decode(a, batch, st);
+      const hipError_t le = kv->mx() ? attn_mx(s, kv, a, rows, g, l) : launch_attn_decode(a, batch, st);
       tr.end(KF_K_ATTN);
       KF_HIP(le, "attention launch");
     }
