@@ -79,10 +79,12 @@ __device__ __forceinline__ void store_out(void* out, int type, int64_t at, float
 constexpr int kWaves = 4;
 constexpr int kMostPages = kMxMaxSplit / kKvPage;
 static_assert(kMostPages <= 64, "a lane holds the id of one page of the split");
-// Probabilities are taken relative to 2^-kShift of a maximum that moves only when a page's exceeds it by
-// kLazyMax (log2 units): the largest lies in [2^kShift, 2^(kShift + kLazyMax)], where its two fp16 parts hold
-// 22 bits and those of small ones the bits above 2^-(25 + kShift) of it, and O is rarely rescaled.
-constexpr float kShift = 4.0f, kLazyMax = 8.0f;
+// Probabilities are taken relative to a maximum that moves only when a page's exceeds it by kLazyMax (log2
+// units), so that O is rarely rescaled, and times 2^kShift: the largest lies in [2^12, 2^14], within fp16, and two
+// fp16 parts, whose finest step is 2^-24, hold every one above 2^-14 of it to 22 bits (one of a long flat tail beside a
+// peak too: without the shift those below 2^-14 would keep 10).  The shift is added after the subtraction, which
+// is exact near the maximum however large the scores are.
+constexpr float kShift = 12.0f, kLazyMax = 2.0f;
 
 // The parts of a pair: the rounded values in lanes of keep 0, what rounding left in lanes of keep 1.
 __device__ __forceinline__ uint32_t part2(float a, float b, float keep) {
@@ -316,15 +318,15 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const P p) {
     float mb = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 4; ++t) mb = fmaxf(mb, fmaxf(fmaxf(sc[t][0], sc[t][1]), fmaxf(sc[t][2], sc[t][3])));
-    mb = groups_max(mb) * unscale - kShift;
+    mb = groups_max(mb) * unscale;
     const float m_new = mb > m_run + kLazyMax ? mb : m_run;
     const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);  // 0 while m_run is -inf
     float ls = 0.f;
     uint32_t pw[8];  // pair k: positions 16 (k / 2) + 4 grp + 2 (k % 2), and the next
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][2 * (k % 2)], unscale, -m_new));
-      const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][2 * (k % 2) + 1], unscale, -m_new));
+      const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][2 * (k % 2)], unscale, -m_new) + kShift);
+      const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][2 * (k % 2) + 1], unscale, -m_new) + kShift);
       ls += x + y;
       pw[k] = part2(x, y, keep);
     }

@@ -117,7 +117,7 @@ def test_long_rows_and_repeated_users(torch, st):
     g.close()
 
 
-@pytest.mark.parametrize("scale_q,scale_k", [(1e-6, 1.0), (1e4, 1e-4), (1.0, 200.0), (3e-30, 1e3)])
+@pytest.mark.parametrize("scale_q,scale_k", [(1e-6, 1.0), (1e4, 1e-4), (1.0, 200.0), (3e-30, 1e3), (1e5, 1e4)])
 def test_queries_and_keys_of_any_size(torch, st, scale_q, scale_k):
     """Tiny and large queries keep their bits, a sharply peaked row finds its key, and values near both ends of the
     format come out in proportion."""
@@ -135,6 +135,31 @@ def test_queries_and_keys_of_any_size(torch, st, scale_q, scale_k):
         err = np.abs(got[:, part] - w[:, part])
         assert np.all(err <= allowed(q[0], k, v[:, :, part], w[:, part], "mxfp4", EPS["float32"]))
     g.sync()
+    kv.close()
+    g.close()
+
+
+def test_a_peak_beside_a_long_flat_tail(torch, st):
+    """One key of probability near a half and 8000 that share the rest, each far below it: they count to the last bit."""
+    hd, n = 64, 8001
+    g = bare_stage(st, 1, hd, group=1)
+    kv = g.kv(1, n, dtype="mxfp4")
+    k = np.zeros((n, 1, hd), np.float32)
+    k[:, 0, 0] = 1.0
+    k[4000, 0, 0] = 6.0
+    v = rows(2, n, 1, hd)
+    v[4000] = 0
+    kv.write(0, 0, 0, on(k), on(v))
+    q = np.zeros((1, 1, hd), np.float32)
+    q[0, 0, 0] = math.log(8000) / 5 * math.sqrt(hd)
+    v = held(v, "mxfp4")
+    got = kv.attend(0, [0], [n], on(q))[0, 0].cpu().numpy()
+    w = want_of(q[0], held(k, "mxfp4"), v)[0]
+    # The tail's keys have one score and so one error: ln 8000 2^-22 of the query's parts, 13 2^-24 of the exponential's
+    # argument, 2^-23 of itself, 2^-22 of its parts, together below 2^-18 of the tail's sum; the fp32 sums of at most 64
+    # steps in a row, each off by 2^-24 of partial sums of the size of `tail`, stay below 2^-18 of that.
+    tail = np.sqrt((np.delete(v[:, 0], 4000, 0) ** 2).sum(0)) / 16000
+    assert np.all(np.abs(got - w) <= 2.0 ** -17 * (np.abs(w) + tail))
     kv.close()
     g.close()
 
@@ -341,3 +366,47 @@ def test_forked_users_decode_together(torch, st, cache):
     shared.close()
     apart.close()
     g.close()
+
+
+def test_a_ring_counts_copies_of_shared_pages(torch, st):
+    """A ring's members admit a call only if their pools hold the copies that shared pages need, and forked users on
+    4-bit caches then generate what users with prompts of their own do."""
+    from paper_2609_34045_amd.ring import Ring
+    shape = synth.SHAPE_TINY
+    model = SeededModel(shape, 64)
+    stages = [st.Stage(shape, 0, 1, model.layer, model.head()), st.Stage(shape, 1, 2, model.layer)]
+    prompt = on(synth.tokens(64, 0, 70, shape.vocab))
+
+    def ring_of(pages):
+        caches = [s.kv(3, 192, pages, dtype="mxfp4") for s in stages]
+        return caches, Ring(stages, caches, 2, 128)
+
+    caches, ring = ring_of(4)
+    first = ring.prefill(0, prompt)
+    for kv in caches:
+        kv.fork(0, 1)
+        kv.fork(0, 2)
+    assert caches[0].pages() == (4, 2)
+    last = first.repeat(3)
+    caches[1].write(1, 2, 128, *(torch.zeros(1, 2, 64, device="cuda") for _ in range(2)))  # takes a page: one left in member 1
+    before = [(kv.pages(), [kv.len(u) for u in range(3)]) for kv in caches]
+    with pytest.raises(st.KFError) as e:
+        ring.generate([[0, 1, 2]], last, 2)
+    assert e.value.status == 2 and "member 1" in e.value.message
+    assert before == [(kv.pages(), [kv.len(u) for u in range(3)]) for kv in caches]
+    caches[1].set_len(2, 70)
+    got = ring.generate([[0, 1, 2]], last, 3).cpu().numpy()
+    assert caches[0].pages() == (4, 0)
+    ring.close()
+    for kv in caches:
+        kv.close()
+    caches, ring = ring_of(9)
+    for u in range(3):
+        assert torch.equal(ring.prefill(u, prompt), first)
+    assert np.array_equal(ring.generate([[0, 1, 2]], last, 3).cpu().numpy(), got)
+    ring.close()
+    for kv in caches:
+        kv.close()
+    for s in stages:
+        s.sync()
+        s.close()

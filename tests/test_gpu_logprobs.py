@@ -90,6 +90,13 @@ def test_rows_of_every_length(torch, g, top, rows, vocab, pad):
     g.sync()
 
 
+def test_more_rows_than_one_launch_takes(torch, g):
+    z = (np.random.default_rng(3).normal(size=(32770, 33)) * 3).astype(np.float32)
+    t = np.arange(32770).astype(np.int32) % 33
+    check(g.logits_logprobs(torch.from_numpy(z).cuda(), torch.from_numpy(t).cuda(), top=2), z, t, 2)
+    g.sync()
+
+
 @pytest.mark.parametrize("vocab", [100, 5000, 70001])
 def test_masks_ties_and_extremes(torch, st, g, vocab):
     """Rows with nothing left, one value left, the type's lowest value, equal values everywhere or at the border of the
