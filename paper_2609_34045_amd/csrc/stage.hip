@@ -8,6 +8,7 @@
 #include <cstdio>
 #include <cstring>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -732,8 +733,30 @@ kf_status kf_stage_get_flags(const kf_stage* s, int32_t* flags) {
 
 // ------------------------------------------------------------------ KV cache
 // n_pages == 0: a reserved cache (every user's pages in user order); else a pool of n_pages.
+// A cache being made: freed with what it has, unless it is whole.
+constexpr int kKvMem = 11;
+struct KvInMaking {
+  kf_kv* kv = nullptr;
+  char* mem[kKvMem] = {};
+  ~KvInMaking() {
+    if (!kv) return;
+    for (char* m : mem)
+      if (m) hipFree(m);
+    delete kv;
+  }
+};
+static kf_status kv_make(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_t n_pages, kf_kv_type type,
+                         kf_kv** out);
 static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_t n_pages, kf_kv_type type,
                            kf_kv** out) {
+  try {
+    return kv_make(s, max_users, max_ctx, n_pages, type, out);
+  } catch (const std::bad_alloc&) {  // of the host tables
+    return fail(KF_ENOMEM, "host allocation");
+  }
+}
+static kf_status kv_make(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_t n_pages, kf_kv_type type,
+                         kf_kv** out) {
   if (!out) return fail(KF_EINVAL, "out is NULL");
   *out = nullptr;
   if (!s) return fail(KF_EINVAL, "stage is NULL");
@@ -744,8 +767,9 @@ static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int3
   const int ppu = pages_for(max_ctx);
   if ((int64_t)max_users * ppu > (1LL << 30)) return fail(KF_ERANGE, "max_users x max_ctx too large");
   const bool paged = n_pages > 0;
-  kf_kv* kv = new (std::nothrow) kf_kv();
-  if (!kv) return fail(KF_ENOMEM, "host allocation");
+  KvInMaking made;
+  kf_kv* kv = made.kv = new kf_kv();
+  char** mem = made.mem;
   kv->st = s;
   kv->max_users = max_users;
   kv->max_ctx = max_ctx;
@@ -772,17 +796,13 @@ static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int3
   const int64_t app = kv->mx() ? 2LL * kMaxBatch * c.n_kv_heads * kKvPage * c.head_dim * 2 : 0;
   const int64_t app_tab = kv->mx() ? (int64_t)kMaxBatch * ppu * 4 : 0;
   const int64_t f16 = kv->mx() ? (int64_t)ppu * kKvPage * c.n_kv_heads * c.head_dim * 2 : 0;
-  constexpr int kMem = 11;
-  char* mem[kMem] = {nullptr};
-  const int64_t sz[kMem] = {cache, kv->mx() ? 0 : cache, rope, rope, pacc, pml, tab, app, f16, f16, app_tab};
-  for (int i = 0; i < kMem; ++i) {
+  const int64_t sz[kKvMem] = {cache, kv->mx() ? 0 : cache, rope, rope, pacc, pml, tab, app, f16, f16, app_tab};
+  for (int i = 0; i < kKvMem; ++i) {
     if (sz[i] == 0) continue;
     kv->bytes += sz[i];
     if (hipMalloc((void**)&mem[i], sz[i]) != hipSuccess) {
       hipGetLastError();
-      for (int j = 0; j < i; ++j)
-        if (mem[j]) hipFree(mem[j]);
-      delete kv;
+      mem[i] = nullptr;
       return fail(KF_ENOMEM, "device allocation of %lld KV bytes", (long long)sz[i]);
     }
   }
@@ -819,12 +839,8 @@ static kf_status kv_create(kf_stage* s, int32_t max_users, int32_t max_ctx, int3
   if (e == hipSuccess && kv->table) e = hipMemset(kv->table, 0, tab);
   if (e == hipSuccess) e = hipMemcpy(kv->rcos, tc.data(), rope, hipMemcpyHostToDevice);
   if (e == hipSuccess) e = hipMemcpy(kv->rsin, ts.data(), rope, hipMemcpyHostToDevice);
-  if (e != hipSuccess) {
-    for (char* m : mem)
-      if (m) hipFree(m);
-    delete kv;
-    return fail(KF_EDEVICE, "KV init: %s", hipGetErrorString(e));
-  }
+  if (e != hipSuccess) return fail(KF_EDEVICE, "KV init: %s", hipGetErrorString(e));
+  made.kv = nullptr;
   s->live_kv++;
   *out = kv;
   return KF_OK;
