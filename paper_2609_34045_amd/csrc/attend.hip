@@ -251,8 +251,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const P p) {
 
   // The query operand, step s: d = grp hd/4 + 8 s .. + 7 of this column's head (columns past G repeat the
   // last one, and are not read).  Asked for after the page, so that one wait covers both.
-  // In log2 units, times a power of two that puts the row's largest value near 2^10, so that the fp16
-  // parts neither overflow nor lose bits below the normal range.
+  // In log2 units, times a power of two that puts the head's largest value near 2^10, so that the fp16
+  // parts neither overflow, up to the largest fp32 number, nor lose bits below the normal range.
   h8 qf[NS];
   float unscale;
   {
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const P p) {
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int j = 0; j < 8; ++j) top = fmaxf(top, __builtin_fabsf(f[s][j]));
-    const int e = min(max((int)(__float_as_uint(groups_max(top)) >> 23) - 127, -90), 110);
+    const int e = min(max((int)(__float_as_uint(groups_max(top)) >> 23) - 127, -90), 127);
     unscale = __uint_as_float((uint32_t)(127 - 13 + e) << 23);
     const float scale = p.a.scale_log2 * __uint_as_float((uint32_t)(127 + 13 - e) << 23);
 #pragma unroll

@@ -139,6 +139,29 @@ def test_queries_and_keys_of_any_size(torch, st, scale_q, scale_k):
     g.close()
 
 
+@pytest.mark.parametrize("io", ["float32", "bfloat16"])
+@pytest.mark.parametrize("power", [110, 113, 117, 121])
+def test_queries_near_the_top_of_the_range(torch, st, io, power):
+    """Queries whose scores with small keys are finite find the key of the largest score: every other probability is
+    2^-(a huge number), so that the row is that key's value to the last bit."""
+    hd, n = 64, 300
+    g = bare_stage(st, 1, hd, group=8)
+    kv = g.kv(1, n, dtype="mxfp4")
+    k, v = rows(1, n, 1, hd, 1e-5), rows(2, n, 1, hd)
+    kv.write(0, 0, 0, on(k), on(v))
+    k, v = held(k, "mxfp4"), held(v, "mxfp4")
+    q = on(rows(3, 1, 8, hd) * np.float32(2.0 ** power), getattr(torch, io))
+    s = q[0].float().cpu().numpy().astype(np.float64) @ k[:, 0].T
+    order = np.sort(s, axis=1)
+    size = np.abs(q[0].float().cpu().numpy().astype(np.float64)) @ np.abs(k[:, 0]).T
+    assert np.all(order[:, -1] - order[:, -2] > 2.0 ** -16 * size.max(1))  # above what 22-bit queries and fp32 sums lose
+    got = kv.attend(0, [0], [n], q)[0].float().cpu().numpy()
+    assert np.array_equal(got, on(v[s.argmax(1), 0].astype(np.float32), getattr(torch, io)).float().cpu().numpy())
+    g.sync()
+    kv.close()
+    g.close()
+
+
 def test_a_peak_beside_a_long_flat_tail(torch, st):
     """One key of probability near a half and 8000 that share the rest, each far below it: they count to the last bit."""
     hd, n = 64, 8001
