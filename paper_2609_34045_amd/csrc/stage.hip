@@ -231,6 +231,14 @@ struct kf_kv {
 
 static int pages_for(int64_t len) { return (int)((len + kKvPage - 1) / kKvPage); }
 
+// Whether the stage's stream is being captured into a graph.
+static bool capturing(const kf_stage* s) {
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s->stream, &capture) == hipSuccess) return capture != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();
+  return true;
+}
+
 // The page of `user` that holds position `pos`, if other users hold it too; else -1.
 static int shared_page(const kf_kv* kv, int user, int64_t pos) {
   const int pg = (int)(pos / kKvPage);
@@ -264,13 +272,16 @@ int kv_append_copies(const kf_kv* kv, int n, const int* users) {
 static kf_status kv_grant(kf_kv* kv, int n, const int* users, const int64_t* from, const int64_t* upto) {
   if (!kv->table) return KF_OK;  // reserved cache: every page is held from the start
   int64_t want = 0;
+  int copies = n > 1 ? kv_append_copies(kv, n, users) : 0;
   for (int i = 0; i < n; ++i) {
     const int need = pages_for(upto[i]) - kv->held[users[i]];
     if (need > 0) want += need;
     if (n == 1)
-      for (int64_t p = from[i]; p < upto[i]; p = (p / kKvPage + 1) * kKvPage) want += shared_page(kv, users[i], p) >= 0;
+      for (int64_t p = from[i]; p < upto[i]; p = (p / kKvPage + 1) * kKvPage) copies += shared_page(kv, users[i], p) >= 0;
   }
-  if (n > 1) want += kv_append_copies(kv, n, users);
+  if (copies && capturing(kv->st))  // each replay would put the page's old contents back
+    return fail(KF_ESTATE, "pages that other users hold too cannot be copied under graph capture");
+  want += copies;
   if (want > (int64_t)kv->free_pages.size())
     return fail(KF_ENOMEM, "KV pool: %lld more pages needed, %zu free of %d", (long long)want, kv->free_pages.size(),
                 kv->n_pages);
@@ -1008,6 +1019,8 @@ kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n) {
     kv->len[dst_user] = n;
     return KF_OK;
   }
+  if (capturing(kv->st))  // each replay would take the destination's own pages out of its table again
+    return fail(KF_ESTATE, "users of a paged cache cannot be forked under graph capture");
   // The pages are shared; whoever writes to one first takes a copy (kv_grant).
   // Those that the destination shares already need no new entry.
   const int pages = pages_for(n);
@@ -1546,11 +1559,7 @@ static bool grow_kept(kf_stage* s, Grown& g, int64_t bytes) {
   if (bytes <= g.cap) return true;
   if (g.n == (int)(sizeof g.all / sizeof g.all[0])) return false;
   bytes = std::max(bytes, 2 * g.cap);
-  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(s->stream, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone) {
-    (void)hipGetLastError();
-    return false;
-  }
+  if (capturing(s)) return false;
   // Relaxed: the allocation leaves captures of other threads alone.
   hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
   (void)hipThreadExchangeStreamCaptureMode(&mode);

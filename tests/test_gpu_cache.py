@@ -280,6 +280,52 @@ def test_a_short_pool_refuses_a_write_to_a_shared_page(torch, st):
     g.close()
 
 
+@pytest.mark.parametrize("dtype", ["f16", "mxfp4"])
+def test_page_sharing_is_refused_under_capture(torch, st, dtype):
+    """A fork, and a write that would copy a shared page, change nothing while a graph is captured; a reserved cache's fork
+    is a copy, and replays."""
+    g = bare_stage(st, 2, 64, layers=2)
+    k, v = rows(1, 100, 2, 64), rows(2, 100, 2, 64)
+    paged, flat = g.kv(3, 256, 8, dtype=dtype), g.kv(2, 256, dtype=dtype)
+    one = [torch.from_numpy(rows(i, 1, 2, 64)).cuda() for i in (3, 4)]
+    kd, vd = torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda()
+    for kv in (paged, flat):
+        for layer in (0, 1):
+            kv.write(layer, 0, 0, kd, vd)
+        kv.set_len(0, 100)
+    paged.fork(0, 1, 90)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g.set_stream(side)
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            flat.fork(0, 1, 80)
+            with pytest.raises(st.KFError, match="capture"):
+                paged.fork(0, 2)
+            with pytest.raises(st.KFError, match="capture"):
+                paged.write(0, 1, 70, *one)
+            paged.write(0, 0, 130, *one)  # on a page of its own
+        assert paged.pages() == (8, 5) and paged.len(2) == 0 and paged.len(1) == 90
+        for _ in range(3):
+            graph.replay()
+            side.synchronize()
+            for layer in (0, 1):
+                check(flat, layer, 1, 0, held(k, dtype)[:80], held(v, dtype)[:80])
+            flat.write(0, 1, 0, vd, kd)  # put right by the next replay
+        paged.write(0, 1, 70, *one)
+        paged.fork(0, 2)
+        assert paged.pages() == (8, 4)
+        check(paged, 0, 0, 0, held(k, dtype), held(v, dtype))
+        check(paged, 0, 2, 64, held(k, dtype)[64:], held(v, dtype)[64:])
+        check(paged, 0, 1, 64, held(k, dtype)[64:70], held(v, dtype)[64:70])
+        check(paged, 0, 1, 70, held(one[0].cpu().numpy(), dtype), held(one[1].cpu().numpy(), dtype))
+    g.sync()
+    for kv in (paged, flat):
+        kv.close()
+    g.close()
+
+
 def test_format_and_bytes(torch, st):
     g = bare_stage(st, 2, 128, layers=3)
     a, b = g.kv(2, 1000), g.kv(2, 1000, dtype="mxfp4")
