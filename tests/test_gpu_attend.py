@@ -117,6 +117,47 @@ def test_long_rows_and_repeated_users(torch, st):
     g.close()
 
 
+def test_the_longest_cache(torch, st):
+    """1,048,576 positions of four users, a cache of more than 2^32 bytes: the last user's last and middle positions are
+    written, read, attended to, forked and copied into a cache of the other type."""
+    hd, nkv, group, n = 128, 8, 2, 1 << 20
+    g = bare_stage(st, nkv, hd, group=group)
+    kv, half = g.kv(4, n, dtype="mxfp4"), g.kv(1, n)
+    assert kv.format()[1] > 1 << 32
+    at = [(500_003, 70), (n - 130, 130)]
+    parts = [(rows(2 * i, m, nkv, hd), rows(2 * i + 1, m, nkv, hd, 1e3)) for i, (_, m) in enumerate(at)]
+    for (p, m), (k, v) in zip(at, parts):
+        kv.write(0, 3, p, on(k), on(v))
+    kv.set_len(3, n)
+    parts = [(held(k, "mxfp4"), held(v, "mxfp4")) for k, v in parts]
+    # the other positions' keys and values are zero: score 0 each, and nothing added
+    k, v = (np.concatenate([parts[0][i], parts[1][i], np.zeros((1, nkv, hd))]) for i in (0, 1))
+    count = np.r_[np.ones(200), n - 200]
+    q = rows(9, 1, nkv * group, hd, 2.0)
+    s = np.einsum("hd,lhd->hl", q[0].astype(np.float64), np.repeat(k, group, axis=1)) / math.sqrt(hd)
+    w = count * np.exp(s - s.max(1, keepdims=True))
+    want = np.einsum("hl,lhd->hd", w, np.repeat(v, group, axis=1)) / w.sum(1, keepdims=True)
+    # `allowed` of the part of the probability that these keys have, and the longer sums: 16 positions of up to 16 pages in a
+    # lane, up to 1024 splits by four waves, 400 additions more than it counts
+    part = (w[:, :-1].sum(1) / w.sum(1))[:, None]
+    tol = (allowed(q[0], k, v, want, "mxfp4", 0) + 2 * 400 * 2.0 ** -24 * np.abs(v).max()) * part + 2.0 ** -24 * np.abs(want).max()
+    assert tol.max() < 0.01 * np.abs(want).max()
+    kv.fork(3, 0)
+    half.copy(kv, 3, 0, 0, n)
+    for cache, user in ((kv, 3), (kv, 0), (half, 0)):
+        for (p, m), (pk, pv) in zip(at, parts):
+            for got, x in zip(cache.read(0, user, p - 1 if p + m < n else p, m + (p + m < n)), (pk, pv)):
+                got = got.cpu().numpy()
+                assert np.array_equal(got[-m:], x) and not got[:-m].any()
+    for user in (3, 0):
+        got = kv.attend(0, [user], [n], on(q))[0].cpu().numpy()
+        assert np.all(np.abs(got - want) <= tol), (np.abs(got - want) / tol).max()
+    g.sync()
+    kv.close()
+    half.close()
+    g.close()
+
+
 @pytest.mark.parametrize("scale_q,scale_k", [(1e-6, 1.0), (1e4, 1e-4), (1.0, 200.0), (3e-30, 1e3), (1e5, 1e4)])
 def test_queries_and_keys_of_any_size(torch, st, scale_q, scale_k):
     """Tiny and large queries keep their bits, a sharply peaked row finds its key, and values near both ends of the

@@ -90,6 +90,17 @@ def test_rows_of_every_length(torch, g, top, rows, vocab, pad):
     g.sync()
 
 
+def test_the_largest_vocabulary(torch, g):
+    """2^20 logits a row, in as many chunks as a row may have, with the largest values at both ends and in runs of one chunk."""
+    n = 1 << 20
+    z = (np.random.default_rng(8).normal(size=(2, n)) * 3).astype(np.float32)
+    z[0, [0, n - 1]] = 40, 41
+    z[1, 8192 * 77:8192 * 77 + 40] = 30
+    t = np.array([n - 1, 8192 * 77 + 39], np.int32)
+    check(g.logits_logprobs(torch.from_numpy(z).cuda(), torch.from_numpy(t).cuda(), top=32), z, t, 32)
+    g.sync()
+
+
 def test_more_rows_than_one_launch_takes(torch, g):
     z = (np.random.default_rng(3).normal(size=(32770, 33)) * 3).astype(np.float32)
     t = np.arange(32770).astype(np.int32) % 33
