@@ -14,10 +14,10 @@
 // Keys order values and, among equals, put the lower index first, so that they are
 // distinct: (order-preserving bits of z, ~index).  Where equal values make the
 // candidates too many the k largest keys are taken one by one.  A second, small launch joins
-// a row's chunks: sums rescaled to the row's maximum, and k rounds of the largest head of the
-// chunks' sorted lists.  Rows of one chunk need no second launch.
+// a row's chunks: sums rescaled to the row's maximum, and the chunks' sorted lists merged
+// in the same way.  Rows of one chunk need no second launch.
 // 256 rows of 151936, k = 20: chunks 32 us (4.9 TB/s; some 20 vector instructions a value keep the ALU 65% busy), join
-// 7.5 us (its rounds depend on each other).  200 rows of 128256 just written by the product: 18 us, 5.8 TB/s.
+// 5.8 us.  200 rows of 128256 just written by the product: 18 us, 5.8 TB/s.
 #include <cmath>
 
 #include "kernels.h"
@@ -255,6 +255,7 @@ __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p
         int r = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q)
+#pragma unroll 4
           for (int i = 0; i < count[q]; ++i) r += cand[q][i] > k;
         if (r < p.top) best[r] = k;
       }
@@ -276,9 +277,11 @@ __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p
 
 // Row blockIdx.x from its chunks (at most kMaxChunks).
 __global__ __launch_bounds__(kT) void logprob_join_kernel(const LogprobParams p) {
-  constexpr int kMaxChunks = 128;
+  constexpr int kMaxChunks = 128, kFew = 6;
   __shared__ float red[4];
-  __shared__ u64 heads[kMaxChunks * kMaxTop], best[kMaxTop];
+  __shared__ u64 heads[kMaxChunks * kMaxTop], cand[kT], best[kMaxTop];
+  __shared__ uint32_t bound;
+  __shared__ int count;
   const int row = blockIdx.x, tid = threadIdx.x, n = p.chunks, top = p.top;
   const float* sums = p.part_sums + (int64_t)row * n * 4;
   for (int i = tid; i < n * top; i += kT) heads[i] = p.part_keys[(int64_t)row * n * top + i];
@@ -292,7 +295,44 @@ __global__ __launch_bounds__(kT) void logprob_join_kernel(const LogprobParams p)
   const float x = fmaxf(m - M, -200.f), f = tid < n && m != -INFINITY ? __expf(x) : 0.f;  // (NaN, of an empty row, gives -200)
   const float S = block_sum(f * s, red);
   const float W = block_sum(f * (w + s * x), red);
-  if (tid < 64) {  // each lane keeps the heads of two chunks' lists
+  // A bound of the k-th largest, as in a chunk: c keys of enough sorted lists reach it where their c-th does, c such that
+  // two thirds of the lists are enough.  What reaches it is ranked by counting.  The few keys of a small k are
+  // taken one by one instead, at 0.3 us each (with its chunks, 1 x 128256, k = 5: 8.5 us, ranked 8.8; k = 20: 13.1 and 11.0).
+  const bool ranked = top > kFew;
+  if (ranked) {
+    if (tid < 64) {  // each lane has the lists of two chunks
+      const int c = min((3 * top + 2 * n - 1) / (2 * n), top);
+      const uint32_t o0 = tid < n ? (uint32_t)(heads[tid * top + c - 1] >> 32) : 0,
+                     o1 = tid + 64 < n ? (uint32_t)(heads[(tid + 64) * top + c - 1] >> 32) : 0;
+      uint32_t all = 0;
+      for (int bit = 31; bit >= 15; --bit) {
+        const uint32_t t = all | 1u << bit;
+        const int lists = __builtin_popcountll(__builtin_amdgcn_ballot_w64(o0 >= t)) + __builtin_popcountll(__builtin_amdgcn_ballot_w64(o1 >= t));
+        if (c * lists >= top) all = t;
+      }
+      if (tid == 0) {
+        bound = max(all, 1u);  // masked values are no candidates
+        count = 0;
+      }
+    }
+    if (tid < kMaxTop) best[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < n * top; i += kT) {
+      const u64 k = heads[i];
+      if ((uint32_t)(k >> 32) < bound) continue;
+      const int at = atomicAdd(&count, 1);  // (their order does not matter: each counts the larger ones)
+      if (at < kT) cand[at] = k;
+    }
+    __syncthreads();
+    if (tid < count && count <= kT) {
+      const u64 k = cand[tid];
+      int r = 0;
+#pragma unroll 8
+      for (int i = 0; i < count; ++i) r += cand[i] > k;
+      if (r < top) best[r] = k;
+    }
+  }
+  if (tid < 64 && (!ranked || count > kT)) {  // few keys, or many equal values: each lane keeps the heads of two chunks' lists
     int at0 = 0, at1 = 0;
     const u64* l0 = heads + tid * top;
     const u64* l1 = heads + (tid + 64) * top;
@@ -378,12 +418,14 @@ __global__ __launch_bounds__(kRowThreads) void rows_to_f16_kernel(const uint16_t
   }
 }
 
-// Values per thread: chunks of 8192 values where they fill the chip (two workgroups a
-// CU) or cover a row that 2048 do not at once, else of 2048.
+// Values per thread: chunks of 8192 values where they give each CU a workgroup or cover a row that 2048 do not at once,
+// else of 2048.  In chunks of 2048 and 8192, k = 20: 4 x 5000 11.5 and 7.0 us, 16 x 32000 12.8 and 14.0, 4 x 128256
+// 13.5 and 14.1; 64 x 32000 14.5 and 14.1, 16 x 128256 15.3 and 14.6, 64 x 128256 26 and 19, 256 x 151936 72 and 37.
+// (Workgroups of 1024 threads that take rows of up to 32768 alone were slower than two launches: 17 us and 12.)
 static int values_per_thread(int rows, int vocab) {
   const int64_t large = (vocab + 8191) / 8192;
   if (vocab <= 2048) return 8;
-  return large == 1 || rows * large >= 512 || (vocab + 2047) / 2048 > 128 ? 32 : 8;
+  return large == 1 || rows * large >= 256 || (vocab + 2047) / 2048 > 128 ? 32 : 8;
 }
 
 hipError_t launch_rows_to_f16(const uint16_t* x, int rows, int K, float eps, uint16_t* x16, float* eps_rows,

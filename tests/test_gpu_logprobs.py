@@ -101,6 +101,27 @@ def test_the_largest_vocabulary(torch, g):
     g.sync()
 
 
+@pytest.mark.parametrize("top", [6, 7, 32])
+@pytest.mark.parametrize("vocab", [2049, 16384, 16385, 60000])
+def test_alternatives_spread_over_chunks(torch, g, top, vocab):
+    """The largest values all in the first, a middle or the last chunk of 2048, one in each, equal everywhere (as many
+    candidates as a workgroup has threads, and more) and fewer left than asked for."""
+    rng = np.random.default_rng(vocab + top)
+    z = rng.normal(size=(8, vocab)).astype(np.float32)
+    z[0, :40] += 20
+    z[1, vocab // 2:vocab // 2 + 40] += 20
+    z[2, -40:] += 20
+    z[3, ::2048] += 20
+    z[4] = 1.25
+    z[5] = -np.inf
+    z[5, rng.permutation(vocab)[:top - 1]] = rng.normal(size=top - 1)
+    z[6, 5:] = -np.inf
+    z[7, ::100] = 4.5
+    t = rng.integers(0, vocab, 8).astype(np.int32)
+    check(g.logits_logprobs(torch.from_numpy(z).cuda(), torch.from_numpy(t).cuda(), top=top), z, t, top)
+    g.sync()
+
+
 def test_more_rows_than_one_launch_takes(torch, g):
     z = (np.random.default_rng(3).normal(size=(32770, 33)) * 3).astype(np.float32)
     t = np.arange(32770).astype(np.int32) % 33
