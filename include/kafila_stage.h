@@ -310,9 +310,9 @@ kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n);
  *          that share pages); lens[b] 0 gives a row of zeros
  *   q_dev : [rows, nq, hd] rotated queries in io (KF_F32, KF_BF16 or KF_F16), 16-byte aligned
  *   out_dev : [rows, nq, hd] in io; may be q_dev
- * Over an MXFP4 cache the products take queries and probabilities in two fp16 parts each (22
- * bits) and fp32 sums; over an fp16 cache they are rounded to fp16, as in a decode step.  A query head
- * that holds a NaN gives NaN.  KF_ERANGE for lens[b] beyond max_ctx or the pages the user holds.
+ * Over caches of both types the products take queries and probabilities in two fp16 parts each (22 bits),
+ * whatever the queries' size, and fp32 sums.  (A decode step on an fp16 cache takes one part of each.)
+ * A query head that holds a NaN or an infinity gives NaN.  KF_ERANGE for lens[b] beyond max_ctx or the pages the user holds.
  * Changes nothing in the cache.  Enqueued on the stage's stream.
  */
 kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* users, const int32_t* lens,

@@ -85,18 +85,6 @@ __device__ __forceinline__ void store_out(void* out, int type, int64_t at, float
 constexpr int kWaves = 4;
 constexpr int kMostPages = kMxMaxSplit / kKvPage;
 static_assert(kMostPages <= 64, "a lane holds the id of one page of the split");
-// Probabilities are taken relative to a maximum that moves only when a page's exceeds it by kLazyMax (log2
-// units), so that O is rarely rescaled, and times 2^kShift: the largest lies in [2^12, 2^14], within fp16, and two
-// fp16 parts, whose finest step is 2^-24, hold every one above 2^-14 of it to 22 bits (one of a long flat tail beside a
-// peak too: without the shift those below 2^-14 would keep 10).  The shift is added after the subtraction, which
-// is exact near the maximum however large the scores are.
-constexpr float kShift = 12.0f, kLazyMax = 2.0f;
-
-// The parts of a pair: the rounded values in lanes of keep 0, what rounding left in lanes of keep 1.
-__device__ __forceinline__ uint32_t part2(float a, float b, float keep) {
-  const h2 hi = __builtin_convertvector(f2{a, b}, h2);
-  return f16_pair(__builtin_fmaf(-keep, (float)hi.x, a), __builtin_fmaf(-keep, (float)hi.y, b));
-}
 
 template <int HD>
 struct MxPage {
@@ -257,8 +245,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const P p) {
 
   // The query operand, step s: d = grp hd/4 + 8 s .. + 7 of this column's head (columns past G repeat the
   // last one, and are not read).  Asked for after the page, so that one wait covers both.
-  // In log2 units, times a power of two that puts the head's largest value near 2^10, so that the fp16
-  // parts neither overflow, up to the largest fp32 number, nor lose bits below the normal range.
+  // In log2 units, times a power of two that puts the head's largest value near 2^10 (query_exponent).
   h8 qf[NS];
   float unscale;
   {
@@ -273,15 +260,15 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const P p) {
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int j = 0; j < 8; ++j) top = fmaxf(top, __builtin_fabsf(f[s][j]));
-    const int e = min(max((int)(__float_as_uint(groups_max(top)) >> 23) - 127, -90), 127);
-    unscale = __uint_as_float((uint32_t)(127 - 13 + e) << 23);
-    const float scale = p.a.scale_log2 * __uint_as_float((uint32_t)(127 + 13 - e) << 23);
+    const int e = query_exponent(groups_max(top));
+    unscale = query_unscale(e);
+    const float scale = p.a.scale_log2 * query_scale(e);
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[s][j] *= scale;
-      qf[s] = __builtin_bit_cast(h8, v4u{part2(f[s][0], f[s][1], keep), part2(f[s][2], f[s][3], keep),
-                                         part2(f[s][4], f[s][5], keep), part2(f[s][6], f[s][7], keep)});
+      qf[s] = __builtin_bit_cast(h8, v4u{f16_part2(f[s][0], f[s][1], keep), f16_part2(f[s][2], f[s][3], keep),
+                                         f16_part2(f[s][4], f[s][5], keep), f16_part2(f[s][6], f[s][7], keep)});
     }
   }
 
@@ -325,16 +312,16 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const P p) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) mb = fmaxf(mb, fmaxf(fmaxf(sc[t][0], sc[t][1]), fmaxf(sc[t][2], sc[t][3])));
     mb = groups_max(mb) * unscale;
-    const float m_new = mb > m_run + kLazyMax ? mb : m_run;
+    const float m_new = mb > m_run + kPartLazy ? mb : m_run;
     const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);  // 0 while m_run is -inf
     float ls = 0.f;
     uint32_t pw[8];  // pair k: positions 16 (k / 2) + 4 grp + 2 (k % 2), and the next
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][2 * (k % 2)], unscale, -m_new) + kShift);
-      const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][2 * (k % 2) + 1], unscale, -m_new) + kShift);
+      const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][2 * (k % 2)], unscale, -m_new) + kPartShift);
+      const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][2 * (k % 2) + 1], unscale, -m_new) + kPartShift);
       ls += x + y;
-      pw[k] = part2(x, y, keep);
+      pw[k] = f16_part2(x, y, keep);
     }
     l_run = l_run * alpha + ls;
     m_run = m_new;
@@ -404,7 +391,7 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(const MxAttnParams p)
   const float* acc = p.a.part_acc + r0 * HD + lane * DPL;
   __shared__ float weight[kAttnMaxSplitCount];
   __shared__ float red[4][HD], red_m[4], red_l[4];
-  // The wave's first splits are asked for with the maxima; past the last split it is read again, at weight 0.
+  // The wave's first splits are asked for with the maxima; past the last split it is read again, and not used.
   float pre[PRE][DPL];
 #pragma unroll
   for (int k = 0; k < PRE; ++k)
@@ -431,9 +418,10 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(const MxAttnParams p)
   float v[DPL] = {};
 #pragma unroll
   for (int k = 0; k < PRE; ++k) {
-    const float f = wave + 4 * k < ns ? weight[wave + 4 * k] : 0.f;
+    const bool mine = wave + 4 * k < ns;  // (weight 0 would make a NaN of an infinite sum)
+    const float f = mine ? weight[wave + 4 * k] : 0.f;
 #pragma unroll
-    for (int i = 0; i < DPL; ++i) v[i] += f * pre[k][i];
+    for (int i = 0; i < DPL; ++i) v[i] = mine ? v[i] + f * pre[k][i] : v[i];
   }
 #pragma unroll 8
   for (int s = wave + 4 * PRE; s < ns; s += 4) {

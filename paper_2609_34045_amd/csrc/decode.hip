@@ -638,8 +638,12 @@ __device__ __forceinline__ void dk_read_vt(uint32_t base, const int (&off)[NT], 
 #define KF_ATTN_LAZY 8.0f
 #endif
 
-// QT: the queries' type (0 fp32, as in a decode step, 1 bf16, 2 fp16).
-template <int HD, int NW, int QT>
+// GIVEN: the attention of given queries of type QT (0 fp32, 1 bf16, 2 fp16; kf_kv_attend), held to 22 bits, as the
+// probabilities are, in two fp16 parts: the up to 8 query slots' second parts take the other 8 columns of the tiles,
+// which a decode step (one part of each) leaves at zero, so that they cost no product, but a lane permute and a few
+// vector instructions a key.  8 KV heads of 128, bf16 queries, one part and two: 2048 positions 8.0 and 8.7 us, four rows of
+// 1024 to 32768 44.0 and 46.4, two of 131072 and 100001 200 and 204 (4.7 TB/s).
+template <int HD, int NW, int QT, bool GIVEN>
 __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_kernel(const AttnParams p) {
   constexpr int KB = 16;             // keys per block
   constexpr int ROWB = HD * 2;       // bytes per key row
@@ -651,7 +655,8 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
   constexpr int RPL = 1024 / ROWB;   // key rows per direct load
   constexpr int NS = HD / 32;        // S MFMA steps (32 d each)
   constexpr int NT = HD / 16;        // O^T tiles (16 d each)
-  constexpr float kLazy = KF_ATTN_LAZY;
+  constexpr float kLazy = GIVEN ? kPartLazy : KF_ATTN_LAZY;
+  static_assert(GIVEN ? kMaxGroup <= 8 : QT == 0, "query slots");
   static_assert(HD == 64 || HD == 128, "head dim");
   static_assert(kKvPage % KB == 0 && kAttnMaxSplit / kKvPage <= 64, "blocks within pages");
   static_assert(HD * 16 * 4 + 32 * 4 <= WAVEB, "a wave's final state fits its stages");
@@ -663,13 +668,15 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
   const int G = p.nq / p.nkv;  // query heads per KV head, at most 16
   const int hq0 = g * G;
   const int hn = lane & 15, q4 = lane >> 4;  // MFMA column (query slot) and 16-lane group
+  const float keep = GIVEN && hn >= 8 ? 1.0f : 0.0f;  // this lane's column holds second parts
 
   // The query slots as fp16 B operands, scaled to log2 units: slot hn, d = 32 s + 8 q4 .. + 7
   // (requested first: the previous kernel has just written them).
   v4f qlo[NS], qhi[NS];
   {
-    const bool hv = hn < G;
-    const int64_t row = (int64_t)b * p.nq * HD + (int64_t)(hq0 + (hv ? hn : 0)) * HD;
+    // (columns past the group repeat a head: their results are not read)
+    const int slot = GIVEN ? min(hn & 7, G - 1) : hn < G ? hn : 0;
+    const int64_t row = (int64_t)b * p.nq * HD + (int64_t)(hq0 + slot) * HD;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       const int64_t at = row + 32 * s + 8 * q4;
@@ -756,7 +763,7 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
   // slot is RMS-normalised (gains gq; its squares summed over the four lanes
   // that hold it) and rotated at the row's new position: the RoPE partner of
   // d = 32 s + 8 q4 + j, d +- HD/2, is step s +- NS/2 of the same lane.
-  const bool qkn = p.kraw != nullptr;
+  const bool qkn = !GIVEN && p.kraw != nullptr;
   const int npos = len - 1;  // row b's new position
   if (qkn) {
     float x[NS][8];
@@ -841,7 +848,23 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
   }
 
   h8 qf[NS];
-  {
+  float unscale = 1.0f;  // of the scores
+  if constexpr (GIVEN) {
+    float top = 0.f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, fmaxf(__builtin_fabsf(qlo[s][r]), __builtin_fabsf(qhi[s][r])));
+    const int e = query_exponent(dk_max32(dk_max16(top)));
+    unscale = query_unscale(e);
+    const float sc = p.scale_log2 * query_scale(e);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const v4f x = qlo[s] * sc, y = qhi[s] * sc;
+      qf[s] = __builtin_bit_cast(h8, v4u{f16_part2(x.x, x.y, keep), f16_part2(x.z, x.w, keep), f16_part2(y.x, y.y, keep),
+                                         f16_part2(y.z, y.w, keep)});
+    }
+  } else {
     const float sc = hn < G ? p.scale_log2 : 0.f;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
@@ -883,6 +906,13 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
       const v4u kf = *reinterpret_cast<const v4u*>(st + koff[s]);
       sc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, kf), qf[s], sc, 0, 0, 0);
     }
+    if constexpr (GIVEN) {  // both parts of a score; an infinite key's first is the score (its second may be NaN)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float other = dpp<kDppRor8>(sc[r]), first = hn < 8 ? sc[r] : other;
+        sc[r] = __builtin_fabsf(first) < INFINITY ? sc[r] + other : first;
+      }
+    }
     const int k0 = (NW * i + wave) * KB + 4 * q4;  // this lane's first key, relative to the split
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -893,14 +923,25 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
     // rescale of O is skipped in nearly every block.  A block always holds a
     // valid key, so its maximum is finite.
     float mb = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
-    mb = dk_max32(dk_max16(mb));
+    mb = dk_max32(dk_max16(mb)) * unscale;
     const float m_new = mb > m_run + kLazy ? mb : m_run;
     const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);  // 0 while m_run is -inf
-    const uint32_t w0 = dk_pack(__builtin_amdgcn_exp2f(sc[0] - m_new), __builtin_amdgcn_exp2f(sc[1] - m_new));
-    const uint32_t w1 = dk_pack(__builtin_amdgcn_exp2f(sc[2] - m_new), __builtin_amdgcn_exp2f(sc[3] - m_new));
-    // the sum is taken over the fp16 probabilities that the P V product uses
-    const float ls = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w1), ones,
-                                            __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w0), ones, 0.f, false), false);
+    uint32_t w0, w1;
+    float ls;
+    if constexpr (GIVEN) {
+      float x[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], unscale, -m_new) + kPartShift);
+      ls = (x[0] + x[1]) + (x[2] + x[3]);
+      w0 = f16_part2(x[0], x[1], keep);
+      w1 = f16_part2(x[2], x[3], keep);
+    } else {
+      w0 = dk_pack(__builtin_amdgcn_exp2f(sc[0] - m_new), __builtin_amdgcn_exp2f(sc[1] - m_new));
+      w1 = dk_pack(__builtin_amdgcn_exp2f(sc[2] - m_new), __builtin_amdgcn_exp2f(sc[3] - m_new));
+      // the sum is taken over the fp16 probabilities that the P V product uses
+      ls = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w1), ones,
+                                  __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w0), ones, 0.f, false), false);
+    }
     l_run = l_run * alpha + ls;
     m_run = m_new;
     if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {
@@ -940,7 +981,9 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
       for (int w = 0; w < NW; ++w) {
         const float* s = reinterpret_cast<const float*>(smem + w * WAVEB);
         const float f = exp2f(s[HD * 16 + h] - M);  // 0 for a wave without keys (its max is -inf)
-        v += f * s[d * 16 + h];
+        float x = s[d * 16 + h];
+        if (GIVEN && __builtin_fabsf(x) < INFINITY) x += s[d * 16 + h + 8];
+        v += f * x;
         l += f * s[HD * 16 + 16 + h];
       }
     }
@@ -1441,20 +1484,21 @@ hipError_t launch_gemv(int epi, int R, int U, bool norm, const GemvParams& p, hi
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_attn_decode(const AttnParams& p, int batch, hipStream_t s, int q_type) {
-  if (p.nq % p.nkv || p.nq / p.nkv > 16) return hipErrorInvalidValue;  // query slots of one MFMA column block
+template <int QT, bool GIVEN>
+static hipError_t attn_decode(const AttnParams& p, int batch, hipStream_t s) {
+  if (p.nq % p.nkv || p.nq / p.nkv > (GIVEN ? 8 : 16)) return hipErrorInvalidValue;  // query slots of one MFMA column block
   const dim3 grid(p.n_split, p.nkv, batch), block(64 * kAttnMfmaWaves);
-  auto launch = [&](auto type) {
-    constexpr int QT = decltype(type)::value;
-    if (p.hd == 128) hipLaunchKernelGGL((attn_decode_mfma_kernel<128, kAttnMfmaWaves, QT>), grid, block, 0, s, p);
-    else if (p.hd == 64) hipLaunchKernelGGL((attn_decode_mfma_kernel<64, kAttnMfmaWaves, QT>), grid, block, 0, s, p);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
-  };
+  if (p.hd == 128) hipLaunchKernelGGL((attn_decode_mfma_kernel<128, kAttnMfmaWaves, QT, GIVEN>), grid, block, 0, s, p);
+  else if (p.hd == 64) hipLaunchKernelGGL((attn_decode_mfma_kernel<64, kAttnMfmaWaves, QT, GIVEN>), grid, block, 0, s, p);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+hipError_t launch_attn_decode(const AttnParams& p, int batch, hipStream_t s) { return attn_decode<0, false>(p, batch, s); }
+hipError_t launch_attn_given(const AttnParams& p, int batch, int q_type, hipStream_t s) {
   switch (q_type) {
-    case 0: return launch(std::integral_constant<int, 0>{});
-    case 1: return launch(std::integral_constant<int, 1>{});
-    case 2: return launch(std::integral_constant<int, 2>{});
+    case 0: return attn_decode<0, true>(p, batch, s);
+    case 1: return attn_decode<1, true>(p, batch, s);
+    case 2: return attn_decode<2, true>(p, batch, s);
     default: return hipErrorInvalidValue;
   }
 }

@@ -108,6 +108,28 @@ __device__ __forceinline__ uint32_t f16_pair(float a, float b) {
   typedef _Float16 h2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, h2));
 }
+// One fp16 part of each of a pair of finite values, which two parts hold to 22 bits: the rounded values for keep 0, what
+// rounding left for keep 1.
+__device__ __forceinline__ uint32_t f16_part2(float a, float b, float keep) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  const h2 hi = __builtin_convertvector(f2{a, b}, h2);
+  return f16_pair(__builtin_fmaf(-keep, (float)hi.x, a), __builtin_fmaf(-keep, (float)hi.y, b));
+}
+// Attention with given queries (kf_kv_attend, and decode steps on MXFP4 caches) takes probabilities relative to a maximum
+// that moves only when a tile's exceeds it by kPartLazy (log2 units), so that O is rarely rescaled, and times 2^kPartShift:
+// the largest lies in [2^12, 2^14], within fp16, and two fp16 parts, whose finest step is 2^-24, hold every one above
+// 2^-14 to 22 bits (one of a long flat tail beside a peak too: without the shift those below 2^-14 of the peak would keep
+// 10).  The shift is added after the subtraction, which is exact near the maximum however large the scores are.
+constexpr float kPartShift = 12.0f, kPartLazy = 2.0f;
+// Queries go into two fp16 parts times a power of two, 2^(13 - e) with e the exponent of the head's largest value (in
+// [-90, 127]), so that they neither overflow, up to the largest fp32 number, nor lose bits below the normal range.
+__device__ __forceinline__ int query_exponent(float top) {
+  const int e = (int)(__float_as_uint(top) >> 23) - 127;
+  return e < -90 ? -90 : e > 127 ? 127 : e;
+}
+__device__ __forceinline__ float query_scale(int e) { return __uint_as_float((uint32_t)(127 + 13 - e) << 23); }
+__device__ __forceinline__ float query_unscale(int e) { return __uint_as_float((uint32_t)(127 - 13 + e) << 23); }
 // 8 of a block's values as fp16 pairs, the other 24 in the 3 lanes beside (lanes 4 k .. 4 k + 3
 // hold a block): their E2M1 codes, and the block's exponent.  A NaN is stored as 0, an infinity as the
 // largest magnitude; both are noted in `bad`.  The convert instruction rounds to nearest even
@@ -290,7 +312,9 @@ hipError_t launch_gemv(int epi, int rows_per_wg, int chunks_in_flight, bool norm
 // The same launch with the stage input (p.src or p.tokens) as its input rows.
 hipError_t launch_gemv_src(int epi, int rows_per_wg, int chunks_in_flight, bool norm, const GemvParams& p,
                            hipStream_t s);
-hipError_t launch_attn_decode(const AttnParams& p, int batch, hipStream_t s, int q_type = 0);  // q of a kf_dtype
+hipError_t launch_attn_decode(const AttnParams& p, int batch, hipStream_t s);
+// The same with given queries, p.q of q_type (a kf_dtype value), and queries and probabilities in two fp16 parts each.
+hipError_t launch_attn_given(const AttnParams& p, int batch, int q_type, hipStream_t s);
 // Head h of row b merged from the attention partials in p, to o16[b][h*hd:(h+1)*hd]
 // (fp16) or, with o16 NULL, to o32[b][h*hd:(h+1)*hd] (fp32).
 // rows: how many partials each row has, or NULL for p.n_split.

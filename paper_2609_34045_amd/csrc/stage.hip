@@ -1195,7 +1195,7 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
     a.q = reinterpret_cast<const float*>(q_dev);
     a.kc = (uint16_t*)ref.k;
     a.vc = (uint16_t*)ref.v;
-    e = launch_attn_decode(a, rows, s->stream, io);
+    e = launch_attn_given(a, rows, io, s->stream);
   }
   if (e == hipSuccess && !p.out) {
     p.out = out_dev;
