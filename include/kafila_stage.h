@@ -297,8 +297,10 @@ kf_status kf_kv_copy(kf_kv* dst, int32_t dst_user, const kf_kv* src, int32_t src
  * its last user gives it back.  KF_EINVAL for src_user == dst_user, KF_ERANGE for n
  * above src_user's length.
  * Which pages are shared is known when a call is made, not when a graph is replayed: under graph
- * capture a paged fork, and a call that would first copy a shared page, is KF_ESTATE, and a
- * graph captured before a fork still writes to the pages its users held then.
+ * capture a paged fork, and a call that would first copy a shared page, is KF_ESTATE.  Pages that a
+ * captured call lends are their user's from that call on, replayed or not.  A replay uses the pages that the
+ * users hold by then, and counts nothing: replay a graph while they hold the positions that it uses, and
+ * capture anew what writes to pages that have been shared since.
  */
 kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n);
 

@@ -319,9 +319,9 @@ __global__ __launch_bounds__(256) void f16_copy_kernel(const CopyParams p, int64
       *reinterpret_cast<const v4u*>(src + 2 * (kv_offset(p.src.pages, p.src_user, (int)g, pos, hd) + d));
 }
 
-__global__ __launch_bounds__(256) void page_copy_kernel(const CacheRef c, const PageCopies u, int64_t page_bytes, int* table,
+__global__ __launch_bounds__(256) void page_copy_kernel(const CacheRef c, const PageCopies u, int64_t page_bytes, const KvTable table,
                                                         const KvTableUpdate t) {
-  if (blockIdx.x + blockIdx.y + blockIdx.z == 0 && (int)threadIdx.x < t.n) table[t.idx[threadIdx.x]] = t.val[threadIdx.x];
+  if (blockIdx.x + blockIdx.y + blockIdx.z == 0) kv_table_apply(table, t, threadIdx.x);
   const int arrays = c.mx ? 1 : 2;
   const int64_t layer = blockIdx.y / arrays;
   uint8_t* base = (blockIdx.y % arrays ? c.v : c.k) + layer * c.layer_bytes;
@@ -330,9 +330,11 @@ __global__ __launch_bounds__(256) void page_copy_kernel(const CacheRef c, const 
   for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < page_bytes / 16; i += (int64_t)gridDim.x * 256) dst[i] = src[i];
 }
 
-__global__ void table_share_kernel(int* table, int src, int dst, int n) {
+__global__ void table_share_kernel(const KvTable t, int src, int dst, int n) {
   const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i < n) table[dst + i] = table[src + i];
+  if (i >= n) return;
+  t.page[dst + i] = t.page[src + i];
+  t.version[dst + i]++;
 }
 
 // ------------------------------------------------------------------ launchers
@@ -441,8 +443,8 @@ hipError_t launch_cache_copy(const CacheRef& dst, int dst_user, const CacheRef& 
   return hipGetLastError();
 }
 
-hipError_t launch_page_copies(const CacheRef& c, const PageCopies& u, int layers, int* table, const KvTableUpdate& t,
-                              hipStream_t s) {
+hipError_t launch_page_copies(const CacheRef& c, const PageCopies& u, int layers, const KvTable& table,
+                              const KvTableUpdate& t, hipStream_t s) {
   if (u.n < 1 || u.n > kPageCopyBatch) return hipErrorInvalidValue;
   const int64_t bytes = c.pages.page_stride * (c.mx ? 1 : 2);
   const unsigned wgs = (unsigned)std::min<int64_t>((bytes / 16 + 1023) / 1024, 64);
@@ -450,8 +452,8 @@ hipError_t launch_page_copies(const CacheRef& c, const PageCopies& u, int layers
   return hipGetLastError();
 }
 
-hipError_t launch_kv_table_share(int* table, int src, int dst, int n, hipStream_t s) {
-  hipLaunchKernelGGL(table_share_kernel, dim3((n + 255) / 256), dim3(256), 0, s, table, src, dst, n);
+hipError_t launch_kv_table_share(const KvTable& t, int src, int dst, int n, hipStream_t s) {
+  hipLaunchKernelGGL(table_share_kernel, dim3((n + 255) / 256), dim3(256), 0, s, t, src, dst, n);
   return hipGetLastError();
 }
 

@@ -1364,10 +1364,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const uint16_t* sk, const 
   }
 }
 
-__global__ void kv_table_update_kernel(int* table, const KvTableUpdate u) {
-  const int i = threadIdx.x;
-  if (i < u.n) table[u.idx[i]] = u.val[i];
-}
+__global__ void kv_table_update_kernel(const KvTable t, const KvTableUpdate u) { kv_table_apply(t, u, threadIdx.x); }
 
 // ------------------------------------------------------------------ launchers
 // A launch that folds RMSNorm into its product: with the gain (p.gain) applied
@@ -1608,9 +1605,9 @@ hipError_t launch_kv_read(const uint16_t* k, const uint16_t* v, const KvPages& k
   return hipGetLastError();
 }
 
-hipError_t launch_kv_table_update(int* table, const KvTableUpdate& u, hipStream_t s) {
+hipError_t launch_kv_table_update(const KvTable& t, const KvTableUpdate& u, hipStream_t s) {
   if (u.n < 1 || u.n > kKvTableBatch) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(kv_table_update_kernel, dim3(1), dim3(kKvTableBatch), 0, s, table, u);
+  hipLaunchKernelGGL(kv_table_update_kernel, dim3(1), dim3(kKvTableBatch), 0, s, t, u);
   return hipGetLastError();
 }
 

@@ -336,16 +336,29 @@ hipError_t launch_kv_write(uint16_t* k, uint16_t* v, const KvPages& kp, int user
                            const void* src_v, int src_type, int n, int nkv, int hd, hipStream_t s);
 hipError_t launch_kv_read(const uint16_t* k, const uint16_t* v, const KvPages& kp, int user, int pos0, float* dst_k,
                           float* dst_v, int n, int nkv, int hd, hipStream_t s);
-// table[idx[i]] = val[i] for i < n (n <= kKvTableBatch): page assignments of a paged cache.
+// The page table of a paged cache as its updates see it: each entry has the number of the update that it holds, so that
+// one that a captured graph replays after later ones changes nothing.
+struct KvTable {
+  int* page;
+  uint32_t* version;
+};
+// page[idx[i]] = val[i] for i < n (n <= kKvTableBatch) where version[idx[i]] is before ver[i], which it becomes; a val of
+// -1 brings the version alone.
 constexpr int kKvTableBatch = 32;
 struct KvTableUpdate {
   int n;
   int idx[kKvTableBatch];
   int val[kKvTableBatch];
+  uint32_t ver[kKvTableBatch];
 };
-hipError_t launch_kv_table_update(int* table, const KvTableUpdate& u, hipStream_t s);
-// table[dst + i] = table[src + i] for i < n: a user that shares another's pages.
-hipError_t launch_kv_table_share(int* table, int src, int dst, int n, hipStream_t s);
+__device__ __forceinline__ void kv_table_apply(const KvTable& t, const KvTableUpdate& u, int i) {
+  if (i >= u.n || (int32_t)(u.ver[i] - t.version[u.idx[i]]) <= 0) return;
+  if (u.val[i] >= 0) t.page[u.idx[i]] = u.val[i];
+  t.version[u.idx[i]] = u.ver[i];
+}
+hipError_t launch_kv_table_update(const KvTable& t, const KvTableUpdate& u, hipStream_t s);
+// page[dst + i] = page[src + i] for i < n, as each entry's next update: a user that shares another's pages.
+hipError_t launch_kv_table_share(const KvTable& t, int src, int dst, int n, hipStream_t s);
 
 // Log probabilities of rows of logits (logprob.hip).
 constexpr int kMaxTop = 32;
@@ -401,7 +414,7 @@ struct PageCopies {
   int src[kPageCopyBatch];
   int dst[kPageCopyBatch];
 };
-hipError_t launch_page_copies(const CacheRef& c, const PageCopies& copies, int layers, int* table,
+hipError_t launch_page_copies(const CacheRef& c, const PageCopies& copies, int layers, const KvTable& table,
                               const KvTableUpdate& u, hipStream_t s);
 
 }  // namespace kf

@@ -193,8 +193,15 @@ struct kf_kv {
   // A reserved cache holds ppu pages per user in user order (no table); a paged
   // cache lends pages from a pool, recorded in a device table with a host mirror.
   int ppu = 0, n_pages = 0;
-  int* table = nullptr;        // device [max_users][ppu] page ids (paged caches only)
+  int* table = nullptr;        // device [max_users][ppu] page ids (paged caches only), then as many update numbers (KvTable)
   std::vector<int> host_table; // mirror of the table (-1: not held)
+  std::vector<uint32_t> version;  // and of the update numbers, all made
+  // Entries whose last update was recorded into a graph, which may be replayed late or never: the calls that read the
+  // table bring them there first (kv_catch_up).  Their number, and the capture that has recorded them all.
+  mutable std::vector<uint8_t> recorded;
+  mutable int64_t n_recorded = 0;
+  mutable unsigned long long recorded_in = 0;
+  KvTable kv_table() const { return KvTable{table, (uint32_t*)(table + host_table.size())}; }
   std::vector<int> held;       // pages each user holds
   std::vector<int> free_pages; // the pool's free pages (paged caches only), next page last
   std::vector<int> refs;       // users that hold each page (paged caches only); a page of several is copied before a write
@@ -231,12 +238,46 @@ struct kf_kv {
 
 static int pages_for(int64_t len) { return (int)((len + kKvPage - 1) / kKvPage); }
 
-// Whether the stage's stream is being captured into a graph.
-static bool capturing(const kf_stage* s) {
+// Whether the stage's stream is being captured into a graph, and a number of the capture.
+static bool capturing(const kf_stage* s, unsigned long long* id = nullptr) {
   hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(s->stream, &capture) == hipSuccess) return capture != hipStreamCaptureStatusNone;
+  unsigned long long n = 0;
+  if (id) *id = 0;
+  if (hipStreamGetCaptureInfo(s->stream, &capture, &n) == hipSuccess) {
+    if (id) *id = n;
+    return capture != hipStreamCaptureStatusNone;
+  }
   (void)hipGetLastError();
   return true;
+}
+
+// Table entries that a capture recorded reach the device by this call, in the stream's order, before a call that reads
+// the table: eager, or recorded again by another capture (each graph brings what its own work reads).  The update numbers
+// let the first of the updates through, and none of them after a later one.
+static kf_status kv_catch_up(const kf_kv* kv) {
+  if (!kv->n_recorded) return KF_OK;
+  unsigned long long id = 0;
+  const bool capture = capturing(kv->st, &id);
+  if (capture && id && id == kv->recorded_in) return KF_OK;
+  KvTableUpdate up{};
+  for (size_t i = 0, left = kv->n_recorded; left; ++i) {
+    if (!kv->recorded[i]) continue;
+    --left;
+    up.idx[up.n] = (int)i;
+    up.val[up.n] = kv->host_table[i];
+    up.ver[up.n++] = kv->version[i];
+    if (up.n == kKvTableBatch || !left) {
+      KF_HIP(launch_kv_table_update(kv->kv_table(), up, kv->st->stream), "page table update");
+      up.n = 0;
+    }
+  }
+  if (capture) {
+    kv->recorded_in = id;
+    return KF_OK;
+  }
+  std::fill(kv->recorded.begin(), kv->recorded.end(), (uint8_t)0);
+  kv->n_recorded = 0;
+  return KF_OK;
 }
 
 // The page of `user` that holds position `pos`, if other users hold it too; else -1.
@@ -271,6 +312,8 @@ int kv_append_copies(const kf_kv* kv, int n, const int* users) {
 // work there reads them.
 static kf_status kv_grant(kf_kv* kv, int n, const int* users, const int64_t* from, const int64_t* upto) {
   if (!kv->table) return KF_OK;  // reserved cache: every page is held from the start
+  const kf_status late = kv_catch_up(kv);
+  if (late != KF_OK) return late;
   int64_t want = 0;
   int copies = n > 1 ? kv_append_copies(kv, n, users) : 0;
   for (int i = 0; i < n; ++i) {
@@ -279,7 +322,10 @@ static kf_status kv_grant(kf_kv* kv, int n, const int* users, const int64_t* fro
     if (n == 1)
       for (int64_t p = from[i]; p < upto[i]; p = (p / kKvPage + 1) * kKvPage) copies += shared_page(kv, users[i], p) >= 0;
   }
-  if (copies && capturing(kv->st))  // each replay would put the page's old contents back
+  if (want + copies == 0) return KF_OK;
+  unsigned long long capture_id = 0;
+  const bool capture = capturing(kv->st, &capture_id);
+  if (copies && capture)  // each replay would put the page's old contents back
     return fail(KF_ESTATE, "pages that other users hold too cannot be copied under graph capture");
   want += copies;
   if (want > (int64_t)kv->free_pages.size())
@@ -289,20 +335,26 @@ static kf_status kv_grant(kf_kv* kv, int n, const int* users, const int64_t* fro
   KvTableUpdate up{};
   PageCopies cp{};
   auto flush = [&]() {
-    if (cp.n) KF_HIP(launch_page_copies(kv->ref(), cp, kv->layers(), kv->table, up, st), "page copies");
-    else if (up.n) KF_HIP(launch_kv_table_update(kv->table, up, st), "page table update");
+    if (cp.n) KF_HIP(launch_page_copies(kv->ref(), cp, kv->layers(), kv->kv_table(), up, st), "page copies");
+    else if (up.n) KF_HIP(launch_kv_table_update(kv->kv_table(), up, st), "page table update");
     cp.n = up.n = 0;
     return KF_OK;
   };
   auto take = [&](int u, int pg) {
-    const int id = kv->free_pages.back();
+    const int id = kv->free_pages.back(), at = u * kv->ppu + pg;
     kv->free_pages.pop_back();
     kv->refs[id] = 1;
-    kv->host_table[(size_t)u * kv->ppu + pg] = id;
-    up.idx[up.n] = u * kv->ppu + pg;
-    up.val[up.n++] = id;
+    kv->host_table[at] = id;
+    if (capture && !kv->recorded[at]) {
+      kv->recorded[at] = 1;
+      kv->n_recorded++;
+    }
+    up.idx[up.n] = at;
+    up.val[up.n] = id;
+    up.ver[up.n++] = ++kv->version[at];
     return id;
   };
+  if (capture) kv->recorded_in = capture_id;  // and those before were caught up in it
   for (int i = 0; i < n; ++i) {
     const int u = users[i];
     for (int64_t p = from[i]; p < upto[i]; p = (p / kKvPage + 1) * kKvPage) {
@@ -794,6 +846,8 @@ static kf_status kv_make(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_
   kv->held.assign(max_users, paged ? 0 : ppu);
   if (paged) {
     kv->host_table.assign((size_t)max_users * ppu, -1);
+    kv->version.assign((size_t)max_users * ppu, 0);
+    kv->recorded.assign((size_t)max_users * ppu, 0);
     kv->refs.assign(n_pages, 0);
     kv->free_pages.reserve(n_pages);
     for (int i = n_pages - 1; i >= 0; --i) kv->free_pages.push_back(i);  // page 0 lent first
@@ -803,7 +857,7 @@ static kf_status kv_make(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_
   const int64_t rope = (int64_t)max_ctx * half * 4;
   const int64_t pacc = (int64_t)kMaxBatch * c.n_q_heads * kv->max_split * c.head_dim * 4;
   const int64_t pml = (int64_t)kMaxBatch * c.n_q_heads * kv->max_split * 2 * 4;
-  const int64_t tab = paged ? (int64_t)max_users * ppu * 4 : 0;
+  const int64_t tab = paged ? (int64_t)max_users * ppu * 8 : 0;
   const int64_t app = kv->mx() ? 2LL * kMaxBatch * c.n_kv_heads * kKvPage * c.head_dim * 2 : 0;
   const int64_t app_tab = kv->mx() ? (int64_t)kMaxBatch * ppu * 4 : 0;
   const int64_t f16 = kv->mx() ? (int64_t)ppu * kKvPage * c.n_kv_heads * c.head_dim * 2 : 0;
@@ -973,6 +1027,8 @@ kf_status kf_kv_read(const kf_kv* kv, int32_t layer, int32_t user, int32_t pos0,
   if ((int64_t)pos0 + n > (int64_t)kv->held[user] * kKvPage)
     return fail(KF_ERANGE, "positions up to %d of user %d are not in the cache (it holds %d pages)", pos0 + n, user,
                 kv->held[user]);
+  st = kv_catch_up(kv);
+  if (st != KF_OK) return st;
   if (kv->mx()) {
     KF_HIP(launch_mx_read(kv->layer_ref(layer), user, pos0, k_dev, v_dev, n, kv->st->stream), "kv_read launch");
     return KF_OK;
@@ -997,7 +1053,8 @@ kf_status kf_kv_copy(kf_kv* dst, int32_t dst_user, const kf_kv* src, int32_t src
     return fail(KF_ERANGE, "positions up to %d of user %d are not in the cache (it holds %d pages)", pos0 + n, src_user,
                 src->held[src_user]);
   const int64_t from = pos0, upto = from + n;
-  st = kv_grant(dst, 1, &dst_user, &from, &upto);
+  if (dst != src) st = kv_catch_up(src);
+  if (st == KF_OK) st = kv_grant(dst, 1, &dst_user, &from, &upto);
   if (st != KF_OK) return st;
   KF_HIP(launch_cache_copy(dst->ref(), dst_user, src->ref(), src_user, pos0, n, dst->layers(), dst->st->err_flag,
                            dst->st->stream),
@@ -1021,6 +1078,8 @@ kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n) {
   }
   if (capturing(kv->st))  // each replay would take the destination's own pages out of its table again
     return fail(KF_ESTATE, "users of a paged cache cannot be forked under graph capture");
+  const kf_status late = kv_catch_up(kv);
+  if (late != KF_OK) return late;
   // The pages are shared; whoever writes to one first takes a copy (kv_grant).
   // Those that the destination shares already need no new entry.
   const int pages = pages_for(n);
@@ -1030,11 +1089,12 @@ kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n) {
   kv_release(kv, dst_user, same);
   for (int pg = same; pg < pages; ++pg) {
     kv->host_table[(size_t)dst_user * kv->ppu + pg] = from[pg];
+    kv->version[(size_t)dst_user * kv->ppu + pg]++;
     kv->refs[from[pg]]++;
   }
   kv->held[dst_user] = pages;
   if (pages > same)
-    KF_HIP(launch_kv_table_share(kv->table, src_user * kv->ppu + same, dst_user * kv->ppu + same, pages - same, st),
+    KF_HIP(launch_kv_table_share(kv->kv_table(), src_user * kv->ppu + same, dst_user * kv->ppu + same, pages - same, st),
            "page table update");
   kv->len[dst_user] = n;
   return KF_OK;
@@ -1160,6 +1220,8 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
     if (lens[b] > max_len) max_len = lens[b];
     total_len += lens[b];
   }
+  const kf_status late = kv_catch_up(kv);
+  if (late != KF_OK) return late;
   kf_stage* s = kv->st;
   const kf_model_config& c = s->cfg;
   const CacheRef ref = kv->layer_ref(layer);
