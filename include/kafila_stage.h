@@ -444,6 +444,10 @@ kf_status kf_head_logprobs(kf_stage* stage, int32_t rows, const void* hidden_dev
  * The same of logits that the caller holds (after masking or a temperature of its own):
  * logits_dev fp32 [rows] rows of `vocab` values, `stride` values apart.  Any stage;
  * the logits may be of another vocabulary than the stage's.
+ * Rows that more than one workgroup takes (longer than 8192 values) have partial results in a workspace
+ * of the stage, 280 KB to 18 MB, allocated by the first calls that need it and kept; KF_ENOMEM where not even
+ * 280 KB can be had, which includes a first call under graph capture.  After any such call every other
+ * one can be captured: where the workspace is small, in more launches, to the same bits.
  */
 kf_status kf_logits_logprobs(kf_stage* stage, int32_t rows, int32_t vocab, int64_t stride, const float* logits_dev,
                              const int32_t* targets_dev, float* logprob_dev, float* entropy_dev, int32_t n_top,

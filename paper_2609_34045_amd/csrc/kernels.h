@@ -376,6 +376,7 @@ struct LogprobParams {
   int32_t* top_ids;        // [rows][top]
   float* top_logprobs;
   int* err_flag;
+  int values;  // per thread (logprob_values of all rows of the call, so that its launches give the bits of one)
   // set by the launcher: partial results of rows of several chunks
   int chunks;
   unsigned long long* part_keys;  // [rows][chunks][top]
@@ -386,8 +387,13 @@ struct LogprobParams {
 // eps_rows = eps 4^e.  Either may be NULL.
 hipError_t launch_rows_to_f16(const uint16_t* x, int rows, int K, float eps, uint16_t* x16, float* eps_rows,
                               float* row_scale, hipStream_t s);
-int logprob_chunks(int rows, int vocab);
-int64_t logprob_part_bytes(int rows, int vocab, int top);  // workspace of a launch (not used where logprob_chunks is 1)
+// How a call's rows are cut: values per thread, of 256 threads a chunk, and the chunks of a row.  More than one have a partial
+// result each in a workspace.  Smaller chunks are for calls of fewer than 256 large ones, so that kLogprobLeast partials hold
+// any such call whole, and a row of any other.  kLogprobMost, 18 MB, are as fast as more: rows past them are other launches.
+int logprob_values(int rows, int vocab);
+int logprob_chunks(int vocab, int values);
+constexpr int kLogprobLeast = 1024, kLogprobMost = 65536;
+constexpr int64_t kLogprobPartBytes = 16 + kMaxTop * 8;  // a partial's, for any number of alternatives
 hipError_t launch_logprobs(LogprobParams p, int rows, char* part, hipStream_t s);
 
 // A cache as the copying kernels see it (cache.hip): fp16 K and V arrays, or one array of MXFP4 records at k.

@@ -30,6 +30,9 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef unsigned long long u64;
 
 constexpr int kT = 256;  // threads
+constexpr int kMaxChunks = 128;  // of a row
+static_assert(kMaxLogprobVocab <= kMaxChunks * kT * 32, "chunks of the longest row");
+static_assert(kLogprobLeast >= 255 * 4 && kLogprobLeast >= kMaxChunks, "partials of a call of small chunks, and of a row");
 
 // The order of values as that of unsigned numbers; -0 and 0 are equal.
 __device__ __forceinline__ uint32_t order_of(float z) {
@@ -277,7 +280,7 @@ __global__ __launch_bounds__(kT) void logprob_chunk_kernel(const LogprobParams p
 
 // Row blockIdx.x from its chunks (at most kMaxChunks).
 __global__ __launch_bounds__(kT) void logprob_join_kernel(const LogprobParams p) {
-  constexpr int kMaxChunks = 128, kFew = 6;
+  constexpr int kFew = 6;
   __shared__ float red[4];
   __shared__ u64 heads[kMaxChunks * kMaxTop], cand[kT], best[kMaxTop];
   __shared__ uint32_t bound;
@@ -422,11 +425,12 @@ __global__ __launch_bounds__(kRowThreads) void rows_to_f16_kernel(const uint16_t
 // else of 2048.  In chunks of 2048 and 8192, k = 20: 4 x 5000 11.5 and 7.0 us, 16 x 32000 12.8 and 14.0, 4 x 128256
 // 13.5 and 14.1; 64 x 32000 14.5 and 14.1, 16 x 128256 15.3 and 14.6, 64 x 128256 26 and 19, 256 x 151936 72 and 37.
 // (Workgroups of 1024 threads that take rows of up to 32768 alone were slower than two launches: 17 us and 12.)
-static int values_per_thread(int rows, int vocab) {
+int logprob_values(int rows, int vocab) {
   const int64_t large = (vocab + 8191) / 8192;
   if (vocab <= 2048) return 8;
   return large == 1 || rows * large >= 256 || (vocab + 2047) / 2048 > 128 ? 32 : 8;
 }
+int logprob_chunks(int vocab, int values) { return (vocab + kT * values - 1) / (kT * values); }
 
 hipError_t launch_rows_to_f16(const uint16_t* x, int rows, int K, float eps, uint16_t* x16, float* eps_rows,
                               float* row_scale, hipStream_t s) {
@@ -434,24 +438,15 @@ hipError_t launch_rows_to_f16(const uint16_t* x, int rows, int K, float eps, uin
   return hipGetLastError();
 }
 
-int logprob_chunks(int rows, int vocab) {
-  const int c = kT * values_per_thread(rows, vocab);
-  return (vocab + c - 1) / c;
-}
-
-int64_t logprob_part_bytes(int rows, int vocab, int top) {
-  const int64_t n = (int64_t)rows * logprob_chunks(rows, vocab);
-  return n * 16 + n * top * 8;
-}
-
 hipError_t launch_logprobs(LogprobParams p, int rows, char* part, hipStream_t s) {
-  if (p.vocab < 1 || p.vocab > kMaxLogprobVocab || rows < 1 || rows > kLogprobRows || p.top < 0 || p.top > kMaxTop)
+  if (p.vocab < 1 || p.vocab > kMaxLogprobVocab || rows < 1 || rows > kLogprobRows || p.top < 0 || p.top > kMaxTop ||
+      (p.values != 8 && p.values != 32) || logprob_chunks(p.vocab, p.values) > kMaxChunks)
     return hipErrorInvalidValue;
-  p.chunks = logprob_chunks(rows, p.vocab);
+  p.chunks = logprob_chunks(p.vocab, p.values);
   p.part_keys = reinterpret_cast<unsigned long long*>(part);
   p.part_sums = reinterpret_cast<float*>(part + (int64_t)rows * p.chunks * p.top * 8);
   const dim3 grid(p.chunks, rows);
-  if (values_per_thread(rows, p.vocab) == 32) hipLaunchKernelGGL(logprob_chunk_kernel<32>, grid, dim3(kT), 0, s, p);
+  if (p.values == 32) hipLaunchKernelGGL(logprob_chunk_kernel<32>, grid, dim3(kT), 0, s, p);
   else hipLaunchKernelGGL(logprob_chunk_kernel<8>, grid, dim3(kT), 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.chunks == 1) return e;

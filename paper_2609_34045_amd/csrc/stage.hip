@@ -1648,19 +1648,36 @@ static kf_status logprob_check(int rows, int64_t vocab, const int32_t* targets, 
   return KF_OK;
 }
 
-// Rows [0, rows) of logits in as few launches as they go in.
+// Partials of the log probabilities for `want` chunks, or as many of a launch's as can be had, and at least
+// kLogprobLeast; 0 where these cannot be had.  Sizes are powers of two, so that a workspace of one size is there for every
+// call of fewer chunks, whatever its rows, vocabulary and alternatives.
+static int64_t logprob_partials(kf_stage* s, int64_t want) {
+  int64_t n = kLogprobLeast;
+  while (n < want && n < kLogprobMost) n *= 2;
+  while (!grow_kept(s, s->lp_part, n * kLogprobPartBytes) && n > kLogprobLeast) n /= 2;
+  const int64_t held = s->lp_part.cap / kLogprobPartBytes;
+  return held < kLogprobLeast ? 0 : held;
+}
+
+// Rows [0, rows) of logits in as few launches as they and the workspace go in.
 static kf_status logprob_launch(kf_stage* s, int rows, const LogprobParams& all) {
-  for (int r0 = 0; r0 < rows; r0 += kLogprobRows) {
-    const int n = rows - r0 < kLogprobRows ? rows - r0 : kLogprobRows;
+  const int values = logprob_values(rows, all.vocab), chunks = logprob_chunks(all.vocab, values);
+  int most = kLogprobRows;
+  if (chunks > 1) {
+    const int64_t held = logprob_partials(s, (int64_t)rows * chunks);
+    if (!held)
+      return fail(KF_ENOMEM, "workspace of the log probabilities (%lld bytes; a first call may not be captured)",
+                  (long long)(kLogprobLeast * kLogprobPartBytes));
+    most = (int)std::min<int64_t>(most, held / chunks);
+  }
+  for (int64_t r0 = 0; r0 < rows; r0 += most) {
+    const int n = (int)std::min<int64_t>(rows - r0, most);
     LogprobParams p = all;
+    p.values = values;
     p.logits += r0 * p.stride;
     if (p.targets) p.targets += r0, p.logprob += r0;
     if (p.entropy) p.entropy += r0;
-    if (p.top) p.top_ids += (int64_t)r0 * p.top, p.top_logprobs += (int64_t)r0 * p.top;
-    if (logprob_chunks(n, p.vocab) > 1 &&
-        !grow_kept(s, s->lp_part, logprob_part_bytes(n, p.vocab, kMaxTop)))
-      return fail(KF_ENOMEM, "workspace of the log probabilities (%lld bytes; a first call may not be captured)",
-                  (long long)logprob_part_bytes(n, p.vocab, kMaxTop));
+    if (p.top) p.top_ids += r0 * p.top, p.top_logprobs += r0 * p.top;
     const Tracer tr = s->tracer();
     tr.begin(KF_K_LOGPROB);
     const hipError_t e = launch_logprobs(p, n, s->lp_part.mem, s->stream);
