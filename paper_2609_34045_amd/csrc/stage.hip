@@ -111,13 +111,14 @@ struct LayerW {
 };
 
 // A workspace grown to the most a call needed.  What it grew out of stays until the stage ends: a captured
-// graph may hold its address.  Each is at least twice the one before, so that all take less than twice the last.
+// graph may hold its address.  Its callers ask for a few sizes, and get what they ask for.
 struct Grown {
   char* mem = nullptr;
   int64_t cap = 0;
-  char* all[48] = {};
+  char* all[8] = {};  // 3 numbers of rows (kf_head_logprobs), or 7 powers of two (logprob_partials)
   int n = 0;
 };
+static_assert(kLogprobMost / kLogprobLeast == 64, "7 sizes");
 
 struct kf_stage {
   kf_model_config cfg;
@@ -1620,7 +1621,6 @@ kf_status kf_head_argmax(kf_stage* s, int32_t rows, const void* hidden, kf_dtype
 static bool grow_kept(kf_stage* s, Grown& g, int64_t bytes) {
   if (bytes <= g.cap) return true;
   if (g.n == (int)(sizeof g.all / sizeof g.all[0])) return false;
-  bytes = std::max(bytes, 2 * g.cap);
   if (capturing(s)) return false;
   // Relaxed: the allocation leaves captures of other threads alone.
   hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;

@@ -2,7 +2,9 @@
 import numpy as np
 import pytest
 
+import synth
 from tests.test_gpu_cache import bare_stage
+from tests.test_gpu_logits import head_stage
 from tests.test_gpu_logprobs import check
 
 pytestmark = pytest.mark.gpu
@@ -91,6 +93,20 @@ def test_many_rows_take_a_bounded_workspace(torch, st):
     assert np.abs(lp[:-1] - (12 - want)).max() < 1e-4 and abs(lp[-1] - (12 - last)) < 1e-4
     ids = r.top_ids.cpu().numpy()
     assert np.all(ids[:-1] == [77, 0]) and list(ids[-1]) == [3, 77]
+    for s in (g, warm):
+        s.sync()
+        s.close()
+
+
+def test_a_workspace_grows_to_what_a_call_asks_for(torch, st):
+    """Twenty rows after four, of a wide row and a small vocabulary (whose logits are a hundredth of the workspace): not
+    twice the first call's."""
+    hidden, vocab = 8192, 500
+    _, _, g = head_stage(st, hidden, vocab, 96)
+    x = torch.from_numpy(synth.hidden_states(96, synth.STREAM_DECODE_HIDDEN, 0, 20, hidden)).bfloat16().cuda()
+    _, _, warm = head_stage(st, hidden, vocab, 96)
+    few, more = (used(torch, lambda own=False, n=n: (g if own else warm).head_logprobs(x[:n])) for n in (4, 20))
+    assert 0 < few < 8 << 20 and 0 < more <= few + (2 << 20), (few, more)
     for s in (g, warm):
         s.sync()
         s.close()
