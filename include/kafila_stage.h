@@ -234,7 +234,7 @@ kf_status kf_kv_create_paged(kf_stage* stage, int32_t max_users, int32_t max_ctx
  * error (KF_ERANGE from kf_stage_sync).
  * Every call takes caches of both types.  Decode attends to the new position as it is
  * stored.  Prefill attends through fp16 pages of one user and layer that an MXFP4 cache keeps
- * beside its own (max_ctx positions).  KF_EINVAL for a negative n_pages or an unknown type.
+ * beside its own (max_ctx positions, or the pool's where those are fewer).  KF_EINVAL for a negative n_pages or an unknown type.
  */
 typedef enum { KF_KV_F16 = 0, KF_KV_MXFP4 = 1 } kf_kv_type;
 kf_status kf_kv_create_typed(kf_stage* stage, int32_t max_users, int32_t max_ctx, int32_t n_pages, kf_kv_type type,

@@ -861,7 +861,7 @@ static kf_status kv_make(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_
   const int64_t tab = paged ? (int64_t)max_users * ppu * 8 : 0;
   const int64_t app = kv->mx() ? 2LL * kMaxBatch * c.n_kv_heads * kKvPage * c.head_dim * 2 : 0;
   const int64_t app_tab = kv->mx() ? (int64_t)kMaxBatch * ppu * 4 : 0;
-  const int64_t f16 = kv->mx() ? (int64_t)ppu * kKvPage * c.n_kv_heads * c.head_dim * 2 : 0;
+  const int64_t f16 = kv->mx() ? (int64_t)std::min(ppu, kv->n_pages) * kKvPage * c.n_kv_heads * c.head_dim * 2 : 0;  // what one user can hold
   const int64_t sz[kKvMem] = {cache, kv->mx() ? 0 : cache, rope, rope, pacc, pml, tab, app, f16, f16, app_tab};
   for (int i = 0; i < kKvMem; ++i) {
     if (sz[i] == 0) continue;
