@@ -167,7 +167,7 @@ kf_status kf_stage_set_stream(kf_stage* stage, void* hip_stream);
  *               fp16 activations: from batch 2 the decode residual copy, SwiGLU output and
  *               merged attention output; in prefill the normalised rows, queries, attention
  *               output and SwiGLU output) reached 65520 in magnitude and was stored as
- *               infinity; or a logit was NaN (skipped by the argmax and the log probabilities; see
+ *               infinity (in an MXFP4 cache as 49152, and a NaN as 0); or a logit was NaN (skipped by the argmax and the log probabilities; see
  *               kf_head_argmax and kf_head_logprobs).
  * The message (kf_last_error) names every condition that occurred.
  */

@@ -774,7 +774,8 @@ kf_status kf_stage_sync(kf_stage* s) {
     std::string msg;
     if (flag & kErrToken) msg += "a token id was outside [0, vocab) (its hidden row or log probability was set to NaN); ";
     if (flag & kErrF16Range)
-      msg += "an activation, key or value held in fp16 reached 65520 in magnitude (stored as infinity); ";
+      msg += "an activation, key or value held in fp16 reached 65520 in magnitude (stored as infinity; in an MXFP4 cache as "
+             "49152, and a NaN as 0); ";
     if (flag & kErrNaNLogit) msg += "a logit was NaN (skipped by the argmax; a row of NaN logits gave token -1); ";
     msg.resize(msg.size() - 2);
     return fail((flag & kErrToken) ? KF_EINVAL : KF_ERANGE, "%s", msg.c_str());

@@ -1,9 +1,9 @@
-"""What an MXFP4 cache keeps beside its pages."""
+"""What an MXFP4 cache keeps beside its pages, and what is said of values that do not fit."""
 import pytest
 
 import synth
 from tests.helpers import SeededModel
-from tests.test_gpu_cache import bare_stage
+from tests.test_gpu_cache import bare_stage, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -57,4 +57,18 @@ def test_prefill_up_to_the_pools_last_page(torch, st):
     g.sync()
     for kv in (small, own):
         kv.close()
+    g.close()
+
+
+def test_what_a_4bit_cache_stored_is_said(torch, st):
+    """The range error says what a value became: an infinity, and in an MXFP4 cache 49152 or, a NaN, 0."""
+    g = bare_stage(st, 1, 64)
+    kv = g.kv(1, 64, dtype="mxfp4")
+    k = torch.from_numpy(rows(1, 1, 1, 64)).cuda()
+    k[0, 0, 3] = float("nan")
+    kv.write(0, 0, 0, k, k)
+    with pytest.raises(st.KFError) as e:
+        g.sync()
+    assert e.value.status == 3 and "49152" in e.value.message and "NaN" in e.value.message
+    kv.close()
     g.close()
