@@ -1676,6 +1676,7 @@ static kf_status logprob_launch(kf_stage* s, int rows, const LogprobParams& all)
     LogprobParams p = all;
     p.values = values;
     p.logits += r0 * p.stride;
+    if (p.row_scale) p.row_scale += r0;
     if (p.targets) p.targets += r0, p.logprob += r0;
     if (p.entropy) p.entropy += r0;
     if (p.top) p.top_ids += r0 * p.top, p.top_logprobs += r0 * p.top;
