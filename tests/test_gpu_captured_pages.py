@@ -193,3 +193,67 @@ def test_a_second_capture_finds_what_the_first_lent(torch, st, dtype):
         check(kv, 0, 0, 0, *y_held)
         check(kv, 0, 1, 0, *other_held)
         check(kv, 0, 2, 0, *y_held)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "mxfp4"])
+def test_captured_decode_and_prefill_that_take_pages(torch, st, dtype):
+    """Steps and chunks that take pages while they are captured, on a paged cache, give at every replay, and in eager
+    calls made before the first one, what they give on a reserved cache; the other users' pages stay as they are."""
+    import synth
+    from tests.helpers import SeededModel
+    shape = synth.SHAPE_TINY
+    g = st.Stage(shape, 0, 2, SeededModel(shape, 98).layer)
+    g.set_flags(st.KF_STAGE_ORDERED)
+    paged, flat = g.kv(4, 320, 14, dtype=dtype), g.kv(4, 320, dtype=dtype)
+    side = torch.cuda.Stream()
+    h = [torch.from_numpy(synth.hidden_states(98, synth.STREAM_PREFILL_HIDDEN, i, n, shape.hidden)).cuda()
+         for i, n in enumerate((64, 64, 100, 2, 128))]
+    out = [torch.empty_like(x) for x in h]
+    pad = torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    g.set_stream(side)
+
+    def chunk(kv):
+        return g.prefill(kv, 2, 0, hidden=h[2], out=out[2], noalloc=True)
+
+    def step(kv):
+        return g.decode(kv, [0, 1], [64, 64], hidden=h[3], out=out[3])
+
+    with torch.cuda.stream(side):
+        for kv in (paged, flat):
+            for u in (3, 0, 1):  # user 3 holds the pool's first pages
+                g.prefill(kv, u, 0, hidden=h[4] if u == 3 else h[u])
+        want = chunk(flat).clone(), step(flat).clone()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            chunk(paged)
+            step(paged)
+            pad.add_(0)
+        assert paged.pages() == (14, 6) and [paged.len(u) for u in range(4)] == [65, 65, 100, 128]
+        for u in (0, 1):
+            paged.set_len(u, 64)
+        paged.set_len(2, 0)
+        eager = chunk(paged).clone(), step(paged).clone()
+        assert all(torch.equal(a, b) for a, b in zip(eager, want))
+        for i in range(3):
+            for o in out:
+                o.zero_()
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(out[2], want[0]) and torch.equal(out[3], want[1]), i
+            for u in range(4):
+                for l in (0, 1):
+                    n = flat.len(u)
+                    assert all(torch.equal(a, b) for a, b in zip(paged.read(l, u, 0, n), flat.read(l, u, 0, n))), (i, u, l)
+            if i == 1:  # moved to other pages, by a fork that goes on writing
+                paged.fork(0, 2)
+                paged.set_len(2, 0)
+                paged.set_len(1, 0)
+                g.prefill(paged, 2, 0, hidden=h[2])
+                g.prefill(paged, 1, 0, hidden=h[1])
+                paged.set_len(1, 65)
+    g.sync()
+    for kv in (paged, flat):
+        kv.close()
+    g.close()
