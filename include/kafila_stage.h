@@ -167,8 +167,8 @@ kf_status kf_stage_set_stream(kf_stage* stage, void* hip_stream);
  *               fp16 activations: from batch 2 the decode residual copy, SwiGLU output and
  *               merged attention output; in prefill the normalised rows, queries, attention
  *               output and SwiGLU output) reached 65520 in magnitude and was stored as
- *               infinity (in an MXFP4 cache as 49152, and a NaN as 0); or a logit was NaN (skipped by the argmax and the log probabilities; see
- *               kf_head_argmax and kf_head_logprobs).
+ *               infinity (in an MXFP4 cache as 49152, and a NaN as 0); or a logit was NaN (skipped by
+ *               the argmax and the log probabilities; see kf_head_argmax and kf_head_logprobs).
  * The message (kf_last_error) names every condition that occurred.
  */
 kf_status kf_stage_sync(kf_stage* stage);
@@ -433,6 +433,8 @@ kf_status kf_head_argmax(kf_stage* stage, int32_t rows, const void* hidden_dev, 
  * The logits of up to 256 rows stay in a workspace of the stage (4 rows for calls of up
  * to 4, 64 up to 64), allocated by the first call that needs it and kept; KF_ENOMEM
  * where not even 4 rows can be had, which includes a first call under graph capture.
+ * More than four bf16 rows (where the matrix holds the gain) take logits of plain fp32 sums, off by some
+ * 4e-7 of their size; kf_head_logits' own are off by 1e-7.
  * Vocabularies up to 2^20 (else KF_EUNSUPPORTED).  Head stages only (else KF_ESTATE).
  */
 #define KF_MAX_TOP 32

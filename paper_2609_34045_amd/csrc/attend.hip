@@ -214,7 +214,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const P p) {
   if constexpr (STEP) {
     if (page0 + pages == (len + kKvPage - 1) / kKvPage) {
       if (wave < 2) append<HD>(p, b, g, wave == 1, lane);
-      // one workgroup reads the page, and its loads follow: the waves' stores are waited for, and no other CU has its lines
+      // One workgroup reads the page.  Its waves share one vector cache, which takes their stores and loads in order: behind
+      // the barrier a load finds what the other waves stored before it, and no wave waits for its stores' way to memory.
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");

@@ -67,8 +67,8 @@ __device__ __forceinline__ int64_t kv_offset(const KvPages& kp, int user, int g,
 // sign.  With that range every stored value is an fp16 number.  K's exponents are bytes
 // e + 127, of which the convert instruction's fp32 scale is made by a shift.  V's are
 // 2^e in fp16: a register of V operands holds two positions, so the products with their
-// two scales are one packed instruction where the pair lies ready (1/32 more bytes, a third
-// fewer instructions in the attention's loop than with bytes that each lane expands).
+// two scales are one packed instruction where the pair lies ready, at 1/32 more bytes
+// (of bytes each lane would have to expand two a pair).
 // Codes and exponents lie in the order in which the attention's lanes take them
 // (mx_* below), so that each of its loads is 16 contiguous bytes a lane.
 constexpr int kMxBlock = 32;
