@@ -129,3 +129,20 @@ def test_an_infinite_value_or_key_shows_in_its_place_only(torch, st, hd, lens):
             assert np.all((np.abs(got[b] - w) <= tol)[:4]), (b, m)
     kv.close()
     g.close()
+
+
+@pytest.mark.parametrize("cache", ["mxfp4", "f16"])
+@pytest.mark.parametrize("n", [3, 700])
+def test_an_infinite_query_gives_nan_in_its_head_only(torch, st, cache, n):
+    g = bare_stage(st, 2, 128, group=3)
+    kv = g.kv(1, n, dtype=cache)
+    kv.write(0, 0, 0, on(rows(1, n, 2, 128)), on(rows(2, n, 2, 128)))
+    q = on(rows(3, 2, 6, 128))
+    clean = kv.attend(0, [0, 0], [n, 2], q)
+    q[0, 4, 100], q[1, 0, 0] = float("inf"), -float("inf")
+    got = kv.attend(0, [0, 0], [n, 2], q)
+    bad = torch.zeros(2, 6, dtype=torch.bool, device="cuda")
+    bad[0, 4] = bad[1, 0] = True
+    assert torch.isnan(got[bad]).all() and torch.equal(got[~bad], clean[~bad])
+    kv.close()
+    g.close()
