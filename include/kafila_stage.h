@@ -51,7 +51,8 @@ extern "C" {
                                for kf_head_logits / kf_head_argmax with hidden_dev NULL.
                             Calls added since leave the others as they are: kf_kv_create_typed,
                             kf_kv_format, kf_kv_copy, kf_kv_fork, kf_kv_attend,
-                            kf_head_logprobs, kf_logits_logprobs */
+                            kf_head_logprobs, kf_logits_logprobs, kf_kv_attend_tree,
+                            kf_kv_accept */
 #define KF_KV_PAGE 64     /* positions per KV cache page */
 #define KF_MAX_BATCH 4
 
@@ -319,6 +320,36 @@ kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n);
  */
 kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* users, const int32_t* lens,
                        const void* q_dev, kf_dtype io, void* out_dev);
+
+/*
+ * Attention of drafted tokens, each with its own branch of a tree of continuations (one
+ * step of speculative decoding, verified in one pass).  Tree b has nodes[b] tokens of users[b],
+ * whose keys and values lie at positions lens[b] + i (kf_kv_write them there first); token i
+ * attends to positions [0, lens[b]), to itself and to its ancestors.
+ *   trees : 1..KF_MAX_BATCH; users may repeat; nodes[b] 0..KF_MAX_NODES (0: no rows)
+ *   parents_dev int32 [sum of nodes] : the parent of each token within its tree, an earlier token;
+ *           -1 where it follows position lens[b] - 1; -2 for a row that only pads the tree, which
+ *           gives zeros and which no token sees (a token that names it as its parent sees itself and what lies
+ *           before the tree).  Any other value counts as -1.
+ *   q_dev, out_dev : [sum of nodes, nq, hd] in io, tree after tree; as for kf_kv_attend
+ * Queries and probabilities keep 22 bits for KF_F32 and KF_F16; for KF_BF16 the probabilities keep 11.  A
+ * position that a token does not see does not reach it, whatever it holds.  KF_ERANGE for positions beyond max_ctx or the pages the user holds.
+ * The splits' partial results use the cache's own workspace, which kf_kv_attend and decode use too.
+ * Changes nothing in the cache.  Enqueued on the stage's stream.
+ */
+#define KF_MAX_NODES 256
+kf_status kf_kv_attend_tree(kf_kv* kv, int32_t layer, int32_t trees, const int32_t* users, const int32_t* lens,
+                            const int32_t* nodes, const int32_t* parents_dev, const void* q_dev, kf_dtype io,
+                            void* out_dev);
+
+/*
+ * The accepted tokens of a tree become context: position len + nodes[i] of the user moves to
+ * len + i, for i < n, in every layer the stage holds, exactly as it is held; the user's length becomes len + n, and the pages
+ * past it are given back.  nodes: host array, ascending, in [0, KF_MAX_NODES); n 0..KF_MAX_NODES (0: the
+ * length alone).  KF_ERANGE for positions beyond max_ctx or the pages the user holds; a
+ * page that other users hold too is copied first, as for any write (KF_ENOMEM; KF_ESTATE under graph capture).
+ */
+kf_status kf_kv_accept(kf_kv* kv, int32_t user, int32_t len, int32_t n, const int32_t* nodes);
 
 /*
  * Forward one token for each of `batch` (1..KF_MAX_BATCH) users (decode): the

@@ -423,4 +423,46 @@ struct PageCopies {
 hipError_t launch_page_copies(const CacheRef& c, const PageCopies& copies, int layers, const KvTable& table,
                               const KvTableUpdate& u, hipStream_t s);
 
+// Attention of trees of drafted tokens over one layer of a cache (tree.hip).
+constexpr int kMaxNodes = 256;  // tokens of a tree
+struct TreeOf {
+  int user, len, nodes;  // the tree's tokens lie at positions [len, len + nodes) of the user
+  int row0;              // its first row of q, parents and out
+  // set by plan_trees: column tiles per KV head, key splits and 64-key blocks of each, workgroups of the tree, and the
+  // first of its splits x nodes rows of partials (where there is more than one split)
+  int tiles, splits, blocks, wgs, part0;
+};
+struct TreeParams {
+  const void* q;           // [rows][nq][hd] rotated queries, of type io
+  void* out;               // the same, of type io (0 fp32, 1 bf16, 2 fp16: the kf_dtype values)
+  int io;
+  const int32_t* parents;  // [rows]: each token's parent within its tree, -1 for none, -2 for a row that only pads
+  const uint16_t *kc, *vc; // layer base of an fp16 cache
+  const uint8_t* rec;      // or of an MXFP4 cache
+  KvPages kv;
+  int nq, nkv, rows, trees;
+  float scale_log2;        // log2(e) / sqrt(hd)
+  float *part_acc, *part_ml;
+  TreeOf tree[kMaxBatch];
+};
+// part_rows: rows of nq heads that part_acc and part_ml hold.
+void plan_trees(TreeParams& p, int n_cu, int64_t part_rows);
+hipError_t launch_attn_tree(const TreeParams& p, int hd, hipStream_t s);
+
+// Some of a user's positions, kept in their order (keep.hip): new position i of dst_user is old position list[i] of
+// src_user, for i in [from, n), in every layer; the same user of one cache: in place.
+struct KeepParams {
+  CacheRef dst, src;
+  int dst_user, src_user;
+  const int* list;         // [layers][nkv][n] ascending old positions, or NULL: first + node[i - first] from `first` on
+  int from, n, nkv;
+  int first;
+  uint8_t node[kMaxNodes];
+  float* weights;          // [layers][users][nkv][stride] of both users, or NULL
+  int users;
+  int64_t stride;
+};
+static_assert(kMaxNodes <= 256, "node");
+hipError_t launch_keep(const KeepParams& p, int hd, int layers, hipStream_t s);
+
 }  // namespace kf

@@ -19,6 +19,7 @@
 #include "prefill.h"
 
 using namespace kf;
+static_assert(kMaxNodes == KF_MAX_NODES, "the header states the limit");
 
 // Launch shapes (compile-time; the defaults are the measured best on MI355X).
 // Decode GEMVs take 8 output rows per workgroup by default (the rules below pick
@@ -1267,6 +1268,99 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
   }
   tr.end(KF_K_ATTN);
   KF_HIP(e, "attention launch");
+  return KF_OK;
+}
+
+kf_status kf_kv_attend_tree(kf_kv* kv, int32_t layer, int32_t trees, const int32_t* users, const int32_t* lens,
+                            const int32_t* nodes, const int32_t* parents_dev, const void* q_dev, kf_dtype io,
+                            void* out_dev) {
+  if (!kv) return fail(KF_EINVAL, "kv is NULL");
+  if (trees < 1 || trees > kMaxBatch) return fail(KF_EINVAL, "trees %d outside [1, %d]", trees, kMaxBatch);
+  if (!users || !lens || !nodes) return fail(KF_EINVAL, "users / lens / nodes is NULL");
+  if (io != KF_F32 && io != KF_BF16 && io != KF_F16) return fail(KF_EINVAL, "io dtype");
+  if ((uintptr_t)q_dev % 16) return fail(KF_EINVAL, "the queries are not 16-byte aligned");
+  const kf_stage* s = kv->st;
+  const kf_model_config& c = s->cfg;
+  TreeParams p{};
+  for (int b = 0; b < trees; ++b) {
+    if (nodes[b] < 0 || nodes[b] > kMaxNodes) return fail(KF_EINVAL, "nodes[%d] = %d outside [0, %d]", b, nodes[b], kMaxNodes);
+    if (lens[b] < 0) return fail(KF_EINVAL, "lens[%d] = %d is negative", b, lens[b]);
+    const kf_status st = kv_slice_check(kv, layer, users[b], lens[b], nodes[b]);
+    if (st != KF_OK) return st;
+    const int64_t upto = (int64_t)lens[b] + nodes[b];
+    if (upto > (int64_t)kv->held[users[b]] * kKvPage)
+      return fail(KF_ERANGE, "positions up to %lld of user %d are not in the cache (it holds %d pages)", (long long)upto,
+                  users[b], kv->held[users[b]]);
+    if (nodes[b]) {
+      p.tree[p.trees].user = users[b];
+      p.tree[p.trees].len = lens[b];
+      p.tree[p.trees].nodes = nodes[b];
+      p.tree[p.trees++].row0 = p.rows;
+      p.rows += nodes[b];
+    }
+  }
+  if (!p.trees) return KF_OK;
+  if (!parents_dev || !q_dev || !out_dev) return fail(KF_EINVAL, "parents / queries / output is NULL");
+  const kf_status late = kv_catch_up(kv);
+  if (late != KF_OK) return late;
+  const CacheRef ref = kv->layer_ref(layer);
+  p.q = q_dev;
+  p.out = out_dev;
+  p.io = io;
+  p.parents = parents_dev;
+  if (kv->mx()) {
+    p.rec = ref.k;
+  } else {
+    p.kc = (const uint16_t*)ref.k;
+    p.vc = (const uint16_t*)ref.v;
+  }
+  p.kv = kv->pages();
+  p.nq = c.n_q_heads;
+  p.nkv = c.n_kv_heads;
+  p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c.head_dim));
+  p.part_acc = kv->part_acc;
+  p.part_ml = kv->part_ml;
+  plan_trees(p, s->n_cu, (int64_t)kMaxBatch * kv->max_split);
+  const Tracer tr = kv->st->tracer();
+  tr.begin(KF_K_ATTN);
+  const hipError_t e = launch_attn_tree(p, c.head_dim, s->stream);
+  tr.end(KF_K_ATTN);
+  KF_HIP(e, "tree attention launch");
+  return KF_OK;
+}
+
+kf_status kf_kv_accept(kf_kv* kv, int32_t user, int32_t len, int32_t n, const int32_t* nodes) {
+  if (!kv) return fail(KF_EINVAL, "kv is NULL");
+  kf_status st = kv_slice_check(kv, kv->st->lo, user, len, 0);
+  if (st != KF_OK) return st;
+  if (n < 0 || n > kMaxNodes) return fail(KF_EINVAL, "n %d outside [0, %d]", n, kMaxNodes);
+  if (n && !nodes) return fail(KF_EINVAL, "nodes is NULL");
+  for (int i = 0; i < n; ++i)
+    if (nodes[i] < 0 || nodes[i] >= kMaxNodes || (i && nodes[i] <= nodes[i - 1]))
+      return fail(KF_EINVAL, "nodes[%d] = %d: ascending, in [0, %d)", i, nodes[i], kMaxNodes);
+  const int64_t last = (int64_t)len + (n ? nodes[n - 1] + 1 : 0);
+  if (last > kv->max_ctx) return fail(KF_ERANGE, "positions up to %lld beyond max_ctx %d", (long long)last, kv->max_ctx);
+  if (last > (int64_t)kv->held[user] * kKvPage)
+    return fail(KF_ERANGE, "positions up to %lld of user %d are not in the cache (it holds %d pages)", (long long)last, user,
+                kv->held[user]);
+  int same = 0;  // the first tokens of the tree lie where they belong
+  while (same < n && nodes[same] == same) ++same;
+  if (same < n) {
+    const int64_t from = len + same, upto = len + n;
+    st = kv_grant(kv, 1, &user, &from, &upto);
+    if (st != KF_OK) return st;
+    KeepParams p{};
+    p.dst = p.src = kv->ref();
+    p.dst_user = p.src_user = user;
+    p.from = (int)from;
+    p.n = (int)upto;
+    p.nkv = kv->st->cfg.n_kv_heads;
+    p.first = len;
+    for (int i = 0; i < n; ++i) p.node[i] = (uint8_t)nodes[i];
+    KF_HIP(launch_keep(p, kv->st->cfg.head_dim, kv->layers(), kv->st->stream), "accepted positions launch");
+  }
+  kv_release(kv, user, pages_for(len + n));
+  kv->len[user] = len + n;
   return KF_OK;
 }
 

@@ -34,7 +34,7 @@ EXPORTS = ("kf_abi_version", "kf_last_error", "kf_stage_bytes", "kf_stage_init",
            "kf_stage_profile", "kf_stage_profile_read", "kf_stage_describe", "kf_kv_describe",
            "kf_kv_create_paged", "kf_kv_pages", "kf_stage_set_flags", "kf_stage_get_flags",
            "kf_stage_prefill_noalloc", "kf_kv_create_typed", "kf_kv_format", "kf_kv_copy", "kf_kv_fork",
-           "kf_kv_attend", "kf_head_logprobs", "kf_logits_logprobs")
+           "kf_kv_attend", "kf_head_logprobs", "kf_logits_logprobs", "kf_kv_attend_tree", "kf_kv_accept")
 KV_TYPES = {"f16": 0, "mxfp4": 1}  # kf_kv_type
 PREFILL_SCRATCH_BYTES = 144 << 20  # KF_PREFILL_SCRATCH_BYTES: the no-allocation prefill's workspace limit
 KF_STAGE_ORDERED = 1  # batch-1 decode adds the heads' output projections in a fixed order
@@ -43,6 +43,7 @@ KF_STAGE_ORDERED = 1  # batch-1 decode adds the heads' output projections in a f
 KERNEL_CLASSES = ("prep", "qkv", "attn", "oproj", "gateup", "down", "lmhead", "argmax", "pf_norm", "pf_qkv", "pf_rope",
                   "pf_attn", "pf_oproj", "pf_gateup", "pf_down", "pf_store", "qknorm", "logprob")
 MAX_TOP = 32  # KF_MAX_TOP
+MAX_NODES = 256  # KF_MAX_NODES: tokens of a drafted tree
 
 
 class LogProbs(NamedTuple):
@@ -125,6 +126,8 @@ def load_library(path: str = LIB_PATH):
         "kf_head_logprobs": (I32, [P, I32, VP, I32, VP, VP, VP, I32, VP, VP]),
         "kf_logits_logprobs": (I32, [P, I32, I32, I64, VP, VP, VP, VP, I32, VP, VP]),
         "kf_kv_attend": (I32, [P, I32, I32, I32P, I32P, VP, I32, VP]),
+        "kf_kv_attend_tree": (I32, [P, I32, I32, I32P, I32P, I32P, VP, VP, I32, VP]),
+        "kf_kv_accept": (I32, [P, I32, I32, I32, I32P]),
         "kf_kv_pages": (I32, [P, I32P, I32P]),
         "kf_stage_set_flags": (I32, [P, I32]),
         "kf_stage_get_flags": (I32, [P, I32P]),
@@ -463,28 +466,56 @@ class KV:
         """``dst_user`` continues from the first ``n`` (default: all) positions of ``src_user`` (kf_kv_fork)."""
         _check(self._lib.kf_kv_fork(self.handle, src_user, dst_user, self.len(src_user) if n is None else n), "kf_kv_fork")
 
-    def attend(self, layer: int, users, lens, q, out=None):
-        """Attention of queries ``q`` ([rows, nq, hd] or [rows, nq * hd]; float32, bfloat16 or float16) over the first
-        ``lens[b]`` positions of ``users[b]`` in one layer (kf_kv_attend); the result has q's shape and type."""
+    def _queries(self, n: int, q, out):
+        """(dtype code, output) of ``n`` rows of queries."""
         import torch
-        n, s = len(users), self.stage.shape
-        if len(lens) != n:
-            raise ValueError("users and lens differ in length")
+        s = self.stage.shape
         _require_device(q, "q")
-        if q.dtype not in (torch.float32, torch.bfloat16, torch.float16):
+        io = {torch.float32: KF_F32, torch.bfloat16: KF_BF16, torch.float16: KF_F16}.get(q.dtype)
+        if io is None:
             raise TypeError(f"q must be float32, bfloat16 or float16, not {q.dtype}")
-        io = {torch.float32: KF_F32, torch.bfloat16: KF_BF16, torch.float16: KF_F16}[q.dtype]
         if tuple(q.shape) not in ((n, s.n_q_heads, s.head_dim), (n, s.n_q_heads * s.head_dim)):
             raise ValueError(f"q of shape {tuple(q.shape)} for {n} rows of {s.n_q_heads} heads of {s.head_dim}")
         if out is None:
-            out = torch.empty_like(q)
-        else:
-            _require_device(out, "out")
-            if out.dtype != q.dtype or out.shape != q.shape:
-                raise ValueError("out must have the shape and type of q")
+            return io, torch.empty_like(q)
+        _require_device(out, "out")
+        if out.dtype != q.dtype or out.shape != q.shape:
+            raise ValueError("out must have the shape and type of q")
+        return io, out
+
+    def attend(self, layer: int, users, lens, q, out=None):
+        """Attention of queries ``q`` ([rows, nq, hd] or [rows, nq * hd]; float32, bfloat16 or float16) over the first
+        ``lens[b]`` positions of ``users[b]`` in one layer (kf_kv_attend); the result has q's shape and type."""
+        n = len(users)
+        if len(lens) != n:
+            raise ValueError("users and lens differ in length")
+        io, out = self._queries(n, q, out)
         u, t = (ctypes.c_int32 * max(n, 1))(*users), (ctypes.c_int32 * max(n, 1))(*lens)
         _check(self._lib.kf_kv_attend(self.handle, layer, n, u, t, _ptr(q), io, _ptr(out)), "kf_kv_attend")
         return out
+
+    def attend_tree(self, layer: int, users, lens, nodes, parents, q, out=None):
+        """Attention of trees of drafted tokens (kf_kv_attend_tree): ``nodes[b]`` tokens at positions ``lens[b]`` + i of
+        ``users[b]``; ``parents`` int32 [rows] (-1: none, -2: a row that pads), ``q`` [rows, nq, hd], tree after tree."""
+        import torch
+        n = len(users)
+        if len(lens) != n or len(nodes) != n:
+            raise ValueError("users, lens and nodes differ in length")
+        rows = sum(nodes)
+        io, out = self._queries(rows, q, out)
+        _require_device(parents, "parents")
+        if parents.dtype != torch.int32 or tuple(parents.shape) != (rows,):
+            raise ValueError(f"parents must be int32 [{rows}]")
+        ints = [(ctypes.c_int32 * max(n, 1))(*x) for x in (users, lens, nodes)]
+        _check(self._lib.kf_kv_attend_tree(self.handle, layer, n, *ints, _ptr(parents), _ptr(q), io, _ptr(out)),
+               "kf_kv_attend_tree")
+        return out
+
+    def accept(self, user: int, length: int, nodes):
+        """Tokens ``nodes`` (ascending) of the tree behind ``length`` positions of ``user`` become positions ``length`` + i,
+        and its length ``length`` + len(nodes) (kf_kv_accept)."""
+        n = len(nodes)
+        _check(self._lib.kf_kv_accept(self.handle, user, length, n, (ctypes.c_int32 * max(n, 1))(*nodes)), "kf_kv_accept")
 
     def describe(self) -> dict:
         owner, mu, mc = ctypes.c_void_p(), ctypes.c_int32(), ctypes.c_int32()

@@ -245,3 +245,17 @@ def test_kernel_classes_match_the_header():
     names = re.findall(r"KF_K_([A-Z_]+)\s*=\s*(\d+),", text)
     for name, idx in names:
         assert stage.KERNEL_CLASSES[int(idx)] == name.lower(), name
+
+
+def test_trees_and_accepted_paths_reject_before_touching_the_device(lib):
+    one = (ctypes.c_int32 * 1)(1)
+    P = ctypes.c_void_p
+    assert lib.kf_kv_attend_tree(None, 0, 1, one, one, one, P(16), P(16), 0, P(16)) == 1
+    assert lib.kf_kv_accept(None, 0, 0, 1, one) == 1
+
+
+def test_limits_match_the_header():
+    from paper_2609_34045_amd import stage
+    text = open(os.path.join(ROOT, "include", "kafila_stage.h")).read()
+    for name, value in (("KF_MAX_NODES", stage.MAX_NODES), ("KF_MAX_TOP", stage.MAX_TOP)):
+        assert int(re.search(r"#define " + name + r" (\d+)", text).group(1)) == value
