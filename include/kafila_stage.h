@@ -52,7 +52,8 @@ extern "C" {
                             Calls added since leave the others as they are: kf_kv_create_typed,
                             kf_kv_format, kf_kv_copy, kf_kv_fork, kf_kv_attend,
                             kf_head_logprobs, kf_logits_logprobs, kf_kv_attend_tree,
-                            kf_kv_accept */
+                            kf_kv_accept, kf_kv_track, kf_kv_weigh, kf_kv_weights,
+                            kf_kv_set_weights, kf_kv_evict */
 #define KF_KV_PAGE 64     /* positions per KV cache page */
 #define KF_MAX_BATCH 4
 
@@ -350,6 +351,48 @@ kf_status kf_kv_attend_tree(kf_kv* kv, int32_t layer, int32_t trees, const int32
  * page that other users hold too is copied first, as for any write (KF_ENOMEM; KF_ESTATE under graph capture).
  */
 kf_status kf_kv_accept(kf_kv* kv, int32_t user, int32_t len, int32_t n, const int32_t* nodes);
+
+/*
+ * From now on the cache adds up the attention weight of every position: for each layer and KV head,
+ * the sum of the probabilities that queries of its group's heads gave the position, in fp32.
+ * Added are every row of a decode step, the last `window` (0..KF_MAX_WEIGH_ROWS) tokens of each
+ * prefill chunk, and what kf_kv_weigh is given.  A position that is written anew (decode, prefill,
+ * kf_kv_write) starts at 0; kf_kv_copy and kf_kv_fork copy the weights (0 from an
+ * untracked cache), kf_kv_accept and kf_kv_evict move them with their positions, and kf_kv_set_len leaves them.
+ * The first call allocates 4 bytes per layer, KV head and position of max_ctx of every user, and once more of one user
+ * (KF_ENOMEM; KF_ESTATE under graph capture), and the weights start at 0; later calls set the window alone.
+ */
+#define KF_MAX_WEIGH_ROWS 32
+kf_status kf_kv_track(kf_kv* kv, int32_t window);
+
+/*
+ * Add the attention weights of given queries in one held layer of a tracked cache (else KF_ESTATE):
+ * row b attends to positions [0, lens[b]) of users[b], as for kf_kv_attend; users may repeat (a
+ * prompt's last queries, say, each over one position more).  rows 1..KF_MAX_WEIGH_ROWS; lens[b] 0 adds nothing.
+ * A query head whose softmax is not finite (a NaN or an infinity among its query or the keys it sees) adds nothing.
+ * The order of all additions is fixed.  Uses the cache's own workspace, as kf_kv_attend does.  Enqueued on the stage's stream.
+ */
+kf_status kf_kv_weigh(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* users, const int32_t* lens, const void* q_dev,
+                      kf_dtype io);
+
+/* Copy the weights of positions [pos0, pos0 + n) of one layer and user out, [nkv, n], or in (a user that was saved, or
+ * weights of the caller's own).  KF_ESTATE for an untracked cache, KF_ERANGE past max_ctx.  Enqueued on the stage's stream. */
+kf_status kf_kv_weights(const kf_kv* kv, int32_t layer, int32_t user, int32_t pos0, int32_t n, float* weights_dev);
+kf_status kf_kv_set_weights(kf_kv* kv, int32_t layer, int32_t user, int32_t pos0, int32_t n, const float* weights_dev);
+
+/*
+ * Give dst_user `keep` positions of src_user (at most its length, else KF_ERANGE) in place of whatever it
+ * held, and the length keep: in each layer and KV head the first `first`, the last `last` (first + last <= keep)
+ * and, of those between, the ones of the largest weights, the lower position of two equal ones and a NaN
+ * below every number.  They keep their order, their exact values and their weights; the keys keep the rotation of
+ * the positions they came from.  dst_user may be src_user (in place); else src_user is left as it is.
+ *   kept_dev : int32 [layers held, nkv, keep], the positions kept, ascending; may be NULL
+ * Tracked caches only (else KF_ESTATE).  In a paged cache dst_user gives its pages back and is lent what keep
+ * positions need; in place, pages that other users hold too are copied first (KF_ENOMEM, with nothing
+ * changed, if the pool cannot lend them), and a call under graph capture is KF_ESTATE.  Enqueued on the stage's stream.
+ */
+kf_status kf_kv_evict(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t keep, int32_t first, int32_t last,
+                      int32_t* kept_dev);
 
 /*
  * Forward one token for each of `batch` (1..KF_MAX_BATCH) users (decode): the

@@ -138,7 +138,86 @@ __global__ __launch_bounds__(1024) void weight_keep_kernel(const KeepParams p) {
   }
 }
 
+// Which positions to keep, one workgroup a layer and KV head: the m-th largest weight by its digits, most significant
+// first (a histogram of the weights that agree so far, and where the m-th lies in it), then
+// the positions above it, and of those equal to it the first, in order.
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048;
+__device__ __forceinline__ uint32_t weight_key(float w) {  // ordered as the weights are; a NaN below all
+  const uint32_t u = __float_as_uint(w + 0.f);
+  return w != w ? 0u : u >> 31 ? ~u : u | 0x80000000u;
+}
+__global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectParams p) {
+  __shared__ int hist[kBins];
+  __shared__ int sums[kSelectWaves];
+  __shared__ int found[2];
+  __shared__ uint32_t counts[2][kSelectWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const float* w = p.weights + blockIdx.y * p.layer + blockIdx.x * p.head;
+  int* list = p.list + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * p.keep;
+  const int lo = p.first, hi = p.len - p.last, m = p.keep - p.first - p.last;
+  for (int i = tid; i < p.first; i += kSelectThreads) list[i] = i;
+  for (int i = tid; i < p.last; i += kSelectThreads) list[p.keep - p.last + i] = hi + i;
+  if (m == 0) return;
+  uint32_t prefix = 0, known = 0;
+  int need = m;  // of the weights that have the prefix, the need-th largest is the one looked for
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
+    for (int b = tid; b < kBins; b += kSelectThreads) hist[b] = 0;
+    __syncthreads();
+    for (int i = lo + tid; i < hi; i += kSelectThreads) {
+      const uint32_t k = weight_key(w[i]);
+      if ((k & known) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1);
+    }
+    __syncthreads();
+    // thread t holds bins kBins - 1 - 2 t and the next lower
+    const int a = hist[kBins - 1 - 2 * tid], b = hist[kBins - 2 - 2 * tid];
+    int upto = a + b;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    for (int i = 0; i < wave; ++i) upto += sums[i];
+    const int before = upto - a - b;
+    if (before < need && need <= upto) {
+      const bool second = before + a < need;
+      found[0] = kBins - 1 - 2 * tid - second;
+      found[1] = need - before - (second ? a : 0);
+    }
+    __syncthreads();
+    prefix |= (uint32_t)found[0] << shift;
+    known |= (uint32_t)(bins - 1) << shift;
+    need = found[1];
+    __syncthreads();
+  }
+  int above = 0, equal = 0;  // before this chunk
+  for (int c0 = lo, turn = 0; c0 < hi; c0 += kSelectThreads, turn ^= 1) {
+    const int i = c0 + tid;
+    const uint32_t k = i < hi ? weight_key(w[i]) : 0u;
+    const uint64_t gt = __ballot(i < hi && k > prefix), eq = __ballot(i < hi && k == prefix), below = (1ull << lane) - 1;
+    if (lane == 0) counts[turn][wave] = (uint32_t)__popcll(gt) | (uint32_t)__popcll(eq) << 16;
+    __syncthreads();
+    uint32_t mine = 0, all = 0;
+#pragma unroll
+    for (int x = 0; x < kSelectWaves; ++x) {
+      all += counts[turn][x];
+      if (x < wave) mine += counts[turn][x];
+    }
+    const int g = above + (int)(mine & 0xffff) + __popcll(gt & below), e = equal + (int)(mine >> 16) + __popcll(eq & below);
+    if ((gt >> lane & 1) || ((eq >> lane & 1) && e < need)) list[p.first + g + min(e, need)] = i;
+    above += (int)(all & 0xffff);
+    equal += (int)(all >> 16);
+  }
+}
+
 // ------------------------------------------------------------------ launchers
+hipError_t launch_select(const SelectParams& p, int nkv, int layers, hipStream_t s) {
+  if (p.keep <= 0) return hipSuccess;
+  hipLaunchKernelGGL(select_kernel, dim3(nkv, layers), dim3(kSelectThreads), 0, s, p);
+  return hipGetLastError();
+}
 template <int HD>
 static hipError_t keep(const KeepParams& p, int layers, hipStream_t s) {
   const bool in_place = p.dst.k == p.src.k && p.dst_user == p.src_user;

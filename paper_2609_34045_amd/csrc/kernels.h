@@ -465,4 +465,51 @@ struct KeepParams {
 static_assert(kMaxNodes <= 256, "node");
 hipError_t launch_keep(const KeepParams& p, int hd, int layers, hipStream_t s);
 
+// The positions that eviction keeps: of each layer's and KV head's len weights the first `first`, the last `last` and the
+// keep - first - last largest of the others, the lower position first among equal ones and a NaN below all;
+// list[layer][head][keep], ascending.
+struct SelectParams {
+  const float* weights;  // of layer 0's head 0 of the user
+  int64_t layer, head;   // strides
+  int len, keep, first, last;
+  int* list;
+};
+hipError_t launch_select(const SelectParams& p, int nkv, int layers, hipStream_t s);
+
+// Attention weights of cached positions (weigh.hip).
+constexpr int kMaxWeighRows = 32;  // rows of a call
+struct WeighUser {
+  int user, row0, rows;  // rows [row0, row0 + rows) are its
+  int len;               // the most positions that one of them attends to
+  int fresh;             // positions from here on have no weight yet: theirs is set, not added to
+  int splits;            // set by the launcher
+};
+struct WeighParams {
+  const void* q;  // [..][nq][hd] rotated queries
+  int q_type;     // 0 fp32, 1 bf16, 2 fp16 (the kf_dtype values)
+  const uint16_t* kc;  // layer base of an fp16 cache
+  const uint8_t* rec;  // or of an MXFP4 cache
+  KvPages kv;
+  int nq, nkv;
+  float scale_log2;
+  float* weights;  // [user][nkv][stride] of the layer
+  int64_t stride;
+  float* part;     // workspace: [row][nq][max_splits][2]
+  // queries as projected, whose norm (gains gq, eps) and rotation to position len - 1 are due; gq NULL: none
+  const uint16_t* gq;
+  const float *rope_cos, *rope_sin;
+  float eps;
+  int users;
+  WeighUser user[kMaxWeighRows];
+  int row[kMaxWeighRows], len[kMaxWeighRows];  // of each row, user after user: its row of q, and its positions
+  int pages, max_splits;                       // set by the launcher: pages per split, splits of a row in `part`
+};
+hipError_t launch_weigh(WeighParams p, int hd, int n_cu, int64_t part_floats, hipStream_t s);
+// Weights of n positions in every layer and KV head, rows `head` and layers `layer` values apart; src.p NULL: zeros.
+struct WeightRows {
+  float* p;
+  int64_t layer, head;
+};
+hipError_t launch_weights_move(const WeightRows& dst, const WeightRows& src, int n, int nkv, int layers, hipStream_t s);
+
 }  // namespace kf

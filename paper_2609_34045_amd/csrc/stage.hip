@@ -19,7 +19,7 @@
 #include "prefill.h"
 
 using namespace kf;
-static_assert(kMaxNodes == KF_MAX_NODES, "the header states the limit");
+static_assert(kMaxNodes == KF_MAX_NODES && kMaxWeighRows == KF_MAX_WEIGH_ROWS, "the header states the limits");
 
 // Launch shapes (compile-time; the defaults are the measured best on MI355X).
 // Decode GEMVs take 8 output rows per workgroup by default (the rules below pick
@@ -221,6 +221,15 @@ struct kf_kv {
     return KvPages{append_table, ppu, (int64_t)st->cfg.n_kv_heads * kKvPage * st->cfg.head_dim};
   }
   uint16_t *f16_k = nullptr, *f16_v = nullptr;
+  // A tracked cache (kf_kv_track): each position's attention weight, [layers][max_users][nkv][max_ctx], what an eviction
+  // keeps, [layers][nkv][max_ctx], and how many of a prefill chunk's last queries count.
+  float* weights = nullptr;
+  int* kept = nullptr;
+  int window = 0;
+  WeightRows weight_rows(int layer, int user, int pos) const {
+    const int64_t head = max_ctx, lay = head * st->cfg.n_kv_heads * max_users;
+    return WeightRows{weights ? weights + (layer - st->lo) * lay + (int64_t)user * st->cfg.n_kv_heads * head + pos : nullptr, lay, head};
+  }
   int64_t page_stride, layer_stride;  // elements
   std::vector<int> len;
   KvPages pages() const { return KvPages{table, ppu, page_stride}; }
@@ -951,7 +960,8 @@ kf_status kf_kv_pages(const kf_kv* kv, int32_t* total, int32_t* free_pages) {
 kf_status kf_kv_destroy(kf_kv* kv) {
   if (!kv) return fail(KF_EINVAL, "kv is NULL");
   hipStreamSynchronize(kv->st->stream);
-  void* mem[] = {kv->k, kv->v, kv->rcos, kv->rsin, kv->part_acc, kv->part_ml, kv->table, kv->append, kv->append_table, kv->f16_k, kv->f16_v};
+  void* mem[] = {kv->k, kv->v, kv->rcos, kv->rsin, kv->part_acc, kv->part_ml, kv->table, kv->append, kv->append_table, kv->f16_k, kv->f16_v,
+                 kv->weights, kv->kept};
   for (void* m : mem)
     if (m) hipFree(m);
   kv->st->live_kv--;
@@ -995,6 +1005,23 @@ static kf_status kv_slice_check(const kf_kv* kv, int layer, int user, int pos0, 
   return KF_OK;
 }
 
+// Positions that are written anew have no attention weight yet (tracked caches).
+static kf_status weights_anew(kf_kv* kv, int layer, int layers, int user, int pos0, int n) {
+  if (!kv->weights || n <= 0) return KF_OK;
+  KF_HIP(launch_weights_move(kv->weight_rows(layer, user, pos0), WeightRows{}, n, kv->st->cfg.n_kv_heads, layers, kv->st->stream),
+         "weights launch");
+  return KF_OK;
+}
+// Those that are copied, the ones they had.
+static kf_status weights_copied(kf_kv* dst, int dst_user, const kf_kv* src, int src_user, int pos0, int n) {
+  if (!dst->weights || n <= 0) return KF_OK;
+  const int lo = dst->st->lo;
+  KF_HIP(launch_weights_move(dst->weight_rows(lo, dst_user, pos0), src->weight_rows(lo, src_user, pos0), n, dst->st->cfg.n_kv_heads,
+                             dst->layers(), dst->st->stream),
+         "weights launch");
+  return KF_OK;
+}
+
 kf_status kf_kv_write(kf_kv* kv, int32_t layer, int32_t user, int32_t pos0, int32_t n, const void* k_dev,
                       const void* v_dev, kf_dtype dtype) {
   if (!kv) return fail(KF_EINVAL, "kv is NULL");
@@ -1006,6 +1033,8 @@ kf_status kf_kv_write(kf_kv* kv, int32_t layer, int32_t user, int32_t pos0, int3
   const kf_model_config& c = kv->st->cfg;
   const int64_t from = pos0, upto = from + n;
   st = kv_grant(kv, 1, &user, &from, &upto);
+  if (st != KF_OK) return st;
+  st = weights_anew(kv, layer, 1, user, pos0, n);
   if (st != KF_OK) return st;
   if (kv->mx()) {
     KF_HIP(launch_mx_write(kv->layer_ref(layer), user, pos0, k_dev, v_dev, (int)dtype, n, kv->st->err_flag, kv->st->stream),
@@ -1062,7 +1091,7 @@ kf_status kf_kv_copy(kf_kv* dst, int32_t dst_user, const kf_kv* src, int32_t src
   KF_HIP(launch_cache_copy(dst->ref(), dst_user, src->ref(), src_user, pos0, n, dst->layers(), dst->st->err_flag,
                            dst->st->stream),
          "kv_copy launch");
-  return KF_OK;
+  return weights_copied(dst, dst_user, src, src_user, pos0, n);
 }
 
 kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n) {
@@ -1077,7 +1106,7 @@ kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n) {
     KF_HIP(launch_cache_copy(kv->ref(), dst_user, kv->ref(), src_user, 0, n, kv->layers(), kv->st->err_flag, st),
            "kv_fork launch");
     kv->len[dst_user] = n;
-    return KF_OK;
+    return weights_copied(kv, dst_user, kv, src_user, 0, n);
   }
   if (capturing(kv->st))  // each replay would take the destination's own pages out of its table again
     return fail(KF_ESTATE, "users of a paged cache cannot be forked under graph capture");
@@ -1100,6 +1129,174 @@ kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n) {
     KF_HIP(launch_kv_table_share(kv->kv_table(), src_user * kv->ppu + same, dst_user * kv->ppu + same, pages - same, st),
            "page table update");
   kv->len[dst_user] = n;
+  return weights_copied(kv, dst_user, kv, src_user, 0, n);
+}
+
+// ------------------------------------------------------------------ attention weights and eviction
+kf_status kf_kv_track(kf_kv* kv, int32_t window) {
+  if (!kv) return fail(KF_EINVAL, "kv is NULL");
+  if (window < 0 || window > kMaxWeighRows) return fail(KF_EINVAL, "window %d outside [0, %d]", window, kMaxWeighRows);
+  if (!kv->weights) {
+    if (capturing(kv->st)) return fail(KF_ESTATE, "a cache's first kf_kv_track cannot be captured");
+    const int64_t kept = (int64_t)kv->layers() * kv->st->cfg.n_kv_heads * kv->max_ctx * 4, all = kept * kv->max_users;
+    char *w = nullptr, *k = nullptr;
+    if (hipMalloc((void**)&w, all) != hipSuccess || hipMalloc((void**)&k, kept) != hipSuccess) {
+      (void)hipGetLastError();
+      if (w) hipFree(w);
+      return fail(KF_ENOMEM, "device allocation of %lld bytes of attention weights", (long long)(all + kept));
+    }
+    const hipError_t e = hipMemset(w, 0, all);
+    if (e != hipSuccess) {
+      hipFree(w);
+      hipFree(k);
+      return fail(KF_EDEVICE, "attention weights: %s", hipGetErrorString(e));
+    }
+    kv->weights = (float*)w;
+    kv->kept = (int*)k;
+    kv->bytes += all + kept;
+  }
+  kv->window = window;
+  return KF_OK;
+}
+
+static kf_status weights_check(const kf_kv* kv, int layer, int user, int pos0, int n, const float* w) {
+  if (!kv) return fail(KF_EINVAL, "kv is NULL");
+  const kf_status st = kv_slice_check(kv, layer, user, pos0, n);
+  if (st != KF_OK) return st;
+  if (!kv->weights) return fail(KF_ESTATE, "the cache is not tracked");
+  if (n && !w) return fail(KF_EINVAL, "weights is NULL");
+  return KF_OK;
+}
+kf_status kf_kv_weights(const kf_kv* kv, int32_t layer, int32_t user, int32_t pos0, int32_t n, float* weights_dev) {
+  const kf_status st = weights_check(kv, layer, user, pos0, n, weights_dev);
+  if (st != KF_OK) return st;
+  KF_HIP(launch_weights_move(WeightRows{weights_dev, 0, n}, kv->weight_rows(layer, user, pos0), n, kv->st->cfg.n_kv_heads, 1,
+                             kv->st->stream),
+         "weights launch");
+  return KF_OK;
+}
+kf_status kf_kv_set_weights(kf_kv* kv, int32_t layer, int32_t user, int32_t pos0, int32_t n, const float* weights_dev) {
+  const kf_status st = weights_check(kv, layer, user, pos0, n, weights_dev);
+  if (st != KF_OK) return st;
+  KF_HIP(launch_weights_move(kv->weight_rows(layer, user, pos0), WeightRows{const_cast<float*>(weights_dev), 0, n}, n,
+                             kv->st->cfg.n_kv_heads, 1, kv->st->stream),
+         "weights launch");
+  return KF_OK;
+}
+
+// Adds the weights of `rows` queries of one layer, row b's over positions [0, lens[b]) of users[b]; those from fresh[b]
+// on (the same for every row of a user) have none yet.  p holds the queries.
+static kf_status weigh_rows(kf_kv* kv, WeighParams& p, int layer, int rows, const int* users, const int* lens, const int* fresh) {
+  const kf_stage* s = kv->st;
+  const kf_model_config& c = s->cfg;
+  const CacheRef ref = kv->layer_ref(layer);
+  if (kv->mx()) p.rec = ref.k;
+  else p.kc = (const uint16_t*)ref.k;
+  p.kv = kv->pages();
+  p.nq = c.n_q_heads;
+  p.nkv = c.n_kv_heads;
+  p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c.head_dim));
+  p.weights = kv->weight_rows(layer, 0, 0).p;
+  p.stride = kv->max_ctx;
+  p.part = kv->part_acc;
+  p.users = 0;
+  int n = 0;
+  for (int b = 0; b < rows; ++b) {  // users in the order of their first rows
+    bool seen = false;
+    for (int j = 0; j < b; ++j) seen |= users[j] == users[b];
+    if (seen) continue;
+    WeighUser& u = p.user[p.users++];
+    u = WeighUser{users[b], n, 0, 0, fresh ? fresh[b] : kv->max_ctx, 1};
+    for (int j = b; j < rows; ++j) {
+      if (users[j] != users[b]) continue;
+      p.row[n] = j;
+      p.len[n++] = lens[j];
+      u.rows++;
+      u.len = std::max(u.len, lens[j]);
+    }
+  }
+  const Tracer tr = kv->st->tracer();
+  tr.begin(KF_K_ATTN);
+  const hipError_t e = launch_weigh(p, c.head_dim, s->n_cu, (int64_t)kMaxBatch * c.n_q_heads * kv->max_split * c.head_dim, s->stream);
+  tr.end(KF_K_ATTN);
+  KF_HIP(e, "attention weights launch");
+  return KF_OK;
+}
+
+kf_status kf_kv_weigh(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* users, const int32_t* lens, const void* q_dev,
+                      kf_dtype io) {
+  if (!kv) return fail(KF_EINVAL, "kv is NULL");
+  if (rows < 1 || rows > kMaxWeighRows) return fail(KF_EINVAL, "rows %d outside [1, %d]", rows, kMaxWeighRows);
+  if (!users || !lens) return fail(KF_EINVAL, "users / lens is NULL");
+  if (!q_dev) return fail(KF_EINVAL, "queries is NULL");
+  if (io != KF_F32 && io != KF_BF16 && io != KF_F16) return fail(KF_EINVAL, "io dtype");
+  if ((uintptr_t)q_dev % 16) return fail(KF_EINVAL, "the queries are not 16-byte aligned");
+  for (int b = 0; b < rows; ++b) {
+    const kf_status st = kv_slice_check(kv, layer, users[b], 0, lens[b]);
+    if (st != KF_OK) return st;
+    if (lens[b] > (int64_t)kv->held[users[b]] * kKvPage)
+      return fail(KF_ERANGE, "positions up to %d of user %d are not in the cache (it holds %d pages)", lens[b], users[b],
+                  kv->held[users[b]]);
+  }
+  if (!kv->weights) return fail(KF_ESTATE, "the cache is not tracked");
+  const kf_status late = kv_catch_up(kv);
+  if (late != KF_OK) return late;
+  WeighParams p{};
+  p.q = q_dev;
+  p.q_type = io;
+  return weigh_rows(kv, p, layer, rows, users, lens, nullptr);
+}
+
+kf_status kf_kv_evict(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t keep, int32_t first, int32_t last,
+                      int32_t* kept_dev) {
+  if (!kv) return fail(KF_EINVAL, "kv is NULL");
+  for (int u : {src_user, dst_user})
+    if (u < 0 || u >= kv->max_users) return fail(KF_EINVAL, "user %d outside [0, %d)", u, kv->max_users);
+  if (keep < 0 || first < 0 || last < 0) return fail(KF_EINVAL, "negative count");
+  if ((int64_t)first + last > keep) return fail(KF_EINVAL, "first %d and last %d are more than %d", first, last, keep);
+  const int len = kv->len[src_user];
+  if (keep > len) return fail(KF_ERANGE, "%d positions of user %d, which holds %d", keep, src_user, len);
+  if (!kv->weights) return fail(KF_ESTATE, "the cache is not tracked");
+  const bool in_place = src_user == dst_user;
+  kf_status st = KF_OK;
+  if (kv->table) {
+    if (capturing(kv->st))  // which pages a user holds is known when a call is made
+      return fail(KF_ESTATE, "positions of a paged cache cannot be evicted under graph capture");
+    const int64_t upto = keep;
+    int64_t from = first;
+    if (!in_place) {
+      int free_after = (int)kv->free_pages.size();
+      for (int i = 0; i < kv->held[dst_user]; ++i) free_after += kv->refs[kv->host_table[(size_t)dst_user * kv->ppu + i]] == 1;
+      if (pages_for(keep) > free_after)
+        return fail(KF_ENOMEM, "KV pool: %d pages needed, %d free of %d", pages_for(keep), free_after, kv->n_pages);
+      kv_release(kv, dst_user, 0);
+      kv->len[dst_user] = 0;
+      from = upto;
+    }
+    st = kv_grant(kv, 1, &dst_user, &from, &upto);
+    if (st != KF_OK) return st;
+  }
+  if (keep) {
+    const WeightRows w = kv->weight_rows(kv->st->lo, src_user, 0);
+    SelectParams sel{w.p, w.layer, w.head, len, keep, first, last, kept_dev ? kept_dev : kv->kept};
+    KeepParams p{};
+    p.dst = p.src = kv->ref();
+    p.dst_user = dst_user;
+    p.src_user = src_user;
+    p.list = sel.list;
+    p.from = in_place ? first : 0;
+    p.n = keep;
+    p.nkv = kv->st->cfg.n_kv_heads;
+    p.weights = kv->weights;
+    p.users = kv->max_users;
+    p.stride = kv->max_ctx;
+    hipError_t e = hipSuccess;
+    if (keep < len || !in_place || kept_dev) e = launch_select(sel, p.nkv, kv->layers(), kv->st->stream);
+    if (e == hipSuccess && (keep < len || !in_place)) e = launch_keep(p, kv->st->cfg.head_dim, kv->layers(), kv->st->stream);
+    KF_HIP(e, "eviction launch");
+  }
+  kv_release(kv, dst_user, pages_for(keep));
+  kv->len[dst_user] = keep;
   return KF_OK;
 }
 
@@ -1357,6 +1554,9 @@ kf_status kf_kv_accept(kf_kv* kv, int32_t user, int32_t len, int32_t n, const in
     p.nkv = kv->st->cfg.n_kv_heads;
     p.first = len;
     for (int i = 0; i < n; ++i) p.node[i] = (uint8_t)nodes[i];
+    p.weights = kv->weights;
+    p.users = kv->max_users;
+    p.stride = kv->max_ctx;
     KF_HIP(launch_keep(p, kv->st->cfg.head_dim, kv->layers(), kv->st->stream), "accepted positions launch");
   }
   kv_release(kv, user, pages_for(len + n));
@@ -1530,6 +1730,19 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
       }
       tr.end(KF_K_OPROJ);
       KF_HIP(le, "o-proj launch");
+    }
+
+    if (kv->weights) {  // the attention's partials, which the workspace held until here, are merged
+      WeighParams w{};
+      w.q = s->q;
+      if (c.qk_norm) {
+        w.gq = L.g_qn;
+        w.rope_cos = kv->rcos;
+        w.rope_sin = kv->rsin;
+        w.eps = c.rms_eps;
+      }
+      const kf_status wst = weigh_rows(kv, w, l, batch, users, a.len, positions);
+      if (wst != KF_OK) return wst;
     }
 
     GemvParams gu{};
@@ -1960,6 +2173,24 @@ static kf_status prefill_impl(kf_stage* s, kf_kv* kv, int32_t user, int32_t pos0
     pl.out = l == s->hi - 1 ? hidden_out_dev : nullptr;
     pl.out_bf16 = io == KF_BF16;
     KF_HIP(prefill_layer(*ws, pa, pl, tr), "prefill layer");
+    if (kv->weights && kv->window) {  // of the chunk's last queries
+      const int rows = std::min(n, kv->window);
+      int users[kMaxWeighRows], lens[kMaxWeighRows], fresh[kMaxWeighRows];
+      for (int i = 0; i < rows; ++i) {
+        users[i] = user;
+        lens[i] = pos0 + n - rows + i + 1;
+        fresh[i] = pos0;
+      }
+      WeighParams w{};
+      w.q = ws->q + (int64_t)(n - rows) * c.n_q_heads * c.head_dim;
+      w.q_type = KF_F16;
+      const kf_status wst = weigh_rows(kv, w, l, rows, users, lens, fresh);
+      if (wst != KF_OK) return wst;
+    }
+  }
+  if (!kv->window) {
+    const kf_status wst = weights_anew(kv, s->lo, kv->layers(), user, pos0, n);
+    if (wst != KF_OK) return wst;
   }
   kv->len[user] += n;
   return KF_OK;

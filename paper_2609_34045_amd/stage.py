@@ -34,7 +34,8 @@ EXPORTS = ("kf_abi_version", "kf_last_error", "kf_stage_bytes", "kf_stage_init",
            "kf_stage_profile", "kf_stage_profile_read", "kf_stage_describe", "kf_kv_describe",
            "kf_kv_create_paged", "kf_kv_pages", "kf_stage_set_flags", "kf_stage_get_flags",
            "kf_stage_prefill_noalloc", "kf_kv_create_typed", "kf_kv_format", "kf_kv_copy", "kf_kv_fork",
-           "kf_kv_attend", "kf_head_logprobs", "kf_logits_logprobs", "kf_kv_attend_tree", "kf_kv_accept")
+           "kf_kv_attend", "kf_head_logprobs", "kf_logits_logprobs", "kf_kv_attend_tree", "kf_kv_accept",
+           "kf_kv_track", "kf_kv_weigh", "kf_kv_weights", "kf_kv_set_weights", "kf_kv_evict")
 KV_TYPES = {"f16": 0, "mxfp4": 1}  # kf_kv_type
 PREFILL_SCRATCH_BYTES = 144 << 20  # KF_PREFILL_SCRATCH_BYTES: the no-allocation prefill's workspace limit
 KF_STAGE_ORDERED = 1  # batch-1 decode adds the heads' output projections in a fixed order
@@ -44,6 +45,7 @@ KERNEL_CLASSES = ("prep", "qkv", "attn", "oproj", "gateup", "down", "lmhead", "a
                   "pf_attn", "pf_oproj", "pf_gateup", "pf_down", "pf_store", "qknorm", "logprob")
 MAX_TOP = 32  # KF_MAX_TOP
 MAX_NODES = 256  # KF_MAX_NODES: tokens of a drafted tree
+MAX_WEIGH_ROWS = 32  # KF_MAX_WEIGH_ROWS: queries of a weighing call, and of a tracked prefill chunk
 
 
 class LogProbs(NamedTuple):
@@ -128,6 +130,11 @@ def load_library(path: str = LIB_PATH):
         "kf_kv_attend": (I32, [P, I32, I32, I32P, I32P, VP, I32, VP]),
         "kf_kv_attend_tree": (I32, [P, I32, I32, I32P, I32P, I32P, VP, VP, I32, VP]),
         "kf_kv_accept": (I32, [P, I32, I32, I32, I32P]),
+        "kf_kv_track": (I32, [P, I32]),
+        "kf_kv_weigh": (I32, [P, I32, I32, I32P, I32P, VP, I32]),
+        "kf_kv_weights": (I32, [P, I32, I32, I32, I32, VP]),
+        "kf_kv_set_weights": (I32, [P, I32, I32, I32, I32, VP]),
+        "kf_kv_evict": (I32, [P, I32, I32, I32, I32, I32, VP]),
         "kf_kv_pages": (I32, [P, I32P, I32P]),
         "kf_stage_set_flags": (I32, [P, I32]),
         "kf_stage_get_flags": (I32, [P, I32P]),
@@ -466,8 +473,8 @@ class KV:
         """``dst_user`` continues from the first ``n`` (default: all) positions of ``src_user`` (kf_kv_fork)."""
         _check(self._lib.kf_kv_fork(self.handle, src_user, dst_user, self.len(src_user) if n is None else n), "kf_kv_fork")
 
-    def _queries(self, n: int, q, out):
-        """(dtype code, output) of ``n`` rows of queries."""
+    def _query_type(self, n: int, q) -> int:
+        """The dtype code of ``n`` rows of queries."""
         import torch
         s = self.stage.shape
         _require_device(q, "q")
@@ -476,6 +483,12 @@ class KV:
             raise TypeError(f"q must be float32, bfloat16 or float16, not {q.dtype}")
         if tuple(q.shape) not in ((n, s.n_q_heads, s.head_dim), (n, s.n_q_heads * s.head_dim)):
             raise ValueError(f"q of shape {tuple(q.shape)} for {n} rows of {s.n_q_heads} heads of {s.head_dim}")
+        return io
+
+    def _queries(self, n: int, q, out):
+        """(dtype code, output) of ``n`` rows of queries."""
+        import torch
+        io = self._query_type(n, q)
         if out is None:
             return io, torch.empty_like(q)
         _require_device(out, "out")
@@ -516,6 +529,47 @@ class KV:
         and its length ``length`` + len(nodes) (kf_kv_accept)."""
         n = len(nodes)
         _check(self._lib.kf_kv_accept(self.handle, user, length, n, (ctypes.c_int32 * max(n, 1))(*nodes)), "kf_kv_accept")
+
+    def track(self, window: int = 0):
+        """From now on the cache adds up its positions' attention weights: of decode steps, of the last ``window`` tokens of
+        prefill chunks, and of ``weigh`` (kf_kv_track)."""
+        _check(self._lib.kf_kv_track(self.handle, window), "kf_kv_track")
+
+    def weigh(self, layer: int, users, lens, q):
+        """Adds the attention weights of queries ``q`` [rows, nq, hd] over the first ``lens[b]`` positions of ``users[b]`` in
+        one layer (kf_kv_weigh)."""
+        n = len(users)
+        if len(lens) != n:
+            raise ValueError("users and lens differ in length")
+        io = self._query_type(n, q)
+        u, t = (ctypes.c_int32 * max(n, 1))(*users), (ctypes.c_int32 * max(n, 1))(*lens)
+        _check(self._lib.kf_kv_weigh(self.handle, layer, n, u, t, _ptr(q), io), "kf_kv_weigh")
+
+    def weights(self, layer: int, user: int, pos0: int, n: int):
+        """The attention weights of positions [pos0, pos0 + n), float32 [nkv, n]."""
+        import torch
+        w = torch.empty((self.stage.shape.n_kv_heads, max(n, 0)), dtype=torch.float32, device="cuda")
+        _check(self._lib.kf_kv_weights(self.handle, layer, user, pos0, n, _ptr(w)), "kf_kv_weights")
+        return w
+
+    def set_weights(self, layer: int, user: int, pos0: int, weights):
+        """Sets the attention weights of positions from ``pos0`` on: float32 [nkv, n]."""
+        import torch
+        _require_device(weights, "weights")
+        if weights.dtype != torch.float32 or weights.dim() != 2 or weights.shape[0] != self.stage.shape.n_kv_heads:
+            raise ValueError(f"weights must be float32 [{self.stage.shape.n_kv_heads}, n]")
+        _check(self._lib.kf_kv_set_weights(self.handle, layer, user, pos0, weights.shape[1], _ptr(weights)), "kf_kv_set_weights")
+
+    def evict(self, src_user: int, dst_user: int, keep: int, first: int = 0, last: int = 0, kept: bool = False):
+        """``dst_user`` gets ``keep`` positions of ``src_user`` (the same user: in place): the ``first`` and ``last`` ones and
+        the heaviest of the others (kf_kv_evict).  With ``kept``, returns which, int32 [layers, nkv, keep]."""
+        import torch
+        at = None
+        if kept:
+            layers = self.stage.hi - self.stage.lo
+            at = torch.empty((layers, self.stage.shape.n_kv_heads, max(keep, 0)), dtype=torch.int32, device="cuda")
+        _check(self._lib.kf_kv_evict(self.handle, src_user, dst_user, keep, first, last, _ptr(at)), "kf_kv_evict")
+        return at
 
     def describe(self) -> dict:
         owner, mu, mc = ctypes.c_void_p(), ctypes.c_int32(), ctypes.c_int32()

@@ -247,15 +247,21 @@ def test_kernel_classes_match_the_header():
         assert stage.KERNEL_CLASSES[int(idx)] == name.lower(), name
 
 
-def test_trees_and_accepted_paths_reject_before_touching_the_device(lib):
+def test_trees_weights_and_evictions_reject_before_touching_the_device(lib):
     one = (ctypes.c_int32 * 1)(1)
     P = ctypes.c_void_p
     assert lib.kf_kv_attend_tree(None, 0, 1, one, one, one, P(16), P(16), 0, P(16)) == 1
     assert lib.kf_kv_accept(None, 0, 0, 1, one) == 1
+    assert lib.kf_kv_track(None, 0) == 1
+    assert lib.kf_kv_weigh(None, 0, 1, one, one, P(16), 0) == 1
+    assert lib.kf_kv_weights(None, 0, 0, 0, 1, P(16)) == 1
+    assert lib.kf_kv_set_weights(None, 0, 0, 0, 1, P(16)) == 1
+    assert lib.kf_kv_evict(None, 0, 1, 1, 0, 0, None) == 1
 
 
 def test_limits_match_the_header():
     from paper_2609_34045_amd import stage
     text = open(os.path.join(ROOT, "include", "kafila_stage.h")).read()
-    for name, value in (("KF_MAX_NODES", stage.MAX_NODES), ("KF_MAX_TOP", stage.MAX_TOP)):
+    for name, value in (("KF_MAX_NODES", stage.MAX_NODES), ("KF_MAX_TOP", stage.MAX_TOP),
+                        ("KF_MAX_WEIGH_ROWS", stage.MAX_WEIGH_ROWS)):
         assert int(re.search(r"#define " + name + r" (\d+)", text).group(1)) == value
