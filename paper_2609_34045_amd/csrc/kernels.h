@@ -428,7 +428,7 @@ constexpr int kMaxNodes = 256;  // tokens of a tree
 struct TreeOf {
   int user, len, nodes;  // the tree's tokens lie at positions [len, len + nodes) of the user
   int row0;              // its first row of q, parents and out
-  // set by plan_trees: column tiles per KV head, key splits and 64-key blocks of each, workgroups of the tree, and the
+  // set by plan_trees: column tiles per KV head, key splits and pages of each, workgroups of the tree, and the
   // first of its splits x nodes rows of partials (where there is more than one split)
   int tiles, splits, blocks, wgs, part0;
 };
