@@ -359,7 +359,7 @@ kf_status kf_kv_accept(kf_kv* kv, int32_t user, int32_t len, int32_t n, const in
  * prefill chunk, and what kf_kv_weigh is given.  A position that is written anew (decode, prefill,
  * kf_kv_write) starts at 0; kf_kv_copy and kf_kv_fork copy the weights (0 from an
  * untracked cache), kf_kv_accept and kf_kv_evict move them with their positions, and kf_kv_set_len leaves them.
- * The first call allocates 4 bytes per layer, KV head and position of max_ctx of every user, and once more of one user
+ * The first call allocates 4 bytes per layer, KV head and position of max_ctx of every user, and a little more than once more of one user
  * (KF_ENOMEM; KF_ESTATE under graph capture), and the weights start at 0; later calls set the window alone.
  */
 #define KF_MAX_WEIGH_ROWS 32

@@ -337,6 +337,11 @@ __global__ void table_share_kernel(const KvTable t, int src, int dst, int n) {
   t.version[dst + i]++;
 }
 
+__global__ void table_save_kernel(const KvTable t, int src, int* out, int n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) out[i] = t.page[src + i];
+}
+
 // ------------------------------------------------------------------ launchers
 static bool aligned16(const void* a, const void* b) { return (((uintptr_t)a | (uintptr_t)b) & 15) == 0; }
 static unsigned pages_spanned(int pos0, int n) { return (unsigned)((pos0 + n - 1) / kKvPage - pos0 / kKvPage + 1); }
@@ -454,6 +459,12 @@ hipError_t launch_page_copies(const CacheRef& c, const PageCopies& u, int layers
 
 hipError_t launch_kv_table_share(const KvTable& t, int src, int dst, int n, hipStream_t s) {
   hipLaunchKernelGGL(table_share_kernel, dim3((n + 255) / 256), dim3(256), 0, s, t, src, dst, n);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_table_save(const KvTable& t, int src, int* out, int n, hipStream_t s) {
+  if (n <= 0) return hipSuccess;
+  hipLaunchKernelGGL(table_save_kernel, dim3((n + 255) / 256), dim3(256), 0, s, t, src, out, n);
   return hipGetLastError();
 }
 

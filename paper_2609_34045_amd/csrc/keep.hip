@@ -1,10 +1,13 @@
 // Kernels that keep some of a user's cached positions (kf_kv_accept, kf_kv_evict): the
-// choice of the heaviest, and the gather of keys, values and weights.
+// choice of the heaviest, and the move of keys, values and weights.
 //
 // A list of ascending positions gives each new position i its old one, list[i] >= i.
-// In place, a workgroup takes the new positions in order, a chunk at a time, reads the
-// old ones of a chunk before it writes any of it, and never needs a position again that an
-// earlier chunk wrote: those lie below the chunk, what it reads does not.
+// The moves go by pages of new positions: a workgroup reads the old ones of a page, for one KV head and layer, and
+// writes them.  In place it must not write before the others have read what lies there.  A few pages (an
+// accepted path) go one after the other in one workgroup: a page reads no position below its own.  Many go side by
+// side: a workgroup takes a page by a ticket, in order, tells by a flag that it has read, and waits for the flags of the
+// pages whose old positions lie in its own (one or two, by the counts that select_kernel leaves).  These have lower
+// tickets, so they have started, and nothing waits before it has read: every wait ends.
 #include <algorithm>
 
 #include "kernels.h"
@@ -15,70 +18,79 @@ namespace {
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 typedef unsigned v2u __attribute__((ext_vector_type(2)));
 
-constexpr int kMoveThreads = 256;
+enum : int { kApart = 0, kInPlace = 1, kFew = 2 };  // another user's pages; in place, side by side; in place, in order
 
 // The old position of new position i (below p.n).
 __device__ __forceinline__ int old_of(const KeepParams& p, const int* list, int i) {
   if (list) return list[i];
   return i < p.first ? i : p.first + p.node[i - p.first];
 }
-__device__ __forceinline__ const int* list_of(const KeepParams& p, int layer, int g) {
-  return p.list ? p.list + ((int64_t)layer * p.nkv + g) * p.n : nullptr;
-}
-}  // namespace
 
-// fp16 keys (blockIdx.z even) or values of one layer and KV head.  In place: one workgroup (grid.x = 1) over all
-// new positions; else workgroup x takes chunk x.
-template <int HD, bool INPLACE>
-__global__ __launch_bounds__(kMoveThreads) void f16_keep_kernel(const KeepParams p) {
-  constexpr int PER = HD / 8, ROWS = kMoveThreads / PER, U = 4, CHUNK = ROWS * U;  // 16-byte pieces per position
-  const int g = blockIdx.y, layer = blockIdx.z >> 1, tid = threadIdx.x, r = tid / PER, d = (tid % PER) * 8;
-  const uint16_t* src = reinterpret_cast<const uint16_t*>((blockIdx.z & 1 ? p.src.v : p.src.k) + layer * p.src.layer_bytes);
-  uint16_t* dst = reinterpret_cast<uint16_t*>((blockIdx.z & 1 ? p.dst.v : p.dst.k) + layer * p.dst.layer_bytes);
-  const int* list = list_of(p, layer, g);
-  const int step = INPLACE ? CHUNK : CHUNK * gridDim.x;
-  for (int c0 = p.from + (INPLACE ? 0 : blockIdx.x * CHUNK); c0 < p.n; c0 += step) {
-    v4u x[U];
+// A page of fp16 keys and values on its way: thread tid has 16 bytes of every ROWS-th position of each.
+template <int HD>
+struct PageF16 {
+  static constexpr int PER = HD / 8, ROWS = 256 / PER, U = kKvPage / ROWS;
+  v4u x[2][U];
+  __device__ __forceinline__ void read(const KeepParams& p, int layer, int g, const int* list, int page, int a, int b) {
+    const int tid = threadIdx.x, d = tid % PER * 8;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = c0 + u * ROWS + r;
-      if (i < p.n) x[u] = *reinterpret_cast<const v4u*>(src + kv_offset(p.src.pages, p.src_user, g, old_of(p, list, i), HD) + d);
-    }
-    if (INPLACE) __syncthreads();
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = c0 + u * ROWS + r;
-      if (i < p.n) *reinterpret_cast<v4u*>(dst + kv_offset(p.dst.pages, p.dst_user, g, i, HD) + d) = x[u];
+      const int t = u * ROWS + tid / PER;
+      if (t < a || t >= b) continue;
+      const int64_t at = 2 * (kv_offset(p.src.pages, p.src_user, g, old_of(p, list, page * kKvPage + t), HD) + d) + layer * p.src.layer_bytes;
+      x[0][u] = *reinterpret_cast<const v4u*>(p.src.k + at);
+      x[1][u] = *reinterpret_cast<const v4u*>(p.src.v + at);
     }
   }
-}
+  __device__ __forceinline__ void write(const KeepParams& p, int layer, int g, int page, int a, int b) {
+    const int tid = threadIdx.x, d = tid % PER * 8;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = u * ROWS + tid / PER;
+      if (t < a || t >= b) continue;
+      const int64_t at = 2 * (kv_offset(p.dst.pages, p.dst_user, g, page * kKvPage + t, HD) + d) + layer * p.dst.layer_bytes;
+      *reinterpret_cast<v4u*>(p.dst.k + at) = x[0][u];
+      *reinterpret_cast<v4u*>(p.dst.v + at) = x[1][u];
+    }
+  }
+};
 
-// MXFP4 records of one layer and KV head, a page of new positions at a time: K's codes are whole bytes of a position,
-// V's pass through LDS, a byte a value, as positions share theirs.
-template <int HD, bool INPLACE>
-__global__ __launch_bounds__(256) void mx_keep_kernel(const KeepParams p) {
-  constexpr int CODES = mx_codes(HD), NB = HD / kMxBlock, KB = HD / 8;  // K code bytes of a position in one lane's run
-  __shared__ __attribute__((aligned(16))) uint8_t nib[kKvPage * HD];
-  const int g = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x;
-  const int* list = list_of(p, layer, g);
-  auto record = [&](const CacheRef& c, int user, int page) {
+// A page of MXFP4 records: K's codes are whole bytes of a position, V's pass through LDS, as positions share theirs: the
+// V codes of the old pages as they are, where these are at most kSpan, or else a byte a value.  Thread (t, quarter q of
+// the head) has K codes and its part of the exponents and scales.
+template <int HD>
+struct PageMx {
+  static constexpr int CODES = mx_codes(HD), NB = HD / kMxBlock, kSpan = 8;
+  static_assert(kSpan * CODES >= kKvPage * HD, "both forms");
+  uint8_t* nib;  // kSpan CODES bytes in LDS
+  int* at;       // [kKvPage] in LDS: the byte of each position's V code of d 0, and its nibble
+  bool whole;    // the old pages' V codes are in LDS
+  v4u kc;
+  uint8_t ke;
+  uint16_t vs;
+  static __device__ __forceinline__ uint8_t* record(const CacheRef& c, int layer, int g, int user, int page) {
     return c.k + layer * c.layer_bytes + (int64_t)kv_page(c.pages, user, page) * c.pages.page_stride + (int64_t)g * mx_record(HD);
-  };
-  const int pages = (p.n + kKvPage - 1) / kKvPage, page0 = p.from / kKvPage;
-  for (int page = page0 + (INPLACE ? 0 : blockIdx.x); page < pages; page += INPLACE ? 1 : gridDim.x) {
-    const int a = max(p.from - page * kKvPage, 0), b = min(p.n - page * kKvPage, kKvPage);
-    uint8_t* out = record(p.dst, p.dst_user, page);
-    // thread (t, quarter q of the head): K codes, its part of the exponents and scales, and hd/4 V codes
-    const int t = tid / 4, q = tid % 4;
-    const bool in = t >= a && t < b;
-    v4u kc = {0, 0, 0, 0};
-    uint8_t ke = 0;
-    uint16_t vs = 0;
-    if (in) {
+  }
+  __device__ __forceinline__ void read(const KeepParams& p, int layer, int g, const int* list, int page, int a, int b) {
+    const int tid = threadIdx.x, t = tid / 4, q = tid % 4;
+    const int p0 = old_of(p, list, page * kKvPage + a) / kKvPage, span = old_of(p, list, page * kKvPage + b - 1) / kKvPage - p0 + 1;
+    whole = span <= kSpan;
+    v4u v[kSpan][CODES / 16 / 256 ? CODES / 16 / 256 : 1];
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < kSpan; ++i) {
+        if (i >= span) break;
+        const v4u* src = reinterpret_cast<const v4u*>(record(p.src, layer, g, p.src_user, p0 + i) + mx_v(HD));
+#pragma unroll
+        for (int j = 0; j * 256 < CODES / 16; ++j)
+          if (j * 256 + tid < CODES / 16) v[i][j] = src[j * 256 + tid];
+      }
+    }
+    if (t >= a && t < b) {
       const int from = old_of(p, list, page * kKvPage + t), s = from % kKvPage;
-      const uint8_t* rec = record(p.src, p.src_user, from / kKvPage);
+      const uint8_t* rec = record(p.src, layer, g, p.src_user, from / kKvPage);
       const uint8_t* k = rec + mx_k_byte<HD>(s, q * (HD / 4));
-      if (KB == 16) {
+      if (HD == 128) {
         kc = *reinterpret_cast<const v4u*>(k);
       } else {
         const v2u w = *reinterpret_cast<const v2u*>(k);
@@ -89,88 +101,205 @@ __global__ __launch_bounds__(256) void mx_keep_kernel(const KeepParams p) {
         ke = rec[CODES + mx_k_exp(s, q)];
         vs = reinterpret_cast<const uint16_t*>(rec + mx_v(HD) + CODES)[mx_v_exp<HD>(s, q)];
       }
-      const uint8_t* v = rec + mx_v(HD);
-#pragma unroll 8
-      for (int j = 0; j < HD / 4; ++j) {
-        const int d = 4 * j + q;
-        nib[t * HD + d] = (v[mx_v_byte(s, d)] >> (4 * (s & 1))) & 15;
+      if (whole) {
+        if (q == 0) at[t] = ((from / kKvPage - p0) * CODES + mx_v_byte(s, 0)) * 2 + (s & 1);
+      } else {
+        const uint8_t* c = rec + mx_v(HD);
+        uint8_t x[HD / 4];
+#pragma unroll
+        for (int j = 0; j < HD / 4; ++j) x[j] = c[mx_v_byte(s, 4 * j + q)];
+#pragma unroll
+        for (int j = 0; j < HD / 4; ++j) nib[t * HD + 4 * j + q] = (x[j] >> (4 * (s & 1))) & 15;
       }
     }
-    __syncthreads();  // in place: everything of the page's old positions is read
-    if (in) {
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < kSpan; ++i) {
+        if (i >= span) break;
+#pragma unroll
+        for (int j = 0; j * 256 < CODES / 16; ++j)
+          if (j * 256 + tid < CODES / 16) reinterpret_cast<v4u*>(nib + i * CODES)[j * 256 + tid] = v[i][j];
+      }
+    }
+  }
+  __device__ __forceinline__ void write(const KeepParams& p, int layer, int g, int page, int a, int b) {
+    const int tid = threadIdx.x, t = tid / 4, q = tid % 4;
+    uint8_t* out = record(p.dst, layer, g, p.dst_user, page);
+    if (t >= a && t < b) {
       uint8_t* k = out + mx_k_byte<HD>(t, q * (HD / 4));
-      if (KB == 16) *reinterpret_cast<v4u*>(k) = kc;
+      if (HD == 128) *reinterpret_cast<v4u*>(k) = kc;
       else *reinterpret_cast<v2u*>(k) = v2u{kc.x, kc.y};
       if (q < NB) {
         out[CODES + mx_k_exp(t, q)] = ke;
         reinterpret_cast<uint16_t*>(out + mx_v(HD) + CODES)[mx_v_exp<HD>(t, q)] = vs;
       }
     }
+    // Dword w = tid + 256 i of the V codes: positions 16 (2 s + j / 4) + 4 grp + j % 4 of d = d0 + 32 i.
     uint32_t* codes = reinterpret_cast<uint32_t*>(out + mx_v(HD));
-    for (int w = tid; w < CODES / 4; w += 256) {  // dword of the V codes: positions 16 (2 s + j / 4) + 4 grp + j % 4 of one d
-      const int lane = (w >> 2) & 63, d = 16 * (2 * (w >> 8) + ((w >> 1) & 1)) + (lane & 15), s = w & 1, grp = lane >> 4;
-      uint32_t x = 0, mask = 0;
+    const int lane = (tid >> 2) & 63, d0 = 16 * ((tid >> 1) & 1) + (lane & 15), s = tid & 1, grp = lane >> 4;
+    uint32_t mask = 0;
+    int from[8], shift[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int pos = 16 * (2 * s + j / 4) + 4 * grp + j % 4;
+      if (pos >= a && pos < b) mask |= 15u << (4 * j);
+      const int w = whole && pos >= a && pos < b ? at[pos] : 0;
+      from[j] = whole ? w / 2 + mx_v_byte(0, d0) : pos * HD + d0;
+      shift[j] = whole ? 4 * (w & 1) : 0;
+    }
+    if (!mask) return;
+#pragma unroll
+    for (int i = 0; i < CODES / 4 / 256; ++i) {
+      uint32_t x = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int pos = 16 * (2 * s + j / 4) + 4 * grp + j % 4;
-        if (pos < a || pos >= b) continue;
-        x |= (uint32_t)nib[pos * HD + d] << (4 * j);
-        mask |= 15u << (4 * j);
+        const uint32_t c = nib[from[j] + i * (whole ? mx_v_byte(0, 32) : 32)];
+        x |= (c >> shift[j] & 15u) << (4 * j);
       }
-      if (mask) codes[w] = mask == ~0u ? x : (codes[w] & ~mask) | x;
+      const int w = tid + 256 * i;
+      codes[w] = mask == ~0u ? x : (codes[w] & ~mask) | (x & mask);
     }
-    __syncthreads();
   }
-}
+};
+template <int HD, bool MX>
+struct PageOf : PageF16<HD> {};
+template <int HD>
+struct PageOf<HD, true> : PageMx<HD> {};
+}  // namespace
 
-// The weights, one workgroup a layer and KV head.
-__global__ __launch_bounds__(1024) void weight_keep_kernel(const KeepParams p) {
-  const int g = blockIdx.x, layer = blockIdx.y;
-  const int* list = list_of(p, layer, g);
-  const float* src = p.weights + (((int64_t)layer * p.users + p.src_user) * p.nkv + g) * p.stride;
-  float* dst = p.weights + (((int64_t)layer * p.users + p.dst_user) * p.nkv + g) * p.stride;
-  for (int c0 = p.from; c0 < p.n; c0 += 1024) {
-    const int i = c0 + threadIdx.x;
-    float x = 0.f;
-    if (i < p.n) x = src[old_of(p, list, i)];
+template <int HD, bool MX, int MODE>
+__global__ __launch_bounds__(256) void keep_kernel(const KeepParams p) {
+  __shared__ __attribute__((aligned(16))) uint8_t nib[MX ? PageMx<HD>::kSpan * PageMx<HD>::CODES : 16];
+  __shared__ int at[MX ? kKvPage : 1];
+  __shared__ int ticket;
+  const int page0 = p.from / kKvPage, pages = (p.n + kKvPage - 1) / kKvPage, heads = p.nkv * p.layers, tid = threadIdx.x;
+  PageOf<HD, MX> x;
+  if constexpr (MX) {
+    x.nib = nib;
+    x.at = at;
+  }
+  // Workgroup x: KV head and layer x % heads, of page x / heads (kInPlace: of the next page that none has), or (kFew) of
+  // all pages.
+  const int lg = blockIdx.x % heads, g = lg % p.nkv, layer = lg / p.nkv;
+  int nth = blockIdx.x / heads;
+  if (MODE == kInPlace) {
+    if (tid == 0) ticket = __hip_atomic_fetch_add(&p.tickets[lg * kTicketStep], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    if (i < p.n) dst[i] = x;
+    nth = ticket;
+  }
+  const int* list = p.list ? p.list + (int64_t)lg * p.n : nullptr;
+  const float* wsrc = p.weights ? p.weights + (((int64_t)layer * p.users + p.weights_src) * p.nkv + g) * p.stride : nullptr;
+  float* wdst = p.weights ? p.weights + (((int64_t)layer * p.users + p.dst_user) * p.nkv + g) * p.stride : nullptr;
+  int page = page0 + (MODE == kFew ? 0 : nth);
+  const int last = MODE == kFew ? pages : page + 1;
+  for (; page < last; ++page) {
+    const int a = max(p.from - page * kKvPage, 0), b = min(p.n - page * kKvPage, kKvPage);
+    // In place, but for a page that takes another's place, which no old position lies in.
+    const bool in_place = MODE != kApart && kv_page(p.src.pages, p.src_user, page) == kv_page(p.dst.pages, p.dst_user, page);
+    // a page whose last position stays where it is has all of them there
+    const bool same = in_place && old_of(p, list, page * kKvPage + b - 1) == page * kKvPage + b - 1;
+    float w = 0.f;
+    if (!same) {
+      x.read(p, layer, g, list, page, a, b);
+      if (wsrc && tid >= a && tid < b) w = wsrc[old_of(p, list, page * kKvPage + tid)];
+    }
+    // Everything is here before anything behind this is written (and, in LDS, read).
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (MODE == kInPlace) {
+      int* flags = p.flags + (int64_t)lg * p.pages;
+      if (tid == 0) __hip_atomic_store(&flags[page], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (same) return;
+      if (in_place && tid < 64) {  // the pages with an old position in this one
+        const int* below = p.below + (int64_t)lg * (p.pages + 1);
+        const int r0 = below[page], r1 = below[page + 1];
+        for (int i = max(r0 / kKvPage, page0) + tid; i < page && i * kKvPage < r1; i += 64)
+          while (!__hip_atomic_load(&flags[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) __builtin_amdgcn_s_sleep(2);
+      }
+      __syncthreads();
+    }
+    if (!same) {
+      x.write(p, layer, g, page, a, b);
+      if (wdst && tid >= a && tid < b) wdst[page * kKvPage + tid] = w;
+    }
+    if (MODE == kFew) __syncthreads();  // LDS is free again
   }
 }
 
 // Which positions to keep, one workgroup a layer and KV head: the m-th largest weight by its digits, most significant
 // first (a histogram of the weights that agree so far, and where the m-th lies in it), then
-// the positions above it, and of those equal to it the first, in order.
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048;
-__device__ __forceinline__ uint32_t weight_key(float w) {  // ordered as the weights are; a NaN below all
+// the positions above it, and of those equal to it the first, in order.  A wave has a run of pages, 64 positions at a
+// time; with NV, the keys of its NV pages stay in registers (NV 0: they are read again at each pass).
+// Bound by one compute unit's vector instructions, some 30 a position and thread: the weights that share the first 11
+// bits are listed, so that the other two digits are looked for among few, and ballots go through scalar instructions.
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048, kCopies = 4, kListed = 8192;
+// Ordered as the weights are; 1 for a NaN, below all, and 0 stands for no weight.
+__device__ __forceinline__ uint32_t weight_key(float w) {
   const uint32_t u = __float_as_uint(w + 0.f);
-  return w != w ? 0u : u >> 31 ? ~u : u | 0x80000000u;
+  return w != w ? 1u : u >> 31 ? ~u : u | 0x80000000u;
 }
+template <int NV>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectParams p) {
-  __shared__ int hist[kBins];
-  __shared__ int sums[kSelectWaves];
-  __shared__ int found[2];
-  __shared__ uint32_t counts[2][kSelectWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ __attribute__((aligned(16))) int hist[kBins * kCopies];  // a lane counts in copy lane % kCopies (many weights may be alike)
+  __shared__ uint32_t listed[kListed];
+  __shared__ int sums[kSelectWaves], of[2][kSelectWaves];
+  __shared__ int found[2], n_listed;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float* w = p.weights + blockIdx.y * p.layer + blockIdx.x * p.head;
-  int* list = p.list + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * p.keep;
+  const int64_t lg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  int* list = p.list + lg * p.keep;
+  int* below = p.below + lg * (p.pages + 1);
   const int lo = p.first, hi = p.len - p.last, m = p.keep - p.first - p.last;
+  // The wave's pages: positions c0 .. c0 + 64 per - 1.
+  const int all = hi > lo ? (hi + kKvPage - 1) / kKvPage - lo / kKvPage : 0, per = NV ? NV : (all + kSelectWaves - 1) / kSelectWaves;
+  const int c0 = (lo / kKvPage + wave * per) * kKvPage + lane;
+  auto load = [&](int j) {
+    const int i = c0 + j * kKvPage;
+    return i >= lo && i < hi ? weight_key(w[i]) : 0u;
+  };
+  uint32_t held[NV ? NV : 1];
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) held[j] = load(j);
+  }
+  auto key = [&](int j) { return NV ? held[NV ? j : 0] : load(j); };
+  auto each = [&](auto what) {
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) what(j);
+    } else {
+      for (int j = 0; j < per; ++j) what(j);
+    }
+  };
+  for (int b = tid; b < kBins * kCopies; b += kSelectThreads) hist[b] = 0;
+  if (tid == 0) n_listed = 0;
   for (int i = tid; i < p.first; i += kSelectThreads) list[i] = i;
   for (int i = tid; i < p.last; i += kSelectThreads) list[p.keep - p.last + i] = hi + i;
+  // for a move in place (kInPlace): how many kept positions lie below each page (those between lo and hi later), no flag
+  // set and no ticket taken
+  for (int i = tid; i <= p.pages; i += kSelectThreads) {
+    if (i < p.pages) p.flags[lg * p.pages + i] = 0;
+    const int at = i * kKvPage;
+    if (at <= lo) below[i] = at;
+    else if (at >= hi) below[i] = min(p.first + m + at - hi, p.keep);
+    else if (m == 0) below[i] = lo;
+  }
+  if (tid == 0) p.tickets[lg * kTicketStep] = 0;
   if (m == 0) return;
-  uint32_t prefix = 0, known = 0;
+  __syncthreads();
+
+  auto count = [&](uint32_t bin) { atomicAdd(&hist[bin * kCopies + lane % kCopies], 1); };
   int need = m;  // of the weights that have the prefix, the need-th largest is the one looked for
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-    for (int b = tid; b < kBins; b += kSelectThreads) hist[b] = 0;
+  // The bin that holds it, from the top; the histogram is empty again afterwards.
+  auto find = [&]() {
     __syncthreads();
-    for (int i = lo + tid; i < hi; i += kSelectThreads) {
-      const uint32_t k = weight_key(w[i]);
-      if ((k & known) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1);
+    int* mine = &hist[(kBins - 2 - 2 * tid) * kCopies];  // thread t: bins kBins - 1 - 2 t and the next lower
+    int a = 0, b = 0;
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      b += mine[i];
+      a += mine[kCopies + i];
     }
-    __syncthreads();
-    // thread t holds bins kBins - 1 - 2 t and the next lower
-    const int a = hist[kBins - 1 - 2 * tid], b = hist[kBins - 2 - 2 * tid];
     int upto = a + b;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -178,8 +307,13 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectPara
       if (lane >= o) upto += x;
     }
     if (lane == 63) sums[wave] = upto;
+#pragma unroll
+    for (int i = 0; i < 2 * kCopies; ++i) mine[i] = 0;
     __syncthreads();
-    for (int i = 0; i < wave; ++i) upto += sums[i];
+    int x = lane < wave ? sums[lane % kSelectWaves] : 0;
+#pragma unroll
+    for (int o = 1; o < kSelectWaves; o <<= 1) x += __shfl_xor(x, o);
+    upto += __builtin_amdgcn_readfirstlane(x);
     const int before = upto - a - b;
     if (before < need && need <= upto) {
       const bool second = before + a < need;
@@ -187,63 +321,116 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectPara
       found[1] = need - before - (second ? a : 0);
     }
     __syncthreads();
-    prefix |= (uint32_t)found[0] << shift;
-    known |= (uint32_t)(bins - 1) << shift;
     need = found[1];
-    __syncthreads();
-  }
-  int above = 0, equal = 0;  // before this chunk
-  for (int c0 = lo, turn = 0; c0 < hi; c0 += kSelectThreads, turn ^= 1) {
-    const int i = c0 + tid;
-    const uint32_t k = i < hi ? weight_key(w[i]) : 0u;
-    const uint64_t gt = __ballot(i < hi && k > prefix), eq = __ballot(i < hi && k == prefix), below = (1ull << lane) - 1;
-    if (lane == 0) counts[turn][wave] = (uint32_t)__popcll(gt) | (uint32_t)__popcll(eq) << 16;
-    __syncthreads();
-    uint32_t mine = 0, all = 0;
-#pragma unroll
-    for (int x = 0; x < kSelectWaves; ++x) {
-      all += counts[turn][x];
-      if (x < wave) mine += counts[turn][x];
+    return (uint32_t)found[0];
+  };
+  each([&](int j) { count(key(j) >> 21); });
+  uint32_t prefix = find() << 21;
+  // The weights with this prefix, listed (or, where they are too many, taken from all again).
+  int n = 0;
+  each([&](int j) { n += __popcll(__ballot(key(j) >> 21 == prefix >> 21)); });
+  if (lane == 0) n = atomicAdd(&n_listed, n);
+  n = __builtin_amdgcn_readfirstlane(n);
+  auto rank = [&](uint64_t x) {  // bits of the lower lanes
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(x >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)x, 0));
+  };
+  each([&](int j) {
+    const uint32_t k = key(j);
+    const bool mine = k >> 21 == prefix >> 21;
+    const uint64_t with = __ballot(mine);
+    const int at = n + rank(with);
+    if (mine && at < kListed) listed[at] = k;
+    n += __popcll(with);
+  });
+  __syncthreads();
+  n = n_listed;
+  auto digit = [&](int shift, int known, uint32_t bins) {
+    if (n <= kListed) {
+      for (int i = tid; i < n; i += kSelectThreads) {
+        const uint32_t k = listed[i];
+        if ((k ^ prefix) >> known == 0) count(k >> shift & (bins - 1));
+      }
+    } else {
+      each([&](int j) {
+        const uint32_t k = key(j);
+        if ((k ^ prefix) >> known == 0) count(k >> shift & (bins - 1));
+      });
     }
-    const int g = above + (int)(mine & 0xffff) + __popcll(gt & below), e = equal + (int)(mine >> 16) + __popcll(eq & below);
-    if ((gt >> lane & 1) || ((eq >> lane & 1) && e < need)) list[p.first + g + min(e, need)] = i;
-    above += (int)(all & 0xffff);
-    equal += (int)(all >> 16);
+    prefix |= find() << shift;
+  };
+  digit(10, 21, 2048);
+  digit(0, 10, 1024);
+
+  int above = 0, equal = 0;  // in the waves before this one, then before the position
+  each([&](int j) {
+    const uint32_t k = key(j);
+    above += __popcll(__ballot(k > prefix));
+    equal += __popcll(__ballot(k == prefix));
+  });
+  if (lane == 0) {
+    of[0][wave] = above;
+    of[1][wave] = equal;
   }
+  __syncthreads();
+  above = lane < wave ? of[0][lane % kSelectWaves] : 0;
+  equal = lane < wave ? of[1][lane % kSelectWaves] : 0;
+#pragma unroll
+  for (int o = 1; o < kSelectWaves; o <<= 1) {
+    above += __shfl_xor(above, o);
+    equal += __shfl_xor(equal, o);
+  }
+  above = __builtin_amdgcn_readfirstlane(above);
+  equal = __builtin_amdgcn_readfirstlane(equal);
+  const int page0 = c0 / kKvPage;
+  int* out = list + p.first;
+  int counts = 0;  // lane j % 64: what lies below page j
+  auto tell = [&](int j, int n) {
+    const int page = page0 + j - n + 1 + lane;
+    if (lane < n && page * kKvPage > lo && page * kKvPage < hi) below[page] = counts;
+  };
+  each([&](int j) {
+    const uint32_t k = key(j);
+    const bool over = k > prefix;
+    bool mine = over;
+    const uint64_t eq = __ballot(k == prefix);
+    const int before = above + min(equal, need);
+    above += __popcll(__ballot(over));
+    if (eq) {  // the first of these that are still needed
+      const int left = need - equal;
+      equal += __popcll(eq);
+      mine |= k == prefix && rank(eq) < left;
+    }
+    if (mine) out[before + rank(__ballot(mine))] = c0 + j * kKvPage;
+    if (lane == j % 64) counts = p.first + before;
+    if (j % 64 == 63 || j == per - 1) tell(j, j % 64 + 1);
+  });
 }
 
 // ------------------------------------------------------------------ launchers
 hipError_t launch_select(const SelectParams& p, int nkv, int layers, hipStream_t s) {
   if (p.keep <= 0) return hipSuccess;
-  hipLaunchKernelGGL(select_kernel, dim3(nkv, layers), dim3(kSelectThreads), 0, s, p);
+  const int pages = std::max((p.len - p.last + kKvPage - 1) / kKvPage - p.first / kKvPage, 0);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(nkv, layers), dim3(kSelectThreads), 0, s, p); };
+  if (pages <= 4 * kSelectWaves) launch(select_kernel<4>);
+  else if (pages <= 16 * kSelectWaves) launch(select_kernel<16>);
+  else if (pages <= 32 * kSelectWaves) launch(select_kernel<32>);
+  else launch(select_kernel<0>);
   return hipGetLastError();
 }
-template <int HD>
-static hipError_t keep(const KeepParams& p, int layers, hipStream_t s) {
-  const bool in_place = p.dst.k == p.src.k && p.dst_user == p.src_user;
-  const int n = p.n - p.from;
-  if (p.src.mx) {
-    const unsigned pages = (unsigned)((p.n + kKvPage - 1) / kKvPage - p.from / kKvPage);
-    if (in_place) hipLaunchKernelGGL((mx_keep_kernel<HD, true>), dim3(1, p.nkv, layers), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((mx_keep_kernel<HD, false>), dim3(pages, p.nkv, layers), dim3(256), 0, s, p);
-  } else {
-    const int chunk = kMoveThreads / (HD / 8) * 4;
-    if (in_place) hipLaunchKernelGGL((f16_keep_kernel<HD, true>), dim3(1, p.nkv, 2 * layers), dim3(kMoveThreads), 0, s, p);
-    else
-      hipLaunchKernelGGL((f16_keep_kernel<HD, false>), dim3((unsigned)((n + chunk - 1) / chunk), p.nkv, 2 * layers),
-                         dim3(kMoveThreads), 0, s, p);
-  }
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess && p.weights) {
-    hipLaunchKernelGGL(weight_keep_kernel, dim3(p.nkv, layers), dim3(1024), 0, s, p);
-    e = hipGetLastError();
-  }
-  return e;
+template <int HD, bool MX>
+static hipError_t keep(const KeepParams& p, hipStream_t s) {
+  const unsigned pages = (unsigned)((p.n + kKvPage - 1) / kKvPage - p.from / kKvPage), heads = p.nkv * p.layers;
+  if (!p.in_place) hipLaunchKernelGGL((keep_kernel<HD, MX, kApart>), dim3(pages * heads), dim3(256), 0, s, p);
+  else if (p.list) hipLaunchKernelGGL((keep_kernel<HD, MX, kInPlace>), dim3(pages * heads), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((keep_kernel<HD, MX, kFew>), dim3(heads), dim3(256), 0, s, p);
+  return hipGetLastError();
 }
-hipError_t launch_keep(const KeepParams& p, int hd, int layers, hipStream_t s) {
+hipError_t launch_keep(const KeepParams& p, int hd, hipStream_t s) {
   if (p.n <= p.from) return hipSuccess;
   if (p.src.mx != p.dst.mx || (!p.list && (p.n - p.first > kMaxNodes || p.from < p.first))) return hipErrorInvalidValue;
-  return hd == 128 ? keep<128>(p, layers, s) : hd == 64 ? keep<64>(p, layers, s) : hipErrorInvalidValue;
+  if (hd == 128) return p.src.mx ? keep<128, true>(p, s) : keep<128, false>(p, s);
+  if (hd == 64) return p.src.mx ? keep<64, true>(p, s) : keep<64, false>(p, s);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace kf

@@ -359,6 +359,8 @@ __device__ __forceinline__ void kv_table_apply(const KvTable& t, const KvTableUp
 hipError_t launch_kv_table_update(const KvTable& t, const KvTableUpdate& u, hipStream_t s);
 // page[dst + i] = page[src + i] for i < n, as each entry's next update: a user that shares another's pages.
 hipError_t launch_kv_table_share(const KvTable& t, int src, int dst, int n, hipStream_t s);
+// out[i] = page[src + i] for i < n.
+hipError_t launch_kv_table_save(const KvTable& t, int src, int* out, int n, hipStream_t s);
 
 // Log probabilities of rows of logits (logprob.hip).
 constexpr int kMaxTop = 32;
@@ -449,21 +451,30 @@ struct TreeParams {
 void plan_trees(TreeParams& p, int n_cu, int64_t part_rows);
 hipError_t launch_attn_tree(const TreeParams& p, int hd, hipStream_t s);
 
+constexpr int kTicketStep = 32;  // a cache line each
 // Some of a user's positions, kept in their order (keep.hip): new position i of dst_user is old position list[i] of
-// src_user, for i in [from, n), in every layer; the same user of one cache: in place.
+// src_user, for i in [from, n), in every layer.  in_place: the two are one, but for pages that src's table still has and
+// dst's does not.
 struct KeepParams {
   CacheRef dst, src;
   int dst_user, src_user;
+  int in_place;
   const int* list;         // [layers][nkv][n] ascending old positions, or NULL: first + node[i - first] from `first` on
-  int from, n, nkv;
+  int from, n, nkv, layers;
   int first;
   uint8_t node[kMaxNodes];
-  float* weights;          // [layers][users][nkv][stride] of both users, or NULL
+  float* weights;          // [layers][users][nkv][stride], from weights_src to dst_user, or NULL
+  int weights_src;
   int users;
   int64_t stride;
+  // in place with a list: what launch_select left with it
+  const int* below;        // [layers][nkv][pages + 1]
+  int* flags;              // [layers][nkv][pages]
+  int* tickets;            // [layers][nkv], kTicketStep apart
+  int pages;
 };
 static_assert(kMaxNodes <= 256, "node");
-hipError_t launch_keep(const KeepParams& p, int hd, int layers, hipStream_t s);
+hipError_t launch_keep(const KeepParams& p, int hd, hipStream_t s);
 
 // The positions that eviction keeps: of each layer's and KV head's len weights the first `first`, the last `last` and the
 // keep - first - last largest of the others, the lower position first among equal ones and a NaN below all;
@@ -473,6 +484,8 @@ struct SelectParams {
   int64_t layer, head;   // strides
   int len, keep, first, last;
   int* list;
+  int *below, *flags, *tickets;  // for launch_keep
+  int pages;                     // of a user
 };
 hipError_t launch_select(const SelectParams& p, int nkv, int layers, hipStream_t s);
 

@@ -222,9 +222,11 @@ struct kf_kv {
   }
   uint16_t *f16_k = nullptr, *f16_v = nullptr;
   // A tracked cache (kf_kv_track): each position's attention weight, [layers][max_users][nkv][max_ctx], what an eviction
-  // keeps, [layers][nkv][max_ctx], and how many of a prefill chunk's last queries count.
+  // keeps ([layers][nkv][max_ctx], then what its move in place needs, kept_ints), and how many of a prefill chunk's last
+  // queries count.
   float* weights = nullptr;
   int* kept = nullptr;
+  int64_t kept_ints() const { return (int64_t)layers() * st->cfg.n_kv_heads * ((int64_t)max_ctx + 2 * ppu + 1 + kTicketStep) + ppu; }
   int window = 0;
   WeightRows weight_rows(int layer, int user, int pos) const {
     const int64_t head = max_ctx, lay = head * st->cfg.n_kv_heads * max_users;
@@ -321,7 +323,8 @@ int kv_append_copies(const kf_kv* kv, int n, const int* users) {
 // that other users hold too, or change nothing and fail when the pool is short.
 // Copies and new table entries are written on the stage's stream before any later
 // work there reads them.
-static kf_status kv_grant(kf_kv* kv, int n, const int* users, const int64_t* from, const int64_t* upto) {
+// contents false: the pages that take the place of shared ones are left to be written whole.
+static kf_status kv_grant(kf_kv* kv, int n, const int* users, const int64_t* from, const int64_t* upto, bool contents = true) {
   if (!kv->table) return KF_OK;  // reserved cache: every page is held from the start
   const kf_status late = kv_catch_up(kv);
   if (late != KF_OK) return late;
@@ -372,8 +375,11 @@ static kf_status kv_grant(kf_kv* kv, int n, const int* users, const int64_t* fro
       const int old = shared_page(kv, u, p);
       if (old < 0) continue;
       kv->refs[old]--;
-      cp.src[cp.n] = old;
-      cp.dst[cp.n++] = take(u, (int)(p / kKvPage));
+      const int fresh = take(u, (int)(p / kKvPage));
+      if (contents) {
+        cp.src[cp.n] = old;
+        cp.dst[cp.n++] = fresh;
+      }
       if (up.n == kKvTableBatch || cp.n == kPageCopyBatch) {
         const kf_status e = flush();
         if (e != KF_OK) return e;
@@ -1138,7 +1144,7 @@ kf_status kf_kv_track(kf_kv* kv, int32_t window) {
   if (window < 0 || window > kMaxWeighRows) return fail(KF_EINVAL, "window %d outside [0, %d]", window, kMaxWeighRows);
   if (!kv->weights) {
     if (capturing(kv->st)) return fail(KF_ESTATE, "a cache's first kf_kv_track cannot be captured");
-    const int64_t kept = (int64_t)kv->layers() * kv->st->cfg.n_kv_heads * kv->max_ctx * 4, all = kept * kv->max_users;
+    const int64_t kept = kv->kept_ints() * 4, all = (int64_t)kv->layers() * kv->st->cfg.n_kv_heads * kv->max_ctx * kv->max_users * 4;
     char *w = nullptr, *k = nullptr;
     if (hipMalloc((void**)&w, all) != hipSuccess || hipMalloc((void**)&k, kept) != hipSuccess) {
       (void)hipGetLastError();
@@ -1258,13 +1264,19 @@ kf_status kf_kv_evict(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t kee
   if (keep > len) return fail(KF_ERANGE, "%d positions of user %d, which holds %d", keep, src_user, len);
   if (!kv->weights) return fail(KF_ESTATE, "the cache is not tracked");
   const bool in_place = src_user == dst_user;
+  bool moved = false;  // in place, but for some pages
+  KvPages source = kv->pages();
   kf_status st = KF_OK;
+  const bool moves = !in_place || keep < len;
   if (kv->table) {
     if (capturing(kv->st))  // which pages a user holds is known when a call is made
       return fail(KF_ESTATE, "positions of a paged cache cannot be evicted under graph capture");
     const int64_t upto = keep;
     int64_t from = first;
-    if (!in_place) {
+    if (in_place) {
+      for (int64_t pos = first; moves && pos < keep && !moved; pos = (pos / kKvPage + 1) * kKvPage) moved = shared_page(kv, src_user, pos) >= 0;
+      if (!moves) from = upto;
+    } else {
       int free_after = (int)kv->free_pages.size();
       for (int i = 0; i < kv->held[dst_user]; ++i) free_after += kv->refs[kv->host_table[(size_t)dst_user * kv->ppu + i]] == 1;
       if (pages_for(keep) > free_after)
@@ -1273,26 +1285,47 @@ kf_status kf_kv_evict(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t kee
       kv->len[dst_user] = 0;
       from = upto;
     }
-    st = kv_grant(kv, 1, &dst_user, &from, &upto);
+    if (moved) {  // pages that others hold too are read where they were, and what is kept goes to others
+      int* old = kv->kept + kv->kept_ints() - kv->ppu;
+      const int need = pages_for(len);
+      st = kv_catch_up(kv);
+      if (st != KF_OK) return st;
+      KF_HIP(launch_kv_table_save(kv->kv_table(), src_user * kv->ppu, old, need, kv->st->stream), "page table copy");
+      source = KvPages{old, 0, kv->page_stride};
+    }
+    st = kv_grant(kv, 1, &dst_user, &from, &upto, !moved);
     if (st != KF_OK) return st;
   }
   if (keep) {
     const WeightRows w = kv->weight_rows(kv->st->lo, src_user, 0);
-    SelectParams sel{w.p, w.layer, w.head, len, keep, first, last, kept_dev ? kept_dev : kv->kept};
+    const int64_t heads = (int64_t)kv->layers() * kv->st->cfg.n_kv_heads;
+    int* below = kv->kept + heads * kv->max_ctx;
+    int* flags = below + heads * (kv->ppu + 1);
+    const SelectParams sel{w.p, w.layer, w.head, len, keep, first, last, kept_dev ? kept_dev : kv->kept, below, flags,
+                           flags + heads * kv->ppu, kv->ppu};
     KeepParams p{};
+    p.below = below;
+    p.flags = flags;
+    p.tickets = sel.tickets;
+    p.pages = kv->ppu;
+    p.layers = kv->layers();
     p.dst = p.src = kv->ref();
     p.dst_user = dst_user;
     p.src_user = src_user;
     p.list = sel.list;
-    p.from = in_place ? first : 0;
+    p.src.pages = source;
+    p.in_place = in_place;
+    // (of a page that is replaced, what lies before `first` too)
+    p.from = !in_place ? 0 : moved ? first / kKvPage * kKvPage : first;
+    p.weights_src = src_user;
     p.n = keep;
     p.nkv = kv->st->cfg.n_kv_heads;
     p.weights = kv->weights;
     p.users = kv->max_users;
     p.stride = kv->max_ctx;
     hipError_t e = hipSuccess;
-    if (keep < len || !in_place || kept_dev) e = launch_select(sel, p.nkv, kv->layers(), kv->st->stream);
-    if (e == hipSuccess && (keep < len || !in_place)) e = launch_keep(p, kv->st->cfg.head_dim, kv->layers(), kv->st->stream);
+    if (moves || kept_dev) e = launch_select(sel, p.nkv, kv->layers(), kv->st->stream);
+    if (e == hipSuccess && moves) e = launch_keep(p, kv->st->cfg.head_dim, kv->st->stream);
     KF_HIP(e, "eviction launch");
   }
   kv_release(kv, dst_user, pages_for(keep));
@@ -1552,12 +1585,15 @@ kf_status kf_kv_accept(kf_kv* kv, int32_t user, int32_t len, int32_t n, const in
     p.from = (int)from;
     p.n = (int)upto;
     p.nkv = kv->st->cfg.n_kv_heads;
+    p.layers = kv->layers();
+    p.in_place = 1;
+    p.weights_src = user;
     p.first = len;
     for (int i = 0; i < n; ++i) p.node[i] = (uint8_t)nodes[i];
     p.weights = kv->weights;
     p.users = kv->max_users;
     p.stride = kv->max_ctx;
-    KF_HIP(launch_keep(p, kv->st->cfg.head_dim, kv->layers(), kv->st->stream), "accepted positions launch");
+    KF_HIP(launch_keep(p, kv->st->cfg.head_dim, kv->st->stream), "accepted positions launch");
   }
   kv_release(kv, user, pages_for(len + n));
   kv->len[user] = len + n;
