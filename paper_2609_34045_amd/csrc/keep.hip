@@ -18,6 +18,11 @@ namespace {
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 typedef unsigned v2u __attribute__((ext_vector_type(2)));
 
+// Replays of two graphs that move in place on one cache share the tickets and flags, and their caller orders them.  Should
+// they run at once all the same, no ticket is taken for a page that is not there, and a wait ends after this many looks
+// (about a tenth of a second; a wait that its flag ends takes microseconds).
+constexpr int kWaits = 1 << 17;
+
 enum : int { kApart = 0, kInPlace = 1, kFew = 2 };  // another user's pages; in place, side by side; in place, in order
 
 // The old position of new position i (below p.n).
@@ -186,6 +191,7 @@ __global__ __launch_bounds__(256) void keep_kernel(const KeepParams p) {
     if (tid == 0) ticket = __hip_atomic_fetch_add(&p.tickets[lg * kTicketStep], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     nth = ticket;
+    if (nth >= pages - page0) return;  // (two replays at once, see kWaits)
   }
   const int* list = p.list ? p.list + (int64_t)lg * p.n : nullptr;
   const float* wsrc = p.weights ? p.weights + (((int64_t)layer * p.users + p.weights_src) * p.nkv + g) * p.stride : nullptr;
@@ -194,7 +200,7 @@ __global__ __launch_bounds__(256) void keep_kernel(const KeepParams p) {
   const int last = MODE == kFew ? pages : page + 1;
   for (; page < last; ++page) {
     const int a = max(p.from - page * kKvPage, 0), b = min(p.n - page * kKvPage, kKvPage);
-    // In place, but for a page that takes another's place, which no old position lies in.
+    // In place, but for a page that takes another's place, which no old key or value lies in.
     const bool in_place = MODE != kApart && kv_page(p.src.pages, p.src_user, page) == kv_page(p.dst.pages, p.dst_user, page);
     // a page whose last position stays where it is has all of them there
     const bool same = in_place && old_of(p, list, page * kKvPage + b - 1) == page * kKvPage + b - 1;
@@ -207,19 +213,24 @@ __global__ __launch_bounds__(256) void keep_kernel(const KeepParams p) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (MODE == kInPlace) {
-      int* flags = p.flags + (int64_t)lg * p.pages;
-      if (tid == 0) __hip_atomic_store(&flags[page], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (tid == 0) __hip_atomic_store(&p.flags[(int64_t)lg * p.pages + page], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (same) return;
-      if (in_place && tid < 64) {  // the pages with an old position in this one
-        const int* below = p.below + (int64_t)lg * (p.pages + 1);
+    }
+    auto wait = [&]() {  // for the pages with an old position in this one
+      const int* flags = p.flags + (int64_t)lg * p.pages;
+      const int* below = p.below + (int64_t)lg * (p.pages + 1);
+      if (tid < 64) {
         const int r0 = below[page], r1 = below[page + 1];
         for (int i = max(r0 / kKvPage, page0) + tid; i < page && i * kKvPage < r1; i += 64)
-          while (!__hip_atomic_load(&flags[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) __builtin_amdgcn_s_sleep(2);
+          for (int n = 0; n < kWaits && !__hip_atomic_load(&flags[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); ++n)
+            __builtin_amdgcn_s_sleep(2);
       }
       __syncthreads();
-    }
+    };
+    if (MODE == kInPlace && in_place) wait();
     if (!same) {
       x.write(p, layer, g, page, a, b);
+      if (MODE == kInPlace && !in_place) wait();  // (its weights lie here)
       if (wdst && tid >= a && tid < b) wdst[page * kKvPage + tid] = w;
     }
     if (MODE == kFew) __syncthreads();  // LDS is free again

@@ -1151,7 +1151,7 @@ kf_status kf_kv_track(kf_kv* kv, int32_t window) {
       if (w) hipFree(w);
       return fail(KF_ENOMEM, "device allocation of %lld bytes of attention weights", (long long)(all + kept));
     }
-    const hipError_t e = hipMemset(w, 0, all);
+    const hipError_t e = hipMemsetAsync(w, 0, all, kv->st->stream);
     if (e != hipSuccess) {
       hipFree(w);
       hipFree(k);

@@ -426,6 +426,51 @@ def test_lists_of_every_length(torch, st, n, keep):
     g.close()
 
 
+@pytest.mark.parametrize("n,equal", [(30000, 30000), (30000, 20000), (8192, 8192), (200, 200)])
+def test_many_equal_weights(torch, st, n, equal):
+    """More equal weights than a list of them holds, in rows that a workgroup has in registers: the lower positions stay."""
+    g = bare_stage(st, 1, 64)
+    kv = g.kv(1, n)
+    kv.track()
+    w = np.full((1, n), 0.5, np.float32)
+    w[0, np.random.default_rng(n).permutation(n)[equal:]] = np.float32(0.5) + np.arange(n - equal, dtype=np.float32) % 7 * np.float32(2.0 ** -20)
+    kv.set_weights(0, 0, 0, on(w))
+    for keep, first, last in ((n // 3, 0, 0), (n - 1, 1, 2), (n // 2, 20, n // 4), (n, 3, 4)):
+        kv.set_len(0, n)
+        kv.write(0, 0, 0, *[torch.zeros((n, 1, 64), device="cuda")] * 2)
+        kv.set_weights(0, 0, 0, on(w))
+        kept = kv.evict(0, 0, keep, first, last, kept=True)
+        assert kept[0, 0].tolist() == kept_of(w[0].tolist(), keep, first, last), (keep, first, last)
+    kv.close()
+    g.close()
+
+
+@pytest.mark.parametrize("cache", ["f16", "mxfp4"])
+def test_weights_of_replaced_pages(torch, st, cache):
+    """In place where all pages are shared: none of them is written, but the weights of the positions they hold are moved
+    within their row, behind those that still read there."""
+    n, keep, nkv, layers = 6000, 2500, 8, 4
+    g = bare_stage(st, nkv, 64, layers=layers)
+    pages = (n + 63) // 64
+    kv = g.kv(2, n, pages + (keep + 63) // 64, dtype=cache)
+    kv.track()
+    x = torch.ones((n, nkv, 64), device="cuda")
+    w = [np.random.default_rng(l).permutation(nkv * n).reshape(nkv, n).astype(np.float32) for l in range(layers)]
+    for l in range(layers):
+        kv.write(l, 0, 0, x, x)
+        kv.set_weights(l, 0, 0, on(w[l]))
+    kv.set_len(0, n)
+    for _ in range(5):
+        kv.fork(0, 1)
+        kept = kv.evict(1, 1, keep, 10, 100, kept=True).cpu().numpy()
+        for l in range(layers):
+            assert np.array_equal(kv.weights(l, 1, 0, keep).cpu().numpy(), np.take_along_axis(w[l], kept[l].astype(np.int64), 1)), l
+    for g_ in range(nkv):
+        assert kept[0, g_].tolist() == kept_of(w[0][g_].tolist(), keep, 10, 100)
+    kv.close()
+    g.close()
+
+
 def test_a_long_eviction(torch, st):
     """262144 positions of one head, nearly all weights equal or different, half of them kept."""
     n, keep = 262144, 131001
