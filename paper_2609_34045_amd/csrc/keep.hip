@@ -4,7 +4,8 @@
 // A list of ascending positions gives each new position i its old one, list[i] >= i.
 // The moves go by pages of new positions: a workgroup reads the old ones of a page, for one KV head and layer, and
 // writes them.  In place it must not write before the others have read what lies there.  A few pages (an
-// accepted path) go one after the other in one workgroup: a page reads no position below its own.  Many go side by
+// accepted path) go four at a time in one workgroup, which reads them all and then writes: a page reads no position below
+// its own.  Many go side by
 // side: a workgroup takes a page by a ticket, in order, tells by a flag that it has read, and waits for the flags of the
 // pages whose old positions lie in its own (one or two, by the counts that select_kernel leaves).  These have lower
 // tickets, so they have started, and nothing waits before it has read: every wait ends.
@@ -40,7 +41,7 @@ struct PageF16 {
   static constexpr int PER = HD / 8, ROWS = 256 / PER, U = kKvPage / ROWS;
   v4u x[2][U];
   __device__ __forceinline__ void read(const KeepParams& p, int layer, int g, const int* list, int page, int a, int b) {
-    const int tid = threadIdx.x, d = tid % PER * 8;
+    const int tid = threadIdx.x % 256, d = tid % PER * 8;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int t = u * ROWS + tid / PER;
@@ -51,7 +52,7 @@ struct PageF16 {
     }
   }
   __device__ __forceinline__ void write(const KeepParams& p, int layer, int g, int page, int a, int b) {
-    const int tid = threadIdx.x, d = tid % PER * 8;
+    const int tid = threadIdx.x % 256, d = tid % PER * 8;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int t = u * ROWS + tid / PER;
@@ -80,7 +81,7 @@ struct PageMx {
     return c.k + layer * c.layer_bytes + (int64_t)kv_page(c.pages, user, page) * c.pages.page_stride + (int64_t)g * mx_record(HD);
   }
   __device__ __forceinline__ void read(const KeepParams& p, int layer, int g, const int* list, int page, int a, int b) {
-    const int tid = threadIdx.x, t = tid / 4, q = tid % 4;
+    const int tid = threadIdx.x % 256, t = tid / 4, q = tid % 4;
     const int p0 = old_of(p, list, page * kKvPage + a) / kKvPage, span = old_of(p, list, page * kKvPage + b - 1) / kKvPage - p0 + 1;
     whole = span <= kSpan;
     v4u v[kSpan][CODES / 16 / 256 ? CODES / 16 / 256 : 1];
@@ -131,7 +132,7 @@ struct PageMx {
     }
   }
   __device__ __forceinline__ void write(const KeepParams& p, int layer, int g, int page, int a, int b) {
-    const int tid = threadIdx.x, t = tid / 4, q = tid % 4;
+    const int tid = threadIdx.x % 256, t = tid / 4, q = tid % 4;
     uint8_t* out = record(p.dst, layer, g, p.dst_user, page);
     if (t >= a && t < b) {
       uint8_t* k = out + mx_k_byte<HD>(t, q * (HD / 4));
@@ -175,19 +176,23 @@ template <int HD>
 struct PageOf<HD, true> : PageMx<HD> {};
 }  // namespace
 
+// A page is 256 threads' work; a kFew workgroup has up to four such groups.
+constexpr int groups_of(int mode) { return mode == kFew ? 4 : 1; }
 template <int HD, bool MX, int MODE>
-__global__ __launch_bounds__(256) void keep_kernel(const KeepParams p) {
-  __shared__ __attribute__((aligned(16))) uint8_t nib[MX ? PageMx<HD>::kSpan * PageMx<HD>::CODES : 16];
-  __shared__ int at[MX ? kKvPage : 1];
+__global__ __launch_bounds__(256 * groups_of(MODE)) void keep_kernel(const KeepParams p) {
+  constexpr int GROUPS = groups_of(MODE), NIB = MX ? PageMx<HD>::kSpan * PageMx<HD>::CODES : 16;
+  __shared__ __attribute__((aligned(16))) uint8_t nib[GROUPS * NIB];
+  __shared__ int at[MX ? GROUPS * kKvPage : 1];
   __shared__ int ticket;
-  const int page0 = p.from / kKvPage, pages = (p.n + kKvPage - 1) / kKvPage, heads = p.nkv * p.layers, tid = threadIdx.x;
+  const int page0 = p.from / kKvPage, pages = (p.n + kKvPage - 1) / kKvPage, heads = p.nkv * p.layers;
+  const int tid = threadIdx.x % 256, group = MODE == kFew ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
   PageOf<HD, MX> x;
   if constexpr (MX) {
-    x.nib = nib;
-    x.at = at;
+    x.nib = nib + group * NIB;
+    x.at = at + group * kKvPage;
   }
   // Workgroup x: KV head and layer x % heads, of page x / heads (kInPlace: of the next page that none has), or (kFew) of
-  // all pages.
+  // all pages, as many at a time as it has groups.
   const int lg = blockIdx.x % heads, g = lg % p.nkv, layer = lg / p.nkv;
   int nth = blockIdx.x / heads;
   if (MODE == kInPlace) {
@@ -199,14 +204,15 @@ __global__ __launch_bounds__(256) void keep_kernel(const KeepParams p) {
   const int* list = p.list ? p.list + (int64_t)lg * p.n : nullptr;
   const float* wsrc = p.weights ? p.weights + (((int64_t)layer * p.users + p.weights_src) * p.nkv + g) * p.stride : nullptr;
   float* wdst = p.weights ? p.weights + (((int64_t)layer * p.users + p.dst_user) * p.nkv + g) * p.stride : nullptr;
-  int page = page0 + (MODE == kFew ? 0 : nth);
-  const int last = MODE == kFew ? pages : page + 1;
-  for (; page < last; ++page) {
+  const int first = page0 + (MODE == kFew ? 0 : nth), end = MODE == kFew ? pages : first + 1;
+  for (int lead = first; lead < end; lead += MODE == kFew ? blockDim.x / 256 : 1) {
+    const int page = lead + group;
+    const bool none = MODE == kFew && page >= end;
     const int a = max(p.from - page * kKvPage, 0), b = min(p.n - page * kKvPage, kKvPage);
     // In place, but for a page that takes another's place, which no old key or value lies in.
-    const bool in_place = MODE != kApart && kv_page(p.src.pages, p.src_user, page) == kv_page(p.dst.pages, p.dst_user, page);
+    const bool in_place = MODE != kApart && !none && kv_page(p.src.pages, p.src_user, page) == kv_page(p.dst.pages, p.dst_user, page);
     // a page whose last position stays where it is has all of them there
-    const bool same = in_place && old_of(p, list, page * kKvPage + b - 1) == page * kKvPage + b - 1;
+    const bool same = none || (in_place && old_of(p, list, page * kKvPage + b - 1) == page * kKvPage + b - 1);
     float w = 0.f;
     if (!same) {
       x.read(p, layer, g, list, page, a, b);
@@ -437,7 +443,7 @@ static hipError_t keep(const KeepParams& p, hipStream_t s) {
   const unsigned pages = (unsigned)((p.n + kKvPage - 1) / kKvPage - p.from / kKvPage), heads = p.nkv * p.layers;
   if (!p.in_place) hipLaunchKernelGGL((keep_kernel<HD, MX, kApart>), dim3(pages * heads), dim3(256), 0, s, p);
   else if (p.list) hipLaunchKernelGGL((keep_kernel<HD, MX, kInPlace>), dim3(pages * heads), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((keep_kernel<HD, MX, kFew>), dim3(heads), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((keep_kernel<HD, MX, kFew>), dim3(heads), dim3(256 * std::min(pages, (unsigned)groups_of(kFew))), 0, s, p);
   return hipGetLastError();
 }
 hipError_t launch_keep(const KeepParams& p, int hd, hipStream_t s) {

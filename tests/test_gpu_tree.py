@@ -268,6 +268,32 @@ def test_accepted_positions_move(torch, st, cache, hd, nkv, n, nodes, path, page
     g.close()
 
 
+@pytest.mark.parametrize("cache", ["f16", "mxfp4"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n,path", [(63, list(range(1, 256))), (60, list(range(0, 70)) + list(range(71, 256))),
+                                    (62, list(range(4)) + list(range(8, 256)))])
+def test_long_paths(torch, st, cache, hd, n, path):
+    """Paths over four and five pages, close behind themselves, with their weights."""
+    nkv, ctx = 2, n + 256
+    g = bare_stage(st, nkv, hd, layers=2)
+    kv = g.kv(1, ctx, dtype=cache)
+    kv.track()
+    data = [(rows(3 + l, ctx, nkv, hd), rows(13 + l, ctx, nkv, hd)) for l in range(2)]
+    w = np.random.default_rng(n).uniform(size=(2, nkv, ctx)).astype(np.float32)
+    at = list(range(n)) + [n + i for i in path]
+    for _ in range(3):
+        for l in range(2):
+            kv.write(l, 0, 0, *(on(x) for x in data[l]))
+            kv.set_weights(l, 0, 0, on(w[l]))
+        kv.accept(0, n, path)
+        for l in range(2):
+            check(kv, l, 0, 0, *(held(x, cache)[at] for x in data[l]), what=f"layer {l}")
+            assert np.array_equal(kv.weights(l, 0, 0, len(at)).cpu().numpy(), w[l][:, at])
+    g.sync()
+    kv.close()
+    g.close()
+
+
 def test_accepting_into_shared_pages(torch, st):
     """A tree on pages that two users share after a fork: the other user's stay as they were."""
     g = bare_stage(st, 1, 64, layers=2)
