@@ -253,7 +253,23 @@ __global__ __launch_bounds__(256 * groups_of(MODE)) void keep_kernel(const KeepP
 // Bound by what one compute unit loads, counts and waits for: 300 positions 8 us, 16384 18, 32000 29 (two thirds of it
 // waits).  The weights that share the first 11 bits are listed, so that the other two digits are looked for among few,
 // and ballots go through scalar instructions.
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048, kCopies = 4, kListed = 8192;
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048, kCopies = 4, kListed = 512;
+// Sums over the lanes up to this one: of its 16, and of all.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int plus_lane(int x) {
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int scan16(int x) {  // row_shr 1, 2, 4, 8
+  return plus_lane<0x118, 0xf>(plus_lane<0x114, 0xf>(plus_lane<0x112, 0xf>(plus_lane<0x111, 0xf>(x))));
+}
+__device__ __forceinline__ int scan64(int x) {  // and row_bcast 15, 31
+  return plus_lane<0x143, 0xc>(plus_lane<0x142, 0xa>(scan16(x)));
+}
+// The sum of the waves' values before this one's.
+__device__ __forceinline__ int before_wave(const int* of, int wave, int lane) {
+  const int x = of[lane % kSelectWaves];
+  return __builtin_amdgcn_readlane(scan16(lane < wave ? x : 0), 15);
+}
 // Ordered as the weights are; 1 for a NaN, below all, and 0 stands for no weight.
 __device__ __forceinline__ uint32_t weight_key(float w) {
   const uint32_t u = __float_as_uint(w + 0.f);
@@ -262,9 +278,9 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 template <int NV>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectParams p) {
   __shared__ __attribute__((aligned(16))) int hist[kBins * kCopies];  // a lane counts in copy lane % kCopies (many weights may be alike)
-  __shared__ uint32_t listed[kListed];
+  __shared__ uint32_t listed[kSelectWaves][kListed];
   __shared__ int sums[kSelectWaves], of[2][kSelectWaves];
-  __shared__ int found[2], n_listed;
+  __shared__ int found[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float* w = p.weights + blockIdx.y * p.layer + blockIdx.x * p.head;
   const int64_t lg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
@@ -274,26 +290,29 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectPara
   // The wave's pages: positions c0 .. c0 + 64 per - 1.
   const int all = hi > lo ? (hi + kKvPage - 1) / kKvPage - lo / kKvPage : 0, per = NV ? NV : (all + kSelectWaves - 1) / kSelectWaves;
   const int c0 = (lo / kKvPage + wave * per) * kKvPage + lane;
-  auto load = [&](int j) {
-    const int i = c0 + j * kKvPage;
-    return i >= lo && i < hi ? weight_key(w[i]) : 0u;
+  constexpr int U = NV ? NV : 8;  // pages at a time
+  uint32_t held[U];
+  auto load = [&](int j0) {
+    float x[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) x[j] = w[min(max(c0 + (j0 + j) * kKvPage, lo), max(hi, 1) - 1)];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      asm volatile("" : "+v"(x[j]));  // (else each load goes behind a branch on its position, and waits for the one before)
+      const int i = c0 + (j0 + j) * kKvPage;
+      held[j] = i >= lo && i < hi ? weight_key(x[j]) : 0u;
+    }
   };
-  uint32_t held[NV ? NV : 1];
-  if constexpr (NV > 0) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) held[j] = load(j);
-  }
-  auto key = [&](int j) { return NV ? held[NV ? j : 0] : load(j); };
+  if constexpr (NV > 0) load(0);
   auto each = [&](auto what) {
-    if constexpr (NV > 0) {
+    for (int j0 = 0; j0 < (NV ? 1 : per); j0 += U) {
+      if constexpr (NV == 0) load(j0);
 #pragma unroll
-      for (int j = 0; j < NV; ++j) what(j);
-    } else {
-      for (int j = 0; j < per; ++j) what(j);
+      for (int j = 0; j < U; ++j)
+        if (NV || j0 + j < per) what(j0 + j, held[j]);
     }
   };
   for (int b = tid; b < kBins * kCopies; b += kSelectThreads) hist[b] = 0;
-  if (tid == 0) n_listed = 0;
   for (int i = tid; i < p.first; i += kSelectThreads) list[i] = i;
   for (int i = tid; i < p.last; i += kSelectThreads) list[p.keep - p.last + i] = hi + i;
   // for a move in place (kInPlace): how many kept positions lie below each page (those between lo and hi later), no flag
@@ -321,20 +340,12 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectPara
       b += mine[i];
       a += mine[kCopies + i];
     }
-    int upto = a + b;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(upto, o);
-      if (lane >= o) upto += x;
-    }
+    int upto = scan64(a + b);
     if (lane == 63) sums[wave] = upto;
 #pragma unroll
     for (int i = 0; i < 2 * kCopies; ++i) mine[i] = 0;
     __syncthreads();
-    int x = lane < wave ? sums[lane % kSelectWaves] : 0;
-#pragma unroll
-    for (int o = 1; o < kSelectWaves; o <<= 1) x += __shfl_xor(x, o);
-    upto += __builtin_amdgcn_readfirstlane(x);
+    upto += before_wave(sums, wave, lane);
     const int before = upto - a - b;
     if (before < need && need <= upto) {
       const bool second = before + a < need;
@@ -345,46 +356,42 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectPara
     need = found[1];
     return (uint32_t)found[0];
   };
-  each([&](int j) { count(key(j) >> 21); });
+  each([&](int, uint32_t k) { count(k >> 21); });
   uint32_t prefix = find() << 21;
-  // The weights with this prefix, listed (or, where they are too many, taken from all again).
-  int n = 0;
-  each([&](int j) { n += __popcll(__ballot(key(j) >> 21 == prefix >> 21)); });
-  if (lane == 0) n = atomicAdd(&n_listed, n);
-  n = __builtin_amdgcn_readfirstlane(n);
+  // The wave's weights with this prefix, listed (or, where they are too many, taken from all again), and how many lie above.
+  int above = 0, n = 0;
   auto rank = [&](uint64_t x) {  // bits of the lower lanes
     return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(x >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)x, 0));
   };
-  each([&](int j) {
-    const uint32_t k = key(j);
+  each([&](int, uint32_t k) {
     const bool mine = k >> 21 == prefix >> 21;
+    above += __popcll(__ballot(k >> 21 > prefix >> 21));
     const uint64_t with = __ballot(mine);
     const int at = n + rank(with);
-    if (mine && at < kListed) listed[at] = k;
+    if (mine && at < kListed) listed[wave][at] = k;
     n += __popcll(with);
   });
-  __syncthreads();
-  n = n_listed;
-  auto digit = [&](int shift, int known, uint32_t bins) {
+  auto each_listed = [&](auto what) {  // all 64 lanes, 0 where there is none
     if (n <= kListed) {
-      for (int i = tid; i < n; i += kSelectThreads) {
-        const uint32_t k = listed[i];
-        if ((k ^ prefix) >> known == 0) count(k >> shift & (bins - 1));
+      for (int i = lane; i - lane < n; i += 64) {
+        const uint32_t k = listed[wave][min(i, kListed - 1)];
+        what(i < n ? k : 0u);
       }
     } else {
-      each([&](int j) {
-        const uint32_t k = key(j);
-        if ((k ^ prefix) >> known == 0) count(k >> shift & (bins - 1));
-      });
+      each([&](int, uint32_t k) { what(k >> 21 == prefix >> 21 ? k : 0u); });
     }
+  };
+  auto digit = [&](int shift, int known, uint32_t bins) {
+    each_listed([&](uint32_t k) {
+      if (k && (k ^ prefix) >> known == 0) count(k >> shift & (bins - 1));
+    });
     prefix |= find() << shift;
   };
   digit(10, 21, 2048);
   digit(0, 10, 1024);
 
-  int above = 0, equal = 0;  // in the waves before this one, then before the position
-  each([&](int j) {
-    const uint32_t k = key(j);
+  int equal = 0;  // (these and those above:) in the wave, in the waves before it, then before the position
+  each_listed([&](uint32_t k) {
     above += __popcll(__ballot(k > prefix));
     equal += __popcll(__ballot(k == prefix));
   });
@@ -393,15 +400,8 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectPara
     of[1][wave] = equal;
   }
   __syncthreads();
-  above = lane < wave ? of[0][lane % kSelectWaves] : 0;
-  equal = lane < wave ? of[1][lane % kSelectWaves] : 0;
-#pragma unroll
-  for (int o = 1; o < kSelectWaves; o <<= 1) {
-    above += __shfl_xor(above, o);
-    equal += __shfl_xor(equal, o);
-  }
-  above = __builtin_amdgcn_readfirstlane(above);
-  equal = __builtin_amdgcn_readfirstlane(equal);
+  above = before_wave(of[0], wave, lane);
+  equal = before_wave(of[1], wave, lane);
   const int page0 = c0 / kKvPage;
   int* out = list + p.first;
   int counts = 0;  // lane j % 64: what lies below page j
@@ -409,8 +409,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectPara
     const int page = page0 + j - n + 1 + lane;
     if (lane < n && page * kKvPage > lo && page * kKvPage < hi) below[page] = counts;
   };
-  each([&](int j) {
-    const uint32_t k = key(j);
+  each([&](int j, uint32_t k) {
     const bool over = k > prefix;
     bool mine = over;
     const uint64_t eq = __ballot(k == prefix);
