@@ -35,7 +35,15 @@ __device__ __forceinline__ int old_of(const KeepParams& p, const int* list, int 
   return i < p.first ? i : p.first + p.node[i - p.first];
 }
 
+// Values that are here at once, and not each where it is used.
+template <int N>
+__device__ __forceinline__ void pin(int (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
+
 // A page of fp16 keys and values on its way: thread tid has 16 bytes of every ROWS-th position of each.
+// (With all list entries and page ids loaded before the rows, 23 us became 25, and an accepted path's 3.8 4.6.)
 template <int HD>
 struct PageF16 {
   static constexpr int PER = HD / 8, ROWS = 256 / PER, U = kKvPage / ROWS;
@@ -51,13 +59,14 @@ struct PageF16 {
       x[1][u] = *reinterpret_cast<const v4u*>(p.src.v + at);
     }
   }
-  __device__ __forceinline__ void write(const KeepParams& p, int layer, int g, int page, int a, int b) {
+  __device__ __forceinline__ void write(const KeepParams& p, int layer, int g, int id, int a, int b) {  // to page id
     const int tid = threadIdx.x % 256, d = tid % PER * 8;
+    const int64_t base = 2 * (id * p.dst.pages.page_stride + (int64_t)g * kKvPage * HD + d) + layer * p.dst.layer_bytes;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int t = u * ROWS + tid / PER;
       if (t < a || t >= b) continue;
-      const int64_t at = 2 * (kv_offset(p.dst.pages, p.dst_user, g, page * kKvPage + t, HD) + d) + layer * p.dst.layer_bytes;
+      const int64_t at = base + 2 * t * HD;
       *reinterpret_cast<v4u*>(p.dst.k + at) = x[0][u];
       *reinterpret_cast<v4u*>(p.dst.v + at) = x[1][u];
     }
@@ -77,27 +86,25 @@ struct PageMx {
   v4u kc;
   uint8_t ke;
   uint16_t vs;
-  static __device__ __forceinline__ uint8_t* record(const CacheRef& c, int layer, int g, int user, int page) {
-    return c.k + layer * c.layer_bytes + (int64_t)kv_page(c.pages, user, page) * c.pages.page_stride + (int64_t)g * mx_record(HD);
-  }
   __device__ __forceinline__ void read(const KeepParams& p, int layer, int g, const int* list, int page, int a, int b) {
     const int tid = threadIdx.x % 256, t = tid / 4, q = tid % 4;
-    const int p0 = old_of(p, list, page * kKvPage + a) / kKvPage, span = old_of(p, list, page * kKvPage + b - 1) / kKvPage - p0 + 1;
+    int old[3];
+    old[0] = old_of(p, list, page * kKvPage + min(max(t, a), b - 1));
+    old[1] = old_of(p, list, page * kKvPage + a);
+    old[2] = old_of(p, list, page * kKvPage + b - 1);
+    pin(old);
+    const int from = old[0], s = from % kKvPage;
+    const int p0 = __builtin_amdgcn_readfirstlane(old[1]) / kKvPage, p1 = __builtin_amdgcn_readfirstlane(old[2]) / kKvPage;
+    const int span = p1 - p0 + 1;
     whole = span <= kSpan;
-    v4u v[kSpan][CODES / 16 / 256 ? CODES / 16 / 256 : 1];
-    if (whole) {
+    int id[kSpan + 1];
 #pragma unroll
-      for (int i = 0; i < kSpan; ++i) {
-        if (i >= span) break;
-        const v4u* src = reinterpret_cast<const v4u*>(record(p.src, layer, g, p.src_user, p0 + i) + mx_v(HD));
-#pragma unroll
-        for (int j = 0; j * 256 < CODES / 16; ++j)
-          if (j * 256 + tid < CODES / 16) v[i][j] = src[j * 256 + tid];
-      }
-    }
-    if (t >= a && t < b) {
-      const int from = old_of(p, list, page * kKvPage + t), s = from % kKvPage;
-      const uint8_t* rec = record(p.src, layer, g, p.src_user, from / kKvPage);
+    for (int i = 0; i < kSpan; ++i) id[i] = kv_page(p.src.pages, p.src_user, min(p0 + i, p1));
+    id[kSpan] = kv_page(p.src.pages, p.src_user, from / kKvPage);
+    pin(id);
+    const int64_t head = layer * p.src.layer_bytes + (int64_t)g * mx_record(HD);
+    const uint8_t* rec = p.src.k + head + (int64_t)id[kSpan] * p.src.pages.page_stride;
+    {
       const uint8_t* k = rec + mx_k_byte<HD>(s, q * (HD / 4));
       if (HD == 128) {
         kc = *reinterpret_cast<const v4u*>(k);
@@ -106,10 +113,21 @@ struct PageMx {
         kc.x = w.x;
         kc.y = w.y;
       }
-      if (q < NB) {
-        ke = rec[CODES + mx_k_exp(s, q)];
-        vs = reinterpret_cast<const uint16_t*>(rec + mx_v(HD) + CODES)[mx_v_exp<HD>(s, q)];
+      ke = rec[CODES + mx_k_exp(s, q % NB)];
+      vs = reinterpret_cast<const uint16_t*>(rec + mx_v(HD) + CODES)[mx_v_exp<HD>(s, q % NB)];
+    }
+    v4u v[kSpan][CODES / 16 / 256 ? CODES / 16 / 256 : 1];
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < kSpan; ++i) {
+        if (i >= span) break;
+        const v4u* src = reinterpret_cast<const v4u*>(p.src.k + head + (int64_t)id[i] * p.src.pages.page_stride + mx_v(HD));
+#pragma unroll
+        for (int j = 0; j * 256 < CODES / 16; ++j)
+          if (j * 256 + tid < CODES / 16) v[i][j] = src[j * 256 + tid];
       }
+    }
+    if (t >= a && t < b) {
       if (whole) {
         if (q == 0) at[t] = ((from / kKvPage - p0) * CODES + mx_v_byte(s, 0)) * 2 + (s & 1);
       } else {
@@ -131,9 +149,9 @@ struct PageMx {
       }
     }
   }
-  __device__ __forceinline__ void write(const KeepParams& p, int layer, int g, int page, int a, int b) {
+  __device__ __forceinline__ void write(const KeepParams& p, int layer, int g, int id, int a, int b) {
     const int tid = threadIdx.x % 256, t = tid / 4, q = tid % 4;
-    uint8_t* out = record(p.dst, layer, g, p.dst_user, page);
+    uint8_t* out = p.dst.k + layer * p.dst.layer_bytes + (int64_t)id * p.dst.pages.page_stride + (int64_t)g * mx_record(HD);
     if (t >= a && t < b) {
       uint8_t* k = out + mx_k_byte<HD>(t, q * (HD / 4));
       if (HD == 128) *reinterpret_cast<v4u*>(k) = kc;
@@ -210,13 +228,15 @@ __global__ __launch_bounds__(256 * groups_of(MODE)) void keep_kernel(const KeepP
     const bool none = MODE == kFew && page >= end;
     const int a = max(p.from - page * kKvPage, 0), b = min(p.n - page * kKvPage, kKvPage);
     // In place, but for a page that takes another's place, which no old key or value lies in.
-    const bool in_place = MODE != kApart && !none && kv_page(p.src.pages, p.src_user, page) == kv_page(p.dst.pages, p.dst_user, page);
+    const int to = none ? 0 : kv_page(p.dst.pages, p.dst_user, page);
+    const bool in_place = MODE != kApart && !none && kv_page(p.src.pages, p.src_user, page) == to;
     // a page whose last position stays where it is has all of them there
     const bool same = none || (in_place && old_of(p, list, page * kKvPage + b - 1) == page * kKvPage + b - 1);
     float w = 0.f;
     if (!same) {
+      int wfrom[1] = {old_of(p, list, page * kKvPage + min(max(tid, a), b - 1))};
       x.read(p, layer, g, list, page, a, b);
-      if (wsrc && tid >= a && tid < b) w = wsrc[old_of(p, list, page * kKvPage + tid)];
+      if (wsrc && tid < kKvPage) w = wsrc[wfrom[0]];
     }
     // Everything is here before anything behind this is written (and, in LDS, read).
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -238,7 +258,7 @@ __global__ __launch_bounds__(256 * groups_of(MODE)) void keep_kernel(const KeepP
     };
     if (MODE == kInPlace && in_place) wait();
     if (!same) {
-      x.write(p, layer, g, page, a, b);
+      x.write(p, layer, g, to, a, b);
       if (MODE == kInPlace && !in_place) wait();  // (its weights lie here)
       if (wdst && tid >= a && tid < b) wdst[page * kKvPage + tid] = w;
     }
