@@ -11,7 +11,7 @@
 // tickets, so they have started, and nothing waits before it has read: every wait ends.
 //
 // Bound by memory: 4096 of 16384 fp16 positions of four layers (8 heads of 128) 134 MB in 23 us, 5.9 TB/s.  In place 8001
-// of 32000 MXFP4 positions of two layers 24 us (746 in one workgroup a head); 5 accepted of 60 tokens in four layers 4 us.
+// of 32000 MXFP4 positions of two layers 22 us (746 in one workgroup a head); 5 accepted of 60 tokens in four layers 4 us.
 #include <algorithm>
 
 #include "kernels.h"
@@ -270,9 +270,9 @@ __global__ __launch_bounds__(256 * groups_of(MODE)) void keep_kernel(const KeepP
 // first (a histogram of the weights that agree so far, and where the m-th lies in it), then
 // the positions above it, and of those equal to it the first, in order.  A wave has a run of pages, 64 positions at a
 // time; with NV, the keys of its NV pages stay in registers (NV 0: they are read again at each pass).
-// Bound by what one compute unit loads, counts and waits for: 300 positions 8 us, 16384 18, 32000 29 (two thirds of it
-// waits).  The weights that share the first 11 bits are listed, so that the other two digits are looked for among few,
-// and ballots go through scalar instructions.
+// Bound by what one compute unit loads and counts: 300 positions 6 us, 16384 12, 32000 18.  Each wave lists its weights
+// that share the first 11 bits (512 at most, else it goes through all again), so that the other two digits are looked for
+// among few, and those few and a count give each wave its place in the list.
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048, kCopies = 4, kListed = 512;
 // Sums over the lanes up to this one: of its 16, and of all.
 template <int CTRL, int ROWS>
