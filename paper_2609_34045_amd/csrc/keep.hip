@@ -391,6 +391,8 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectPara
     if (mine && at < kListed) listed[wave][at] = k;
     n += __popcll(with);
   });
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (the lanes read each other's)
+  __builtin_amdgcn_wave_barrier();
   auto each_listed = [&](auto what) {  // all 64 lanes, 0 where there is none
     if (n <= kListed) {
       for (int i = lane; i - lane < n; i += 64) {
