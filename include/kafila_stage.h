@@ -53,7 +53,7 @@ extern "C" {
                             kf_kv_format, kf_kv_copy, kf_kv_fork, kf_kv_attend,
                             kf_head_logprobs, kf_logits_logprobs, kf_kv_attend_tree,
                             kf_kv_accept, kf_kv_track, kf_kv_weigh, kf_kv_weights,
-                            kf_kv_set_weights, kf_kv_evict */
+                            kf_kv_set_weights, kf_kv_evict, kf_kv_dropped, kf_kv_set_dropped */
 #define KF_KV_PAGE 64     /* positions per KV cache page */
 #define KF_MAX_BATCH 4
 
@@ -385,8 +385,9 @@ kf_status kf_kv_set_weights(kf_kv* kv, int32_t layer, int32_t user, int32_t pos0
  * Give dst_user `keep` positions of src_user (at most its length, else KF_ERANGE) in place of whatever it
  * held, and the length keep: in each layer and KV head the first `first`, the last `last` (first + last <= keep)
  * and, of those between, the ones of the largest weights, the lower position of two equal ones and a NaN
- * below every number.  They keep their order, their exact values and their weights; the keys keep the rotation of
- * the positions they came from.  dst_user may be src_user (in place); else src_user is left as it is.
+ * below every number.  They keep their order, their exact values and their weights.  The keys keep the rotation of
+ * the positions they came from, and the tokens that follow (kf_stage_decode, kf_stage_prefill) are rotated as the
+ * source's would have been: to their slot plus what was dropped (kf_kv_dropped).  dst_user may be src_user (in place); else src_user is left as it is.
  *   kept_dev : int32 [layers held, nkv, keep], the positions kept, ascending; may be NULL
  * Tracked caches only (else KF_ESTATE).  In a paged cache dst_user gives its pages back and is lent what keep
  * positions need; in place, other pages take the place of those that other users hold too (KF_ENOMEM, with nothing
@@ -395,6 +396,17 @@ kf_status kf_kv_set_weights(kf_kv* kv, int32_t layer, int32_t user, int32_t pos0
  */
 kf_status kf_kv_evict(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t keep, int32_t first, int32_t last,
                       int32_t* kept_dev);
+
+/*
+ * How many positions evictions have dropped before a user's next token: the token at slot p is rotated to position
+ * p + dropped, and callers that rotate their own queries and keys do the same.  Evictions add to it; kf_kv_fork, and a
+ * kf_kv_copy from position 0, take it along; an empty user (length 0) has none.  Setting it (0 .. INT32_MAX - max_ctx, else
+ * KF_ERANGE) is for users that were saved and written back.  The cache's table of rotations grows with it: 8 bytes for each
+ * position and pair of a head (KF_ENOMEM, with nothing changed).  A call that cannot allocate, under graph capture or
+ * kf_stage_prefill_noalloc, and that lacks rows is KF_ESTATE: an eviction outside a capture makes those that its user can need.
+ */
+kf_status kf_kv_dropped(const kf_kv* kv, int32_t user, int32_t* dropped);
+kf_status kf_kv_set_dropped(kf_kv* kv, int32_t user, int32_t dropped);
 
 /*
  * Forward one token for each of `batch` (1..KF_MAX_BATCH) users (decode): the

@@ -462,6 +462,21 @@ hipError_t launch_kv_table_share(const KvTable& t, int src, int dst, int n, hipS
   return hipGetLastError();
 }
 
+__global__ __launch_bounds__(256) void rope_rows_kernel(const RopeRows p) {
+  const int64_t at = p.from * p.half + (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= p.n * p.half) return;
+  double s, c;
+  sincos((double)(at / p.half) * p.w[at % p.half], &s, &c);
+  p.cos[at] = (float)c;
+  p.sin[at] = (float)s;
+}
+
+hipError_t launch_rope_rows(const RopeRows& p, hipStream_t s) {
+  if (p.half > 128 || p.n <= p.from) return p.half > 128 ? hipErrorInvalidValue : hipSuccess;
+  hipLaunchKernelGGL(rope_rows_kernel, dim3(((p.n - p.from) * p.half + 255) / 256), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
 hipError_t launch_kv_table_save(const KvTable& t, int src, int* out, int n, hipStream_t s) {
   if (n <= 0) return hipSuccess;
   hipLaunchKernelGGL(table_save_kernel, dim3((n + 255) / 256), dim3(256), 0, s, t, src, out, n);

@@ -196,8 +196,8 @@ __device__ __forceinline__ EpiPre gemv_epi_prefetch(const GemvParams& p, int wg,
       const int wg_per_head = p.hd / R, head = wg / wg_per_head, i0 = (wg % wg_per_head) * (R / 2);
       const int r = tid / B, b = tid % B, half = p.hd / 2;
       if (head < p.nq + p.nkv) {
-        e.a = p.rope_cos[(int64_t)p.pos[b] * half + i0 + r];
-        e.b = p.rope_sin[(int64_t)p.pos[b] * half + i0 + r];
+        e.a = p.rope_cos[(int64_t)p.rot[b] * half + i0 + r];
+        e.b = p.rope_sin[(int64_t)p.rot[b] * half + i0 + r];
       }
     }
   } else if (EPI == kEpiResid) {
@@ -787,8 +787,8 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
     }
 #pragma unroll
     for (int s = 0; s < NS / 2; ++s) {
-      const v4f* cp = reinterpret_cast<const v4f*>(p.rope_cos + (int64_t)npos * (HD / 2) + 32 * s + 8 * q4);
-      const v4f* sp = reinterpret_cast<const v4f*>(p.rope_sin + (int64_t)npos * (HD / 2) + 32 * s + 8 * q4);
+      const v4f* cp = reinterpret_cast<const v4f*>(p.rope_cos + (int64_t)p.rot[b] * (HD / 2) + 32 * s + 8 * q4);
+      const v4f* sp = reinterpret_cast<const v4f*>(p.rope_sin + (int64_t)p.rot[b] * (HD / 2) + 32 * s + 8 * q4);
       const v4f c0 = cp[0], c1 = cp[1], n0 = sp[0], n1 = sp[1];
       const float c[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
       const float sn[8] = {n0.x, n0.y, n0.z, n0.w, n1.x, n1.y, n1.z, n1.w};
@@ -836,7 +836,7 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
     uint16_t k16[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float cs = p.rope_cos[(int64_t)npos * (HD / 2) + i0 + j], sn = p.rope_sin[(int64_t)npos * (HD / 2) + i0 + j];
+      const float cs = p.rope_cos[(int64_t)p.rot[b] * (HD / 2) + i0 + j], sn = p.rope_sin[(int64_t)p.rot[b] * (HD / 2) + i0 + j];
       k16[j] = f16_checked(x[j] * cs + sgn * y[j] * sn, bad);
     }
     knew = v4u{k16[0] | ((uint32_t)k16[1] << 16), k16[2] | ((uint32_t)k16[3] << 16),

@@ -212,10 +212,11 @@ struct GemvParams {
   uint16_t* vc;
   KvPages kv;
   int nq, nkv, hd;
-  const float* rope_cos;  // [max_ctx][hd/2]
+  const float* rope_cos;  // [positions][hd/2]
   const float* rope_sin;
   int users[kMaxBatch];
   int pos[kMaxBatch];
+  int rot[kMaxBatch];     // the position that row b is rotated to: pos, and what was dropped before it
   // Blocks with per-head q/k norms: when set, q goes to `q` and k to kraw
   // ([B][nkv][hd] fp32) as projected (after the attention RMSNorm), without
   // RoPE; the decode attention finishes both.  v goes to the cache as usual.
@@ -268,8 +269,9 @@ struct AttnParams {
   const float* kraw;      // [B][nkv][hd]
   const uint16_t* gq;     // [hd] bf16
   const uint16_t* gk;
-  const float* rope_cos;  // [max_ctx][hd/2]
+  const float* rope_cos;  // [positions][hd/2]
   const float* rope_sin;
+  int rot[kMaxBatch];     // the position that row b's query and new key are rotated to
   float eps;
   int* err_flag;          // sticky error bits: kErrF16Range for an fp16 store out of range
 };
@@ -359,6 +361,14 @@ __device__ __forceinline__ void kv_table_apply(const KvTable& t, const KvTableUp
 hipError_t launch_kv_table_update(const KvTable& t, const KvTableUpdate& u, hipStream_t s);
 // page[dst + i] = page[src + i] for i < n, as each entry's next update: a user that shares another's pages.
 hipError_t launch_kv_table_share(const KvTable& t, int src, int dst, int n, hipStream_t s);
+// Rows [from, n) of a RoPE table, [n][half]: cosines and sines of position times w[i].
+struct RopeRows {
+  double w[128];  // half of them
+  float *cos, *sin;
+  int half;
+  int64_t from, n;
+};
+hipError_t launch_rope_rows(const RopeRows& p, hipStream_t s);
 // out[i] = page[src + i] for i < n.
 hipError_t launch_kv_table_save(const KvTable& t, int src, int* out, int n, hipStream_t s);
 
@@ -508,13 +518,14 @@ struct WeighParams {
   float* weights;  // [user][nkv][stride] of the layer
   int64_t stride;
   float* part;     // workspace: [row][nq][max_splits][2]
-  // queries as projected, whose norm (gains gq, eps) and rotation to position len - 1 are due; gq NULL: none
+  // queries as projected, whose norm (gains gq, eps) and rotation to position rot are due; gq NULL: none
   const uint16_t* gq;
   const float *rope_cos, *rope_sin;
   float eps;
   int users;
   WeighUser user[kMaxWeighRows];
   int row[kMaxWeighRows], len[kMaxWeighRows];  // of each row, user after user: its row of q, and its positions
+  int rot[kMaxWeighRows];                      // (with gq)
   int pages, max_splits;                       // set by the launcher: pages per split, splits of a row in `part`
 };
 hipError_t launch_weigh(WeighParams p, int hd, int n_cu, int64_t part_floats, hipStream_t s);

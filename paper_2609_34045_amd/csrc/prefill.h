@@ -14,7 +14,7 @@ struct PrefillArgs {
   int pos0;       // position of the first token
   int user;       // the user's row of the KV cache
   KvPages kv;
-  const float* rope_cos;  // [max_ctx][hd/2]
+  const float* rope_cos;  // [positions][hd/2], from the one that slot 0 is rotated to
   const float* rope_sin;
   int* err_flag;  // sticky error bits (kErrF16Range for an fp16 activation, key or value out of range)
   hipStream_t stream;

@@ -205,12 +205,15 @@ struct kf_kv {
   mutable unsigned long long recorded_in = 0;
   KvTable kv_table() const { return KvTable{table, (uint32_t*)(table + host_table.size())}; }
   std::vector<int> held;       // pages each user holds
+  std::vector<int> dropped;    // positions that evictions dropped before each user's next: what it is rotated by beyond its slot
   std::vector<int> free_pages; // the pool's free pages (paged caches only), next page last
   std::vector<int> refs;       // users that hold each page (paged caches only); a page of several is copied before a write
   kf_kv_type type = KF_KV_F16;
   uint16_t *k = nullptr, *v = nullptr;  // KF_KV_MXFP4: the records at k, no v, and strides in bytes
   int64_t bytes = 0;                    // device bytes of everything here
   float *rcos = nullptr, *rsin = nullptr;
+  int64_t rope_rows = 0;                // of them
+  std::vector<float*> old_ropes;        // shorter tables, which captured steps may still read
   float *part_acc = nullptr, *part_ml = nullptr;
   // KF_KV_MXFP4: a decode step's new keys and values, which the QKV launch leaves in fp16 as in an fp16
   // cache, row b's in page b (append_table gives that page for every position); and one layer of one user's
@@ -861,6 +864,7 @@ static kf_status kv_make(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_
   kv->page_stride = kv->mx() ? (int64_t)c.n_kv_heads * mx_record(c.head_dim) : (int64_t)c.n_kv_heads * kKvPage * c.head_dim;
   kv->layer_stride = kv->page_stride * kv->n_pages;
   kv->len.assign(max_users, 0);
+  kv->dropped.assign(max_users, 0);
   kv->held.assign(max_users, paged ? 0 : ppu);
   if (paged) {
     kv->host_table.assign((size_t)max_users * ppu, -1);
@@ -893,6 +897,7 @@ static kf_status kv_make(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_
   kv->v = (uint16_t*)mem[1];
   kv->rcos = (float*)mem[2];
   kv->rsin = (float*)mem[3];
+  kv->rope_rows = max_ctx;
   kv->part_acc = (float*)mem[4];
   kv->part_ml = (float*)mem[5];
   kv->table = (int*)mem[6];
@@ -970,6 +975,7 @@ kf_status kf_kv_destroy(kf_kv* kv) {
                  kv->weights, kv->kept};
   for (void* m : mem)
     if (m) hipFree(m);
+  for (float* m : kv->old_ropes) hipFree(m);
   kv->st->live_kv--;
   delete kv;
   return KF_OK;
@@ -999,6 +1005,47 @@ kf_status kf_kv_set_len(kf_kv* kv, int32_t user, int32_t len) {
   if (st != KF_OK) return st;
   kv_release(kv, user, pages_for(len));
   kv->len[user] = len;
+  if (len == 0) kv->dropped[user] = 0;
+  return KF_OK;
+}
+
+// RoPE rows of positions [0, n).  A longer table holds the same rows; captured steps go on reading the one that they were
+// recorded with.
+static kf_status rope_upto(kf_kv* kv, int64_t n, bool allocate = true) {
+  if (n <= kv->rope_rows) return KF_OK;
+  if (!allocate || capturing(kv->st))
+    return fail(KF_ESTATE, "rotations to position %lld need a longer table, which this call may not allocate", (long long)(n - 1));
+  const kf_model_config& c = kv->st->cfg;
+  const int64_t rows = std::max(n, 2 * kv->rope_rows), half = c.head_dim / 2;
+  float *cs = nullptr, *sn = nullptr;
+  if (hipMalloc((void**)&cs, rows * half * 4) != hipSuccess || hipMalloc((void**)&sn, rows * half * 4) != hipSuccess) {
+    (void)hipGetLastError();
+    if (cs) hipFree(cs);
+    return fail(KF_ENOMEM, "device allocation of %lld bytes of rotations", (long long)(rows * half * 8));
+  }
+  RopeRows p{};
+  for (int64_t i = 0; i < half; ++i) p.w[i] = std::pow((double)c.rope_theta, -2.0 * (double)i / (double)c.head_dim);
+  p.cos = cs;
+  p.sin = sn;
+  p.half = (int)half;
+  p.from = kv->rope_rows;
+  p.n = rows;
+  const int64_t had = kv->rope_rows * half * 4;
+  hipError_t e = hipMemcpyAsync(cs, kv->rcos, had, hipMemcpyDeviceToDevice, kv->st->stream);
+  if (e == hipSuccess) e = hipMemcpyAsync(sn, kv->rsin, had, hipMemcpyDeviceToDevice, kv->st->stream);
+  if (e == hipSuccess) e = launch_rope_rows(p, kv->st->stream);
+  if (e != hipSuccess) {
+    hipStreamSynchronize(kv->st->stream);
+    hipFree(cs);
+    hipFree(sn);
+    return fail(KF_EDEVICE, "rotations: %s", hipGetErrorString(e));
+  }
+  kv->old_ropes.push_back(kv->rcos);
+  kv->old_ropes.push_back(kv->rsin);
+  kv->rcos = cs;
+  kv->rsin = sn;
+  kv->rope_rows = rows;
+  kv->bytes += rows * half * 8;
   return KF_OK;
 }
 
@@ -1097,6 +1144,7 @@ kf_status kf_kv_copy(kf_kv* dst, int32_t dst_user, const kf_kv* src, int32_t src
   KF_HIP(launch_cache_copy(dst->ref(), dst_user, src->ref(), src_user, pos0, n, dst->layers(), dst->st->err_flag,
                            dst->st->stream),
          "kv_copy launch");
+  if (pos0 == 0) dst->dropped[dst_user] = src->dropped[src_user];
   return weights_copied(dst, dst_user, src, src_user, pos0, n);
 }
 
@@ -1112,6 +1160,7 @@ kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n) {
     KF_HIP(launch_cache_copy(kv->ref(), dst_user, kv->ref(), src_user, 0, n, kv->layers(), kv->st->err_flag, st),
            "kv_fork launch");
     kv->len[dst_user] = n;
+    kv->dropped[dst_user] = n ? kv->dropped[src_user] : 0;
     return weights_copied(kv, dst_user, kv, src_user, 0, n);
   }
   if (capturing(kv->st))  // each replay would take the destination's own pages out of its table again
@@ -1135,6 +1184,7 @@ kf_status kf_kv_fork(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t n) {
     KF_HIP(launch_kv_table_share(kv->kv_table(), src_user * kv->ppu + same, dst_user * kv->ppu + same, pages - same, st),
            "page table update");
   kv->len[dst_user] = n;
+  kv->dropped[dst_user] = n ? kv->dropped[src_user] : 0;
   return weights_copied(kv, dst_user, kv, src_user, 0, n);
 }
 
@@ -1190,6 +1240,22 @@ kf_status kf_kv_set_weights(kf_kv* kv, int32_t layer, int32_t user, int32_t pos0
   return KF_OK;
 }
 
+kf_status kf_kv_dropped(const kf_kv* kv, int32_t user, int32_t* dropped) {
+  if (!kv || !dropped) return fail(KF_EINVAL, "NULL argument");
+  if (user < 0 || user >= kv->max_users) return fail(KF_EINVAL, "user %d outside [0, %d)", user, kv->max_users);
+  *dropped = kv->dropped[user];
+  return KF_OK;
+}
+kf_status kf_kv_set_dropped(kf_kv* kv, int32_t user, int32_t dropped) {
+  if (!kv) return fail(KF_EINVAL, "kv is NULL");
+  if (user < 0 || user >= kv->max_users) return fail(KF_EINVAL, "user %d outside [0, %d)", user, kv->max_users);
+  if (dropped < 0 || (int64_t)dropped + kv->max_ctx > INT32_MAX) return fail(KF_ERANGE, "%d positions dropped", dropped);
+  const kf_status st = rope_upto(kv, (int64_t)dropped + kv->max_ctx);
+  if (st != KF_OK) return st;
+  kv->dropped[user] = dropped;
+  return KF_OK;
+}
+
 // Adds the weights of `rows` queries of one layer, row b's over positions [0, lens[b]) of users[b]; those from fresh[b]
 // on (the same for every row of a user) have none yet.  p holds the queries.
 static kf_status weigh_rows(kf_kv* kv, WeighParams& p, int layer, int rows, const int* users, const int* lens, const int* fresh) {
@@ -1216,6 +1282,7 @@ static kf_status weigh_rows(kf_kv* kv, WeighParams& p, int layer, int rows, cons
     for (int j = b; j < rows; ++j) {
       if (users[j] != users[b]) continue;
       p.row[n] = j;
+      p.rot[n] = lens[j] - 1 + kv->dropped[users[j]];
       p.len[n++] = lens[j];
       u.rows++;
       u.len = std::max(u.len, lens[j]);
@@ -1263,6 +1330,12 @@ kf_status kf_kv_evict(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t kee
   const int len = kv->len[src_user];
   if (keep > len) return fail(KF_ERANGE, "%d positions of user %d, which holds %d", keep, src_user, len);
   if (!kv->weights) return fail(KF_ESTATE, "the cache is not tracked");
+  const int64_t dropped = keep ? (int64_t)kv->dropped[src_user] + len - keep : 0;
+  if (dropped + kv->max_ctx > INT32_MAX) return fail(KF_ERANGE, "%lld positions dropped", (long long)dropped);
+  if (!capturing(kv->st)) {
+    const kf_status grown = rope_upto(kv, dropped + kv->max_ctx);
+    if (grown != KF_OK) return grown;
+  }
   const bool in_place = src_user == dst_user;
   bool moved = false;  // in place, but for some pages
   KvPages source = kv->pages();
@@ -1330,6 +1403,7 @@ kf_status kf_kv_evict(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t kee
   }
   kv_release(kv, dst_user, pages_for(keep));
   kv->len[dst_user] = keep;
+  kv->dropped[dst_user] = (int)dropped;
   return KF_OK;
 }
 
@@ -1597,6 +1671,7 @@ kf_status kf_kv_accept(kf_kv* kv, int32_t user, int32_t len, int32_t n, const in
   }
   kv_release(kv, user, pages_for(len + n));
   kv->len[user] = len + n;
+  if (len + n == 0) kv->dropped[user] = 0;
   return KF_OK;
 }
 
@@ -1637,7 +1712,9 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     from[b] = positions[b];
     upto[b] = from[b] + 1;
   }
-  const kf_status gst = kv_grant(kv, batch, users, from, upto);
+  kf_status gst = KF_OK;
+  for (int b = 0; b < batch && gst == KF_OK; ++b) gst = rope_upto(kv, (int64_t)positions[b] + kv->dropped[users[b]] + 1);
+  if (gst == KF_OK) gst = kv_grant(kv, batch, users, from, upto);
   if (gst != KF_OK) return gst;
   s->kept_rows = 0;  // the residual rows change from here on; set again when the step completes
 
@@ -1672,6 +1749,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     for (int b = 0; b < kMaxBatch; ++b) {
       g.users[b] = b < batch ? users[b] : 0;
       g.pos[b] = b < batch ? positions[b] : 0;
+      g.rot[b] = b < batch ? positions[b] + kv->dropped[users[b]] : 0;
     }
     if (kv->mx()) {  // kept in fp16 for attn_mx, which stores them
       g.kv = kv->append_pages();
@@ -1723,6 +1801,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     for (int b = 0; b < kMaxBatch; ++b) {
       a.users[b] = b < batch ? users[b] : 0;
       a.len[b] = b < batch ? positions[b] + 1 : 0;
+      a.rot[b] = g.rot[b];
     }
     if (kv->mx()) attn_split_mx(c.n_kv_heads, batch, a.len, kv->max_split, s->n_cu, a, rows);
     {
@@ -2150,8 +2229,6 @@ static kf_status prefill_impl(kf_stage* s, kf_kv* kv, int32_t user, int32_t pos0
   pa.pos0 = pos0;
   pa.user = user;
   pa.kv = kv->pages();
-  pa.rope_cos = kv->rcos;
-  pa.rope_sin = kv->rsin;
   pa.err_flag = s->err_flag;
   pa.stream = s->stream;
   PrefillWorkspace scratch_ws;
@@ -2170,8 +2247,11 @@ static kf_status prefill_impl(kf_stage* s, kf_kv* kv, int32_t user, int32_t pos0
     KF_HIP(e, "prefill workspace");
   }
   const int64_t from = pos0, upto = from + n;
-  const kf_status gst = kv_grant(kv, 1, &user, &from, &upto);
+  kf_status gst = rope_upto(kv, upto + kv->dropped[user], !no_alloc);
+  if (gst == KF_OK) gst = kv_grant(kv, 1, &user, &from, &upto);
   if (gst != KF_OK) return gst;
+  pa.rope_cos = kv->rcos + (int64_t)kv->dropped[user] * (c.head_dim / 2);
+  pa.rope_sin = kv->rsin + (int64_t)kv->dropped[user] * (c.head_dim / 2);
   const Tracer tr = no_alloc ? Tracer{} : s->tracer();  // event records may create events
   if (kv->mx()) {  // the chunk works on one layer's positions in fp16 pages (prefill_layer brings them there)
     pa.kv = KvPages{nullptr, kv->ppu, (int64_t)c.n_kv_heads * kKvPage * c.head_dim};

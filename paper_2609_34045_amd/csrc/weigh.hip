@@ -122,7 +122,7 @@ __device__ __forceinline__ void queries(const WeighParams& p, const Split& s, v4
         for (int o = 1; o < PER; o <<= 1) ss += __shfl_xor(ss, o);
         const float rs = 1.0f / sqrtf(ss / (float)HD + p.eps);
         float gain[8], cs[8], sn[8];
-        const int64_t at = (int64_t)(p.len[r] - 1) * (HD / 2) + 8 * c % (HD / 2);
+        const int64_t at = (int64_t)p.rot[r] * (HD / 2) + 8 * c % (HD / 2);
         load_q8(p.gq, 1, 8 * c, gain);
         load_q8(p.rope_cos, 0, at, cs);
         load_q8(p.rope_sin, 0, at, sn);

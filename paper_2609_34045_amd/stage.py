@@ -35,7 +35,7 @@ EXPORTS = ("kf_abi_version", "kf_last_error", "kf_stage_bytes", "kf_stage_init",
            "kf_kv_create_paged", "kf_kv_pages", "kf_stage_set_flags", "kf_stage_get_flags",
            "kf_stage_prefill_noalloc", "kf_kv_create_typed", "kf_kv_format", "kf_kv_copy", "kf_kv_fork",
            "kf_kv_attend", "kf_head_logprobs", "kf_logits_logprobs", "kf_kv_attend_tree", "kf_kv_accept",
-           "kf_kv_track", "kf_kv_weigh", "kf_kv_weights", "kf_kv_set_weights", "kf_kv_evict")
+           "kf_kv_track", "kf_kv_weigh", "kf_kv_weights", "kf_kv_set_weights", "kf_kv_evict", "kf_kv_dropped", "kf_kv_set_dropped")
 KV_TYPES = {"f16": 0, "mxfp4": 1}  # kf_kv_type
 PREFILL_SCRATCH_BYTES = 144 << 20  # KF_PREFILL_SCRATCH_BYTES: the no-allocation prefill's workspace limit
 KF_STAGE_ORDERED = 1  # batch-1 decode adds the heads' output projections in a fixed order
@@ -135,6 +135,8 @@ def load_library(path: str = LIB_PATH):
         "kf_kv_weights": (I32, [P, I32, I32, I32, I32, VP]),
         "kf_kv_set_weights": (I32, [P, I32, I32, I32, I32, VP]),
         "kf_kv_evict": (I32, [P, I32, I32, I32, I32, I32, VP]),
+        "kf_kv_dropped": (I32, [P, I32, I32P]),
+        "kf_kv_set_dropped": (I32, [P, I32, I32]),
         "kf_kv_pages": (I32, [P, I32P, I32P]),
         "kf_stage_set_flags": (I32, [P, I32]),
         "kf_stage_get_flags": (I32, [P, I32P]),
@@ -570,6 +572,16 @@ class KV:
             at = torch.empty((layers, self.stage.shape.n_kv_heads, max(keep, 0)), dtype=torch.int32, device="cuda")
         _check(self._lib.kf_kv_evict(self.handle, src_user, dst_user, keep, first, last, _ptr(at)), "kf_kv_evict")
         return at
+
+    def dropped(self, user: int) -> int:
+        """Positions dropped before the user's next token, which is rotated to its slot plus these (kf_kv_dropped)."""
+        n = ctypes.c_int32()
+        _check(self._lib.kf_kv_dropped(self.handle, user, ctypes.byref(n)), "kf_kv_dropped")
+        return n.value
+
+    def set_dropped(self, user: int, dropped: int):
+        """Sets it, for a user that was saved and written back (kf_kv_set_dropped)."""
+        _check(self._lib.kf_kv_set_dropped(self.handle, user, dropped), "kf_kv_set_dropped")
 
     def describe(self) -> dict:
         owner, mu, mc = ctypes.c_void_p(), ctypes.c_int32(), ctypes.c_int32()

@@ -257,6 +257,7 @@ def test_trees_weights_and_evictions_reject_before_touching_the_device(lib):
     assert lib.kf_kv_weights(None, 0, 0, 0, 1, P(16)) == 1
     assert lib.kf_kv_set_weights(None, 0, 0, 0, 1, P(16)) == 1
     assert lib.kf_kv_evict(None, 0, 1, 1, 0, 0, None) == 1
+    assert lib.kf_kv_dropped(None, 0, one) == 1 and lib.kf_kv_set_dropped(None, 0, 1) == 1
 
 
 def test_limits_match_the_header():

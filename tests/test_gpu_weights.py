@@ -712,3 +712,105 @@ def test_captured_decode_steps_on_a_tracked_cache(torch, st):
     g.sync()
     kv.close()
     g.close()
+
+
+def layer64(x, w, shape, k, v, new, rot):
+    """One layer in 64 bits over rows x at rotations rot; row i sees the cached keys and values [.., nkv, hd] up to `new` + i,
+    which hold the rows' own.  Returns the rows' outputs, queries and keys."""
+    hd = shape.head_dim
+    xn = so.rms_norm(x, w["attn_norm"], shape.rms_eps)
+    q, key = ((xn @ w[n].T).reshape(len(x), -1, hd) for n in ("wq", "wk"))
+    if shape.qk_norm:
+        q, key = so.rms_norm(q, w["q_norm"], shape.rms_eps), so.rms_norm(key, w["k_norm"], shape.rms_eps)
+    q, key = so.rope(q, np.asarray(rot), shape.rope_theta), so.rope(key, np.asarray(rot), shape.rope_theta)
+    upto = [new + i + 1 for i in range(len(x))]
+    x = x + so.attention_rows(q, [k[:n] for n in upto], [v[:n] for n in upto], shape.n_kv_heads) @ w["wo"].T
+    return x + so.mlp_swiglu(so.rms_norm(x, w["mlp_norm"], shape.rms_eps), w["wg"], w["wu"], w["wd"]), q, key
+
+
+@pytest.mark.parametrize("cache", ["f16", "mxfp4"])
+@pytest.mark.parametrize("shape", [synth.ModelShape(2, 512, 8, 2, 64, 1408, 1000), synth.ModelShape(2, 384, 8, 2, 64, 1024, 1000, qk_norm=True),
+                                   synth.ModelShape(2, 512, 8, 2, 128, 704, 0, qk_norm=True)], ids=["tiny", "qwen3", "hd128"])
+def test_tokens_after_an_eviction_keep_their_distances(torch, st, cache, shape):
+    """A prompt is cut, then decode steps (alone and beside a user that lost nothing), a chunk, a second cut that takes the
+    rotations past max_ctx, and a step of a fork: every token is rotated as if nothing had been dropped."""
+    cfg, n, ctx = 77, 150, 160
+    model = SeededModel(shape, cfg)
+    w = [{k: so.bf16_to_f64(v) for k, v in model.layer(l).items()} for l in range(2)]
+    g = st.Stage(shape, 0, 2, model.layer)
+    kv = g.kv(3, ctx, 12, dtype=cache)
+    kv.track(8)
+    for u in range(2):
+        g.prefill(kv, u, 0, hidden=on(synth.hidden_states(cfg, synth.STREAM_PREFILL_HIDDEN, u, n - 80 * u, shape.hidden)))
+    assert [kv.dropped(u) for u in range(3)] == [0, 0, 0]
+    seen = [n, n - 80, 0]  # tokens of each user's text
+
+    def compare(user, x, got, m):
+        """The last m tokens of the user, whose outputs are `got`; what they attend to is read back."""
+        new = kv.len(user) - m
+        assert seen[user] - kv.dropped(user) == new
+        rot = [seen[user] + i for i in range(m)]
+        x = np.asarray(x, np.float64)
+        for l in range(2):
+            k, v = (t.double().cpu().numpy() for t in kv.read(l, user, 0, new + m))
+            x, q, key = layer64(x, w[l], shape, k, v, new, rot)
+            # fp16 operands and cache: some 2^-10 of the largest.  A 4-bit block's largest value is M < 7 units, its codes end
+            # in 3, 4 and 6: a value up to 4 is off by 1/2 at most and M is 3.5 at least, so by M / 7; one of 4 to 5 by what
+            # it has beyond 4, (M - 4) / M <= 1/5 of M at M = 5; one past 5 by 1, 1/5 of M at most.
+            assert np.abs(k[new:] - key).max() <= (3e-3 if cache == "f16" else 0.2 + 3e-3) * np.abs(key).max(), (user, l)
+            if m == 1:
+                # a query off by 2^-8 (a layer's fp16 operands) moves a score by that of its sum of |products|
+                a, _ = weight_of(q[0], k, new + 1)
+                G = shape.n_q_heads // shape.n_kv_heads
+                S = max((np.abs(k[:, h // G]) @ np.abs(q[0, h])).max() for h in range(shape.n_q_heads)) / math.sqrt(shape.head_dim)
+                b = kv.weights(l, user, 0, new + 1).double().cpu().numpy() - before[user, l]
+                assert np.all(np.abs(a - b) <= a * math.expm1(2 * 2.0 ** -8 * S) + 1e-5), (user, l)
+        got = got.double().cpu().numpy()
+        assert np.all(np.abs(got - x).max(1) <= 1e-2 * np.abs(x).max(1)), user
+        seen[user] += m
+
+    def decode(step, users):
+        x = synth.hidden_states(cfg, synth.STREAM_DECODE_HIDDEN, step, len(users), shape.hidden)
+        for u in users:
+            for l in range(2):
+                old = kv.weights(l, u, 0, kv.len(u)).double().cpu().numpy()
+                before[u, l] = np.concatenate([old, np.zeros((shape.n_kv_heads, 1))], 1)
+        out = g.decode(kv, users, [kv.len(u) for u in users], hidden=on(x))
+        for i, u in enumerate(users):
+            compare(u, x[i:i + 1], out[i:i + 1], 1)
+    before = {}
+    kv.evict(0, 0, 90, 4, 20)
+    assert kv.dropped(0) == 60 and kv.len(0) == 90
+    decode(0, [0])
+    decode(1, [0, 1])
+    x = synth.hidden_states(cfg, synth.STREAM_PREFILL_HIDDEN, 7, 33, shape.hidden)
+    compare(0, x, g.prefill(kv, 0, kv.len(0), hidden=on(x), noalloc=True), 33)
+    kv.evict(0, 0, 50, 4, 20)  # the next token's rotation is past max_ctx
+    assert kv.dropped(0) == 60 + 125 - 50 and seen[0] > ctx
+    decode(2, [1, 0])
+    kv.fork(0, 2)
+    seen[2] = seen[0]
+    assert kv.dropped(2) == kv.dropped(0)
+    decode(3, [2])
+    kv.evict(0, 2, 10, 1, 9)
+    seen[2] = seen[0]
+    decode(4, [2, 0])
+    kv.set_len(2, 0)
+    assert kv.dropped(2) == 0
+    other = g.kv(1, ctx, dtype=cache)
+    other.copy(kv, 0, 0, 5, 10)
+    assert other.dropped(0) == 0
+    other.copy(kv, 0, 0, 0, 20)
+    assert other.dropped(0) == kv.dropped(0)
+    other.set_dropped(0, 7)
+    assert other.dropped(0) == 7
+    for bad in (-1, 2 ** 31 - ctx):
+        with pytest.raises(st.KFError) as e:
+            other.set_dropped(0, bad)
+        assert e.value.status == st.KF_ERANGE
+    with pytest.raises(st.KFError):
+        other.dropped(1)
+    g.sync()
+    kv.close()
+    other.close()
+    g.close()
