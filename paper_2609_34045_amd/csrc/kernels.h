@@ -518,6 +518,11 @@ struct WeighParams {
   float* weights;  // [user][nkv][stride] of the layer
   int64_t stride;
   float* part;     // workspace: [row][nq][max_splits][2]
+  // or, of a decode step, what its attention left, in log2 units and with sums times 2^ml_shift: row b's ml_n[b] splits of
+  // [b][nq][ml_splits][2]; then the first pass is not taken
+  const float* ml;
+  int ml_splits, ml_n[kMaxBatch];
+  float ml_shift;
   // queries as projected, whose norm (gains gq, eps) and rotation to position rot are due; gq NULL: none
   const uint16_t* gq;
   const float *rope_cos, *rope_sin;

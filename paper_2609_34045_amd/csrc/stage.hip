@@ -1856,6 +1856,10 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
         w.rope_sin = kv->rsin;
         w.eps = c.rms_eps;
       }
+      w.ml = kv->part_ml;
+      w.ml_splits = kv->max_split;
+      w.ml_shift = kv->mx() ? kPartShift : 0.f;
+      for (int b = 0; b < batch; ++b) w.ml_n[b] = kv->mx() ? rows.n[b] : n_split;
       const kf_status wst = weigh_rows(kv, w, l, batch, users, a.len, positions);
       if (wst != KF_OK) return wst;
     }

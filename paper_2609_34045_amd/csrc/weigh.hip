@@ -11,6 +11,7 @@
 // In the first pass the tiles are K Q^T, whose lanes hold a column each, in the
 // second Q K^T, whose lanes hold a position, so that both sums run along registers.
 // A position has one writer, so the order of all additions is fixed.
+// A decode step's attention has left (M, L) of its splits, and the second pass is enough.
 //
 // What bounds it: the keys are read twice, once from HBM and once mostly from the caches behind it, which at 7 TB/s is 5 us
 // of the 17 + 16 us that 32 rows of 32 heads at 16384 fp16 positions take (8 KV heads, bf16 queries; 34 MB of keys), and
@@ -301,40 +302,44 @@ __global__ __launch_bounds__(64 * waves_for(COLS)) void weigh_add_kernel(const W
   // The splits' maxima and sums joined, `per` threads a column; the first of them come while the queries do.
   constexpr int U = 4;
   int per = 1;
-  while (per < 64 && 2 * per * s.cols <= 64 * kWaves && per < w.splits) per *= 2;
-  const int c = tid / per, cc = min(c, s.cols - 1);
-  const float2* part = reinterpret_cast<const float2*>(p.part) + (((int64_t)s.row0 + cc / G) * p.nq + s.g * G + cc % G) * p.max_splits;
+  // (a step's users have one row each)
+  const int splits = p.ml ? p.ml_n[p.row[s.row0]] : w.splits;
+  while (per < 64 && 2 * per * s.cols <= 64 * kWaves && per < splits) per *= 2;
+  const int c = tid / per, cc = min(c, s.cols - 1), r = s.row0 + cc / G;
+  const float2* part = p.ml ? reinterpret_cast<const float2*>(p.ml) + ((int64_t)p.row[r] * p.nq + s.g * G + cc % G) * p.ml_splits
+                            : reinterpret_cast<const float2*>(p.part) + ((int64_t)r * p.nq + s.g * G + cc % G) * p.max_splits;
   float2 x[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) x[u] = part[min(tid % per + u * per, w.splits - 1)];
+  for (int u = 0; u < U; ++u) x[u] = part[min(tid % per + u * per, splits - 1)];
   queries<HD, PARTS, COLS>(p, s, q, scale);
   __syncthreads();
   if (c < COLS) {
     float M = -INFINITY, L = 0.f;
+    const float unit = c < s.cols ? p.ml ? 1.0f : scale[c] : 0.f;  // of a maximum, to log2 units
     if (c < s.cols) {
-      for (int z0 = tid % per; z0 < w.splits; z0 += U * per) {
+      for (int z0 = tid % per; z0 < splits; z0 += U * per) {
         float m = M;
 #pragma unroll
         for (int u = 0; u < U; ++u) m = fmaxf(m, x[u].x);
         // (M is -inf where every score was NaN: that sum stays NaN)
-        L = M == -INFINITY ? L : L * __builtin_amdgcn_exp2f((M - m) * scale[c]);
+        L = M == -INFINITY ? L : L * __builtin_amdgcn_exp2f((M - m) * unit);
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (z0 + u * per < w.splits) L += m == -INFINITY ? x[u].y : x[u].y * __builtin_amdgcn_exp2f((x[u].x - m) * scale[c]);
+          if (z0 + u * per < splits) L += m == -INFINITY ? x[u].y : x[u].y * __builtin_amdgcn_exp2f((x[u].x - m) * unit);
         M = m;
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = part[min(z0 + (U + u) * per, w.splits - 1)];
+        for (int u = 0; u < U; ++u) x[u] = part[min(z0 + (U + u) * per, splits - 1)];
       }
     }
     for (int o = 1; o < per; o <<= 1) {
       const float m2 = __shfl_xor(M, o), l2 = __shfl_xor(L, o), m = fmaxf(M, m2);
-      const float k = c < s.cols ? scale[c] : 0.f;
-      L = m == -INFINITY ? L + l2 : L * __builtin_amdgcn_exp2f((M - m) * k) + l2 * __builtin_amdgcn_exp2f((m2 - m) * k);
+      L = m == -INFINITY ? L + l2 : L * __builtin_amdgcn_exp2f((M - m) * unit) + l2 * __builtin_amdgcn_exp2f((m2 - m) * unit);
       M = m;
     }
     const bool good = c < s.cols && M > -INFINITY && M < INFINITY && L > 0.f && L < INFINITY;
     if (tid % per == 0)
-      of[c] = v4f{M, c < s.cols ? scale[c] : 0.f, -__builtin_amdgcn_logf(L), __int_as_float(good ? p.len[s.row0 + c / G] : 0)};
+      of[c] = v4f{p.ml ? 0.f : M, c < s.cols ? scale[c] : 0.f, (p.ml ? p.ml_shift - M : 0.f) - __builtin_amdgcn_logf(L),
+                  __int_as_float(good ? p.len[s.row0 + c / G] : 0)};
   }
   for (int c = tid + 64 * kWaves / per; c < COLS; c += 64 * kWaves) of[c] = v4f{0.f, 0.f, 0.f, 0.f};
   __syncthreads();
@@ -391,7 +396,7 @@ __global__ __launch_bounds__(256) void weights_move_kernel(const WeightRows dst,
 // ------------------------------------------------------------------ launchers
 template <int HD, bool MX, int PARTS, int COLS>
 static hipError_t weigh(const WeighParams& p, int wgs, hipStream_t s) {
-  hipLaunchKernelGGL((weigh_max_kernel<HD, MX, PARTS, COLS>), dim3(wgs), dim3(64 * waves_for(COLS)), 0, s, p);
+  if (!p.ml) hipLaunchKernelGGL((weigh_max_kernel<HD, MX, PARTS, COLS>), dim3(wgs), dim3(64 * waves_for(COLS)), 0, s, p);
   hipLaunchKernelGGL((weigh_add_kernel<HD, MX, PARTS, COLS>), dim3(wgs), dim3(64 * waves_for(COLS)), 0, s, p);
   return hipGetLastError();
 }
