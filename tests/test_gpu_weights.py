@@ -814,3 +814,44 @@ def test_tokens_after_an_eviction_keep_their_distances(torch, st, cache, shape):
     kv.close()
     other.close()
     g.close()
+
+
+def test_rotations_that_a_capture_cannot_allocate(torch, st):
+    """A captured eviction leaves the table of rotations as it is: a captured step or a chunk without allocations that needs
+    more is refused with nothing changed, and an eager step makes it."""
+    shape = synth.ModelShape(1, 512, 8, 2, 64, 1408, 1000)
+    model = SeededModel(shape, 5)
+    g = st.Stage(shape, 0, 1, model.layer)
+    n = 100
+    kv = g.kv(2, n)
+    kv.track()
+    g.prefill(kv, 0, 0, hidden=on(synth.hidden_states(5, synth.STREAM_PREFILL_HIDDEN, 0, n, shape.hidden)))
+    x = on(synth.hidden_states(5, synth.STREAM_DECODE_HIDDEN, 0, 1, shape.hidden))
+    out = torch.empty_like(x)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g.set_stream(side)
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            kv.evict(0, 1, 40, 2, 30)
+            with pytest.raises(st.KFError) as e:
+                g.decode(kv, [1], [40], hidden=x, out=out)
+            assert e.value.status == st.KF_ESTATE
+        for _ in range(3):
+            graph.replay()
+            side.synchronize()
+        assert (kv.len(1), kv.dropped(1)) == (40, 60)
+        with pytest.raises(st.KFError) as e:
+            g.prefill(kv, 1, 40, hidden=x, out=out, noalloc=True)
+        assert e.value.status == st.KF_ESTATE and kv.len(1) == 40
+        w = {k: so.bf16_to_f64(v) for k, v in model.layer(0).items()}
+        for step in range(2):
+            g.decode(kv, [1], [40 + step], hidden=x, out=out)
+            k, v = (t.double().cpu().numpy() for t in kv.read(0, 1, 0, 41 + step))
+            want, _, key = layer64(x.double().cpu().numpy(), w, shape, k, v, 40 + step, [n + step])
+            assert np.abs(k[40 + step:] - key).max() <= 3e-3 * np.abs(key).max()
+            assert np.abs(out.double().cpu().numpy() - want).max() <= 1e-2 * np.abs(want).max()
+    g.sync()
+    kv.close()
+    g.close()
