@@ -292,7 +292,8 @@ __global__ __launch_bounds__(64 * waves_for(COLS)) void weigh_add_kernel(const W
   constexpr int NS = HD / 32, PER = HD / 8, kWaves = waves_for(COLS);
   __shared__ v4u q[PARTS * COLS * PER];
   __shared__ float scale[COLS];
-  __shared__ v4f of[COLS];  // M, scale, -log2 L and the positions (0: the column adds nothing)
+  __shared__ v4f of[COLS];      // M, scale, what a step's own M adds, and the positions (0: the column adds nothing)
+  __shared__ float over[COLS];  // 1 / L (its logarithm in the exponent would be off by 2^-21 at 16384 positions)
   const Split s = split_of(p);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, grp = lane >> 4;
   const int G = p.nq / p.nkv;
@@ -337,11 +338,16 @@ __global__ __launch_bounds__(64 * waves_for(COLS)) void weigh_add_kernel(const W
       M = m;
     }
     const bool good = c < s.cols && M > -INFINITY && M < INFINITY && L > 0.f && L < INFINITY;
-    if (tid % per == 0)
-      of[c] = v4f{p.ml ? 0.f : M, c < s.cols ? scale[c] : 0.f, (p.ml ? p.ml_shift - M : 0.f) - __builtin_amdgcn_logf(L),
+    if (tid % per == 0) {
+      of[c] = v4f{p.ml ? 0.f : M, c < s.cols ? scale[c] : 0.f, p.ml ? p.ml_shift - M : 0.f,
                   __int_as_float(good ? p.len[s.row0 + c / G] : 0)};
+      over[c] = good ? 1.0f / L : 0.f;
+    }
   }
-  for (int c = tid + 64 * kWaves / per; c < COLS; c += 64 * kWaves) of[c] = v4f{0.f, 0.f, 0.f, 0.f};
+  for (int c = tid + 64 * kWaves / per; c < COLS; c += 64 * kWaves) {
+    of[c] = v4f{0.f, 0.f, 0.f, 0.f};
+    over[c] = 0.f;
+  }
   __syncthreads();
   float* out = p.weights + ((int64_t)w.user * p.nkv + s.g) * p.stride;
   for (int i = wave; i < s.pages; i += kWaves) {
@@ -369,11 +375,12 @@ __global__ __launch_bounds__(64 * waves_for(COLS)) void weigh_add_kernel(const W
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const v4f c = of[ct * 16 + 4 * grp + r];
+        const float inv = over[ct * 16 + 4 * grp + r];
         const int left = __float_as_int(c.w) - page * kKvPage;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][r] - c.x, c.y, c.z));
-          sum[t] += 16 * t + r16 < left ? x : 0.f;
+          sum[t] = __builtin_fmaf(16 * t + r16 < left ? x : 0.f, inv, sum[t]);
         }
       }
     }
