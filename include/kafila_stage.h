@@ -389,7 +389,8 @@ kf_status kf_kv_set_weights(kf_kv* kv, int32_t layer, int32_t user, int32_t pos0
  * and, of those between, the ones of the largest weights, the lower position of two equal ones and a NaN
  * below every number.  They keep their order, their exact values and their weights.  The keys keep the rotation of
  * the positions they came from, and the tokens that follow (kf_stage_decode, kf_stage_prefill) are rotated as the
- * source's would have been: to their slot plus what was dropped (kf_kv_dropped).  dst_user may be src_user (in place); else src_user is left as it is.
+ * source's would have been: to their slot plus what was dropped (kf_kv_dropped).  dst_user may be src_user (in
+ * place); else src_user is left as it is.
  *   kept_dev : int32 [layers held, nkv, keep], the positions kept, ascending; may be NULL
  * Tracked caches only (else KF_ESTATE).  In a paged cache dst_user gives its pages back and is lent what keep
  * positions need; in place, other pages take the place of those that other users hold too (KF_ENOMEM, with nothing

@@ -5,20 +5,24 @@
 //
 // A softmax's weights are known once its maximum M and sum L are, so there are two
 // passes over the keys: weigh_max_kernel leaves (M, L) of each split of the positions,
-// weigh_add_kernel joins them and adds.  Values are not read.  A workgroup takes the pages of a split
-// of one KV head for all of a user's columns (its rows times the G heads), whose queries it keeps in LDS as fp16 operands,
-// two parts of fp32 ones; a wave takes a page at a time, its K operand in registers, decoded there from an MXFP4 cache.
-// In the first pass the tiles are K Q^T, whose lanes hold a column each, in the
-// second Q K^T, whose lanes hold a position, so that both sums run along registers.
-// A position has one writer, so the order of all additions is fixed.
-// A decode step's attention has left (M, L) of its splits, and the second pass is enough.
+// weigh_add_kernel joins them and adds.  A decode step's attention has left them, and
+// the second pass is enough.  Values are not read.  A workgroup takes the pages of a
+// split of one KV head for all of a user's columns (its rows times the G heads), whose
+// queries it keeps in LDS as fp16 operands, two parts of fp32 ones; a wave takes a page
+// at a time, its K operand in registers, decoded there from an MXFP4 cache.  In the
+// first pass the tiles are K Q^T, whose lanes hold a column each, in the second Q K^T,
+// whose lanes hold a position, so that both sums run along registers.  A position has
+// one writer, so the order of all additions is fixed.
 //
-// What bounds it: the keys are read twice, once from HBM and once mostly from the caches behind it, which at 7 TB/s is 5 us
-// of the 17 + 16 us that 32 rows of 32 heads at 16384 fp16 positions take (8 KV heads, bf16 queries; 34 MB of keys), and
-// 4.5 of the 11.5 + 13 us of one fp32 row each of four users at 32768, 16384, 8192 and 1024 MXFP4 positions (32 MB).  The rest is the way to the first
-// product (launch, page table, queries, in the second pass the splits' sums: some 7 us a pass) and,
-// for many rows, the exponentials and their sums on the vector units.  So a wave's first page is asked for before the queries are prepared,
-// and all of a round's loads of queries before the first is used (54 -> 33 us for the 32 rows).
+// What bounds it: one row a user reads K at 6.0 TB/s (131072 positions of 8 heads of 128
+// in fp16: 45 + 46 us).  For 32 rows of 32 heads at 16384 positions (34 MB of keys, 5 us
+// at 7 TB/s) the passes take 17 + 16 us, and 11.5 + 13 for one fp32 row each of four
+// users at 32768, 16384, 8192 and 1024 MXFP4 positions (32 MB).  The rest is the way to
+// the first product (launch, page table, queries, in the second pass the splits' sums:
+// 5 us a pass, 9 with 128 columns) and, for many rows, the exponentials and their sums on
+// the vector units.  So a wave's first page is asked for before the queries are prepared,
+// and all of a round's loads of queries before the first is used (54 -> 33 us for the 32
+// rows).
 #include <algorithm>
 #include <climits>
 
