@@ -142,8 +142,8 @@ __device__ __forceinline__ void append(const MxStepParams& p, int b, int g, bool
     const float rs = 1.0f / sqrtf(ss / (float)HD + p.eps);
     float gain[8], c[8], sn[8];
     load_q8(p.gk, 1, d0, gain);
-    load_q8(p.rope_cos, 0, (int64_t)p.a.rot[b] * (HD / 2) + d0 % (HD / 2), c);
-    load_q8(p.rope_sin, 0, (int64_t)p.a.rot[b] * (HD / 2) + d0 % (HD / 2), sn);
+    load_q8(p.rope_cos, 0, (int64_t)(pos + p.ahead.n[b]) * (HD / 2) + d0 % (HD / 2), c);
+    load_q8(p.rope_sin, 0, (int64_t)(pos + p.ahead.n[b]) * (HD / 2) + d0 % (HD / 2), sn);
     const float sign = d0 < HD / 2 ? -1.f : 1.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void attn_mx_kernel(const P p) {
     for (int s = 0; s < NS; ++s)
       load_q8(p.q, p.q_type, ((int64_t)b * p.a.nq + hq0 + min(head, G - 1)) * HD + grp * (HD / 4) + 8 * s, f[s]);
     if constexpr (STEP) {
-      if (p.gq) norm_rope<HD>(p, f, grp, p.a.rot[b]);
+      if (p.gq) norm_rope<HD>(p, f, grp, len - 1 + p.ahead.n[b]);
     }
 #pragma unroll
     for (int s = 0; s < NS; ++s)

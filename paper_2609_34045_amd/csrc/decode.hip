@@ -196,8 +196,8 @@ __device__ __forceinline__ EpiPre gemv_epi_prefetch(const GemvParams& p, int wg,
       const int wg_per_head = p.hd / R, head = wg / wg_per_head, i0 = (wg % wg_per_head) * (R / 2);
       const int r = tid / B, b = tid % B, half = p.hd / 2;
       if (head < p.nq + p.nkv) {
-        e.a = p.rope_cos[(int64_t)p.rot[b] * half + i0 + r];
-        e.b = p.rope_sin[(int64_t)p.rot[b] * half + i0 + r];
+        e.a = p.rope_cos[(int64_t)(p.pos[b] + p.ahead[b]) * half + i0 + r];
+        e.b = p.rope_sin[(int64_t)(p.pos[b] + p.ahead[b]) * half + i0 + r];
       }
     }
   } else if (EPI == kEpiResid) {
@@ -644,7 +644,7 @@ __device__ __forceinline__ void dk_read_vt(uint32_t base, const int (&off)[NT], 
 // vector instructions a key.  8 KV heads of 128, bf16 queries, one part and two: 2048 positions 8.0 and 8.7 us, four rows of
 // 1024 to 32768 44.0 and 46.4, two of 131072 and 100001 200 and 204 (4.7 TB/s).
 template <int HD, int NW, int QT, bool GIVEN>
-__global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_kernel(const AttnParams p) {
+__global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_kernel(const AttnParams p, const RowsAhead ahead) {
   constexpr int KB = 16;             // keys per block
   constexpr int ROWB = HD * 2;       // bytes per key row
   constexpr int CPR = ROWB / 16;     // 16-byte chunks per row
@@ -765,6 +765,7 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
   // d = 32 s + 8 q4 + j, d +- HD/2, is step s +- NS/2 of the same lane.
   const bool qkn = !GIVEN && p.kraw != nullptr;
   const int npos = len - 1;  // row b's new position
+  const int rot = npos + ahead.n[b];
   if (qkn) {
     float x[NS][8];
 #pragma unroll
@@ -787,8 +788,8 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
     }
 #pragma unroll
     for (int s = 0; s < NS / 2; ++s) {
-      const v4f* cp = reinterpret_cast<const v4f*>(p.rope_cos + (int64_t)p.rot[b] * (HD / 2) + 32 * s + 8 * q4);
-      const v4f* sp = reinterpret_cast<const v4f*>(p.rope_sin + (int64_t)p.rot[b] * (HD / 2) + 32 * s + 8 * q4);
+      const v4f* cp = reinterpret_cast<const v4f*>(p.rope_cos + (int64_t)rot * (HD / 2) + 32 * s + 8 * q4);
+      const v4f* sp = reinterpret_cast<const v4f*>(p.rope_sin + (int64_t)rot * (HD / 2) + 32 * s + 8 * q4);
       const v4f c0 = cp[0], c1 = cp[1], n0 = sp[0], n1 = sp[1];
       const float c[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
       const float sn[8] = {n0.x, n0.y, n0.z, n0.w, n1.x, n1.y, n1.z, n1.w};
@@ -836,7 +837,7 @@ __global__ __launch_bounds__(64 * NW, NW >= 8 ? 1 : 2) void attn_decode_mfma_ker
     uint16_t k16[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float cs = p.rope_cos[(int64_t)p.rot[b] * (HD / 2) + i0 + j], sn = p.rope_sin[(int64_t)p.rot[b] * (HD / 2) + i0 + j];
+      const float cs = p.rope_cos[(int64_t)rot * (HD / 2) + i0 + j], sn = p.rope_sin[(int64_t)rot * (HD / 2) + i0 + j];
       k16[j] = f16_checked(x[j] * cs + sgn * y[j] * sn, bad);
     }
     knew = v4u{k16[0] | ((uint32_t)k16[1] << 16), k16[2] | ((uint32_t)k16[3] << 16),
@@ -1482,20 +1483,22 @@ hipError_t launch_gemv(int epi, int R, int U, bool norm, const GemvParams& p, hi
 }
 
 template <int QT, bool GIVEN>
-static hipError_t attn_decode(const AttnParams& p, int batch, hipStream_t s) {
+static hipError_t attn_decode(const AttnParams& p, const RowsAhead& ahead, int batch, hipStream_t s) {
   if (p.nq % p.nkv || p.nq / p.nkv > (GIVEN ? 8 : 16)) return hipErrorInvalidValue;  // query slots of one MFMA column block
   const dim3 grid(p.n_split, p.nkv, batch), block(64 * kAttnMfmaWaves);
-  if (p.hd == 128) hipLaunchKernelGGL((attn_decode_mfma_kernel<128, kAttnMfmaWaves, QT, GIVEN>), grid, block, 0, s, p);
-  else if (p.hd == 64) hipLaunchKernelGGL((attn_decode_mfma_kernel<64, kAttnMfmaWaves, QT, GIVEN>), grid, block, 0, s, p);
+  if (p.hd == 128) hipLaunchKernelGGL((attn_decode_mfma_kernel<128, kAttnMfmaWaves, QT, GIVEN>), grid, block, 0, s, p, ahead);
+  else if (p.hd == 64) hipLaunchKernelGGL((attn_decode_mfma_kernel<64, kAttnMfmaWaves, QT, GIVEN>), grid, block, 0, s, p, ahead);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
-hipError_t launch_attn_decode(const AttnParams& p, int batch, hipStream_t s) { return attn_decode<0, false>(p, batch, s); }
+hipError_t launch_attn_decode(const AttnParams& p, const RowsAhead& ahead, int batch, hipStream_t s) {
+  return attn_decode<0, false>(p, ahead, batch, s);
+}
 hipError_t launch_attn_given(const AttnParams& p, int batch, int q_type, hipStream_t s) {
   switch (q_type) {
-    case 0: return attn_decode<0, true>(p, batch, s);
-    case 1: return attn_decode<1, true>(p, batch, s);
-    case 2: return attn_decode<2, true>(p, batch, s);
+    case 0: return attn_decode<0, true>(p, {}, batch, s);
+    case 1: return attn_decode<1, true>(p, {}, batch, s);
+    case 2: return attn_decode<2, true>(p, {}, batch, s);
     default: return hipErrorInvalidValue;
   }
 }

@@ -216,7 +216,7 @@ struct GemvParams {
   const float* rope_sin;
   int users[kMaxBatch];
   int pos[kMaxBatch];
-  int rot[kMaxBatch];     // the position that row b is rotated to: pos, and what was dropped before it
+  int ahead[kMaxBatch];   // row b is rotated to position pos + ahead (a sum, so that pos is loaded early too)
   // Blocks with per-head q/k norms: when set, q goes to `q` and k to kraw
   // ([B][nkv][hd] fp32) as projected (after the attention RMSNorm), without
   // RoPE; the decode attention finishes both.  v goes to the cache as usual.
@@ -271,9 +271,14 @@ struct AttnParams {
   const uint16_t* gk;
   const float* rope_cos;  // [positions][hd/2]
   const float* rope_sin;
-  int rot[kMaxBatch];     // the position that row b's query and new key are rotated to
   float eps;
   int* err_flag;          // sticky error bits: kErrF16Range for an fp16 store out of range
+};
+
+// Row b's query and new key are rotated to position len - 1 + n[b].  (Not a part of AttnParams, which other kernels take
+// too: 16 bytes more of arguments there cost the output projection 0.4 us of 8.3.)
+struct RowsAhead {
+  int n[kMaxBatch];
 };
 
 // Attention over an MXFP4 cache (attend.hip): a's queries and cache pointers are not
@@ -302,6 +307,7 @@ struct MxStepParams : MxAttnParams {  // q: fp32; normalised and rotated here wh
   const uint16_t *gq, *gk;  // per-head norm gains [hd] bf16, or NULL
   const float *rope_cos, *rope_sin;
   float eps;
+  RowsAhead ahead;
 };
 
 // Launchers (return hipGetLastError() of the launch).
@@ -314,7 +320,7 @@ hipError_t launch_gemv(int epi, int rows_per_wg, int chunks_in_flight, bool norm
 // The same launch with the stage input (p.src or p.tokens) as its input rows.
 hipError_t launch_gemv_src(int epi, int rows_per_wg, int chunks_in_flight, bool norm, const GemvParams& p,
                            hipStream_t s);
-hipError_t launch_attn_decode(const AttnParams& p, int batch, hipStream_t s);
+hipError_t launch_attn_decode(const AttnParams& p, const RowsAhead& ahead, int batch, hipStream_t s);
 // The same with given queries, p.q of q_type (a kf_dtype value), and queries and probabilities in two fp16 parts each.
 hipError_t launch_attn_given(const AttnParams& p, int batch, int q_type, hipStream_t s);
 // Head h of row b merged from the attention partials in p, to o16[b][h*hd:(h+1)*hd]

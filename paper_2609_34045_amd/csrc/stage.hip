@@ -1504,6 +1504,7 @@ static hipError_t attn_mx(kf_stage* s, kf_kv* kv, const AttnParams& a, const Row
   p.gk = a.gk;
   p.rope_cos = kv->rcos;
   p.rope_sin = kv->rsin;
+  std::copy(g.ahead, g.ahead + kMaxBatch, p.ahead.n);
   p.eps = s->cfg.rms_eps;
   return launch_attn_mx_step(p, g.batch, s->stream);
 }
@@ -1749,7 +1750,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     for (int b = 0; b < kMaxBatch; ++b) {
       g.users[b] = b < batch ? users[b] : 0;
       g.pos[b] = b < batch ? positions[b] : 0;
-      g.rot[b] = b < batch ? positions[b] + kv->dropped[users[b]] : 0;
+      g.ahead[b] = b < batch ? kv->dropped[users[b]] : 0;
     }
     if (kv->mx()) {  // kept in fp16 for attn_mx, which stores them
       g.kv = kv->append_pages();
@@ -1795,18 +1796,19 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
     a.split = split;
     a.n_split = n_split;
     RowSplits rows{};  // MXFP4 caches
+    RowsAhead ahead{};
     a.max_split = kv->max_split;
     a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)hd));
     a.err_flag = s->err_flag;
     for (int b = 0; b < kMaxBatch; ++b) {
       a.users[b] = b < batch ? users[b] : 0;
       a.len[b] = b < batch ? positions[b] + 1 : 0;
-      a.rot[b] = g.rot[b];
+      ahead.n[b] = g.ahead[b];
     }
     if (kv->mx()) attn_split_mx(c.n_kv_heads, batch, a.len, kv->max_split, s->n_cu, a, rows);
     {
       tr.begin(KF_K_ATTN);
-      const hipError_t le = kv->mx() ? attn_mx(s, kv, a, rows, g, l) : launch_attn_decode(a, batch, st);
+      const hipError_t le = kv->mx() ? attn_mx(s, kv, a, rows, g, l) : launch_attn_decode(a, ahead, batch, st);
       tr.end(KF_K_ATTN);
       KF_HIP(le, "attention launch");
     }
