@@ -216,7 +216,6 @@ struct GemvParams {
   const float* rope_sin;
   int users[kMaxBatch];
   int pos[kMaxBatch];
-  int ahead[kMaxBatch];   // row b is rotated to position pos + ahead (a sum, so that pos is loaded early too)
   // Blocks with per-head q/k norms: when set, q goes to `q` and k to kraw
   // ([B][nkv][hd] fp32) as projected (after the attention RMSNorm), without
   // RoPE; the decode attention finishes both.  v goes to the cache as usual.
@@ -240,8 +239,13 @@ struct GemvParams {
 
   // kEpiLMHead
   float* logits;       // optional [B][N]
-  float* part_val;     // [B][n_wg]
-  int* part_idx;       // [B][n_wg]
+  union {              // (no longer arguments than without: they cost each launch)
+    struct {
+      float* part_val;  // [B][n_wg]
+      int* part_idx;    // [B][n_wg]
+    };
+    int ahead[kMaxBatch];  // kEpiQKV: row b is rotated to position pos + ahead (a sum, so that pos is loaded early too)
+  };
   int n_wg;
   const float* eps_rows;  // [B] or NULL: eps of each row, for input rows that were scaled (launch_rows_to_f16)
 };
