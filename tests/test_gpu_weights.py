@@ -855,3 +855,42 @@ def test_rotations_that_a_capture_cannot_allocate(torch, st):
     g.sync()
     kv.close()
     g.close()
+
+
+@pytest.mark.parametrize("cache", ["f16", "mxfp4"])
+@pytest.mark.parametrize("shape", [synth.ModelShape(1, 512, 8, 2, 64, 704, 0), synth.ModelShape(1, 512, 8, 2, 128, 704, 0, qk_norm=True)],
+                         ids=["hd64", "hd128"])
+def test_tracked_steps_over_many_splits(torch, st, cache, shape):
+    """A step's weights come from its attention's own maxima and sums, of one split or of many, in batches of very different
+    lengths."""
+    model = SeededModel(shape, 11)
+    w = {k: so.bf16_to_f64(v) for k, v in model.layer(0).items()}
+    g = st.Stage(shape, 0, 1, model.layer)
+    lens = [20000, 70, 0, 4097]
+    kv = g.kv(4, max(lens) + 8, dtype=cache)
+    kv.track()
+    for u, n in enumerate(lens):
+        if n:
+            kv.write(0, u, 0, on(rows(u, n, 2, shape.head_dim)), on(rows(9 + u, n, 2, shape.head_dim)))
+        kv.set_len(u, n)
+    for step, users in enumerate(([0], [3, 0], [2, 0, 1, 3], [1])):
+        x = synth.hidden_states(11, synth.STREAM_DECODE_HIDDEN, step, len(users), shape.hidden)
+        before = [kv.weights(0, u, 0, kv.len(u) + 1).double().cpu().numpy() for u in users]
+        at = [kv.len(u) for u in users]
+        g.decode(kv, users, at, hidden=on(x))
+        for i, u in enumerate(users):
+            n = at[i] + 1
+            k, v = (t.double().cpu().numpy() for t in kv.read(0, u, 0, n))
+            _, q, _ = layer64(np.asarray(x[i:i + 1], np.float64), w, shape, k, v, at[i], [at[i]])
+            before[i][:, at[i]] = 0
+            a, e = weight_of(q[0], k, n)
+            # as test_prefill_and_decode_steps_add_theirs has it, and the fp16 probabilities whose sum the attention takes
+            # (2^-11 of each, and 2^-25 of the largest where they end)
+            G = shape.n_q_heads // shape.n_kv_heads
+            S = max((np.abs(k[:, h // G]) @ np.abs(q[0, h])).max() for h in range(shape.n_q_heads)) / math.sqrt(shape.head_dim)
+            tol = e + a * (math.expm1(2 * 2 * 2.0 ** -11 * S) + 2.0 ** -11 + n * 2.0 ** -25) + 2.0 ** -24 * (1 + before[i])
+            got = kv.weights(0, u, 0, n).double().cpu().numpy() - before[i]
+            assert np.all(np.abs(got - a) <= tol), (step, u)
+    g.sync()
+    kv.close()
+    g.close()
