@@ -333,8 +333,7 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
  *           gives zeros and which no token sees (a token that names it as its parent sees itself and what lies
  *           before the tree).  Any other value counts as -1.
  *   q_dev, out_dev : [sum of nodes, nq, hd] in io, tree after tree; as for kf_kv_attend
- * Queries and probabilities keep 22 bits for KF_F32 and KF_F16; for KF_BF16 the probabilities keep 11.  A
- * position that a token does not see does not reach it, whatever it holds.  KF_ERANGE for
+ * Queries and probabilities keep 22 bits.  A position that a token does not see does not reach it, whatever it holds.  KF_ERANGE for
  * positions beyond max_ctx or the pages the user holds.
  * The splits' partial results use the cache's own workspace, which kf_kv_attend and decode use too.
  * Changes nothing in the cache.  Enqueued on the stage's stream.

@@ -11,13 +11,13 @@
 // O^T += V^T P^T, all on 32x32x16 fp16 MFMAs.  K and V pass through LDS, so that the
 // waves share what they read; the splits of a row meet in tree_merge_kernel.
 //
-// PARTS: the fp16 parts that queries and probabilities are taken in.  One for bf16 queries, which fp16 holds
-// exactly (the probabilities are off by 2^-11 of each, an eighth of half a step of the bf16 result); two, each
-// product taken with both, for fp32 and fp16 queries: 22 bits.
+// Probabilities are taken in two fp16 parts, each product with both: 22 bits, whatever the type.  PARTS: the same of the
+// queries.  One for bf16 queries: times the power of two of their head, fp16 holds those down to 2^-27 of its largest
+// exactly, and smaller ones to 2^-38 of that; two for fp32 and fp16 queries.
 //
 // What bounds it: the matrix and vector units, in turn.  128 fp32 tokens of 64 heads at 40001 positions (8 KV heads of
 // 128): 336 GFLOP of products in 300 to 340 us, a large library product's rate; 64 bf16 tokens of 32 heads at 32768
-// 48 us (34 GFLOP, 30 us at that rate; 10 are a launch's fixed part), where each unit is busy 45% of the time.
+// with the merge 72 us (51 GFLOP, 45 us at that rate; 10 are a launch's fixed part and 8 the merge).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -163,9 +163,6 @@ __global__ __launch_bounds__(256, 2) void attn_tree_kernel(const TreeParams p) {
   constexpr int TILEB = kKB * ROWB;          // a block of K or V
   constexpr int RPI = 64 / CPR;              // key rows per 1 KB direct load
   constexpr int LPW = TILEB / 1024 / 4;      // direct loads per wave per block of K or V
-  // One part: probabilities lie below 2^15, those above 2^-21 of the peak keep 11 bits and those below 2^-31 are lost (of 2^20
-  // such, 2^-11 of the sum), and the sums are rescaled a third as often.
-  constexpr float kShift = PARTS == 2 ? kPartShift : 7.0f, kLazy = PARTS == 2 ? kPartLazy : 8.0f;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * TILEB];  // two stages: K, V behind it
   __shared__ uint64_t see[kMaxNodes][kMaxNodes / 64];
   __shared__ int up[kMaxNodes];
@@ -417,7 +414,7 @@ __global__ __launch_bounds__(256, 2) void attn_tree_kernel(const TreeParams p) {
   f32x16 st[NT], zero;
 #pragma unroll
   for (int v = 0; v < 16; ++v) zero[v] = 0.f;
-  v4u pf[PARTS][2 * NT];  // P^T fragments of a block's key steps
+  v4u pf[2][2 * NT];  // P^T fragments of a block's key steps, in two parts
   auto step = [&](int blk, auto parity) {
     constexpr int P = decltype(parity)::value;
     uint8_t* const stage = smem + P * 2 * TILEB;
@@ -447,7 +444,7 @@ __global__ __launch_bounds__(256, 2) void attn_tree_kernel(const TreeParams p) {
         __builtin_amdgcn_sched_barrier(0);
       }
       if (tail) mask(blk, st);
-      // The reference of the softmax moves only when a block's maximum exceeds it by kLazy, so that O is rarely rescaled.
+      // The reference of the softmax moves only when a block's maximum exceeds it by kPartLazy, so that O is rarely rescaled.
       float mb = -INFINITY;
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -455,34 +452,28 @@ __global__ __launch_bounds__(256, 2) void attn_tree_kernel(const TreeParams p) {
         for (int v = 0; v < 16; ++v) mb = fmaxf(mb, st[t][v]);
       mb = max32(mb);
       // Until a position is seen the maximum is -inf, and 0 stands in, so that nothing is added.
-      const float m_new = (mb - m_run) * sscale > kLazy ? mb : m_run;
+      const float m_new = (mb - m_run) * sscale > kPartLazy ? mb : m_run;
       const float m_ref = m_new == -INFINITY ? 0.f : m_new;
       const float alpha = __builtin_amdgcn_exp2f((m_run - m_ref) * sscale);
       m_run = m_new;
       // A probability is 2^(s sscale + c); c is rounded, to 2^-5 at scores of 2^20, the same way for all of a block, and
       // past those the distance from the reference is taken first, exact near it.
-      float c = __builtin_fmaf(-m_ref, sscale, kShift);
+      float c = __builtin_fmaf(-m_ref, sscale, kPartShift);
       if (__ballot(!(__builtin_fabsf(c) < 0x1p20f))) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int v = 0; v < 16; ++v) st[t][v] -= m_ref;
-        c = kShift;
+        c = kPartShift;
       }
       float ls = 0.f;
-      const h2 ones = {(_Float16)1.0f, (_Float16)1.0f};
 #pragma unroll
       for (int i = 0; i < 16 * NT; i += 2) {
         const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i / 16][i % 16], sscale, c));
         const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i / 16][i % 16 + 1], sscale, c));
-        const uint32_t w = f16_pair(x, y);
-        pf[0][i / 8][i / 2 % 4] = w;
-        if constexpr (PARTS == 2) {
-          pf[1][i / 8][i / 2 % 4] = f16_part2(x, y, 1.0f);
-          ls += x + y;
-        } else {  // of what the product takes
-          ls = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w), ones, ls, false);
-        }
+        pf[0][i / 8][i / 2 % 4] = f16_pair(x, y);
+        pf[1][i / 8][i / 2 % 4] = f16_part2(x, y, 1.0f);
+        ls += x + y;
       }
       l_run = l_run * alpha + sum32(ls);
       if (__ballot(alpha != 1.0f)) {
@@ -498,7 +489,7 @@ __global__ __launch_bounds__(256, 2) void attn_tree_kernel(const TreeParams p) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) o[i % DB] = mfma32(vr[i % AHEAD], pf[part][i / DB], o[i % DB]);
+        for (int part = 0; part < 2; ++part) o[i % DB] = mfma32(vr[i % AHEAD], pf[part][i / DB], o[i % DB]);
         if (i + AHEAD < NV) vr[i % AHEAD] = vread(stage + TILEB, i + AHEAD);
       }
     }
