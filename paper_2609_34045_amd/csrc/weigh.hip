@@ -268,11 +268,15 @@ __global__ __launch_bounds__(64 * waves_for(COLS)) void weigh_max_kernel(const W
         for (int r = 0; r < 4; ++r) l += __builtin_amdgcn_exp2f((sc[t][r] - ref) * ss);
       l = groups_sum(l);
       l += run_l[wave][col] * __builtin_amdgcn_exp2f((m_old - ref) * ss);
+      __builtin_amdgcn_wave_barrier();
       if (grp == 0) {
         run_m[wave][col] = m_new;
         run_l[wave][col] = l;
       }
     }
+    // The lanes of all groups go on from what those of the first have stored.
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
     if (!MX && i + kWaves < s.pages) load_keys<HD, MX>(p, user, s.g, page + kWaves, next);
   }
   __syncthreads();
