@@ -355,9 +355,10 @@ kf_status kf_kv_accept(kf_kv* kv, int32_t user, int32_t len, int32_t n, const in
 /*
  * From now on the cache adds up the attention weight of every position: for each layer and KV head,
  * the sum of the probabilities that queries of its group's heads gave the position, in fp32.
- * Added are every row of a decode step (with the maxima and sums of its own attention), the last
- * `window` (0..KF_MAX_WEIGH_ROWS) tokens of each prefill chunk, and what kf_kv_weigh is given; not
- * kf_kv_attend and kf_kv_attend_tree.  A position that is written anew (decode, prefill, kf_kv_write)
+ * Added are every row of a decode step, the last `window` (0..KF_MAX_WEIGH_ROWS) tokens of each prefill
+ * chunk, and what kf_kv_weigh is given; not kf_kv_attend and kf_kv_attend_tree.  A head's probabilities add up to 1
+ * within fp32 sums: queries keep 22 bits in maximum, sum and exponent alike (a prefill chunk's 11, as fp16 has
+ * them), also of a step whose attention rounds them to 11.  A position that is written anew (decode, prefill, kf_kv_write)
  * starts at 0; kf_kv_copy and kf_kv_fork copy the weights (0 from an untracked cache), kf_kv_accept and
  * kf_kv_evict move them with their positions, and kf_kv_set_len leaves them.
  * The first call allocates 4 bytes per layer, KV head and position of max_ctx of every user, and a

@@ -528,7 +528,7 @@ struct WeighParams {
   float* weights;  // [user][nkv][stride] of the layer
   int64_t stride;
   float* part;     // workspace: [row][nq][max_splits][2]
-  // or, of a decode step, what its attention left, in log2 units and with sums times 2^ml_shift: row b's ml_n[b] splits of
+  // or, of a decode step on an MXFP4 cache, what its attention left, in log2 units and with sums times 2^ml_shift: row b's ml_n[b] splits of
   // [b][nq][ml_splits][2]; then the first pass is not taken
   const float* ml;
   int ml_splits, ml_n[kMaxBatch];

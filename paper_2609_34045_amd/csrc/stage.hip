@@ -1858,10 +1858,14 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
         w.rope_sin = kv->rsin;
         w.eps = c.rms_eps;
       }
-      w.ml = kv->part_ml;
-      w.ml_splits = kv->max_split;
-      w.ml_shift = kv->mx() ? kPartShift : 0.f;
-      for (int b = 0; b < batch; ++b) w.ml_n[b] = kv->mx() ? rows.n[b] : n_split;
+      // Over an MXFP4 cache the attention's maxima and sums are those of queries of 22 bits too.  (Over fp16 they are of one
+      // rounded part, which moves all of a head's scores alike where its keys do: weights divided by them would not add up to 1.)
+      if (kv->mx()) {
+        w.ml = kv->part_ml;
+        w.ml_splits = kv->max_split;
+        w.ml_shift = kPartShift;
+        for (int b = 0; b < batch; ++b) w.ml_n[b] = rows.n[b];
+      }
       const kf_status wst = weigh_rows(kv, w, l, batch, users, a.len, positions);
       if (wst != KF_OK) return wst;
     }

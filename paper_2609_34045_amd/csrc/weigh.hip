@@ -5,8 +5,10 @@
 //
 // A softmax's weights are known once its maximum M and sum L are, so there are two
 // passes over the keys: weigh_max_kernel leaves (M, L) of each split of the positions,
-// weigh_add_kernel joins them and adds.  A decode step's attention has left them, and
-// the second pass is enough.  Values are not read.  A workgroup takes the pages of a
+// weigh_add_kernel joins them and adds.  A decode step's attention over an MXFP4 cache
+// has left them, and the second pass is enough; over an fp16 cache it takes queries of
+// 11 bits, where these have 22, and both passes are needed: p's sums of 1 hang on both
+// having the same scores.  Values are not read.  A workgroup takes the pages of a
 // split of one KV head for all of a user's columns (its rows times the G heads), whose
 // queries it keeps in LDS as fp16 operands, two parts of fp32 ones; a wave takes a page
 // at a time, its K operand in registers, decoded there from an MXFP4 cache.  In the
