@@ -170,7 +170,9 @@ kf_status kf_stage_set_stream(kf_stage* stage, void* hip_stream);
  *               merged attention output; in prefill the normalised rows, queries, attention
  *               output and SwiGLU output) reached 65520 in magnitude and was stored as
  *               infinity (in an MXFP4 cache as 49152, and a NaN as 0); or a logit was NaN (skipped by
- *               the argmax and the log probabilities; see kf_head_argmax and kf_head_logprobs).
+ *               the argmax and the log probabilities; see kf_head_argmax and kf_head_logprobs);
+ *   KF_ESTATE : two captured evictions in place of one cache were replayed at the same time, and pages
+ *               of positions were left where they were (see kf_kv_evict).
  * The message (kf_last_error) names every condition that occurred.
  */
 kf_status kf_stage_sync(kf_stage* stage);
@@ -395,7 +397,8 @@ kf_status kf_kv_set_weights(kf_kv* kv, int32_t layer, int32_t user, int32_t pos0
  * Tracked caches only (else KF_ESTATE).  In a paged cache dst_user gives its pages back and is lent what keep
  * positions need; in place, other pages take the place of those that other users hold too (KF_ENOMEM, with nothing
  * changed, if the pool cannot lend them), and a call under graph capture is KF_ESTATE.  Uses the cache's own workspace:
- * captured evictions of one cache are not replayed at the same time.  Enqueued on the stage's stream.
+ * captured evictions of one cache are not replayed at the same time (KF_ESTATE from kf_stage_sync, with what the users hold
+ * lost, where that is seen).  Enqueued on the stage's stream.
  */
 kf_status kf_kv_evict(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t keep, int32_t first, int32_t last,
                       int32_t* kept_dev);

@@ -22,11 +22,6 @@ namespace {
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 typedef unsigned v2u __attribute__((ext_vector_type(2)));
 
-// Replays of two graphs that move in place on one cache share the tickets and flags, and their caller orders them.  Should
-// they run at once all the same, no ticket is taken for a page that is not there, and a wait ends after this many looks
-// (about a tenth of a second; a wait that its flag ends takes microseconds).
-constexpr int kWaits = 1 << 17;
-
 enum : int { kApart = 0, kInPlace = 1, kFew = 2 };  // another user's pages; in place, side by side; in place, in order
 
 // The old position of new position i (below p.n).
@@ -194,6 +189,11 @@ template <int HD>
 struct PageOf<HD, true> : PageMx<HD> {};
 }  // namespace
 
+// Replays of two graphs that move in place on one cache share the tickets and flags, and their caller orders them.  Should
+// they run at once all the same, no ticket is taken for a page that is not there, and a wait ends after p.waits looks: such
+// a page is left as it is, since what lies there may still have to be read, and the stage's error says so.
+int keep_waits = 1 << 17;
+
 // A page is 256 threads' work; a kFew workgroup has up to four such groups.
 constexpr int groups_of(int mode) { return mode == kFew ? 4 : 1; }
 template <int HD, bool MX, int MODE>
@@ -217,7 +217,10 @@ __global__ __launch_bounds__(256 * groups_of(MODE)) void keep_kernel(const KeepP
     if (tid == 0) ticket = __hip_atomic_fetch_add(&p.tickets[lg * kTicketStep], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     nth = ticket;
-    if (nth >= pages - page0) return;  // (two replays at once, see kWaits)
+    if (nth >= pages - page0) {  // two replays at once
+      raise_err(p.err_flag, tid == 0, kErrEvictions);
+      return;
+    }
   }
   const int* list = p.list ? p.list + (int64_t)lg * p.n : nullptr;
   const float* wsrc = p.weights ? p.weights + (((int64_t)layer * p.users + p.weights_src) * p.nkv + g) * p.stride : nullptr;
@@ -245,21 +248,29 @@ __global__ __launch_bounds__(256 * groups_of(MODE)) void keep_kernel(const KeepP
       if (tid == 0) __hip_atomic_store(&p.flags[(int64_t)lg * p.pages + page], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (same) return;
     }
-    auto wait = [&]() {  // for the pages with an old position in this one
+    auto waited = [&]() -> bool {  // for the pages with an old position in this one
+      bool late = false;
       const int* flags = p.flags + (int64_t)lg * p.pages;
       const int* below = p.below + (int64_t)lg * (p.pages + 1);
       if (tid < 64) {
         const int r0 = below[page], r1 = below[page + 1];
-        for (int i = max(r0 / kKvPage, page0) + tid; i < page && i * kKvPage < r1; i += 64)
-          for (int n = 0; n < kWaits && !__hip_atomic_load(&flags[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); ++n)
-            __builtin_amdgcn_s_sleep(2);
+        for (int i = max(r0 / kKvPage, page0) + tid; i < page && i * kKvPage < r1; i += 64) {
+          bool set = false;
+          for (int n = 0; n < p.waits && !set; ++n) {
+            set = __hip_atomic_load(&flags[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (!set) __builtin_amdgcn_s_sleep(2);
+          }
+          late |= !set;
+        }
       }
-      __syncthreads();
+      late = __syncthreads_or(late);
+      raise_err(p.err_flag, late && tid == 0, kErrEvictions);
+      return !late;
     };
-    if (MODE == kInPlace && in_place) wait();
+    if (MODE == kInPlace && in_place && !waited()) return;
     if (!same) {
       x.write(p, layer, g, to, a, b);
-      if (MODE == kInPlace && !in_place) wait();  // (its weights lie here)
+      if (MODE == kInPlace && !in_place && !waited()) return;  // (its weights lie here)
       if (wdst && tid >= a && tid < b) wdst[page * kKvPage + tid] = w;
     }
     if (MODE == kFew) __syncthreads();  // LDS is free again

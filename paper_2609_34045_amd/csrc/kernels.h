@@ -29,6 +29,7 @@ enum : int {
   kErrToken = 1,      // a token id outside [0, vocab): its hidden row became NaN
   kErrF16Range = 2,   // an activation, key or value stored in fp16 was at or beyond 65520 in magnitude
   kErrNaNLogit = 4,   // a logit was NaN (the argmax skips it; a row of NaN gives token -1)
+  kErrEvictions = 8,  // two moves in place on one cache ran at the same time: positions were left where they were
 };
 
 // fp32 to fp16 bits (round to nearest even), noting in `bad` a value that fp16
@@ -492,9 +493,13 @@ struct KeepParams {
   int* flags;              // [layers][nkv][pages]
   int* tickets;            // [layers][nkv], kTicketStep apart
   int pages;
+  int waits;               // looks at a flag before a page is given up (kErrEvictions)
+  int* err_flag;
 };
 static_assert(kMaxNodes <= 256, "node");
 hipError_t launch_keep(const KeepParams& p, int hd, hipStream_t s);
+// What kf_kv_evict takes for waits: about a tenth of a second, where a wait that its flag ends takes microseconds.
+extern int keep_waits;
 
 // The positions that eviction keeps: of each layer's and KV head's len weights the first `first`, the last `last` and the
 // keep - first - last largest of the others, the lower position first among equal ones and a NaN below all;

@@ -796,8 +796,9 @@ kf_status kf_stage_sync(kf_stage* s) {
       msg += "an activation, key or value held in fp16 reached 65520 in magnitude (stored as infinity; in an MXFP4 cache as "
              "49152, and a NaN as 0); ";
     if (flag & kErrNaNLogit) msg += "a logit was NaN (skipped by the argmax; a row of NaN logits gave token -1); ";
+    if (flag & kErrEvictions) msg += "two evictions in place of one cache ran at the same time (pages of positions were not moved); ";
     msg.resize(msg.size() - 2);
-    return fail((flag & kErrToken) ? KF_EINVAL : KF_ERANGE, "%s", msg.c_str());
+    return fail((flag & kErrToken) ? KF_EINVAL : (flag & kErrEvictions) ? KF_ESTATE : KF_ERANGE, "%s", msg.c_str());
   }
   return KF_OK;
 }
@@ -1381,6 +1382,8 @@ kf_status kf_kv_evict(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t kee
     p.flags = flags;
     p.tickets = sel.tickets;
     p.pages = kv->ppu;
+    p.waits = keep_waits;
+    p.err_flag = kv->st->err_flag;
     p.layers = kv->layers();
     p.dst = p.src = kv->ref();
     p.dst_user = dst_user;

@@ -1,0 +1,71 @@
+"""Evictions in place, whose pages are moved side by side: what lies there is read before it is overwritten, or the stage says so."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from tests.test_gpu_attend import on, st, torch  # noqa: F401 (fixtures)
+from tests.test_gpu_cache import bare_stage, check, held, rows
+from tests.test_gpu_weights import evicted, kept_of, some_weights
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture
+def no_patience(st):
+    """Pages that would wait for others give up at once (csrc/kernels.h declares the limit; the mangled name is the C++ ABI's)."""
+    limit = ctypes.c_int.in_dll(st.load_library(), "_ZN2kf10keep_waitsE")
+    old, limit.value = limit.value, 0
+    assert old > 1000
+    yield limit
+    limit.value = old
+
+
+@pytest.mark.parametrize("cache", ["f16", "mxfp4"])
+@pytest.mark.parametrize("shared", [False, True])
+def test_a_wait_that_ends_without_its_flag_is_told(torch, st, no_patience, cache, shared):
+    """Every page but the first waits for the one before it.  None of those is written, keys, values (in place) and weights
+    alike, and the stage reports it once; the next eviction is as ever."""
+    nkv, n, keep, layers = 2, 1000, 500, 2
+    g = bare_stage(st, nkv, 64, layers=layers)
+    kv = g.kv(2, n, 16 + 8, dtype=cache)
+    kv.track()
+    data = [(rows(2 * l, n, nkv, 64), rows(2 * l + 1, n, nkv, 64)) for l in range(layers)]
+    w = [some_weights(l, nkv, n) for l in range(layers)]
+    for l in range(layers):
+        kv.write(l, 0, 0, *(on(x) for x in data[l]))
+        kv.set_weights(l, 0, 0, on(w[l]))
+    kv.set_len(0, n)
+    user = 0
+    if shared:  # other pages take the places of all that are written
+        kv.fork(0, 1)
+        user = 1
+    kept = kv.evict(user, user, keep, 0, 0, kept=True).cpu().numpy().astype(np.int64)
+    with pytest.raises(st.KFError) as e:
+        g.sync()
+    assert e.value.status == st.KF_ESTATE and "evictions" in e.value.message
+    g.sync()
+    for l in range(layers):
+        at = np.array([kept_of(w[l][h].tolist(), keep, 0, 0) for h in range(nkv)])
+        assert np.array_equal(kept[l], at)
+        got = kv.weights(l, user, 0, n).cpu().numpy()
+        assert np.array_equal(got[:, :64], np.take_along_axis(w[l], at[:, :64], 1), equal_nan=True)
+        assert np.array_equal(got[:, 64:], w[l][:, 64:], equal_nan=True)
+        pick = lambda x: np.stack([held(x, cache)[at[h], h] for h in range(nkv)], 1)  # noqa: E731
+        check(kv, l, user, 0, *(pick(x)[:64] for x in data[l]), what="first page")
+        if not shared:
+            check(kv, l, 0, 64, *(held(x, cache)[64:keep] for x in data[l]), what="pages left as they were")
+        else:
+            check(kv, l, 0, 0, *(held(x, cache) for x in data[l]), what="source")
+    no_patience.value = 1 << 17
+    for u in {0, user}:
+        kv.set_len(u, 0)
+    for l in range(layers):
+        kv.write(l, 0, 0, *(on(x) for x in data[l]))
+        kv.set_weights(l, 0, 0, on(w[l]))
+    kv.set_len(0, n)
+    kept = kv.evict(0, 0, keep, 0, 0, kept=True)
+    evicted(kv, layers, nkv, cache, data, w, 0, 0, keep, 0, 0, kept)
+    g.sync()
+    kv.close()
+    g.close()
