@@ -69,3 +69,39 @@ def test_a_wait_that_ends_without_its_flag_is_told(torch, st, no_patience, cache
     g.sync()
     kv.close()
     g.close()
+
+
+@pytest.mark.parametrize("cache", ["f16", "mxfp4"])
+@pytest.mark.parametrize("hd,nkv,layers,n,keep,first,last", [(128, 8, 4, 12000, 7001, 4, 500), (64, 3, 2, 30011, 20003, 70, 0), (128, 1, 1, 20000, 3, 0, 1)])
+@pytest.mark.parametrize("shared", [False, True])
+def test_contents_of_more_pages_than_fit_side_by_side(torch, st, cache, hd, nkv, layers, n, keep, first, last, shared):
+    """Every key and value of evictions in place whose pages outnumber the workgroups that the GPU holds at once (110 pages of
+    32 heads in the first case, of 2048), each position its own: on pages of the user's, and where another user holds them too."""
+    g = bare_stage(st, nkv, hd, layers=layers)
+    pages = (n + 63) // 64
+    kv = g.kv(2, n, pages + (keep + 63) // 64, dtype=cache)
+    kv.track()
+    r = torch.Generator(device="cuda").manual_seed(n)
+    data, w = [], []
+    for l in range(layers):
+        kv.write(l, 0, 0, *(torch.empty((n, nkv, hd), device="cuda").normal_(generator=r) for _ in range(2)))
+        data.append([t.clone() for t in kv.read(l, 0, 0, n)])
+        w.append(some_weights(l, nkv, n))
+        kv.set_weights(l, 0, 0, on(w[l]))
+    kv.set_len(0, n)
+    user = 0
+    if shared:
+        kv.fork(0, 1)
+        user = 1
+    kept = kv.evict(user, user, keep, first, last, kept=True).long()
+    g.sync()
+    for l in range(layers):
+        assert kept[l].tolist() == [kept_of(w[l][h].tolist(), keep, first, last) for h in range(nkv)]
+        at = kept[l].t()  # [keep, nkv]
+        for got, x in zip(kv.read(l, user, 0, keep), data[l]):
+            assert torch.equal(got, x.gather(0, at[:, :, None].expand(-1, -1, hd)))
+        assert np.array_equal(kv.weights(l, user, 0, keep).cpu().numpy(), np.take_along_axis(w[l], kept[l].cpu().numpy(), 1), equal_nan=True)
+        if shared:
+            assert all(torch.equal(a, b) for a, b in zip(kv.read(l, 0, 0, n), data[l]))
+    kv.close()
+    g.close()
