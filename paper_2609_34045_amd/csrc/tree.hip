@@ -98,18 +98,22 @@ __device__ __forceinline__ int vt_slot(int d, int c) { return c ^ ((d >> 1) & 7)
 template <int N>
 __device__ __forceinline__ void direct_loads(const char* base, const uint32_t (&at)[N], uint32_t dst) {
   static_assert(N == 2 || N == 4, "loads of a block");
+  uint32_t m0;  // as it was, and is again afterwards
   if constexpr (N == 2)
     asm volatile(
-        "s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
-        "s_add_u32 m0, m0, 4096\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" ::"s"(dst), "v"(at[0]), "v"(at[1]), "s"(base)
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %2, %4\n\t"
+        "s_add_u32 m0, m0, 4096\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %4\n\ts_mov_b32 m0, %0"
+        : "=&s"(m0)
+        : "s"(dst), "v"(at[0]), "v"(at[1]), "s"(base)
         : "memory", "scc");
   else
     asm volatile(
-        "s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
-        "s_add_u32 m0, m0, 4096\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %5\n\t"
-        "s_add_u32 m0, m0, 4096\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5\n\t"
-        "s_add_u32 m0, m0, 4096\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %5" ::"s"(dst), "v"(at[0]), "v"(at[1]), "v"(at[N - 2]),
-        "v"(at[N - 1]), "s"(base)
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %2, %6\n\t"
+        "s_add_u32 m0, m0, 4096\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %6\n\t"
+        "s_add_u32 m0, m0, 4096\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %6\n\t"
+        "s_add_u32 m0, m0, 4096\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %6\n\ts_mov_b32 m0, %0"
+        : "=&s"(m0)
+        : "s"(dst), "v"(at[0]), "v"(at[1]), "v"(at[N - 2]), "v"(at[N - 1]), "s"(base)
         : "memory", "scc");
 }
 // Waits for this wave's vector memory operations, the direct loads among them.
