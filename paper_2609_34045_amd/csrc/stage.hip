@@ -1259,7 +1259,8 @@ kf_status kf_kv_set_dropped(kf_kv* kv, int32_t user, int32_t dropped) {
 
 // Adds the weights of `rows` queries of one layer, row b's over positions [0, lens[b]) of users[b]; those from fresh[b]
 // on (the same for every row of a user) have none yet.  p holds the queries.
-static kf_status weigh_rows(kf_kv* kv, WeighParams& p, int layer, int rows, const int* users, const int* lens, const int* fresh) {
+static kf_status weigh_rows(kf_kv* kv, WeighParams& p, int layer, int rows, const int* users, const int* lens, const int* fresh,
+                            const Tracer& tr) {
   const kf_stage* s = kv->st;
   const kf_model_config& c = s->cfg;
   const CacheRef ref = kv->layer_ref(layer);
@@ -1289,7 +1290,6 @@ static kf_status weigh_rows(kf_kv* kv, WeighParams& p, int layer, int rows, cons
       u.len = std::max(u.len, lens[j]);
     }
   }
-  const Tracer tr = kv->st->tracer();
   tr.begin(KF_K_ATTN);
   const hipError_t e = launch_weigh(p, c.head_dim, s->n_cu, (int64_t)kMaxBatch * c.n_q_heads * kv->max_split * c.head_dim, s->stream);
   tr.end(KF_K_ATTN);
@@ -1318,7 +1318,7 @@ kf_status kf_kv_weigh(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* use
   WeighParams p{};
   p.q = q_dev;
   p.q_type = io;
-  return weigh_rows(kv, p, layer, rows, users, lens, nullptr);
+  return weigh_rows(kv, p, layer, rows, users, lens, nullptr, kv->st->tracer());
 }
 
 kf_status kf_kv_evict(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t keep, int32_t first, int32_t last,
@@ -1869,7 +1869,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
         w.ml_shift = kPartShift;
         for (int b = 0; b < batch; ++b) w.ml_n[b] = rows.n[b];
       }
-      const kf_status wst = weigh_rows(kv, w, l, batch, users, a.len, positions);
+      const kf_status wst = weigh_rows(kv, w, l, batch, users, a.len, positions, tr);
       if (wst != KF_OK) return wst;
     }
 
@@ -2313,7 +2313,7 @@ static kf_status prefill_impl(kf_stage* s, kf_kv* kv, int32_t user, int32_t pos0
       WeighParams w{};
       w.q = ws->q + (int64_t)(n - rows) * c.n_q_heads * c.head_dim;
       w.q_type = KF_F16;
-      const kf_status wst = weigh_rows(kv, w, l, rows, users, lens, fresh);
+      const kf_status wst = weigh_rows(kv, w, l, rows, users, lens, fresh, tr);
       if (wst != KF_OK) return wst;
     }
   }

@@ -107,3 +107,22 @@ def test_a_steps_weights_add_up_to_its_heads(torch, st, cache, shape, lens):
     g.sync()
     kv.close()
     g.close()
+
+
+@pytest.mark.parametrize("cache", ["f16", "mxfp4"])
+def test_a_chunk_without_allocations_records_no_times(torch, st, cache):
+    """kf_stage_prefill_noalloc creates no events, on a tracked cache neither; other tracked calls are timed."""
+    shape = synth.SHAPE_TINY
+    g = st.Stage(shape, 0, 2, SeededModel(shape, 6).layer)
+    kv = g.kv(1, 200, dtype=cache)
+    kv.track(8)
+    h = on(synth.hidden_states(6, synth.STREAM_PREFILL_HIDDEN, 0, 50, shape.hidden))
+    g.profile(True)
+    g.prefill(kv, 0, 0, hidden=h, out=torch.empty_like(h), noalloc=True)
+    assert g.profile_read() == {}
+    g.prefill(kv, 0, 50, hidden=h)
+    assert g.profile_read()["attn"][0] == 2
+    g.profile(False)
+    g.sync()
+    kv.close()
+    g.close()
