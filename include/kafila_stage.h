@@ -335,7 +335,8 @@ kf_status kf_kv_attend(kf_kv* kv, int32_t layer, int32_t rows, const int32_t* us
  *           gives zeros and which no token sees (a token that names it as its parent sees itself and what lies
  *           before the tree).  Any other value counts as -1.
  *   q_dev, out_dev : [sum of nodes, nq, hd] in io, tree after tree; as for kf_kv_attend
- * Queries and probabilities keep 22 bits.  A position that a token does not see does not reach it, whatever it holds.  KF_ERANGE for
+ * Queries and probabilities keep 22 bits.  A position that a token does not see does not reach it, whatever it holds; an
+ * infinite value that it sees shows in its place alone, and a key whose score is -inf counts for nothing.  KF_ERANGE for
  * positions beyond max_ctx or the pages the user holds.
  * The splits' partial results use the cache's own workspace, which kf_kv_attend and decode use too.
  * Changes nothing in the cache.  Enqueued on the stage's stream.

@@ -170,6 +170,7 @@ __global__ __launch_bounds__(256, 2) void attn_tree_kernel(const TreeParams p) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * TILEB];  // two stages: K, V behind it
   __shared__ uint64_t see[kMaxNodes][kMaxNodes / 64];
   __shared__ int up[kMaxNodes];
+  __shared__ int again;  // some result is no number
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // Consecutive workgroups go to the 8 XCDs in turn: numbering the work XCD by XCD keeps the tiles that read the
@@ -296,6 +297,7 @@ __global__ __launch_bounds__(256, 2) void attn_tree_kernel(const TreeParams p) {
       }
     }
   };
+  if (tid == 0) again = 0;
   if constexpr (MX) load_mx(blk0);
   else load_f16(blk0, 0);
 
@@ -334,11 +336,7 @@ __global__ __launch_bounds__(256, 2) void attn_tree_kernel(const TreeParams p) {
   if constexpr (MX) store_mx(smem);
 
   f32x16 o[DB];
-  float m_run = -INFINITY, l_run = 0.f;
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) o[d][v] = 0.f;
+  float m_run, l_run;
 
   // ---- operands
   // Byte offsets of this lane's fragments within a block: K's of slice s and the first tile; V's of d block d, whose key step st (16 keys) takes
@@ -392,7 +390,8 @@ __global__ __launch_bounds__(256, 2) void attn_tree_kernel(const TreeParams p) {
       for (int v = 0; v < 16; ++v)
         if (!((uint32_t)(sees >> (32 * t)) >> (8 * (v >> 2) + (v & 3)) & 1u)) st[t][v] = -INFINITY;
   };
-  bool odd = false;  // some value was no number, the same in every thread
+  bool odd = false;      // some value was no number, the same in every thread
+  bool careful = false;  // the second time over the blocks, likewise
   // An infinity or NaN among the values that some tokens do not see would reach them as 0 times it: out of the
   // products with it, and into the sums of those that see it behind the loop.
   auto take_out = [&](uint8_t* vs) {
@@ -432,7 +431,7 @@ __global__ __launch_bounds__(256, 2) void attn_tree_kernel(const TreeParams p) {
     }
     const bool tail = blk * kKB + kKB > tr.len;  // positions of the tree, or past it
     if constexpr (!MX) {
-      if (tail) take_out(stage + TILEB);
+      if (tail || careful) take_out(stage + TILEB);
     }
     if (live) {
       constexpr int NI = NT * NS, RING = 4;
@@ -446,6 +445,19 @@ __global__ __launch_bounds__(256, 2) void attn_tree_kernel(const TreeParams p) {
           st[i % NT] = mfma32(ring[i % RING], qf[part][i / NT], i / NT || part ? st[i % NT] : zero);
         if (i + RING < NI) ring[i % RING] = kread(stage, i + RING);
         __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (!MX && PARTS == 2) {
+        if (__builtin_expect(careful, 0)) {  // an infinite key's score is that of the first parts: with the second, of another sign or 0, it is NaN
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            f32x16 first = zero;
+#pragma unroll
+            for (int s = 0; s < NS; ++s) first = mfma32(kread(stage, s * NT + t), qf[0][s], first);
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+              if (__builtin_fabsf(first[v]) == INFINITY) st[t][v] = first[v];
+          }
+        }
       }
       if (tail) mask(blk, st);
       // The reference of the softmax moves only when a block's maximum exceeds it by kPartLazy, so that O is rarely rescaled.
@@ -501,15 +513,41 @@ __global__ __launch_bounds__(256, 2) void attn_tree_kernel(const TreeParams p) {
       if (more) store_mx(next);
     }
   };
-  for (int blk = blk0; blk < blk1; blk += 2) {
-    step(blk, std::integral_constant<int, 0>());
-    if (blk + 1 < blk1) step(blk + 1, std::integral_constant<int, 1>());
+  for (;;) {
+    m_run = -INFINITY;
+    l_run = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[d][v] = 0.f;
+    for (int blk = blk0; blk < blk1; blk += 2) {
+      step(blk, std::integral_constant<int, 0>());
+      if (blk + 1 < blk1) step(blk + 1, std::integral_constant<int, 1>());
+    }
+    // An fp16 cache may hold infinities (what did not fit), and two parts of which one is 0 or of another sign make NaN of
+    // them: where a result is no number, all blocks once more, with infinite values taken out and infinite keys looked at.
+    if (MX || careful) break;
+    f32x16 sum = o[0];
+#pragma unroll
+    for (int d = 1; d < DB; ++d) sum += o[d];
+    float all = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) all += sum[v];
+    if (__ballot(!(__builtin_fabsf(all) < INFINITY)) && lane == 0) again = 1;
+    __syncthreads();
+    careful = __builtin_amdgcn_readfirstlane(again);
+    if (__builtin_expect(!careful, 1)) break;
+    if constexpr (!MX) {
+      pb = blk0;
+      load_pids();
+      load_f16(blk0, 0);
+    }
   }
 
   if constexpr (!MX) {
     if (odd) {
 #pragma unroll 1
-      for (int k = max(blk0, tr.len / kKB) * kKB; k < min(blk1 * kKB, total); ++k) {
+      for (int k = (careful ? blk0 : max(blk0, tr.len / kKB)) * kKB; k < min(blk1 * kKB, total); ++k) {
         const uint16_t* v = p.vc + kv_offset(p.kv, tr.user, g, k, HD) + 4 * half_sel;
         const int a = k - tr.len;
         if (a >= 0 && !(see[node][a >> 6] >> (a & 63) & 1)) continue;

@@ -6,7 +6,7 @@ import pytest
 
 from tests.test_gpu_attend import EPS, on, st, torch  # noqa: F401 (fixtures)
 from tests.test_gpu_cache import bare_stage, held, rows
-from tests.test_gpu_tree import want_of
+from tests.test_gpu_tree import allowed, draft, sees, want_of
 
 pytestmark = pytest.mark.gpu
 
@@ -55,5 +55,40 @@ def test_two_positions_weigh_as_22_bits_give(torch, st, cache, hd, group, io):
         worst = max(worst, float((np.abs(got - exact) / tol).max()))
     assert worst <= 1, worst
     g.sync()
+    kv.close()
+    g.close()
+
+
+@pytest.mark.parametrize("io", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("hd,n,m,paged", [(128, 1100, 30, False), (64, 5000, 70, True), (64, 64, 1, False), (128, 20, 3, True)])
+def test_infinities_that_a_token_sees(torch, st, io, hd, n, m, paged):
+    """An fp16 cache may hold infinities (what did not fit), before the tree and in it.  A value's makes its place of the output
+    infinite, with its sign, in every row that sees it, and no other place; a key's of a score of -inf counts for nothing."""
+    nkv, group = 2, 4
+    g = bare_stage(st, nkv, hd, group=group)
+    kv = g.kv(1, n + m, (n + m + 63) // 64 if paged else None)
+    k, v = rows(1, n + m, nkv, hd), rows(2, n + m, nkv, hd)
+    par = draft(4, m)
+    p = torch.tensor(par, dtype=torch.int32, device="cuda")
+    q = on(np.abs(rows(3, m, nkv * group, hd, 0.3)) + np.float32(1e-3), getattr(torch, io))
+    kv.write(0, 0, 0, on(k), on(v))
+    clean = kv.attend_tree(0, [0], [n], [m], p, q).float().cpu().numpy()
+    bad = v.copy()
+    bad[3, 0, 5], bad[n // 2, 1, 7], bad[n, 1, 40] = np.inf, -np.inf, np.inf  # the last: of the first token
+    kv.write(0, 0, 0, on(k), on(bad))
+    got = kv.attend_tree(0, [0], [n], [m], p, q).float().cpu().numpy()
+    want = clean.copy()
+    want[:, :group, 5], want[:, group:, 7] = np.inf, -np.inf
+    want[sees(par)[:, 0], group:, 40] = np.inf
+    assert np.array_equal(got, want)
+    bad = k.copy()
+    bad[2, 0, 9] = bad[n - 1, 0, 30] = -np.inf
+    kv.write(0, 0, 0, on(bad), on(v))
+    got = kv.attend_tree(0, [0], [n], [m], p, q).double().cpu().numpy()
+    left = [t for t in range(n + m) if t not in (2, n - 1)]
+    qf, kf, vf = q.float().cpu().numpy(), held(k, "f16"), held(v, "f16")
+    w = want_of(qf, kf[left], vf[left], n - 2, par)
+    assert np.all((np.abs(got - w) <= allowed(qf, kf, vf, w, io))[:, :group])
+    assert np.array_equal(got[:, group:], clean[:, group:].astype(np.float64))
     kv.close()
     g.close()
