@@ -463,17 +463,18 @@ hipError_t launch_kv_table_share(const KvTable& t, int src, int dst, int n, hipS
 }
 
 __global__ __launch_bounds__(256) void rope_rows_kernel(const RopeRows p) {
-  const int64_t at = p.from * p.half + (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= p.n * p.half) return;
-  double s, c;
-  sincos((double)(at / p.half) * p.w[at % p.half], &s, &c);
-  p.cos[at] = (float)c;
-  p.sin[at] = (float)s;
+  for (int64_t at = p.from * p.half + (int64_t)blockIdx.x * 256 + threadIdx.x; at < p.n * p.half; at += (int64_t)gridDim.x * 256) {
+    double s, c;
+    sincos((double)(at / p.half) * p.w[at % p.half], &s, &c);
+    p.cos[at] = (float)c;
+    p.sin[at] = (float)s;
+  }
 }
 
 hipError_t launch_rope_rows(const RopeRows& p, hipStream_t s) {
   if (p.half > 128 || p.n <= p.from) return p.half > 128 ? hipErrorInvalidValue : hipSuccess;
-  hipLaunchKernelGGL(rope_rows_kernel, dim3(((p.n - p.from) * p.half + 255) / 256), dim3(256), 0, s, p);
+  const int64_t wgs = std::min<int64_t>(((p.n - p.from) * p.half + 255) / 256, 1 << 20);  // (a grid has fewer than 2^32 threads)
+  hipLaunchKernelGGL(rope_rows_kernel, dim3((unsigned)wgs), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
