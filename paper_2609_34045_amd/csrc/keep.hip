@@ -202,17 +202,17 @@ __global__ __launch_bounds__(256 * groups_of(MODE)) void keep_kernel(const KeepP
   __shared__ __attribute__((aligned(16))) uint8_t nib[GROUPS * NIB];
   __shared__ int at[MX ? GROUPS * kKvPage : 1];
   __shared__ int ticket;
-  const int page0 = p.from / kKvPage, pages = (p.n + kKvPage - 1) / kKvPage, heads = p.nkv * p.layers;
+  const int page0 = p.from / kKvPage, pages = (p.n + kKvPage - 1) / kKvPage;
   const int tid = threadIdx.x % 256, group = MODE == kFew ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
   PageOf<HD, MX> x;
   if constexpr (MX) {
     x.nib = nib + group * NIB;
     x.at = at + group * kKvPage;
   }
-  // Workgroup x: KV head and layer x % heads, of page x / heads (kInPlace: of the next page that none has), or (kFew) of
-  // all pages, as many at a time as it has groups.
-  const int lg = blockIdx.x % heads, g = lg % p.nkv, layer = lg / p.nkv;
-  int nth = blockIdx.x / heads;
+  // Workgroup (x, y): KV head and layer x, page y (kInPlace: the next page that none has), or (kFew) all pages, as many at a
+  // time as it has groups.
+  const int lg = blockIdx.x, g = lg % p.nkv, layer = lg / p.nkv;
+  int nth = blockIdx.y;
   if (MODE == kInPlace) {
     if (tid == 0) ticket = __hip_atomic_fetch_add(&p.tickets[lg * kTicketStep], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
@@ -473,8 +473,9 @@ hipError_t launch_select(const SelectParams& p, int nkv, int layers, hipStream_t
 template <int HD, bool MX>
 static hipError_t keep(const KeepParams& p, hipStream_t s) {
   const unsigned pages = (unsigned)((p.n + kKvPage - 1) / kKvPage - p.from / kKvPage), heads = p.nkv * p.layers;
-  if (!p.in_place) hipLaunchKernelGGL((keep_kernel<HD, MX, kApart>), dim3(pages * heads), dim3(256), 0, s, p);
-  else if (p.list) hipLaunchKernelGGL((keep_kernel<HD, MX, kInPlace>), dim3(pages * heads), dim3(256), 0, s, p);
+  const dim3 grid(heads, pages);  // (as one number, 1024 heads of 2^20 positions would be 2^32 threads, which a grid cannot have)
+  if (!p.in_place) hipLaunchKernelGGL((keep_kernel<HD, MX, kApart>), grid, dim3(256), 0, s, p);
+  else if (p.list) hipLaunchKernelGGL((keep_kernel<HD, MX, kInPlace>), grid, dim3(256), 0, s, p);
   else hipLaunchKernelGGL((keep_kernel<HD, MX, kFew>), dim3(heads), dim3(256 * std::min(pages, (unsigned)groups_of(kFew))), 0, s, p);
   return hipGetLastError();
 }

@@ -105,3 +105,34 @@ def test_contents_of_more_pages_than_fit_side_by_side(torch, st, cache, hd, nkv,
             assert all(torch.equal(a, b) for a, b in zip(kv.read(l, 0, 0, n), data[l]))
     kv.close()
     g.close()
+
+
+def test_1024_heads_of_a_million_positions(torch, st):
+    """An eviction in place of 2^20 positions in 16 layers of 64 heads, 75 GB in 4 bits: 2^32 threads' work.  One position goes, so
+    that every other one moves; some are looked at in the first and last layer."""
+    nkv, layers, n = 64, 16, 1 << 20
+    g = bare_stage(st, nkv, 64, layers=layers)
+    kv = g.kv(1, n, dtype="mxfp4")
+    kv.track()
+    at = [0, 777, 400_000, n - 500]  # first position of each part that has keys and values
+    data = {}
+    w = torch.ones((nkv, n), device="cuda")
+    gone = [700 + 3 * h for h in range(nkv)]
+    w[torch.arange(nkv), torch.tensor(gone)] = 0.5
+    for l in range(layers):
+        kv.set_weights(l, 0, 0, w)
+        if l in (0, layers - 1):
+            for p in at:
+                data[l, p] = [rows(100 * l + p + i, 500, nkv, 64) for i in range(2)]
+                kv.write(l, 0, p, *(on(x) for x in data[l, p]))
+            kv.set_weights(l, 0, 0, w)  # (written positions start at 0)
+    kv.set_len(0, n)
+    kv.evict(0, 0, n - 1)
+    for l in (0, layers - 1):
+        for p in at[2:]:
+            check(kv, l, 0, p - 1, *(held(x, "mxfp4") for x in data[l, p]), what=(l, p))
+        check(kv, l, 0, 0, *(held(x, "mxfp4") for x in data[l, 0]), what="before")
+        assert kv.weights(l, 0, 0, n - 1).eq(1).all()
+    g.sync()
+    kv.close()
+    g.close()
