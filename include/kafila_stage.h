@@ -408,8 +408,9 @@ kf_status kf_kv_evict(kf_kv* kv, int32_t src_user, int32_t dst_user, int32_t kee
  * How many positions evictions have dropped before a user's next token: the token at slot p is rotated to position
  * p + dropped, and callers that rotate their own queries and keys do the same.  Evictions add to it; kf_kv_fork, and a
  * kf_kv_copy from position 0, take it along; an empty user (length 0) has none.  Setting it (0 .. INT32_MAX - max_ctx, else
- * KF_ERANGE) is for users that were saved and written back.  The cache's table of rotations grows with it: 8 bytes for each
- * position and pair of a head (KF_ENOMEM, with nothing changed).  A call that cannot allocate, under graph capture or
+ * KF_ERANGE) is for users that were saved and written back.  The cache's table of rotations grows with it, to the farthest
+ * position that a user can reach: 8 bytes for each position and pair of a head and up to a quarter more, beside which the new
+ * table is made (KF_ENOMEM, with nothing changed); tables that captured steps read are kept while the cache is.  A call that cannot allocate, under graph capture or
  * kf_stage_prefill_noalloc, and that lacks rows is KF_ESTATE: an eviction outside a capture makes those that its user can need.
  */
 kf_status kf_kv_dropped(const kf_kv* kv, int32_t user, int32_t* dropped);

@@ -213,7 +213,8 @@ struct kf_kv {
   int64_t bytes = 0;                    // device bytes of everything here
   float *rcos = nullptr, *rsin = nullptr;
   int64_t rope_rows = 0;                // of them
-  std::vector<float*> old_ropes;        // shorter tables, which captured steps may still read
+  bool rope_recorded = false;           // a captured step or chunk reads it
+  std::vector<float*> old_ropes;        // shorter tables that such read
   float *part_acc = nullptr, *part_ml = nullptr;
   // KF_KV_MXFP4: a decode step's new keys and values, which the QKV launch leaves in fp16 as in an fp16
   // cache, row b's in page b (append_table gives that page for every position); and one layer of one user's
@@ -1010,14 +1011,14 @@ kf_status kf_kv_set_len(kf_kv* kv, int32_t user, int32_t len) {
   return KF_OK;
 }
 
-// RoPE rows of positions [0, n).  A longer table holds the same rows; captured steps go on reading the one that they were
-// recorded with.
+// RoPE rows of positions [0, n), a quarter more than before at least.  A longer table holds the same rows; captured steps go on
+// reading the one that they were recorded with, and one that none has read is freed.
 static kf_status rope_upto(kf_kv* kv, int64_t n, bool allocate = true) {
   if (n <= kv->rope_rows) return KF_OK;
   if (!allocate || capturing(kv->st))
     return fail(KF_ESTATE, "rotations to position %lld need a longer table, which this call may not allocate", (long long)(n - 1));
   const kf_model_config& c = kv->st->cfg;
-  const int64_t rows = std::max(n, 2 * kv->rope_rows), half = c.head_dim / 2;
+  const int64_t rows = std::max(n, kv->rope_rows + kv->rope_rows / 4), half = c.head_dim / 2;
   float *cs = nullptr, *sn = nullptr;
   if (hipMalloc((void**)&cs, rows * half * 4) != hipSuccess || hipMalloc((void**)&sn, rows * half * 4) != hipSuccess) {
     (void)hipGetLastError();
@@ -1041,8 +1042,16 @@ static kf_status rope_upto(kf_kv* kv, int64_t n, bool allocate = true) {
     hipFree(sn);
     return fail(KF_EDEVICE, "rotations: %s", hipGetErrorString(e));
   }
-  kv->old_ropes.push_back(kv->rcos);
-  kv->old_ropes.push_back(kv->rsin);
+  if (kv->rope_recorded) {
+    kv->old_ropes.push_back(kv->rcos);
+    kv->old_ropes.push_back(kv->rsin);
+    kv->rope_recorded = false;
+  } else {  // (the copies above still read it)
+    hipStreamSynchronize(kv->st->stream);
+    hipFree(kv->rcos);
+    hipFree(kv->rsin);
+    kv->bytes -= kv->rope_rows * half * 8;
+  }
   kv->rcos = cs;
   kv->rsin = sn;
   kv->rope_rows = rows;
@@ -1720,6 +1729,7 @@ kf_status kf_stage_decode(kf_stage* s, kf_kv* kv, int32_t batch, const int32_t* 
   for (int b = 0; b < batch && gst == KF_OK; ++b) gst = rope_upto(kv, (int64_t)positions[b] + kv->dropped[users[b]] + 1);
   if (gst == KF_OK) gst = kv_grant(kv, batch, users, from, upto);
   if (gst != KF_OK) return gst;
+  kv->rope_recorded = kv->rope_recorded || capturing(s);
   s->kept_rows = 0;  // the residual rows change from here on; set again when the step completes
 
   const Tracer tr = s->tracer();
@@ -2263,6 +2273,7 @@ static kf_status prefill_impl(kf_stage* s, kf_kv* kv, int32_t user, int32_t pos0
   kf_status gst = rope_upto(kv, upto + kv->dropped[user], !no_alloc);
   if (gst == KF_OK) gst = kv_grant(kv, 1, &user, &from, &upto);
   if (gst != KF_OK) return gst;
+  kv->rope_recorded = kv->rope_recorded || capturing(s);
   pa.rope_cos = kv->rcos + (int64_t)kv->dropped[user] * (c.head_dim / 2);
   pa.rope_sin = kv->rsin + (int64_t)kv->dropped[user] * (c.head_dim / 2);
   const Tracer tr = no_alloc ? Tracer{} : s->tracer();  // event records may create events
