@@ -867,6 +867,7 @@ static kf_status kv_make(kf_stage* s, int32_t max_users, int32_t max_ctx, int32_
   kv->layer_stride = kv->page_stride * kv->n_pages;
   kv->len.assign(max_users, 0);
   kv->dropped.assign(max_users, 0);
+  kv->old_ropes.reserve(256);  // two a growth, by a quarter, up to 2^31 rows: calls from C add to it
   kv->held.assign(max_users, paged ? 0 : ppu);
   if (paged) {
     kv->host_table.assign((size_t)max_users * ppu, -1);
