@@ -17,7 +17,7 @@
 //
 // What bounds it: the matrix and vector units, in turn.  128 fp32 tokens of 64 heads at 40001 positions (8 KV heads of
 // 128): 336 GFLOP of products in 300 to 340 us, a large library product's rate; 64 bf16 tokens of 32 heads at 32768
-// with the merge 72 us (51 GFLOP, 45 us at that rate; 10 are a launch's fixed part and 8 the merge).
+// 66 us (51 GFLOP, 45 us at that rate; 10 are a launch's fixed part), where each unit is busy 53% of the time.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
