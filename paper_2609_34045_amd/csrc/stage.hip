@@ -253,6 +253,13 @@ struct kf_kv {
   int layers() const { return st->hi - st->lo; }
 };
 
+// While it lives, this thread's allocations leave captures of other streams alone.
+struct AllocBesideCaptures {
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+  AllocBesideCaptures() { (void)hipThreadExchangeStreamCaptureMode(&mode); }
+  ~AllocBesideCaptures() { (void)hipThreadExchangeStreamCaptureMode(&mode); }
+};
+
 static int pages_for(int64_t len) { return (int)((len + kKvPage - 1) / kKvPage); }
 
 // Whether the stage's stream is being captured into a graph, and a number of the capture.
@@ -1021,6 +1028,7 @@ static kf_status rope_upto(kf_kv* kv, int64_t n, bool allocate = true) {
   const kf_model_config& c = kv->st->cfg;
   const int64_t rows = std::max(n, kv->rope_rows + kv->rope_rows / 4), half = c.head_dim / 2;
   float *cs = nullptr, *sn = nullptr;
+  const AllocBesideCaptures beside;
   if (hipMalloc((void**)&cs, rows * half * 4) != hipSuccess || hipMalloc((void**)&sn, rows * half * 4) != hipSuccess) {
     (void)hipGetLastError();
     if (cs) hipFree(cs);
@@ -1207,6 +1215,7 @@ kf_status kf_kv_track(kf_kv* kv, int32_t window) {
     if (capturing(kv->st)) return fail(KF_ESTATE, "a cache's first kf_kv_track cannot be captured");
     const int64_t kept = kv->kept_ints() * 4, all = (int64_t)kv->layers() * kv->st->cfg.n_kv_heads * kv->max_ctx * kv->max_users * 4;
     char *w = nullptr, *k = nullptr;
+    const AllocBesideCaptures beside;
     if (hipMalloc((void**)&w, all) != hipSuccess || hipMalloc((void**)&k, kept) != hipSuccess) {
       (void)hipGetLastError();
       if (w) hipFree(w);

@@ -120,3 +120,37 @@ def test_captured_steps_outlive_the_table_that_they_read(torch, st, chunk):
     g.sync()
     kv.close()
     g.close()
+
+
+def test_tables_grow_beside_a_capture_of_another_stage(torch, st):
+    """While one stage's stream is captured, another stage's cache is tracked for the first time, evicted and taken far: its
+    allocations leave the capture as it is."""
+    model = SeededModel(SHAPE, 31)
+    a, b = (st.Stage(SHAPE, 0, 1, model.layer) for _ in range(2))
+    b.set_flags(st.KF_STAGE_ORDERED)
+    ka, kb = a.kv(1, 100), b.kv(1, 100)
+    ka.write(0, 0, 0, on(rows(1, 60, 2, 128)), on(rows(2, 60, 2, 128)))
+    ka.set_len(0, 60)
+    x = on(synth.hidden_states(31, synth.STREAM_DECODE_HIDDEN, 0, 1, SHAPE.hidden))
+    y = torch.empty_like(x)
+    want = b.decode(kb, [0], [0], hidden=x).clone()
+    kb.set_len(0, 0)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    b.set_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        b.decode(kb, [0], [0], hidden=x, out=y)
+        ka.track()
+        ka.evict(0, 0, 40)
+        ka.set_dropped(0, 5000)
+    for _ in range(3):
+        y.zero_()
+        graph.replay()
+        side.synchronize()
+        assert torch.equal(y, want)
+    assert (ka.len(0), ka.dropped(0)) == (40, 5000)
+    a.sync()
+    b.sync()
+    for t in (ka, kb, a, b):
+        t.close()
